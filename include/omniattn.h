@@ -1,7 +1,8 @@
 /*
  * omniattn.h - C ABI of the MI355X (gfx950) sparse MLA decode library.
  *
- * One operation: decode-phase attention for absorbed multi-head latent
+ * For layers with grouped queries instead of a latent cache see "Grouped-query layers" at the end.
+ * The rest is about one operation: decode-phase attention for absorbed multi-head latent
  * attention, restricted to the KV positions that OmniAttn's cache-compression
  * rule keeps.  For sequence b of length L_b the kept set is the first S
  * ("sink") positions and the last W ("recent") positions, as a set union
@@ -270,6 +271,120 @@ int32_t omniattn_ring_slot(int32_t sink, int32_t window, int32_t logical_page);
 int omniattn_ring_append(const omniattn_problem_t* prob, int32_t* seq_lens, const void* new_rows,
                          const float* new_scales, const int32_t* seq_pages, void* kv_cache,
                          float* kv_scales, int32_t* page_table, void* hip_stream);
+
+/*
+ * Grouped-query layers: a paged cache in 8 bits and the three calls of a step.
+ *
+ * The same rule (the first `sink` and the last `window` tokens are kept) for layers whose cache holds K and V rows
+ * of num_kv_heads heads instead of one latent row per token.  The cache holds e4m3 codes; `scale_tokens` tokens of
+ * one head share a scale.  Nothing here needs a length on the host: lengths, page tables, slots and the division of
+ * the work are read and made on the device, so a whole step can be captured once and replayed while the requests grow.
+ *
+ *   1. omniattn_table_extend   every request grows by its new tokens and takes the pages it needs
+ *   2. omniattn_gqa_append     the new K and V rows of a layer go to their slots, rounded to 8 bits
+ *   3. omniattn_gqa_decode     the new tokens' queries against the layer's cache
+ *   and omniattn_table_release when requests have finished.
+ *
+ * All of them are asynchronous on `hip_stream`, allocate nothing, do not synchronise and return the codes above.
+ * Sizes and alignment are checked, contents of device arrays are not: page ids lie in [0, num_pages), a request's
+ * entries of page_table cover its length, free_pages[0 .. free_count) are distinct.
+ */
+typedef struct {
+  int32_t batch;              /* B >= 1 requests                                                  */
+  int32_t page_size;          /* must be 128 tokens                                               */
+  int32_t max_pages_per_seq;  /* columns of page_table                                            */
+  int32_t max_tokens;         /* entries of slot_map                                              */
+  int64_t page_table_stride;  /* int32 elements from one row to the next, >= max_pages_per_seq     */
+  int64_t num_pages;          /* pages of the pool, and entries of free_pages; < 2^24             */
+} omniattn_table_t;
+
+/*
+ * One step's tables.  Request b has seq_lens[b] tokens and brings new_lens[b] >= 0.  In the order of the requests,
+ * each takes the pages it lacks, ceil((L + n) / 128) - ceil(L / 128), from the top of the stack free_pages (page number
+ * k of the call is free_pages[free_count - 1 - k]) and writes them into its row of page_table.
+ *
+ *   seq_lens, new_lens, q_start, slot_map, ...   device, int32
+ *   seq_lens_out    [B]      lengths with the new tokens.  May be seq_lens itself.
+ *   free_count_out  [1]      height of the stack afterwards.  May be free_count itself.
+ *   q_start         [B + 1]  first new token of each request among the call's tokens (running sum of new_lens,
+ *                           negative ones as 0; it stops at 2^31 - 1)
+ *   slot_map        [max_tokens]  per new token: page * 128 + place in the page; -1 behind the last token
+ * Arrays of input and output that are not the same must not overlap.
+ * A request that does not fit is refused as a whole: its row of page_table would be too short, a length is negative,
+ * its tokens reach past max_tokens, or the sum of the pages that requests up to it lack exceeds the stack (requests
+ * that lack no page are not affected by that).  Its length stays, its tokens' slots are -1; q_start counts them all the
+ * same, since they have their places among the call's rows.
+ *
+ * omniattn_table_release puts the pages of the requests with done[b] != 0 back on the stack, in their order, and sets
+ * their lengths to 0.  (seq_lens, free_pages and free_count change in place.)
+ */
+int omniattn_table_extend(const omniattn_table_t* table, const int32_t* seq_lens, const int32_t* new_lens,
+                          const int32_t* free_pages, const int32_t* free_count, int32_t* page_table,
+                          int32_t* seq_lens_out, int32_t* free_count_out, int32_t* q_start, int32_t* slot_map,
+                          void* hip_stream);
+int omniattn_table_release(const omniattn_table_t* table, const int32_t* done, int32_t* seq_lens,
+                           const int32_t* page_table, int32_t* free_pages, int32_t* free_count, void* hip_stream);
+
+typedef struct {
+  int32_t batch;              /* B >= 1 requests                                                  */
+  int32_t num_queries;        /* N: rows of q, all requests' query tokens together                */
+  int32_t num_q_heads;        /* a multiple of num_kv_heads                                       */
+  int32_t num_kv_heads;
+  int32_t head_dim;           /* 64, 128 or 256                                                   */
+  int32_t page_size;          /* must be 128 tokens                                               */
+  int32_t scale_tokens;       /* tokens of one head that share a scale: 32, 64 or 128             */
+  int32_t max_pages_per_seq;
+  int64_t page_table_stride;  /* int32 elements from one row of page_table to the next            */
+  int64_t num_pages;          /* pages of the cache, < 2^24                                       */
+  int32_t sink;               /* S >= 0                                                           */
+  int32_t window;             /* W >= 0; S + W >= L keeps everything                              */
+  float softmax_scale;
+  int32_t out_dtype;          /* OMNIATTN_BF16 | OMNIATTN_FP32                                    */
+} omniattn_gqa_t;
+
+/*
+ * New K and V rows into the cache.  (Of `gqa`: num_kv_heads, head_dim, page_size, scale_tokens and num_pages count.)
+ *   k_new, v_new        device, bf16 [num_tokens, num_kv_heads, head_dim]; k_stride and v_stride elements from one token
+ *                       to the next (multiples of 8, rows 16-byte aligned)
+ *   slot_map            device, int32 [num_tokens]; tokens with a slot that is not in the cache are left out
+ *   k_cache, v_cache    device, e4m3 [num_pages, num_kv_heads, 128, head_dim]
+ *   k_scales, v_scales  device, fp32 [num_pages, num_kv_heads, 128 / scale_tokens]
+ * A block's scale is a power of two, the smallest (from 2^-126) by which its largest finite magnitude is at most 448; 0
+ * for a block of zeros.  A number that is not finite becomes NaN.  Tokens of one block in a call have to follow one
+ * another in the call and in the block (as slot_map of omniattn_table_extend has them).  A block whose first token is
+ * written begins anew.  Otherwise its earlier tokens stay: the scale is the larger of the old one and the new tokens',
+ * and where it has grown the earlier codes are multiplied by old / new and rounded again (exact but for numbers that
+ * become subnormal).  Tokens behind the last one written are undefined.
+ */
+int omniattn_gqa_append(const omniattn_gqa_t* gqa, int32_t num_tokens, const void* k_new, int64_t k_stride, const void* v_new,
+                        int64_t v_stride, const int32_t* slot_map, void* k_cache, void* v_cache, float* k_scales,
+                        float* v_scales, void* hip_stream);
+
+/*
+ * Attention of the call's query tokens over the cache.  Request b has seq_lens[b] tokens in the cache; its queries are its
+ * last n = q_start[b + 1] - q_start[b] tokens, query t sees the keys before and at its own position L - n + t, and keeps of
+ * them the first `sink` and the last `window`.
+ *   q           device, bf16 [N, num_q_heads, head_dim]; q_stride elements from one token to the next (a multiple of 8)
+ *   k_scales, v_scales   finite, >= 0 for blocks that hold kept tokens; any numbers, not only powers of two
+ *   page_table  device, int32 [B, max_pages_per_seq]; entries of pages without kept tokens are not read
+ *   seq_lens    device, int32 [B]
+ *   q_start     device, int32 [B + 1], ascending, at most N; NULL: one query for each request (N = B)
+ *   out         device, out_dtype [N, num_q_heads, head_dim]; rows of no request are left as they are
+ *   lse         device, fp32 [N, num_q_heads], natural logarithm.  A query that keeps nothing gives 0 and -inf.
+ *   workspace   device, omniattn_gqa_workspace_bytes(gqa) bytes, 256-byte aligned; calls in flight at once need one each
+ * Tokens that a query does not keep may hold anything (NaN too) without effect on it; a kept NaN makes the row NaN.
+ * Same inputs give bitwise identical results.  Arithmetic: codes and queries enter the matrix instructions exactly (bf16),
+ * logits, sums and outputs are held in fp32; the weights are rounded to f16 (relative 2^-11, down to 2^-25 of a
+ * row's largest weight; fp32 results: to two f16 terms, 2^-22 down to 2^-14 and 2^-36 of the largest below that).
+ *
+ * omniattn_gqa_workspace_bytes depends on the current device and on batch, num_queries, the head counts and head_dim;
+ * 0 for an invalid problem.
+ */
+size_t omniattn_gqa_workspace_bytes(const omniattn_gqa_t* gqa);
+int omniattn_gqa_decode(const omniattn_gqa_t* gqa, const void* q, int64_t q_stride, const void* k_cache, const void* v_cache,
+                        const float* k_scales, const float* v_scales, const int32_t* page_table, const int32_t* seq_lens,
+                        const int32_t* q_start, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                        void* hip_stream);
 
 const char* omniattn_strerror(int code);
 /* Text of the last HIP error seen by the calling thread ("" if none). */

@@ -19,6 +19,14 @@ from .binding import (  # noqa: F401
     omniattn_ring_slot,
     omniattn_ring_append,
     decode,
+    omniattn_table_extend,
+    omniattn_table_release,
+    omniattn_gqa_append,
+    omniattn_gqa_workspace_bytes,
+    omniattn_gqa_decode,
+    gqa_decode,
+    Table,
+    Gqa,
     lib_path,
     load_library,
     BF16,

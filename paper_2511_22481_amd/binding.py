@@ -33,6 +33,24 @@ class Problem(ctypes.Structure):
     ]
 
 
+class Table(ctypes.Structure):
+    """omniattn_table_t"""
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("page_size", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32), ("max_tokens", ctypes.c_int32),
+        ("page_table_stride", ctypes.c_int64), ("num_pages", ctypes.c_int64),
+    ]
+
+
+class Gqa(ctypes.Structure):
+    """omniattn_gqa_t"""
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("num_queries", ctypes.c_int32), ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("scale_tokens", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
+        ("page_table_stride", ctypes.c_int64), ("num_pages", ctypes.c_int64), ("sink", ctypes.c_int32), ("window", ctypes.c_int32),
+        ("softmax_scale", ctypes.c_float), ("out_dtype", ctypes.c_int32),
+    ]
+
+
 def lib_path():
     return _LIB_PATH
 
@@ -89,6 +107,16 @@ def load_library():
     lib.omniattn_ring_slot.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]
     lib.omniattn_ring_append.restype = ctypes.c_int
     lib.omniattn_ring_append.argtypes = [ctypes.POINTER(Problem), P, P, P, P, P, P, P, P]
+    lib.omniattn_table_extend.restype = ctypes.c_int
+    lib.omniattn_table_extend.argtypes = [ctypes.POINTER(Table)] + [P] * 10
+    lib.omniattn_table_release.restype = ctypes.c_int
+    lib.omniattn_table_release.argtypes = [ctypes.POINTER(Table)] + [P] * 6
+    lib.omniattn_gqa_append.restype = ctypes.c_int
+    lib.omniattn_gqa_append.argtypes = [ctypes.POINTER(Gqa), ctypes.c_int32, P, ctypes.c_int64, P, ctypes.c_int64] + [P] * 6
+    lib.omniattn_gqa_workspace_bytes.restype = ctypes.c_size_t
+    lib.omniattn_gqa_workspace_bytes.argtypes = [ctypes.POINTER(Gqa)]
+    lib.omniattn_gqa_decode.restype = ctypes.c_int
+    lib.omniattn_gqa_decode.argtypes = [ctypes.POINTER(Gqa), P, ctypes.c_int64] + [P] * 10 + [ctypes.c_size_t, P]
     lib.omniattn_strerror.restype = ctypes.c_char_p
     lib.omniattn_strerror.argtypes = [ctypes.c_int]
     lib.omniattn_last_hip_error.restype = ctypes.c_char_p
@@ -353,3 +381,139 @@ def decode(q, kv_cache, kv_scales, page_table, seq_lens_host, sink, window, soft
         ws = torch.empty(plan.workspace_bytes, dtype=torch.uint8, device=q.device)
     omniattn_decode(plan, q, kv_cache, kv_scales, page_table, out, lse, ws)
     return out, lse, plan
+
+
+@functools.lru_cache(maxsize=64)
+def _table_record(batch, max_pages, stride, max_tokens, num_pages):
+    """The record that the library reads (and does not keep or change) on every call for a pool and its tables."""
+    return ctypes.pointer(Table(batch, 128, max_pages, max_tokens, stride, num_pages))
+
+
+@functools.lru_cache(maxsize=256)
+def _gqa_record(batch, num_queries, num_q_heads, num_kv_heads, head_dim, page_size, scale_tokens, max_pages, stride, num_pages, sink, window,
+                softmax_scale, out_dtype):
+    return ctypes.pointer(Gqa(batch, num_queries, num_q_heads, num_kv_heads, head_dim, page_size, scale_tokens, max_pages, stride, num_pages,
+                              sink, window, softmax_scale, out_dtype))
+
+
+def _want(ok, what):
+    if not ok:
+        raise OmniAttnError(-1, what)
+
+
+def _ints(t, n, name):
+    """A contiguous int32 CUDA tensor of n elements."""
+    import torch
+    _want(t.dtype is torch.int32 and t.is_cuda and t.is_contiguous() and t.numel() == n, f"{name}: int32 CUDA tensor of {n} elements wanted")
+    return t.data_ptr()
+
+
+def _table(page_table, batch, num_pages, max_tokens):
+    import torch
+    _want(page_table.dtype is torch.int32 and page_table.is_cuda and page_table.dim() == 2 and page_table.shape[0] == batch
+          and page_table.stride(1) == 1, "page_table: int32 CUDA tensor [batch, pages] wanted, its rows contiguous")
+    return _table_record(batch, page_table.shape[1], page_table.stride(0), max_tokens, num_pages)
+
+
+def omniattn_table_extend(seq_lens, new_lens, free_pages, free_count, page_table, seq_lens_out, free_count_out, q_start, slot_map, stream=None):
+    """Tables of one step on the GPU: every request grows by its new tokens and takes pages from the stack of free ones (all int32
+    CUDA tensors; page_table, seq_lens_out, free_count_out, q_start [batch + 1] and slot_map are written).  seq_lens_out may be
+    seq_lens, free_count_out may be free_count.  A request that does not fit keeps its length and gets slots -1."""
+    batch, tokens = seq_lens.shape[0], slot_map.shape[0]
+    rec = _table(page_table, batch, free_pages.shape[0], tokens)
+    _check(load_library().omniattn_table_extend(
+        rec, _ints(seq_lens, batch, "seq_lens"), _ints(new_lens, batch, "new_lens"), _ints(free_pages, free_pages.shape[0], "free_pages"),
+        _ints(free_count, 1, "free_count"), page_table.data_ptr(), _ints(seq_lens_out, batch, "seq_lens_out"),
+        _ints(free_count_out, 1, "free_count_out"), _ints(q_start, batch + 1, "q_start"), _ints(slot_map, tokens, "slot_map"),
+        _current_stream() if stream is None else stream.cuda_stream))
+
+
+def omniattn_table_release(seq_lens, done, page_table, free_pages, free_count, stream=None):
+    """Pages of the requests with done[b] != 0 go back on the stack, their lengths become 0 (seq_lens, free_pages and free_count
+    change in place)."""
+    batch = seq_lens.shape[0]
+    rec = _table(page_table, batch, free_pages.shape[0], 0)
+    _check(load_library().omniattn_table_release(
+        rec, _ints(done, batch, "done"), _ints(seq_lens, batch, "seq_lens"), page_table.data_ptr(), _ints(free_pages, free_pages.shape[0], "free_pages"),
+        _ints(free_count, 1, "free_count"), _current_stream() if stream is None else stream.cuda_stream))
+
+
+def _cache_shape(k_cache, v_cache, k_scales, v_scales):
+    """(pages, KV heads, page size, head width, tokens to a scale) of a layer's cache."""
+    import torch
+    shape, scales = k_cache.shape, k_scales.shape
+    _want(len(shape) == 4 and len(scales) == 3 and scales[:2] == shape[:2] and v_cache.shape == shape and v_scales.shape == scales,
+          "cache [pages, KV heads, 128, head width] with scales [pages, KV heads, 128 / tokens] wanted, for K and V alike")
+    _want(k_cache.dtype is torch.float8_e4m3fn and v_cache.dtype is torch.float8_e4m3fn and k_scales.dtype is torch.float32
+          and v_scales.dtype is torch.float32, "cache of float8_e4m3fn with scales of float32 wanted")
+    _want(k_cache.is_contiguous() and v_cache.is_contiguous() and k_scales.is_contiguous() and v_scales.is_contiguous()
+          and k_cache.is_cuda and v_cache.is_cuda and k_scales.is_cuda and v_scales.is_cuda, "cache and scales: contiguous CUDA tensors wanted")
+    _want(scales[2] > 0 and shape[2] % scales[2] == 0, "scales: they divide a page")
+    return shape[0], shape[1], shape[2], shape[3], shape[2] // scales[2]
+
+
+def _rows_of(t, heads, dim, name):
+    """Address and token stride of bf16 rows [tokens, heads, dim]."""
+    import torch
+    _want(t.dtype is torch.bfloat16 and t.is_cuda and t.dim() == 3 and t.shape[1] == heads and t.shape[2] == dim
+          and t.stride(2) == 1 and (t.stride(1) == dim or heads == 1), f"{name}: bf16 CUDA tensor [tokens, {heads}, {dim}] wanted, a token's rows contiguous")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else heads * dim)
+
+
+def omniattn_gqa_append(k_new, v_new, slot_map, k_cache, v_cache, k_scales, v_scales, stream=None):
+    """New K and V rows (bf16 [tokens, KV heads, head width], any token stride) to their slots in a layer's cache, rounded to e4m3
+    with a scale for each block of tokens and head.  k_cache, v_cache, k_scales and v_scales are written."""
+    pages, heads, page, dim, tokens = _cache_shape(k_cache, v_cache, k_scales, v_scales)
+    n = slot_map.shape[0]
+    _want(k_new.shape[0] == n and v_new.shape[0] == n, "k_new, v_new and slot_map: as many tokens wanted")
+    k, k_stride = _rows_of(k_new, heads, dim, "k_new")
+    v, v_stride = _rows_of(v_new, heads, dim, "v_new")
+    rec = _gqa_record(1, 0, heads, heads, dim, page, tokens, 1, 1, pages, 0, 0, 1.0, BF16)
+    _check(load_library().omniattn_gqa_append(
+        rec, n, k, k_stride, v, v_stride, _ints(slot_map, n, "slot_map"), k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(),
+        v_scales.data_ptr(), _current_stream() if stream is None else stream.cuda_stream))
+
+
+def omniattn_gqa_workspace_bytes(batch, num_queries, num_q_heads, num_kv_heads, head_dim):
+    """Bytes of workspace that omniattn_gqa_decode needs for such a call on the current device."""
+    rec = _gqa_record(batch, num_queries, num_q_heads, num_kv_heads, head_dim, 128, 128, 1, 1, 1, 0, 0, 1.0, BF16)
+    n = int(load_library().omniattn_gqa_workspace_bytes(rec))
+    _want(n > 0, "no valid problem, or no GPU")
+    return n
+
+
+def omniattn_gqa_decode(q, k_cache, v_cache, k_scales, v_scales, page_table, seq_lens, q_start, out, lse, workspace, *, sink, window,
+                        softmax_scale, stream=None):
+    """Attention of the query tokens q (bf16 [tokens, query heads, head width], any token stride) over a layer's cache.  q_start (int32
+    [batch + 1]): request b's queries are tokens q_start[b] .. q_start[b + 1], the last ones of its seq_lens[b]; None: one each.
+    out (bf16 or fp32, shaped like q) and lse (fp32 [tokens, query heads]) are written."""
+    import torch
+    pages, heads, page, dim, tokens = _cache_shape(k_cache, v_cache, k_scales, v_scales)
+    batch, n, q_heads = seq_lens.shape[0], q.shape[0], q.shape[1]
+    src, q_stride = _rows_of(q, q_heads, dim, "q")
+    _want(page_table.dtype is torch.int32 and page_table.is_cuda and page_table.dim() == 2 and page_table.shape[0] == batch
+          and page_table.stride(1) == 1, "page_table: int32 CUDA tensor [batch, pages] wanted, its rows contiguous")
+    _want((out.dtype is torch.bfloat16 or out.dtype is torch.float32) and out.shape == q.shape and out.is_contiguous() and out.is_cuda,
+          "out: contiguous bf16 or fp32 CUDA tensor shaped like q wanted")
+    _want(lse.dtype is torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous() and lse.is_cuda, "lse: contiguous fp32 CUDA tensor [tokens, query heads] wanted")
+    rec = _gqa_record(batch, n, q_heads, heads, dim, page, tokens, page_table.shape[1], page_table.stride(0), pages, operator.index(sink),
+                      operator.index(window), float(softmax_scale), FP32 if out.dtype is torch.float32 else BF16)
+    _check(load_library().omniattn_gqa_decode(
+        rec, src, q_stride, k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), page_table.data_ptr(),
+        _ints(seq_lens, batch, "seq_lens"), _ints(q_start, batch + 1, "q_start") if q_start is not None else None, out.data_ptr(), lse.data_ptr(),
+        _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0,
+        _current_stream() if stream is None else stream.cuda_stream))
+
+
+def gqa_decode(q, k_cache, v_cache, k_scales, v_scales, page_table, seq_lens, sink, window, softmax_scale, q_start=None, out_dtype=None):
+    """Convenience wrapper of omniattn_gqa_decode: allocates results and workspace with torch.  Returns (out, lse)."""
+    import torch
+    if not q.is_cuda:
+        raise OmniAttnError(-4, "omniattn runs on the GPU only: tensors must be CUDA tensors")
+    out = torch.empty(q.shape, dtype=torch.bfloat16 if out_dtype is None else out_dtype, device=q.device)
+    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    size = omniattn_gqa_workspace_bytes(seq_lens.shape[0], q.shape[0], q.shape[1], k_cache.shape[1], q.shape[2])
+    workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+    omniattn_gqa_decode(q, k_cache, v_cache, k_scales, v_scales, page_table, seq_lens, q_start, out, lse, workspace, sink=sink, window=window,
+                        softmax_scale=softmax_scale)
+    return out, lse

@@ -6,8 +6,9 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libomniattn.so")
-SOURCES = ["decode_kernels.hip", "decode_mid_kernel.hip", "decode_narrow_kernel.hip", "append_kernels.hip", "api.cpp", "plan.cpp"]
-HEADERS = ["kernels.h", "plan.h", "decode_common.h", os.path.join("..", "..", "include", "omniattn.h")]
+SOURCES = ["decode_kernels.hip", "decode_mid_kernel.hip", "decode_narrow_kernel.hip", "append_kernels.hip",
+           "table_kernels.hip", "gqa_append_kernel.hip", "gqa_decode_kernel.hip", "api.cpp", "api_gqa.cpp", "plan.cpp"]
+HEADERS = ["kernels.h", "gqa.h", "plan.h", "decode_common.h", os.path.join("..", "..", "include", "omniattn.h")]
 
 
 def hipcc():
@@ -73,7 +74,8 @@ def check_generated_code(verbose=False):
     with tempfile.TemporaryDirectory() as tmp:
         for src, kernel, builtins in (("decode_kernels.hip", "decode_kernel", False),
                                       ("decode_mid_kernel.hip", "decode_mid_kernel", True),
-                                      ("decode_narrow_kernel.hip", "decode_narrow_kernel", False)):
+                                      ("decode_narrow_kernel.hip", "decode_narrow_kernel", False),
+                                      ("gqa_decode_kernel.hip", "gqa_decode_kernel", True)):
             out = os.path.join(tmp, src + ".s")
             cmd = [hipcc(), "--offload-arch=gfx950", "-O3", "-std=c++20",
                    "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

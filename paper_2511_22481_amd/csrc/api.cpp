@@ -11,6 +11,7 @@
 #include <new>
 #include <string>
 
+#include "gqa.h"
 #include "kernels.h"
 #include "plan.h"
 
@@ -50,15 +51,18 @@ struct omniattn_plan_s {
 
 static __device__ __align__(256) unsigned char scratch[OMNIATTN_STATIC_SCRATCH_BYTES];
 
-namespace {
+static thread_local std::string g_hip_error;
 
-thread_local std::string g_hip_error;
-
-int hip_fail(hipError_t e, const char* what) {
-  g_hip_error = std::string(what) + ": " + hipGetErrorString(e);
+int omniattn::hip_fail(hipError_t e, const char* what) {
+  try {
+    g_hip_error = std::string(what) + ": " + hipGetErrorString(e);
+  } catch (...) {  // (no memory for the text)
+  }
   (void)hipGetLastError();  // clear the sticky "last error" so later calls are not blamed
   return OMNIATTN_EHIP;
 }
+
+namespace {
 
 #define OA_HIP(call)                                  \
   do {                                                \

@@ -1,0 +1,659 @@
+// Attention of grouped-query layers over the paged 8-bit cache.
+//
+// Query token t of a request with L tokens, n of them new, sees the keys j < L - n + t + 1 that the compression rule
+// keeps (j < S, or among the last W of them): out = sum_j p_j v_j / sum_j p_j, p_j = exp(scale q.k_j), lse = ln sum p_j.
+//
+// Work.  The query rows (t, head of the group) of one (request, KV head) are cut into blocks of 16, 32 or 64; a block
+// reads the pages that hold kept tokens.  All (block, page) pairs of the call, in order of request, KV head and block,
+// are dealt out evenly: work group u of U takes pairs [u T / U, (u + 1) T / U).  Every work group finds its share by
+// itself from the lengths on the device, so the host needs to know nothing but the sizes of the arrays.  A block whose
+// pages went to several groups leaves one partial row each, which gqa_combine_kernel joins.
+//
+// A page.  The four waves take 32 of its 128 tokens each and keep a running maximum, sum and output of their own; they meet
+// only at the end of a block's share.  K rows come from memory in the operand order of S^T = K Q^T (16x16x32 bf16 matrix
+// instructions; an e4m3 code is exact in bf16), V rows as 8 tokens x D/16 columns per lane, which a byte permutation turns
+// into the operand of O^T += V^T P^T (f16: exact for the codes, and 2^-11 relative for the weights, which the reference
+// scales into [0, 2^15]).  The contraction's order of tokens is free, so P^T is what S^T's layout already gives each lane.
+// No LDS and no barrier in the loop.  A block's scale is one number per wave and page: K's goes into the softmax factor,
+// V's multiplies the page's product when it is added.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "decode_common.h"
+#include "gqa.h"
+
+namespace omniattn {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+
+constexpr int kThreads = 256;
+constexpr int kWaveTokens = 32;
+// Weights are 2^(s - m + kLift) for the reference m, which a logit (log2) may exceed by kSlack before it is raised: the largest
+// weight is at most 2^15 (f16 holds 65504), and weights keep full precision down to 2^-25 of the largest.
+constexpr float kLift = 11.f, kSlack = 4.f;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// What a request brings: its tokens, its first query token and how many it has.
+struct Request {
+  int L, begin, n;
+};
+__device__ __forceinline__ Request request_of(const GqaDecodeParams& p, int b) {
+  Request r;
+  r.L = min(max(p.seq_lens[b], 0), p.max_pages * kPage);
+  const int lo = p.q_start ? p.q_start[b] : b, hi = p.q_start ? p.q_start[b + 1] : b + 1;
+  r.begin = min(max(lo, 0), p.num_queries);
+  r.n = min(max(hi, r.begin), p.num_queries) - r.begin;
+  return r;
+}
+// Pages of a block of query rows: the union of its queries' kept sets.
+struct Block {
+  int t0, t1;  // its query tokens, both included
+  TileLayout pages;
+  __device__ __forceinline__ int units() const { return max(pages.count(), 1); }  // (nothing kept: one, for the empty result)
+};
+template <int ROWS>
+__device__ __forceinline__ Block block_of(const GqaDecodeParams& p, const Request& r, int rb) {
+  Block k;
+  k.t0 = rb * ROWS / p.group;
+  k.t1 = min(r.n - 1, ((rb + 1) * ROWS - 1) / p.group);
+  k.pages = tile_layout(r.L - r.n + k.t1 + 1, p.S, p.W > 0 ? p.W + (k.t1 - k.t0) : 0, kPage);
+  return k;
+}
+template <int ROWS>
+__device__ __forceinline__ int blocks_of(const GqaDecodeParams& p, const Request& r) {
+  return (int)(((int64_t)r.n * p.group + ROWS - 1) / ROWS);
+}
+// (block, page) pairs of one KV head of a request
+template <int ROWS>
+__device__ __forceinline__ int64_t cost_of(const GqaDecodeParams& p, const Request& r) {
+  const int blocks = blocks_of<ROWS>(p, r);
+  int64_t sum = 0;
+  for (int rb = 0; rb < blocks; ++rb) sum += block_of<ROWS>(p, r, rb).units();
+  return sum;
+}
+
+__device__ __forceinline__ float row_max(float x) {  // over the four lanes that hold tokens of the same row
+  float y = x;
+  swap16(x, y);
+  x = fmaxf(x, y);
+  y = x;
+  swap32(x, y);
+  return fmaxf(x, y);
+}
+__device__ __forceinline__ float row_sum(float x) {
+  float y = x;
+  swap16(x, y);
+  x += y;
+  y = x;
+  swap32(x, y);
+  return x + y;
+}
+
+// Two tokens' codes of four columns (a word each) as f16 pairs, one column's two tokens to a word.
+__device__ __forceinline__ uint32_t f16_pair(uint32_t w, bool upper) {
+  return upper ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, true))
+               : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, false));
+}
+__device__ __forceinline__ uint32_t bf16_pair(uint32_t w, bool upper) {
+  return upper ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.0f, true))
+               : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.0f, false));
+}
+
+// Codes of one (page, KV head): `bytes` of them may be read, behind that the loads return zeros and touch no memory.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t codes_at(const uint8_t* base, uint32_t bytes) {
+  const uint64_t a = uniform64((uint64_t)(uintptr_t)base);
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(uintptr_t)a, 0, (int)__builtin_amdgcn_readfirstlane(bytes), 0x00027000);
+}
+
+template <int D, int RT, bool OUT32>
+struct Gqa {
+  static constexpr int kRows = 16 * RT;
+  static constexpr int kCols = D / 16;    // columns of V per lane
+  static constexpr int kWords = D / 64;   // 64-byte pieces of a K row; also words of V per lane and token
+  static constexpr int kOStride = D + 4;  // floats of a row in LDS
+  static constexpr size_t kLds = (size_t)4 * kRows * kOStride * 4 + 2 * 4 * kRows * 8;
+};
+
+template <int WORDS>
+struct VWord { typedef u32x4 type; };
+template <>
+struct VWord<1> { typedef uint32_t type; };
+template <>
+struct VWord<2> { typedef u32x2 type; };
+
+template <int D>
+struct Tile {
+  static constexpr int kWords = D / 64;
+  u32x4 k[2][kWords];                     // [16-token half][64-byte piece]
+  typename VWord<kWords>::type v[8];      // [token of the lane]
+};
+
+template <int WORDS>
+__device__ __forceinline__ uint32_t word(const typename VWord<WORDS>::type& v, int i) {
+  if constexpr (WORDS == 1) return v;
+  else return v[i];
+}
+
+template <int D>
+__device__ __forceinline__ void load_k(Tile<D>& t, __amdgpu_buffer_rsrc_t rsrc, int at) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c)
+      t.k[h][c] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at + h * 16 * D + c * 64, 0, 0));
+}
+template <int D>
+__device__ __forceinline__ void load_v(Tile<D>& t, __amdgpu_buffer_rsrc_t rsrc, int at) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int off = at + (j < 4 ? j : 12 + j) * D;
+    if constexpr (D == 64) t.v[j] = __builtin_amdgcn_raw_buffer_load_b32(rsrc, off, 0, 0);
+    else if constexpr (D == 128) t.v[j] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rsrc, off, 0, 0));
+    else t.v[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, 0, 0));
+  }
+}
+
+// Whether one of four codes is NaN (0x7f or 0xff).
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
+template <int D, int RT, bool OUT32>
+__global__ __launch_bounds__(kThreads, RT * D <= 128 ? 2 : 1) void gqa_decode_kernel(GqaDecodeParams p) {
+  using C = Gqa<D, RT, OUT32>;
+  constexpr int R = C::kRows, kCols = C::kCols, kWords = C::kWords;
+  extern __shared__ __align__(16) float lds[];
+  float* const o_lds = lds;                                    // [4 waves][R][kOStride]
+  float2* const ml_lds = (float2*)(lds + 4 * R * C::kOStride); // [2][4 waves][R]
+  __shared__ int64_t ends[kThreads];
+  __shared__ int64_t wave_tot[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n16 = lane & 15, g = lane >> 4;
+
+  // Share of this work group: running sum of the pairs over the batch, a run of requests per thread.
+  const int per = (p.batch + kThreads - 1) / kThreads;
+  {
+    int64_t sum = 0;
+    for (int i = 0; i < per; ++i) {
+      const int b = tid * per + i;
+      if (b < p.batch) sum += cost_of<R>(p, request_of(p, b)) * p.kv_heads;
+    }
+    for (int d = 1; d < 64; d *= 2) {
+      const int64_t y = __shfl_up(sum, d);
+      if (lane >= d) sum += y;
+    }
+    if (lane == 63) wave_tot[wave] = sum;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) sum += wave_tot[w];
+    ends[tid] = sum;
+    __syncthreads();
+  }
+  const int64_t T = ends[kThreads - 1];
+  const int64_t U = min((int64_t)gridDim.x, T);
+  if ((int64_t)blockIdx.x >= U) return;
+  int64_t at = (int64_t)blockIdx.x * T / U;
+  const int64_t stop = (int64_t)(blockIdx.x + 1) * T / U;
+  // the request, KV head and block that pair `at` belongs to
+  int b, h, rb;
+  int64_t first;  // first pair of the block
+  Request rq;
+  Block bk;
+  {
+    int lo = 0, hi = kThreads - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (ends[mid] > at) hi = mid;
+      else lo = mid + 1;
+    }
+    first = lo ? ends[lo - 1] : 0;
+    b = __builtin_amdgcn_readfirstlane(lo * per);
+    int64_t cost;
+    for (;; ++b) {
+      rq = request_of(p, b);
+      cost = cost_of<R>(p, rq);
+      if (at < first + cost * p.kv_heads) break;
+      first += cost * p.kv_heads;
+    }
+    h = (int)((at - first) / cost);
+    first += h * cost;
+    for (rb = 0;; ++rb) {
+      bk = block_of<R>(p, rq, rb);
+      if (at < first + bk.units()) break;
+      first += bk.units();
+    }
+  }
+  const size_t head_bytes = (size_t)kPage * D;
+  const int k_at = (wave * kWaveTokens + n16) * D + g * 16;
+  const int v_at = (wave * kWaveTokens + 4 * g) * D + n16 * kCols;
+  const int blocks_per_page = kPage >> p.scale_shift, my_block = (wave * kWaveTokens) >> p.scale_shift;
+  int parity = 0, first_partial = 0;  // first_partial: 1 once this work group has left its first block behind
+
+  while (true) {
+    const int64_t end = min(stop, first + bk.units());
+    const int tile_lo = (int)(at - first), tile_hi = min((int)(end - first), bk.pages.count());
+    const bool whole = at == first && end == first + bk.units();
+
+    // Query rows of the block: lane n16 of every group of 16 holds one row of each row tile, the columns that its K
+    // loads bring.  Rows past the last hold zeros.
+    bf16x8 q[RT][2 * kWords];
+    int reach[RT];  // tokens that the row's query sees
+    const int rows_left = (int)min((int64_t)rq.n * p.group - (int64_t)rb * R, (int64_t)R);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int row = rt * 16 + n16;
+      const int t = (rb * R + row) / p.group, gi = (rb * R + row) - t * p.group;
+      const bool valid = row < rows_left;
+      reach[rt] = valid ? rq.L - rq.n + t + 1 : 0;
+      const uint16_t* src = p.q + (int64_t)(rq.begin + t) * p.q_stride + (size_t)(h * p.group + gi) * D + g * 16;
+#pragma unroll
+      for (int c = 0; c < kWords; ++c) {
+        q[rt][2 * c] = valid ? *(const bf16x8*)(src + c * 64) : bf16x8{};
+        q[rt][2 * c + 1] = valid ? *(const bf16x8*)(src + c * 64 + 8) : bf16x8{};
+      }
+    }
+    const int reach_lo = rq.L - rq.n + bk.t0 + 1, reach_hi = rq.L - rq.n + bk.t1 + 1;
+
+    f32x4 o[RT][kCols];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      m[rt] = -INFINITY;
+      l[rt] = 0.f;
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) o[rt][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    if (tile_lo < tile_hi) {
+      const int32_t* table = p.page_table + b * p.table_stride;
+      // pages of up to 64 tiles at a time, one per lane
+      int held = tile_lo;
+      int ids = table[bk.pages.logical(min(held + lane, tile_hi - 1))];
+      Tile<D> t;
+      float ks, vs;
+      auto request = [&](int tile, __amdgpu_buffer_rsrc_t& rk, __amdgpu_buffer_rsrc_t& rv, float& ks_, float& vs_) {
+        if (tile - held >= 64) {
+          held = tile;
+          ids = table[bk.pages.logical(min(held + lane, tile_hi - 1))];
+        }
+        const int page = __builtin_amdgcn_readlane(ids, tile - held);
+        const size_t ph = (size_t)page * p.kv_heads + h;
+        const int live = min(reach_hi - bk.pages.logical(tile) * kPage, kPage);
+        rk = codes_at(p.k_cache + ph * head_bytes, live * D);
+        rv = codes_at(p.v_cache + ph * head_bytes, live * D);
+        ks_ = p.k_scales[ph * blocks_per_page + my_block];
+        vs_ = p.v_scales[ph * blocks_per_page + my_block];
+      };
+      __amdgpu_buffer_rsrc_t rk, rv;
+      request(tile_lo, rk, rv, ks, vs);
+      load_k<D>(t, rk, k_at);
+      load_v<D>(t, rv, v_at);
+      for (int tile = tile_lo; tile < tile_hi; ++tile) {
+        const int pos0 = bk.pages.logical(tile) * kPage + wave * kWaveTokens;
+        // every query sees and keeps all 32 tokens
+        const bool full = pos0 + kWaveTokens <= reach_lo && (pos0 + kWaveTokens <= p.S || pos0 >= reach_hi - p.W);
+        // S^T of the wave's tokens: lane (n16, g) has tokens 16 h2 + 4 g + i of row n16
+        f32x4 s[RT][2];
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2) {
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) s[rt][h2] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int c = 0; c < kWords; ++c)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              u32x4 w;
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                w[2 * i] = bf16_pair(t.k[h2][c][2 * u + i], false);
+                w[2 * i + 1] = bf16_pair(t.k[h2][c][2 * u + i], true);
+              }
+#pragma unroll
+              for (int rt = 0; rt < RT; ++rt)
+                s[rt][h2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), q[rt][2 * c + u], s[rt][h2], 0, 0, 0);
+            }
+        }
+        const float factor = p.scale_log2 * ks;
+        // (the scale of a block without kept tokens may be anything)
+        const bool some = pos0 < reach_hi && (pos0 < p.S || (p.W > 0 && pos0 + kWaveTokens > reach_lo - p.W));
+        const float v_scale = some ? vs : 0.f;
+        const bool more = tile + 1 < tile_hi;
+        if (more) {
+          request(tile + 1, rk, rv, ks, vs);
+          load_k<D>(t, rk, k_at);
+        }
+        f16x8 w_hi[RT], w_lo[RT];
+        uint32_t keep_bits = 0;  // tokens (of the lane's 8) that its row tile's row keeps, 8 bits a row tile
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = s[rt][i / 4][i % 4] * factor;
+          if (!full) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int pos = pos0 + 16 * (i / 4) + 4 * g + i % 4;
+              const bool keep = retained(pos, reach[rt], p.S, p.W);
+              x[i] = keep ? x[i] : -INFINITY;
+              keep_bits |= (keep ? 1u : 0u) << (8 * rt + i);
+            }
+          }
+          float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+          if (__any(top > m[rt] + kSlack)) {
+            top = row_max(top);
+            const float next = top > m[rt] + kSlack ? top : m[rt];
+            const float shrink = next == m[rt] ? 1.f : exp2_fast(m[rt] - next);
+            m[rt] = next;
+            l[rt] *= shrink;
+#pragma unroll
+            for (int c = 0; c < kCols; ++c)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[rt][c][i] *= shrink;
+          }
+          // (a row that has kept nothing so far has reference -inf, and only masked logits)
+          const float ref = m[rt] == -INFINITY ? 0.f : m[rt] - kLift;
+          float w[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            w[i] = exp2_fast(x[i] - ref);
+            w_hi[rt][i] = (_Float16)w[i];
+            if constexpr (OUT32) w_lo[rt][i] = (_Float16)(w[i] - (float)w_hi[rt][i]);
+          }
+          l[rt] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+        }
+        uint32_t seen_nan = 0;
+        if (!full) {
+          // tokens that no row of the block keeps may hold anything
+          uint32_t any_nan = 0;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int pos = pos0 + (j < 4 ? 0 : 16) + 4 * g + j % 4;
+            const bool keep = pos < reach_hi && (pos < p.S || (p.W > 0 && pos >= reach_lo - p.W));
+            if (!keep) t.v[j] = typename VWord<kWords>::type{};
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) any_nan |= nan_codes(word<kWords>(t.v[j], i));
+          }
+          if (bk.t1 > bk.t0) seen_nan = __ballot(any_nan != 0) != 0;
+        }
+#pragma unroll
+        for (int wd = 0; wd < kWords; ++wd) {
+          uint32_t pair[2][4];  // [lower or upper two columns][tokens 2 j, 2 j + 1]
+          uint32_t nans[2][4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t a = word<kWords>(t.v[2 * j], wd), c = word<kWords>(t.v[2 * j + 1], wd);
+            pair[0][j] = __builtin_amdgcn_perm(c, a, 0x05010400);
+            pair[1][j] = __builtin_amdgcn_perm(c, a, 0x07030602);
+          }
+#pragma unroll
+          for (int col = 0; col < 4; ++col) {
+            u32x4 f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[j] = f16_pair(pair[col / 2][j], col % 2);
+            f16x8 vt = __builtin_bit_cast(f16x8, f);
+            f16x8 bad = {};
+            if (seen_nan) {
+              // NaN in a value row reaches the rows that keep the token, and only those
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                const bool is = vt[j] != vt[j];
+                bad[j] = is ? (_Float16)1.f : (_Float16)0.f;
+                vt[j] = is ? (_Float16)0.f : vt[j];
+              }
+            }
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+              f32x4 part = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, w_hi[rt], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+              if constexpr (OUT32) part = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, w_lo[rt], part, 0, 0, 0);
+              if (seen_nan) {
+                f16x8 kept;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) kept[j] = (keep_bits >> (8 * rt + j)) & 1 ? (_Float16)1.f : (_Float16)0.f;
+                const f32x4 hits = __builtin_amdgcn_mfma_f32_16x16x32_f16(bad, kept, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) part[i] = hits[i] > 0.f ? NAN : part[i];
+              }
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[rt][4 * wd + col][i] = fmaf(part[i], v_scale, o[rt][4 * wd + col][i]);
+            }
+          }
+        }
+        if (more) load_v<D>(t, rv, v_at);
+      }
+    }
+
+    // The waves' shares meet: reference and sum first, then the outputs at the common reference.
+    float2* const ml = ml_lds + parity * 4 * R;
+    parity ^= 1;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      l[rt] = row_sum(l[rt]);
+      if (g == 0) ml[wave * R + rt * 16 + n16] = make_float2(m[rt], l[rt]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w * R + rt * 16 + n16].x);
+      // (a wave that kept nothing has zeros, or NaN that has to stay: nothing is skipped)
+      const float shrink = m[rt] == top ? 1.f : exp2_fast(m[rt] - top);
+      float* const dst = o_lds + (wave * R + rt * 16 + n16) * C::kOStride;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < kCols; c += 4)
+          *(f32x4*)(dst + (4 * g + i) * kCols + c) =
+              f32x4{o[rt][c][i] * shrink, o[rt][c + 1][i] * shrink, o[rt][c + 2][i] * shrink, o[rt][c + 3][i] * shrink};
+    }
+    __syncthreads();
+    const int slot = 2 * blockIdx.x + first_partial;
+    constexpr int kChunks = D / 8;
+    for (int k = tid; k < rows_left * kChunks; k += kThreads) {
+      const int row = k / kChunks, col = k % kChunks * 8;
+      f32x4 a = {0.f, 0.f, 0.f, 0.f}, c = a;
+      float top = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w * R + row].x);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float2 e = ml[w * R + row];
+        sum += e.y * (e.x == top ? 1.f : exp2_fast(e.x - top));
+        const f32x4* src = (const f32x4*)(o_lds + (w * R + row) * C::kOStride + col);
+        a += src[0];
+        c += src[1];
+      }
+      const int t = (rb * R + row) / p.group, gi = (rb * R + row) - t * p.group;
+      const int64_t out_row = (int64_t)(rq.begin + t) * p.q_heads + h * p.group + gi;
+      if (whole) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;  // (nothing kept: 0 and -inf)
+        if constexpr (OUT32) {
+          f32x4* dst = (f32x4*)((float*)p.out + out_row * D + col);
+          dst[0] = a * inv;
+          dst[1] = c * inv;
+        } else {
+          bf16x8 y;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            y[i] = (__bf16)(a[i] * inv);
+            y[4 + i] = (__bf16)(c[i] * inv);
+          }
+          *(bf16x8*)((uint16_t*)p.out + out_row * D + col) = y;
+        }
+        if (col == 0) {
+          p.lse[out_row] = sum == 0.f ? -INFINITY : (top + __log2f(sum) - kLift) * 0.69314718055994531f;
+          p.rows[out_row] = make_int2(0, 0);
+        }
+      } else {
+        float* dst = p.part_o + ((size_t)slot * R + row) * D + col;
+        ((f32x4*)dst)[0] = a;
+        ((f32x4*)dst)[1] = c;
+        if (col == 0) {
+          p.part_ml[(size_t)slot * R + row] = make_float2(top, sum);
+          if (at == first) {
+            // the work group that takes a block's first pair knows which ones take the others
+            const int64_t last = ((first + bk.units()) * U + T - 1) / T - 1;
+            p.rows[out_row] = make_int2(slot, (int)(last - blockIdx.x + 1) * 64 + row);
+          }
+        }
+      }
+    }
+    first_partial = 1;
+    at = end;
+    if (at >= stop) break;
+    // next block
+    first += bk.units();
+    if (++rb == blocks_of<R>(p, rq)) {
+      rb = 0;
+      if (++h == p.kv_heads) {
+        h = 0;
+        do rq = request_of(p, ++b);
+        while (rq.n == 0);
+      }
+    }
+    bk = block_of<R>(p, rq, rb);
+  }
+}
+
+// Joins the partial rows of blocks whose pages went to several work groups: sum_i 2^(m_i - m) (o_i, l_i).  Partial i of a
+// row lies in the slot of the i-th work group: the first one may have had another block before (slot 2 u + 1), the others
+// begin with this one (2 u).  WAVES waves share a row, each every WAVES-th partial.
+template <int D, bool OUT32, int WAVES>
+__global__ __launch_bounds__(256) void gqa_combine_kernel(GqaDecodeParams p, int block_rows, int units) {
+  constexpr int kPer = D / 64;  // columns per lane
+  typedef __attribute__((ext_vector_type(kPer))) float vec;
+  __shared__ float sh_o[WAVES > 1 ? 4 : 1][WAVES > 1 ? D : 1];
+  __shared__ float2 sh_ml[4];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * (4 / WAVES) + wave / WAVES;
+  if (row >= (int64_t)p.num_queries * p.q_heads) return;
+  // (rows of no request: nothing was written for them)
+  if (p.q_start && (row / p.q_heads < p.q_start[0] || row / p.q_heads >= p.q_start[p.batch])) return;
+  const int2 d = p.rows[row];
+  const int count = __builtin_amdgcn_readfirstlane(d.y / 64), in_block = d.y % 64;
+  if (count <= 0 || d.x < 0 || d.x / 2 + count > units) return;
+  const int u0 = d.x / 2;
+  float m = -INFINITY, l = 0.f;
+  vec o = {};
+  constexpr int kBatch = 8;
+  for (int i0 = wave % WAVES; i0 < count; i0 += kBatch * WAVES) {
+    float2 e[kBatch];
+    vec x[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int i = min(i0 + k * WAVES, count - 1);
+      const size_t slot = i == 0 ? d.x : 2 * (u0 + i);
+      e[k] = p.part_ml[slot * block_rows + in_block];
+      x[k] = *(const vec*)(p.part_o + (slot * block_rows + in_block) * D + lane * kPer);
+    }
+    float top = m;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) top = fmaxf(top, e[k].x);
+    float f = m == top ? 1.f : exp2_fast(m - top);
+    l *= f;
+    o *= f;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k)
+      if (i0 + k * WAVES < count) {
+        f = e[k].x == top ? 1.f : exp2_fast(e[k].x - top);
+        l += f * e[k].y;
+        o += f * x[k];
+      }
+    m = top;
+  }
+  if constexpr (WAVES > 1) {
+    if (lane == 0) sh_ml[wave] = make_float2(m, l);
+    *(vec*)(&sh_o[wave][lane * kPer]) = o;
+    __syncthreads();
+    if (wave) return;
+    float top = m;
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, sh_ml[w].x);
+    float f = m == top ? 1.f : exp2_fast(m - top);
+    l *= f;
+    o *= f;
+    for (int w = 1; w < WAVES; ++w) {
+      f = sh_ml[w].x == top ? 1.f : exp2_fast(sh_ml[w].x - top);
+      l += f * sh_ml[w].y;
+      o += f * *(const vec*)(&sh_o[w][lane * kPer]);
+    }
+    m = top;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if constexpr (OUT32) {
+    *(vec*)((float*)p.out + row * D + lane * kPer) = o * inv;
+  } else {
+    typedef __attribute__((ext_vector_type(kPer))) __bf16 bvec;
+    bvec y;
+    if constexpr (kPer == 1) {
+      ((__bf16*)p.out)[row * D + lane] = (__bf16)(o[0] * inv);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) y[i] = (__bf16)(o[i] * inv);
+      *(bvec*)((uint16_t*)p.out + row * D + lane * kPer) = y;
+    }
+  }
+  if (lane == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + __log2f(l) - kLift) * 0.69314718055994531f;
+}
+
+template <int D, int RT, bool OUT32>
+hipError_t start(const GqaDecodeParams& p, int units, hipStream_t stream) {
+  constexpr size_t lds = Gqa<D, RT, OUT32>::kLds;
+  hipLaunchKernelGGL((gqa_decode_kernel<D, RT, OUT32>), dim3(units), dim3(kThreads), lds, stream, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t rows = (int64_t)p.num_queries * p.q_heads;
+  // Few rows: four waves to a row.
+  if (rows <= 2048) hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 4>), dim3((uint32_t)rows), dim3(256), 0, stream, p, 16 * RT, units);
+  else hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 1>), dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, stream, p, 16 * RT, units);
+  return hipGetLastError();
+}
+
+template <int D, int RT>
+hipError_t allow_lds() {
+  hipError_t e = hipFuncSetAttribute((const void*)gqa_decode_kernel<D, RT, false>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)Gqa<D, RT, false>::kLds);
+  if (e == hipSuccess) e = hipFuncSetAttribute((const void*)gqa_decode_kernel<D, RT, true>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)Gqa<D, RT, true>::kLds);
+  return e;
+}
+
+}  // namespace
+
+GqaShape gqa_shape(int batch, int num_queries, int group, int head_dim) {
+  const int64_t rows = (int64_t)((num_queries + batch - 1) / batch) * group;
+  int rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  if (head_dim == 256 && rt > 2) rt = 2;
+  return GqaShape{rt, rt * head_dim <= 128 ? 2 : 1};
+}
+
+hipError_t init_gqa_kernels() {
+  hipError_t e = allow_lds<64, 1>();
+  if (e == hipSuccess) e = allow_lds<64, 2>();
+  if (e == hipSuccess) e = allow_lds<64, 4>();
+  if (e == hipSuccess) e = allow_lds<128, 1>();
+  if (e == hipSuccess) e = allow_lds<128, 2>();
+  if (e == hipSuccess) e = allow_lds<128, 4>();
+  if (e == hipSuccess) e = allow_lds<256, 1>();
+  if (e == hipSuccess) e = allow_lds<256, 2>();
+  return e;
+}
+
+hipError_t launch_gqa_decode(const GqaDecodeParams& p, const GqaShape& shape, int units, hipStream_t stream) {
+  auto with = [&](auto d, auto rt) {
+    return p.out_fp32 ? start<decltype(d)::value, decltype(rt)::value, true>(p, units, stream)
+                      : start<decltype(d)::value, decltype(rt)::value, false>(p, units, stream);
+  };
+  using std::integral_constant;  // (the kernel variants)
+  auto dims = [&](auto rt) {
+    if (p.head_dim == 64) return with(integral_constant<int, 64>{}, rt);
+    if (p.head_dim == 128) return with(integral_constant<int, 128>{}, rt);
+    if constexpr (decltype(rt)::value <= 2) return with(integral_constant<int, 256>{}, rt);
+    else return hipErrorInvalidValue;
+  };
+  if (shape.row_tiles == 1) return dims(integral_constant<int, 1>{});
+  if (shape.row_tiles == 2) return dims(integral_constant<int, 2>{});
+  return dims(integral_constant<int, 4>{});
+}
+
+}  // namespace omniattn
