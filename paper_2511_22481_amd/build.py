@@ -48,7 +48,7 @@ def build(force=True, verbose=False):
         os.remove(STAMP)
     cmd = [hipcc(), "--offload-arch=gfx950", "-O3", "-std=c++20", "-fPIC", "-shared",
            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-           "-Wno-unused-command-line-argument", "-x", "hip"]
+           "-Wno-unused-command-line-argument", "-parallel-jobs=8", "-x", "hip"]
     cmd += [os.path.join(CSRC, f) for f in SOURCES]
     cmd += ["-o", LIB]
     res = subprocess.run(cmd, capture_output=True, text=True)

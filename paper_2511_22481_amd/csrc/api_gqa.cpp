@@ -76,7 +76,7 @@ Workspace workspace_of(const omniattn_gqa_t* g, const GqaShape& shape, int units
   Workspace w;
   w.rows = 0;
   w.ml = align256((size_t)g->num_queries * g->num_q_heads * sizeof(int2));
-  w.o = w.ml + align256(slots * sizeof(float2));
+  w.o = w.ml + align256(slots * sizeof(float4));
   w.bytes = w.o + slots * g->head_dim * sizeof(float);
   return w;
 }
@@ -203,7 +203,7 @@ int omniattn_gqa_decode(const omniattn_gqa_t* gqa, const void* q, int64_t q_stri
   p.out = out;
   p.lse = lse;
   p.rows = (int2*)((char*)workspace + w.rows);
-  p.part_ml = (float2*)((char*)workspace + w.ml);
+  p.part_ml = (float4*)((char*)workspace + w.ml);
   p.part_o = (float*)((char*)workspace + w.o);
   p.batch = gqa->batch;
   p.num_queries = gqa->num_queries;
@@ -217,10 +217,10 @@ int omniattn_gqa_decode(const omniattn_gqa_t* gqa, const void* q, int64_t q_stri
   p.scale_shift = gqa->scale_tokens == 32 ? 5 : gqa->scale_tokens == 64 ? 6 : 7;
   p.out_fp32 = gqa->out_dtype == OMNIATTN_FP32;
   p.scale_log2 = gqa->softmax_scale * 1.4426950408889634f;
-  // Not more work groups than (block, page) pairs there can be.
+  // Not more work groups than there can be units of work (each block counts 2 beside its pages).
   const int64_t blocks = ((int64_t)p.num_queries * p.group + shape.block_rows() - 1) / shape.block_rows() + p.batch;
   const int64_t pages = std::min<int64_t>(p.max_pages, ((int64_t)p.S + kPage - 1) / kPage + ((int64_t)p.W + shape.block_rows() + kPage - 1) / kPage + 1);
-  units = (int)std::min<int64_t>(units, blocks * p.kv_heads * pages);
+  units = (int)std::min<int64_t>(units, blocks * p.kv_heads * (pages + 2));
   OA_HIP(launch_gqa_decode(p, shape, units, (hipStream_t)hip_stream));
   return OMNIATTN_OK;
 }

@@ -63,14 +63,14 @@ struct GqaDecodeParams {
   void* out;
   float* lse;
   int2* rows;               // per output row: first partial slot; number of partials * 64 + row inside its block (0 partials: done)
-  float2* part_ml;          // [slots, block rows]: reference (log2) and sum of a partial row
+  float4* part_ml;          // [slots, block rows]: a partial row's reference (log2) and sum of weights, and its output's reference
   float* part_o;            // [slots, block rows, head_dim]: weighted sums, not yet divided
   int batch, num_queries, q_heads, kv_heads, group, head_dim;
   int max_pages, S, W, scale_shift;  // scale_shift: log2 of the tokens that share a scale
   int out_fp32;
   float scale_log2;         // softmax_scale * log2(e)
 };
-// Rows of a block (16, 32 or 64) and work groups a compute unit holds, for the average number of query rows per request.
+// Rows of a block (16, 32, 48 or 64) and work groups a compute unit holds, for the average number of query rows per request.
 struct GqaShape {
   int row_tiles, groups_per_cu;
   int block_rows() const { return 16 * row_tiles; }

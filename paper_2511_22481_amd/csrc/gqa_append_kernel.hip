@@ -6,8 +6,10 @@
 // an exact power of two, and only those that become subnormal are rounded again.)  code = e4m3(x / scale), to nearest
 // even; a number that is not finite becomes the NaN code and does not count towards a.
 //
-// One work group takes one (run of tokens in one block, head, K or V): the run's rows stay in registers between the
-// maximum and the rounding, so they are read once.
+// A work group looks through C consecutive tokens of the call for runs (tokens that follow one another in one block) that begin
+// there, for one head and K or V.  A long run is the work of all its waves: the rows stay in registers between the maximum
+// and the rounding, so they are read once.  Runs that fit one pass of a wave (a decode step's single tokens) are dealt out to
+// the waves.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -52,78 +54,145 @@ __device__ __forceinline__ uint32_t recode(uint32_t codes, float ratio) {
   return encode4(a[0] * ratio, a[1] * ratio, b[0] * ratio, b[1] * ratio);
 }
 
-// C: consecutive tokens of the call that a work group looks through for runs that begin there.
+// What a run's block and cache are, for one thread's eight columns.
+struct Run {
+  uint8_t* codes;   // of the run's first token
+  float* scale;
+  int off;          // tokens that the block has before the run
+};
+
+template <int D>
+__device__ __forceinline__ Run run_at(const GqaAppendParams& p, int kv, int head, int slot, int col) {
+  const int page = slot / kPage, in_page = slot % kPage, each = p.scale_tokens;
+  const size_t ph = (size_t)page * p.kv_heads + head;
+  return Run{p.cache[kv] + (ph * kPage + in_page) * D + col, p.scales[kv] + ph * (kPage / each) + in_page / each, slot % each};
+}
+
+// The earlier tokens of a block whose scale has grown; `row` of `rows` threads that share the work by rows.
+template <int D>
+__device__ __forceinline__ void regrow(const Run& run, float old, float scale, int row, int rows) {
+  if (run.off > 0 && scale > old) {
+    const float ratio = old / scale;
+    for (int k = row - run.off; k < 0; k += rows) {
+      u32x2* at = (u32x2*)(run.codes + (ptrdiff_t)k * D);
+      const u32x2 c = *at;
+      *at = u32x2{recode(c[0], ratio), recode(c[1], ratio)};
+    }
+  }
+}
+
+__device__ __forceinline__ uint32_t largest(const u32x4& x) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) top = max(top, max(finite_bits(x[j]), finite_bits(x[j] >> 16)));
+  return top;
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  for (int d = 1; d < 64; d *= 2) x = max(x, (uint32_t)__shfl_xor(x, d));
+  return x;
+}
+
 template <int D>
 __global__ __launch_bounds__(kThreads) void gqa_append_kernel(GqaAppendParams p, int C) {
   constexpr int kPer = D / 8;                // threads that share a row, 8 numbers each
-  constexpr int kRows = kThreads / kPer;     // rows of a pass
+  constexpr int kWaveRows = 64 / kPer;       // rows of a wave's pass: runs up to this long are one wave's
+  constexpr int kRows = kThreads / kPer;     // rows of the work group's pass
   constexpr int kPasses = kPage / kRows;     // a run has up to 128 rows
   __shared__ uint32_t tot[2][4];
-  const int tid = threadIdx.x, row = tid / kPer, col = (tid % kPer) * 8;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int row = tid / kPer, col = (tid % kPer) * 8;
   const int head = blockIdx.x % p.kv_heads, kv = blockIdx.x / p.kv_heads % 2;
-  const int i0 = (int)(blockIdx.x / (2 * p.kv_heads)) * C, i1 = min(i0 + C, p.num_tokens);
+  const int i0 = (int)(blockIdx.x / (2 * p.kv_heads)) * C, many = min(C, p.num_tokens - i0);
   const uint16_t* rows = p.rows[kv] + (size_t)head * D + col;
   const int64_t stride = p.stride[kv];
   const int each = p.scale_tokens;
-  int parity = 0;
-  int before = i0 > 0 ? p.slot_map[i0 - 1] : -1;
-  for (int i = i0; i < i1; ++i) {
-    const int slot = p.slot_map[i], off = slot % each;
-    const bool begins = (uint32_t)slot < p.num_slots && !(off != 0 && before == slot - 1);
-    before = slot;
-    if (!begins) continue;
-    // the run's length: tokens that follow in the call and in the block
-    const int most = min(each - off, p.num_tokens - i);
+
+  // Slots of the tokens looked through and of the 128 behind them, four to a lane; bit i of `next`: token i0 + i continues the
+  // run of the one before it.  (Every wave does this for itself.)
+  int slot[4];
+  uint64_t next[4], valid[2];
+  {
+    const int left = p.num_tokens - i0, want = min(left, C + kPage);
+    int prev = i0 > 0 ? p.slot_map[i0 - 1] : -1;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const int i = w * 64 + lane;
+      slot[w] = i < want ? p.slot_map[i0 + i] : -1;
+    }
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      int before = __shfl_up(slot[w], 1);
+      if (lane == 0) before = prev;
+      prev = __builtin_amdgcn_readlane(slot[w], 63);
+      const bool in_cache = (uint32_t)slot[w] < p.num_slots;
+      next[w] = __ballot(in_cache && before >= 0 && slot[w] == before + 1 && slot[w] % each != 0);
+      if (w < 2) valid[w] = __ballot(in_cache && w * 64 + lane < many);
+    }
+  }
+  // length of the run that begins at token i (of those looked through)
+  auto length = [&](int i, int off) {
     int r = 1;
-    for (; r < most; r += 64) {
-      const int k = r + (tid & 63);
-      const uint64_t other = __ballot(k >= most || p.slot_map[i + k] != slot + k);
-      if (other) {
-        r += __builtin_ctzll(other);
-        break;
-      }
+    for (int j = i + 1; j < 256; j = (j | 63) + 1) {
+      const uint64_t rest = ~(next[j >> 6] >> (j & 63));
+      const int ones = rest ? __builtin_ctzll(rest) : 64;
+      r += min(ones, 64 - (j & 63));
+      if (ones < 64 - (j & 63)) break;
     }
-    r = min(r, most);
-    u32x4 x[kPasses];
-    uint32_t top = 0;
+    return min(r, each - off);
+  };
+  auto slot_of = [&](int i) { return __builtin_amdgcn_readlane(i < 64 ? slot[0] : slot[1], i & 63); };
+
+  // long runs
+  int parity = 0, turn = 0;
 #pragma unroll
-    for (int s = 0; s < kPasses; ++s) {
-      const int k = s * kRows + row;
-      if (s * kRows < r) {  // (uniform)
-        x[s] = k < r ? *(const u32x4*)(rows + (int64_t)(i + k) * stride) : u32x4{0, 0, 0, 0};
-      }
-    }
-    const int page = slot / kPage, in_page = slot % kPage;
-    float* scale_at = p.scales[kv] + ((size_t)page * p.kv_heads + head) * (kPage / each) + in_page / each;
-    const float old = off > 0 ? *scale_at : 0.f;
+  for (int w = 0; w < 2; ++w) {
+    for (uint64_t begin = valid[w] & ~next[w]; begin; begin &= begin - 1) {
+      const int i = w * 64 + __builtin_ctzll(begin), s0 = slot_of(i);
+      const int r = length(i, s0 % each);
+      if (r <= kWaveRows) continue;
+      u32x4 x[kPasses];
 #pragma unroll
-    for (int s = 0; s < kPasses; ++s) {
-      if (s * kRows < r) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) top = max(top, max(finite_bits(x[s][j]), finite_bits(x[s][j] >> 16)));
+      for (int s = 0; s < kPasses; ++s) {
+        const int k = s * kRows + row;
+        if (s * kRows < r) x[s] = k < r ? *(const u32x4*)(rows + (int64_t)(i0 + i + k) * stride) : u32x4{0, 0, 0, 0};
       }
-    }
-    for (int d = 1; d < 64; d *= 2) top = max(top, (uint32_t)__shfl_xor(top, d));
-    if ((tid & 63) == 0) tot[parity][tid >> 6] = top;
-    __syncthreads();  // (also: every thread has read the old scale)
-    top = max(max(tot[parity][0], tot[parity][1]), max(tot[parity][2], tot[parity][3]));
-    parity ^= 1;
-    const float scale = fmaxf(old, block_scale(top)), inv = scale > 0.f ? 1.f / scale : 0.f;
-    uint8_t* codes = p.cache[kv] + (((size_t)page * p.kv_heads + head) * kPage + in_page) * D + col;
+      const Run run = run_at<D>(p, kv, head, s0, col);
+      const float old = run.off > 0 ? *run.scale : 0.f;
+      uint32_t top = 0;
 #pragma unroll
-    for (int s = 0; s < kPasses; ++s) {
-      const int k = s * kRows + row;
-      if (k < r) *(u32x2*)(codes + (size_t)k * D) = u32x2{encode_words(x[s][0], x[s][1], inv), encode_words(x[s][2], x[s][3], inv)};
-    }
-    if (off > 0 && scale > old) {  // tokens that the block held before take the grown scale
-      const float ratio = old / scale;
-      for (int k = row - off; k < 0; k += kRows) {
-        u32x2* at = (u32x2*)(codes + (ptrdiff_t)k * D);
-        const u32x2 c = *at;
-        *at = u32x2{recode(c[0], ratio), recode(c[1], ratio)};
+      for (int s = 0; s < kPasses; ++s)
+        if (s * kRows < r) top = max(top, largest(x[s]));
+      top = wave_max(top);
+      if (lane == 0) tot[parity][wave] = top;
+      __syncthreads();  // (also: every thread has read the old scale)
+      top = max(max(tot[parity][0], tot[parity][1]), max(tot[parity][2], tot[parity][3]));
+      parity ^= 1;
+      const float scale = fmaxf(old, block_scale(top)), inv = scale > 0.f ? 1.f / scale : 0.f;
+#pragma unroll
+      for (int s = 0; s < kPasses; ++s) {
+        const int k = s * kRows + row;
+        if (k < r) *(u32x2*)(run.codes + (size_t)k * D) = u32x2{encode_words(x[s][0], x[s][1], inv), encode_words(x[s][2], x[s][3], inv)};
       }
+      regrow<D>(run, old, scale, row, kRows);
+      if (tid == 0) *run.scale = scale;
     }
-    if (tid == 0) *scale_at = scale;
+  }
+  // short ones
+  const int wrow = lane / kPer;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    for (uint64_t begin = valid[w] & ~next[w]; begin; begin &= begin - 1) {
+      const int i = w * 64 + __builtin_ctzll(begin), s0 = slot_of(i);
+      const int r = length(i, s0 % each);
+      if (r > kWaveRows || (turn++ & 3) != wave) continue;
+      const u32x4 x = wrow < r ? *(const u32x4*)(rows + (int64_t)(i0 + i + wrow) * stride) : u32x4{0, 0, 0, 0};
+      const Run run = run_at<D>(p, kv, head, s0, col);
+      const float old = run.off > 0 ? *run.scale : 0.f;
+      const float scale = fmaxf(old, block_scale(wave_max(largest(x)))), inv = scale > 0.f ? 1.f / scale : 0.f;
+      if (wrow < r) *(u32x2*)(run.codes + (size_t)wrow * D) = u32x2{encode_words(x[0], x[1], inv), encode_words(x[2], x[3], inv)};
+      regrow<D>(run, old, scale, wrow, kWaveRows);
+      if (lane == 0) *run.scale = scale;
+    }
   }
 }
 
@@ -131,9 +200,9 @@ __global__ __launch_bounds__(kThreads) void gqa_append_kernel(GqaAppendParams p,
 
 hipError_t launch_gqa_append(const GqaAppendParams& p, hipStream_t stream) {
   if (p.num_tokens <= 0) return hipSuccess;
-  // About 8192 work groups, or fewer; no more tokens to one than its scale's block has.
+  // About 2048 work groups, or fewer; no more tokens to one than its scale's block has.
   int C = 1;
-  while (C < p.scale_tokens && (int64_t)p.num_tokens * p.kv_heads * 2 > (int64_t)8192 * C) C *= 2;
+  while (C < p.scale_tokens && (int64_t)p.num_tokens * p.kv_heads * 2 > (int64_t)2048 * C) C *= 2;
   const dim3 grid((uint32_t)(((int64_t)p.num_tokens + C - 1) / C * p.kv_heads * 2));
   if (p.head_dim == 64) hipLaunchKernelGGL(gqa_append_kernel<64>, grid, dim3(kThreads), 0, stream, p, C);
   else if (p.head_dim == 128) hipLaunchKernelGGL(gqa_append_kernel<128>, grid, dim3(kThreads), 0, stream, p, C);

@@ -4,8 +4,8 @@
 // keeps (j < S, or among the last W of them): out = sum_j p_j v_j / sum_j p_j, p_j = exp(scale q.k_j), lse = ln sum p_j.
 //
 // Work.  The query rows (t, head of the group) of one (request, KV head) are cut into blocks of 16, 32 or 64; a block
-// reads the pages that hold kept tokens.  All (block, page) pairs of the call, in order of request, KV head and block,
-// are dealt out evenly: work group u of U takes pairs [u T / U, (u + 1) T / U).  Every work group finds its share by
+// reads the pages that hold kept tokens.  A block counts as many units as it has pages, and kStart.  All units of the call, in
+// order of request, KV head and block, are dealt out evenly: work group u of U takes units [u T / U, (u + 1) T / U).  Every work group finds its share by
 // itself from the lengths on the device, so the host needs to know nothing but the sizes of the arrays.  A block whose
 // pages went to several groups leaves one partial row each, which gqa_combine_kernel joins.
 //
@@ -33,11 +33,16 @@ typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 
 constexpr int kThreads = 256;
 constexpr int kWaveTokens = 32;
+// Work groups of a compute unit, as far as their registers allow.
+constexpr int groups_per_cu(int head_dim, int row_tiles) { return head_dim * row_tiles <= 64 ? 4 : head_dim * row_tiles <= 128 ? 2 : 1; }
 // Weights are 2^(s - m + kLift) for the reference m, which a logit (log2) may exceed by kSlack before it is raised: the largest
 // weight is at most 2^15 (f16 holds 65504), and weights keep full precision down to 2^-25 of the largest.
 constexpr float kLift = 11.f, kSlack = 4.f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// What a block costs beside its pages, in pages: its query, the meeting of the waves, its results.
+constexpr int kStart = 2;
 
 // What a request brings: its tokens, its first query token and how many it has.
 struct Request {
@@ -55,7 +60,7 @@ __device__ __forceinline__ Request request_of(const GqaDecodeParams& p, int b) {
 struct Block {
   int t0, t1;  // its query tokens, both included
   TileLayout pages;
-  __device__ __forceinline__ int units() const { return max(pages.count(), 1); }  // (nothing kept: one, for the empty result)
+  __device__ __forceinline__ int units() const { return kStart + pages.count(); }
 };
 template <int ROWS>
 __device__ __forceinline__ Block block_of(const GqaDecodeParams& p, const Request& r, int rb) {
@@ -69,7 +74,7 @@ template <int ROWS>
 __device__ __forceinline__ int blocks_of(const GqaDecodeParams& p, const Request& r) {
   return (int)(((int64_t)r.n * p.group + ROWS - 1) / ROWS);
 }
-// (block, page) pairs of one KV head of a request
+// Units of work (pages, and kStart for each block) of one KV head of a request
 template <int ROWS>
 __device__ __forceinline__ int64_t cost_of(const GqaDecodeParams& p, const Request& r) {
   const int blocks = blocks_of<ROWS>(p, r);
@@ -117,7 +122,7 @@ struct Gqa {
   static constexpr int kCols = D / 16;    // columns of V per lane
   static constexpr int kWords = D / 64;   // 64-byte pieces of a K row; also words of V per lane and token
   static constexpr int kOStride = D + 4;  // floats of a row in LDS
-  static constexpr size_t kLds = (size_t)4 * kRows * kOStride * 4 + 2 * 4 * kRows * 8;
+  static constexpr size_t kLds = (size_t)4 * kRows * kOStride * 4 + 2 * 4 * kRows * 16;
 };
 
 template <int WORDS>
@@ -162,285 +167,432 @@ __device__ __forceinline__ void load_v(Tile<D>& t, __amdgpu_buffer_rsrc_t rsrc, 
 // Whether one of four codes is NaN (0x7f or 0xff).
 __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
+// Orders LDS between the waves of a work group without waiting for the loads of the next block, which are under way.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// The share of work group u of U: units [bound(u), bound(u + 1)), bound(u) = floor(u T / U).
+struct Shares {
+  int64_t T, each;  // each = T / U
+  int U, rest;      // rest = T % U
+  __device__ __forceinline__ int64_t bound(int u) const { return u * each + u * rest / U; }  // (U is at most 2^12)
+  // the work group that has unit x
+  __device__ __forceinline__ int owner(int64_t x) const {
+    int u = min((int)((double)x * U / (double)T), U - 1);
+    while (bound(u) > x) --u;
+    while (bound(u + 1) <= x) ++u;
+    return u;
+  }
+};
+
 template <int D, int RT, bool OUT32>
-__global__ __launch_bounds__(kThreads, RT * D <= 128 ? 2 : 1) void gqa_decode_kernel(GqaDecodeParams p) {
+__global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_kernel(GqaDecodeParams p) {
   using C = Gqa<D, RT, OUT32>;
   constexpr int R = C::kRows, kCols = C::kCols, kWords = C::kWords;
   extern __shared__ __align__(16) float lds[];
   float* const o_lds = lds;                                    // [4 waves][R][kOStride]
-  float2* const ml_lds = (float2*)(lds + 4 * R * C::kOStride); // [2][4 waves][R]
-  __shared__ int64_t ends[kThreads];
+  float4* const ml_lds = (float4*)(lds + 4 * R * C::kOStride); // [2][4 waves][R]
   __shared__ int64_t wave_tot[4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  __shared__ int4 requests[kThreads];  // (batches of up to 256: L, begin, n, units of one KV head)
+  __shared__ int64_t found_off;
+  __shared__ int found_at;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int n16 = lane & 15, g = lane >> 4;
 
-  // Share of this work group: running sum of the pairs over the batch, a run of requests per thread.
+  // Share of this work group: running sum of the units over the batch, a run of requests per thread.  The thread whose requests
+  // hold the share's first unit says so.
   const int per = (p.batch + kThreads - 1) / kThreads;
+  Shares shares;
+  int64_t begin, off;
+  int at_request;
   {
-    int64_t sum = 0;
+    int64_t mine = 0;
     for (int i = 0; i < per; ++i) {
       const int b = tid * per + i;
-      if (b < p.batch) sum += cost_of<R>(p, request_of(p, b)) * p.kv_heads;
+      if (b < p.batch) {
+        const Request r = request_of(p, b);
+        const int64_t cost = cost_of<R>(p, r);
+        mine += cost * p.kv_heads;
+        if (per == 1) requests[tid] = make_int4(r.L, r.begin, r.n, (int)cost);
+      }
     }
+    int64_t sum = mine;
     for (int d = 1; d < 64; d *= 2) {
       const int64_t y = __shfl_up(sum, d);
       if (lane >= d) sum += y;
     }
     if (lane == 63) wave_tot[wave] = sum;
     __syncthreads();
-    for (int w = 0; w < wave; ++w) sum += wave_tot[w];
-    ends[tid] = sum;
+    shares.T = 0;
+    for (int w = 0; w < 4; ++w) {
+      if (w == wave) sum += shares.T;
+      shares.T += (int64_t)uniform64(wave_tot[w]);
+    }
+    shares.U = (int)min((int64_t)gridDim.x, shares.T);
+    if ((int)blockIdx.x >= shares.U) return;
+    if (shares.T >> 31) shares.each = shares.T / shares.U;
+    else shares.each = (uint32_t)shares.T / (uint32_t)shares.U;
+    shares.rest = (int)(shares.T - shares.each * shares.U);
+    begin = shares.bound(blockIdx.x);
+    if (sum - mine <= begin && begin < sum) {
+      found_at = tid;
+      found_off = begin - (sum - mine);
+    }
     __syncthreads();
+    at_request = uniform(found_at) * per;
+    off = (int64_t)uniform64(found_off);
   }
-  const int64_t T = ends[kThreads - 1];
-  const int64_t U = min((int64_t)gridDim.x, T);
-  if ((int64_t)blockIdx.x >= U) return;
-  int64_t at = (int64_t)blockIdx.x * T / U;
-  const int64_t stop = (int64_t)(blockIdx.x + 1) * T / U;
-  // the request, KV head and block that pair `at` belongs to
-  int b, h, rb;
-  int64_t first;  // first pair of the block
-  Request rq;
-  Block bk;
-  {
-    int lo = 0, hi = kThreads - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      if (ends[mid] > at) hi = mid;
-      else lo = mid + 1;
+  auto request = [&](int b) {
+    if (per == 1) {
+      const int4 r = requests[b];
+      return Request{uniform(r.x), uniform(r.y), uniform(r.z)};
     }
-    first = lo ? ends[lo - 1] : 0;
-    b = __builtin_amdgcn_readfirstlane(lo * per);
+    const Request r = request_of(p, b);
+    return Request{uniform(r.L), uniform(r.begin), uniform(r.n)};
+  };
+  const int64_t stop = shares.bound(blockIdx.x + 1);
+
+  // The part of a block that this work group computes.
+  struct Piece {
+    int b, h, rb;
+    Request rq;
+    Block bk;
+    int off;               // the block's units before it
+    int tile_lo, tile_hi;  // its pages, by their number among the block's
+    int64_t left;          // units of the share from its first one on
+  };
+  auto cut = [&](Piece& w) {
+    w.bk = block_of<R>(p, w.rq, w.rb);
+    w.tile_lo = max(w.off - kStart, 0);
+    w.tile_hi = (int)min(max(w.left + w.off - kStart, (int64_t)0), (int64_t)w.bk.pages.count());
+  };
+  // Whether there is something to do: pages, or the empty result of a block that keeps nothing, which is whose share has its first unit.
+  auto counts = [&](const Piece& w) { return w.tile_lo < w.tile_hi || (w.bk.pages.count() == 0 && w.off == 0); };
+  // The next block with something to do for this work group; false if there is none.
+  auto follow = [&](Piece& w) {
+    do {
+      w.left -= w.bk.units() - w.off;
+      w.off = 0;
+      if (w.left <= 0) return false;
+      if (++w.rb >= blocks_of<R>(p, w.rq)) {
+        w.rb = 0;
+        if (++w.h == p.kv_heads) {
+          w.h = 0;
+          do w.rq = request(++w.b);
+          while (w.rq.n == 0);
+        }
+      }
+      cut(w);
+    } while (!counts(w));
+    return true;
+  };
+  Piece now;
+  now.left = stop - begin;
+  if (per == 1) {
+    now.b = at_request;
+    const int4 r = requests[now.b];
+    now.rq = Request{uniform(r.x), uniform(r.y), uniform(r.z)};
+    const uint32_t cost = uniform(r.w);
+    now.h = (int)((uint32_t)off / cost);  // (one request's units are below 2^31)
+    off -= (int64_t)now.h * cost;
+  } else {
     int64_t cost;
-    for (;; ++b) {
-      rq = request_of(p, b);
-      cost = cost_of<R>(p, rq);
-      if (at < first + cost * p.kv_heads) break;
-      first += cost * p.kv_heads;
+    for (now.b = at_request;; ++now.b) {
+      now.rq = request(now.b);
+      cost = cost_of<R>(p, now.rq);
+      if (off < cost * p.kv_heads) break;
+      off -= cost * p.kv_heads;
     }
-    h = (int)((at - first) / cost);
-    first += h * cost;
-    for (rb = 0;; ++rb) {
-      bk = block_of<R>(p, rq, rb);
-      if (at < first + bk.units()) break;
-      first += bk.units();
-    }
+    now.h = (int)((uint32_t)off / (uint32_t)cost);
+    off -= now.h * cost;
   }
+  for (now.rb = 0;; ++now.rb) {
+    const int units = block_of<R>(p, now.rq, now.rb).units();
+    if (off < units) break;
+    off -= units;
+  }
+  now.off = (int)off;
+  cut(now);
+  if (!counts(now) && !follow(now)) return;
+
   const size_t head_bytes = (size_t)kPage * D;
   const int k_at = (wave * kWaveTokens + n16) * D + g * 16;
   const int v_at = (wave * kWaveTokens + 4 * g) * D + n16 * kCols;
   const int blocks_per_page = kPage >> p.scale_shift, my_block = (wave * kWaveTokens) >> p.scale_shift;
   int parity = 0, first_partial = 0;  // first_partial: 1 once this work group has left its first block behind
 
-  while (true) {
-    const int64_t end = min(stop, first + bk.units());
-    const int tile_lo = (int)(at - first), tile_hi = min((int)(end - first), bk.pages.count());
-    const bool whole = at == first && end == first + bk.units();
-
-    // Query rows of the block: lane n16 of every group of 16 holds one row of each row tile, the columns that its K
-    // loads bring.  Rows past the last hold zeros.
-    bf16x8 q[RT][2 * kWords];
-    int reach[RT];  // tokens that the row's query sees
-    const int rows_left = (int)min((int64_t)rq.n * p.group - (int64_t)rb * R, (int64_t)R);
+  // Page-table entries of up to 64 of a block's pages from number `held` on, one per lane.
+  auto entries = [&](int b, const TileLayout& pages, int from) {
+    const int last = pages.count() - 1;
+    return last >= 0 ? p.page_table[b * p.table_stride + pages.logical(min(from + lane, last))] : 0;
+  };
+  // Query rows of a block: lane n16 of every group of 16 holds one row of each row tile, the columns that its K loads
+  // bring.  Rows past the last hold zeros.  reach: tokens that the row's query sees.
+  bf16x8 q[RT][2 * kWords];
+  int reach[RT];
+  auto rows_of = [&](const Piece& w) { return (int)min((int64_t)w.rq.n * p.group - (int64_t)w.rb * R, (int64_t)R); };
+  auto load_q = [&](const Piece& w) {
+    const int rows = rows_of(w);
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       const int row = rt * 16 + n16;
-      const int t = (rb * R + row) / p.group, gi = (rb * R + row) - t * p.group;
-      const bool valid = row < rows_left;
-      reach[rt] = valid ? rq.L - rq.n + t + 1 : 0;
-      const uint16_t* src = p.q + (int64_t)(rq.begin + t) * p.q_stride + (size_t)(h * p.group + gi) * D + g * 16;
+      const uint32_t t = (uint32_t)(w.rb * R + row) / (uint32_t)p.group, gi = (uint32_t)(w.rb * R + row) - t * p.group;
+      const bool valid = row < rows;
+      reach[rt] = valid ? w.rq.L - w.rq.n + (int)t + 1 : 0;
+      const uint16_t* src = p.q + (int64_t)(w.rq.begin + (int)t) * p.q_stride + (size_t)(w.h * p.group + (int)gi) * D + g * 16;
 #pragma unroll
       for (int c = 0; c < kWords; ++c) {
         q[rt][2 * c] = valid ? *(const bf16x8*)(src + c * 64) : bf16x8{};
         q[rt][2 * c + 1] = valid ? *(const bf16x8*)(src + c * 64 + 8) : bf16x8{};
       }
     }
-    const int reach_lo = rq.L - rq.n + bk.t0 + 1, reach_hi = rq.L - rq.n + bk.t1 + 1;
+  };
+  // What a page's loads need: where its codes are, and the wave's two scales.
+  __amdgpu_buffer_rsrc_t rk, rv;
+  float ks = 0.f, vs = 0.f;
+  auto aim = [&](const Piece& w, int tile, int ids, int held) {
+    const int page = __builtin_amdgcn_readlane(ids, tile - held);
+    const size_t ph = (size_t)page * p.kv_heads + w.h;
+    const int seen = w.rq.L - w.rq.n + w.bk.t1 + 1;
+    const int live = min(seen - w.bk.pages.logical(tile) * kPage, kPage);
+    rk = codes_at(p.k_cache + ph * head_bytes, live * D);
+    rv = codes_at(p.v_cache + ph * head_bytes, live * D);
+    ks = p.k_scales[ph * blocks_per_page + my_block];
+    vs = p.v_scales[ph * blocks_per_page + my_block];
+  };
 
+  Tile<D> t;
+  int held = now.tile_lo, ids = entries(now.b, now.bk.pages, held);
+  load_q(now);
+  if (now.tile_lo < now.tile_hi) {
+    aim(now, now.tile_lo, ids, held);
+    load_k<D>(t, rk, k_at);
+    load_v<D>(t, rv, v_at);
+  }
+  // Entries of the next request's first block, asked for as soon as the one before it begins: short requests come and go faster
+  // than a chain of loads from the table to the codes.
+  int ahead_b = -1, ahead_ids = 0;
+
+  while (true) {
+    Piece next = now;
+    const bool more_blocks = follow(next);
+    const bool next_loads = more_blocks && next.tile_lo < next.tile_hi;
+    // (its entries: the same as this block's for another KV head; asked for before; or asked for now)
+    const bool same_ids = next.b == now.b && next.rb == now.rb, have_ids = next.b == ahead_b && next.rb == 0 && next.tile_lo < 64;
+    int next_ids = ahead_ids;
+    if (next_loads && !same_ids && !have_ids) next_ids = entries(next.b, next.bk.pages, next.tile_lo);
+    if (ahead_b <= now.b) {
+      ahead_b = now.b + 1;
+      if (ahead_b < p.batch) {
+        const Request r = request(ahead_b);
+        if (r.n > 0) ahead_ids = entries(ahead_b, block_of<R>(p, r, 0).pages, 0);
+      }
+    }
+    const int reach_lo = now.rq.L - now.rq.n + now.bk.t0 + 1, reach_hi = now.rq.L - now.rq.n + now.bk.t1 + 1;
+
+    auto turn_to_next = [&] {
+      if (same_ids) {
+        if (next.tile_lo < held || next.tile_lo - held >= 64) {
+          held = next.tile_lo;
+          ids = entries(next.b, next.bk.pages, held);
+        }
+      } else {
+        held = have_ids ? 0 : next.tile_lo;
+        ids = next_ids;
+      }
+      aim(next, next.tile_lo, ids, held);
+    };
+
+    // O holds sum 2^(x - n + kLift) v_scale v_code and l sum 2^(x - m + kLift) for the row's logits x (log2): two references,
+    // so that neither a small nor a large scale of a block of values costs the weights their range.
     f32x4 o[RT][kCols];
-    float m[RT], l[RT];
+    float m[RT], n[RT], l[RT], ratio[RT];  // ratio = 2^(m - n)
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      m[rt] = -INFINITY;
-      l[rt] = 0.f;
+      m[rt] = n[rt] = -INFINITY;
+      l[rt] = ratio[rt] = 0.f;
 #pragma unroll
       for (int c = 0; c < kCols; ++c) o[rt][c] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    if (tile_lo < tile_hi) {
-      const int32_t* table = p.page_table + b * p.table_stride;
-      // pages of up to 64 tiles at a time, one per lane
-      int held = tile_lo;
-      int ids = table[bk.pages.logical(min(held + lane, tile_hi - 1))];
-      Tile<D> t;
-      float ks, vs;
-      auto request = [&](int tile, __amdgpu_buffer_rsrc_t& rk, __amdgpu_buffer_rsrc_t& rv, float& ks_, float& vs_) {
-        if (tile - held >= 64) {
-          held = tile;
-          ids = table[bk.pages.logical(min(held + lane, tile_hi - 1))];
-        }
-        const int page = __builtin_amdgcn_readlane(ids, tile - held);
-        const size_t ph = (size_t)page * p.kv_heads + h;
-        const int live = min(reach_hi - bk.pages.logical(tile) * kPage, kPage);
-        rk = codes_at(p.k_cache + ph * head_bytes, live * D);
-        rv = codes_at(p.v_cache + ph * head_bytes, live * D);
-        ks_ = p.k_scales[ph * blocks_per_page + my_block];
-        vs_ = p.v_scales[ph * blocks_per_page + my_block];
-      };
-      __amdgpu_buffer_rsrc_t rk, rv;
-      request(tile_lo, rk, rv, ks, vs);
-      load_k<D>(t, rk, k_at);
-      load_v<D>(t, rv, v_at);
-      for (int tile = tile_lo; tile < tile_hi; ++tile) {
-        const int pos0 = bk.pages.logical(tile) * kPage + wave * kWaveTokens;
-        // every query sees and keeps all 32 tokens
-        const bool full = pos0 + kWaveTokens <= reach_lo && (pos0 + kWaveTokens <= p.S || pos0 >= reach_hi - p.W);
-        // S^T of the wave's tokens: lane (n16, g) has tokens 16 h2 + 4 g + i of row n16
-        f32x4 s[RT][2];
+    for (int tile = now.tile_lo; tile < now.tile_hi; ++tile) {
+      const int pos0 = now.bk.pages.logical(tile) * kPage + wave * kWaveTokens;
+      // every query sees and keeps all 32 tokens
+      const bool full = pos0 + kWaveTokens <= reach_lo && (pos0 + kWaveTokens <= p.S || pos0 >= reach_hi - p.W);
+      // S^T of the wave's tokens: lane (n16, g) has tokens 16 h2 + 4 g + i of row n16
+      f32x4 s[RT][2];
 #pragma unroll
-        for (int h2 = 0; h2 < 2; ++h2) {
+      for (int h2 = 0; h2 < 2; ++h2) {
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) s[rt][h2] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int rt = 0; rt < RT; ++rt) s[rt][h2] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int c = 0; c < kWords; ++c)
+        for (int c = 0; c < kWords; ++c)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              u32x4 w;
+          for (int u = 0; u < 2; ++u) {
+            u32x4 w;
 #pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                w[2 * i] = bf16_pair(t.k[h2][c][2 * u + i], false);
-                w[2 * i + 1] = bf16_pair(t.k[h2][c][2 * u + i], true);
-              }
-#pragma unroll
-              for (int rt = 0; rt < RT; ++rt)
-                s[rt][h2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), q[rt][2 * c + u], s[rt][h2], 0, 0, 0);
+            for (int i = 0; i < 2; ++i) {
+              w[2 * i] = bf16_pair(t.k[h2][c][2 * u + i], false);
+              w[2 * i + 1] = bf16_pair(t.k[h2][c][2 * u + i], true);
             }
-        }
-        const float factor = p.scale_log2 * ks;
-        // (the scale of a block without kept tokens may be anything)
-        const bool some = pos0 < reach_hi && (pos0 < p.S || (p.W > 0 && pos0 + kWaveTokens > reach_lo - p.W));
-        const float v_scale = some ? vs : 0.f;
-        const bool more = tile + 1 < tile_hi;
-        if (more) {
-          request(tile + 1, rk, rv, ks, vs);
-          load_k<D>(t, rk, k_at);
-        }
-        f16x8 w_hi[RT], w_lo[RT];
-        uint32_t keep_bits = 0;  // tokens (of the lane's 8) that its row tile's row keeps, 8 bits a row tile
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          float x[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = s[rt][i / 4][i % 4] * factor;
-          if (!full) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int pos = pos0 + 16 * (i / 4) + 4 * g + i % 4;
-              const bool keep = retained(pos, reach[rt], p.S, p.W);
-              x[i] = keep ? x[i] : -INFINITY;
-              keep_bits |= (keep ? 1u : 0u) << (8 * rt + i);
-            }
+            for (int rt = 0; rt < RT; ++rt)
+              s[rt][h2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), q[rt][2 * c + u], s[rt][h2], 0, 0, 0);
           }
-          float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-          if (__any(top > m[rt] + kSlack)) {
-            top = row_max(top);
-            const float next = top > m[rt] + kSlack ? top : m[rt];
-            const float shrink = next == m[rt] ? 1.f : exp2_fast(m[rt] - next);
-            m[rt] = next;
-            l[rt] *= shrink;
+      }
+      // (the scale of a block without kept tokens may be anything)
+      const bool some = pos0 < reach_hi && (pos0 < p.S || (p.W > 0 && pos0 + kWaveTokens > reach_lo - p.W));
+      const float factor = p.scale_log2 * ks, v_scale = some ? vs : 0.f;
+      // (at least 2^-100: ratio stays finite)
+      const float v_log = fmaxf(__log2f(v_scale), -100.f);
+      int seen[RT];
 #pragma unroll
-            for (int c = 0; c < kCols; ++c)
+      for (int rt = 0; rt < RT; ++rt) seen[rt] = reach[rt];
+      // the next page's loads, of this block or the next one, as soon as their registers are free
+      bool more = true;
+      if (tile + 1 < now.tile_hi) {
+        if (tile + 1 - held >= 64) {
+          held = tile + 1;
+          ids = entries(now.b, now.bk.pages, held);
+        }
+        aim(now, tile + 1, ids, held);
+      } else if (next_loads) {
+        turn_to_next();
+      } else {
+        more = false;
+      }
+      if (more) load_k<D>(t, rk, k_at);
+      if (tile + 1 == now.tile_hi && more_blocks) load_q(next);
+
+      f16x8 w_hi[RT], w_lo[RT];
+      uint32_t keep_bits = 0;  // tokens (of the lane's 8) that its row tile's row keeps, 8 bits a row tile
 #pragma unroll
-              for (int i = 0; i < 4; ++i) o[rt][c][i] *= shrink;
-          }
-          // (a row that has kept nothing so far has reference -inf, and only masked logits)
-          const float ref = m[rt] == -INFINITY ? 0.f : m[rt] - kLift;
-          float w[8];
+      for (int rt = 0; rt < RT; ++rt) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = s[rt][i / 4][i % 4] * factor;
+        if (!full) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            w[i] = exp2_fast(x[i] - ref);
-            w_hi[rt][i] = (_Float16)w[i];
-            if constexpr (OUT32) w_lo[rt][i] = (_Float16)(w[i] - (float)w_hi[rt][i]);
+            const int pos = pos0 + 16 * (i / 4) + 4 * g + i % 4;
+            const bool keep = retained(pos, seen[rt], p.S, p.W);
+            x[i] = keep ? x[i] : -INFINITY;
+            keep_bits |= (keep ? 1u : 0u) << (8 * rt + i);
           }
-          l[rt] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
         }
-        uint32_t seen_nan = 0;
-        if (!full) {
-          // tokens that no row of the block keeps may hold anything
-          uint32_t any_nan = 0;
+        float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+        if (__any(top > fminf(m[rt], n[rt] - v_log) + kSlack)) {
+          top = row_max(top);
+          const float next_m = top > m[rt] + kSlack ? top : m[rt];
+          const float next_n = top + v_log > n[rt] + kSlack ? top + v_log : n[rt];
+          l[rt] *= next_m == m[rt] ? 1.f : exp2_fast(m[rt] - next_m);
+          const float shrink = next_n == n[rt] ? 1.f : exp2_fast(n[rt] - next_n);
+          m[rt] = next_m;
+          n[rt] = next_n;
+          ratio[rt] = next_n == -INFINITY ? 0.f : exp2_fast(next_m - next_n);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int pos = pos0 + (j < 4 ? 0 : 16) + 4 * g + j % 4;
-            const bool keep = pos < reach_hi && (pos < p.S || (p.W > 0 && pos >= reach_lo - p.W));
-            if (!keep) t.v[j] = typename VWord<kWords>::type{};
+          for (int c = 0; c < kCols; ++c)
 #pragma unroll
-            for (int i = 0; i < kWords; ++i) any_nan |= nan_codes(word<kWords>(t.v[j], i));
-          }
-          if (bk.t1 > bk.t0) seen_nan = __ballot(any_nan != 0) != 0;
+            for (int i = 0; i < 4; ++i) o[rt][c][i] *= shrink;
+        }
+        // (a row that has kept nothing so far has reference -inf, and only masked logits)
+        const float ref = m[rt] == -INFINITY ? 0.f : m[rt] - kLift, value = ratio[rt] * v_scale;
+        float w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          w[i] = exp2_fast(x[i] - ref);
+          float y = w[i] * value;
+          // (fixed here: the compiler may fuse the product with one of its two uses and round the other in two steps, which
+          // near a tie of f16 leaves the second term for another first term)
+          if constexpr (OUT32) asm("" : "+v"(y));
+          w_hi[rt][i] = (_Float16)y;
+          if constexpr (OUT32) w_lo[rt][i] = (_Float16)(y - (float)w_hi[rt][i]);
+        }
+        l[rt] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+      }
+      uint32_t seen_nan = 0;
+      if (!full) {
+        // tokens that no row of the block keeps may hold anything
+        uint32_t any_nan = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int pos = pos0 + (j < 4 ? 0 : 16) + 4 * g + j % 4;
+          const bool keep = pos < reach_hi && (pos < p.S || (p.W > 0 && pos >= reach_lo - p.W));
+          if (!keep) t.v[j] = typename VWord<kWords>::type{};
+#pragma unroll
+          for (int i = 0; i < kWords; ++i) any_nan |= nan_codes(word<kWords>(t.v[j], i));
+        }
+        if (now.bk.t1 > now.bk.t0) seen_nan = __ballot(any_nan != 0) != 0;
+      }
+#pragma unroll
+      for (int wd = 0; wd < kWords; ++wd) {
+        uint32_t pair[2][4];  // [lower or upper two columns][tokens 2 j, 2 j + 1]
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t a = word<kWords>(t.v[2 * j], wd), c = word<kWords>(t.v[2 * j + 1], wd);
+          pair[0][j] = __builtin_amdgcn_perm(c, a, 0x05010400);
+          pair[1][j] = __builtin_amdgcn_perm(c, a, 0x07030602);
         }
 #pragma unroll
-        for (int wd = 0; wd < kWords; ++wd) {
-          uint32_t pair[2][4];  // [lower or upper two columns][tokens 2 j, 2 j + 1]
-          uint32_t nans[2][4];
+        for (int col = 0; col < 4; ++col) {
+          u32x4 f;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t a = word<kWords>(t.v[2 * j], wd), c = word<kWords>(t.v[2 * j + 1], wd);
-            pair[0][j] = __builtin_amdgcn_perm(c, a, 0x05010400);
-            pair[1][j] = __builtin_amdgcn_perm(c, a, 0x07030602);
+          for (int j = 0; j < 4; ++j) f[j] = f16_pair(pair[col / 2][j], col % 2);
+          f16x8 vt = __builtin_bit_cast(f16x8, f);
+          f16x8 bad = {};
+          if (seen_nan) {
+            // NaN in a value row reaches the rows that keep the token, and only those
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const bool is = vt[j] != vt[j];
+              bad[j] = is ? (_Float16)1.f : (_Float16)0.f;
+              vt[j] = is ? (_Float16)0.f : vt[j];
+            }
           }
 #pragma unroll
-          for (int col = 0; col < 4; ++col) {
-            u32x4 f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) f[j] = f16_pair(pair[col / 2][j], col % 2);
-            f16x8 vt = __builtin_bit_cast(f16x8, f);
-            f16x8 bad = {};
+          for (int rt = 0; rt < RT; ++rt) {
+            f32x4& acc = o[rt][4 * wd + col];
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, w_hi[rt], acc, 0, 0, 0);
+            if constexpr (OUT32) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, w_lo[rt], acc, 0, 0, 0);
             if (seen_nan) {
-              // NaN in a value row reaches the rows that keep the token, and only those
+              f16x8 kept;
 #pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                const bool is = vt[j] != vt[j];
-                bad[j] = is ? (_Float16)1.f : (_Float16)0.f;
-                vt[j] = is ? (_Float16)0.f : vt[j];
-              }
-            }
+              for (int j = 0; j < 8; ++j) kept[j] = (keep_bits >> (8 * rt + j)) & 1 ? (_Float16)1.f : (_Float16)0.f;
+              const f32x4 hits = __builtin_amdgcn_mfma_f32_16x16x32_f16(bad, kept, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-              f32x4 part = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, w_hi[rt], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-              if constexpr (OUT32) part = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, w_lo[rt], part, 0, 0, 0);
-              if (seen_nan) {
-                f16x8 kept;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) kept[j] = (keep_bits >> (8 * rt + j)) & 1 ? (_Float16)1.f : (_Float16)0.f;
-                const f32x4 hits = __builtin_amdgcn_mfma_f32_16x16x32_f16(bad, kept, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) part[i] = hits[i] > 0.f ? NAN : part[i];
-              }
-#pragma unroll
-              for (int i = 0; i < 4; ++i) o[rt][4 * wd + col][i] = fmaf(part[i], v_scale, o[rt][4 * wd + col][i]);
+              for (int i = 0; i < 4; ++i) acc[i] = hits[i] > 0.f ? NAN : acc[i];
             }
           }
         }
-        if (more) load_v<D>(t, rv, v_at);
+      }
+      if (more) load_v<D>(t, rv, v_at);
+    }
+    if (now.tile_lo >= now.tile_hi && more_blocks) {  // (nothing kept: the next block's loads have not been asked for yet)
+      load_q(next);
+      if (next_loads) {
+        turn_to_next();
+        load_k<D>(t, rk, k_at);
+        load_v<D>(t, rv, v_at);
       }
     }
 
-    // The waves' shares meet: reference and sum first, then the outputs at the common reference.
-    float2* const ml = ml_lds + parity * 4 * R;
+    // The waves' shares meet: references and sum first, then the outputs at the common reference.
+    float4* const ml = ml_lds + parity * 4 * R;
     parity ^= 1;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       l[rt] = row_sum(l[rt]);
-      if (g == 0) ml[wave * R + rt * 16 + n16] = make_float2(m[rt], l[rt]);
+      if (g == 0) ml[wave * R + rt * 16 + n16] = make_float4(m[rt], l[rt], n[rt], 0.f);
     }
-    __syncthreads();
+    lds_barrier();
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       float top = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w * R + rt * 16 + n16].x);
+      for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w * R + rt * 16 + n16].z);
       // (a wave that kept nothing has zeros, or NaN that has to stay: nothing is skipped)
-      const float shrink = m[rt] == top ? 1.f : exp2_fast(m[rt] - top);
+      const float shrink = n[rt] == top ? 1.f : exp2_fast(n[rt] - top);
       float* const dst = o_lds + (wave * R + rt * 16 + n16) * C::kOStride;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -449,27 +601,32 @@ __global__ __launch_bounds__(kThreads, RT * D <= 128 ? 2 : 1) void gqa_decode_ke
           *(f32x4*)(dst + (4 * g + i) * kCols + c) =
               f32x4{o[rt][c][i] * shrink, o[rt][c + 1][i] * shrink, o[rt][c + 2][i] * shrink, o[rt][c + 3][i] * shrink};
     }
-    __syncthreads();
+    lds_barrier();
     const int slot = 2 * blockIdx.x + first_partial;
     constexpr int kChunks = D / 8;
-    for (int k = tid; k < rows_left * kChunks; k += kThreads) {
+    const int rows = rows_of(now);
+    const bool whole = now.tile_lo == 0 && now.tile_hi == now.bk.pages.count();
+    for (int k = tid; k < rows * kChunks; k += kThreads) {
       const int row = k / kChunks, col = k % kChunks * 8;
       f32x4 a = {0.f, 0.f, 0.f, 0.f}, c = a;
-      float top = -INFINITY, sum = 0.f;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w * R + row].x);
+      float top = -INFINITY, vtop = -INFINITY, sum = 0.f;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const float2 e = ml[w * R + row];
+        top = fmaxf(top, ml[w * R + row].x);
+        vtop = fmaxf(vtop, ml[w * R + row].z);
+      }
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float4 e = ml[w * R + row];
         sum += e.y * (e.x == top ? 1.f : exp2_fast(e.x - top));
         const f32x4* src = (const f32x4*)(o_lds + (w * R + row) * C::kOStride + col);
         a += src[0];
         c += src[1];
       }
-      const int t = (rb * R + row) / p.group, gi = (rb * R + row) - t * p.group;
-      const int64_t out_row = (int64_t)(rq.begin + t) * p.q_heads + h * p.group + gi;
+      const uint32_t qt = (uint32_t)(now.rb * R + row) / (uint32_t)p.group, gi = (uint32_t)(now.rb * R + row) - qt * p.group;
+      const int64_t out_row = (int64_t)(now.rq.begin + (int)qt) * p.q_heads + now.h * p.group + (int)gi;
       if (whole) {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;  // (nothing kept: 0 and -inf)
+        const float inv = sum == 0.f ? 0.f : exp2_fast(vtop - top) / sum;  // (nothing kept: 0 and -inf)
         if constexpr (OUT32) {
           f32x4* dst = (f32x4*)((float*)p.out + out_row * D + col);
           dst[0] = a * inv;
@@ -492,33 +649,22 @@ __global__ __launch_bounds__(kThreads, RT * D <= 128 ? 2 : 1) void gqa_decode_ke
         ((f32x4*)dst)[0] = a;
         ((f32x4*)dst)[1] = c;
         if (col == 0) {
-          p.part_ml[(size_t)slot * R + row] = make_float2(top, sum);
-          if (at == first) {
-            // the work group that takes a block's first pair knows which ones take the others
-            const int64_t last = ((first + bk.units()) * U + T - 1) / T - 1;
-            p.rows[out_row] = make_int2(slot, (int)(last - blockIdx.x + 1) * 64 + row);
-          }
+          p.part_ml[(size_t)slot * R + row] = make_float4(top, sum, vtop, 0.f);
+          // the work group that takes a block's first page knows which ones take the others
+          if (now.tile_lo == 0) p.rows[out_row] = make_int2(slot, (shares.owner(stop - now.left - now.off + now.bk.units() - 1) - (int)blockIdx.x + 1) * 64 + row);
         }
       }
     }
     first_partial = 1;
-    at = end;
-    if (at >= stop) break;
-    // next block
-    first += bk.units();
-    if (++rb == blocks_of<R>(p, rq)) {
-      rb = 0;
-      if (++h == p.kv_heads) {
-        h = 0;
-        do rq = request_of(p, ++b);
-        while (rq.n == 0);
-      }
-    }
-    bk = block_of<R>(p, rq, rb);
+    if (!more_blocks) break;
+    now = next;
   }
 }
 
-// Joins the partial rows of blocks whose pages went to several work groups: sum_i 2^(m_i - m) (o_i, l_i).  Partial i of a
+// 2^(ref - top); 1 where both are -inf (no tokens)
+__device__ __forceinline__ float factor(float ref, float top) { return ref == top ? 1.f : exp2_fast(ref - top); }
+
+// Joins the partial rows of blocks whose pages went to several work groups: o = sum_i 2^(n_i - n) o_i, l = sum_i 2^(m_i - m) l_i.  Partial i of a
 // row lies in the slot of the i-th work group: the first one may have had another block before (slot 2 u + 1), the others
 // begin with this one (2 u).  WAVES waves share a row, each every WAVES-th partial.
 template <int D, bool OUT32, int WAVES>
@@ -526,7 +672,7 @@ __global__ __launch_bounds__(256) void gqa_combine_kernel(GqaDecodeParams p, int
   constexpr int kPer = D / 64;  // columns per lane
   typedef __attribute__((ext_vector_type(kPer))) float vec;
   __shared__ float sh_o[WAVES > 1 ? 4 : 1][WAVES > 1 ? D : 1];
-  __shared__ float2 sh_ml[4];
+  __shared__ float4 sh_ml[4];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int64_t row = (int64_t)blockIdx.x * (4 / WAVES) + wave / WAVES;
   if (row >= (int64_t)p.num_queries * p.q_heads) return;
@@ -536,11 +682,11 @@ __global__ __launch_bounds__(256) void gqa_combine_kernel(GqaDecodeParams p, int
   const int count = __builtin_amdgcn_readfirstlane(d.y / 64), in_block = d.y % 64;
   if (count <= 0 || d.x < 0 || d.x / 2 + count > units) return;
   const int u0 = d.x / 2;
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, n = -INFINITY, l = 0.f;
   vec o = {};
   constexpr int kBatch = 8;
   for (int i0 = wave % WAVES; i0 < count; i0 += kBatch * WAVES) {
-    float2 e[kBatch];
+    float4 e[kBatch];
     vec x[kBatch];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
@@ -549,51 +695,53 @@ __global__ __launch_bounds__(256) void gqa_combine_kernel(GqaDecodeParams p, int
       e[k] = p.part_ml[slot * block_rows + in_block];
       x[k] = *(const vec*)(p.part_o + (slot * block_rows + in_block) * D + lane * kPer);
     }
-    float top = m;
+    float top = m, vtop = n;
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) top = fmaxf(top, e[k].x);
-    float f = m == top ? 1.f : exp2_fast(m - top);
-    l *= f;
-    o *= f;
+    for (int k = 0; k < kBatch; ++k) {
+      top = fmaxf(top, e[k].x);
+      vtop = fmaxf(vtop, e[k].z);
+    }
+    l *= factor(m, top);
+    o *= factor(n, vtop);
 #pragma unroll
     for (int k = 0; k < kBatch; ++k)
       if (i0 + k * WAVES < count) {
-        f = e[k].x == top ? 1.f : exp2_fast(e[k].x - top);
-        l += f * e[k].y;
-        o += f * x[k];
+        l += factor(e[k].x, top) * e[k].y;
+        o += factor(e[k].z, vtop) * x[k];
       }
     m = top;
+    n = vtop;
   }
   if constexpr (WAVES > 1) {
-    if (lane == 0) sh_ml[wave] = make_float2(m, l);
+    if (lane == 0) sh_ml[wave] = make_float4(m, l, n, 0.f);
     *(vec*)(&sh_o[wave][lane * kPer]) = o;
     __syncthreads();
     if (wave) return;
-    float top = m;
-    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, sh_ml[w].x);
-    float f = m == top ? 1.f : exp2_fast(m - top);
-    l *= f;
-    o *= f;
+    float top = m, vtop = n;
     for (int w = 1; w < WAVES; ++w) {
-      f = sh_ml[w].x == top ? 1.f : exp2_fast(sh_ml[w].x - top);
-      l += f * sh_ml[w].y;
-      o += f * *(const vec*)(&sh_o[w][lane * kPer]);
+      top = fmaxf(top, sh_ml[w].x);
+      vtop = fmaxf(vtop, sh_ml[w].z);
+    }
+    l *= factor(m, top);
+    o *= factor(n, vtop);
+    for (int w = 1; w < WAVES; ++w) {
+      l += factor(sh_ml[w].x, top) * sh_ml[w].y;
+      o += factor(sh_ml[w].z, vtop) * *(const vec*)(&sh_o[w][lane * kPer]);
     }
     m = top;
+    n = vtop;
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float inv = l == 0.f ? 0.f : exp2_fast(n - m) / l;
   if constexpr (OUT32) {
     *(vec*)((float*)p.out + row * D + lane * kPer) = o * inv;
+  } else if constexpr (kPer == 1) {
+    ((__bf16*)p.out)[row * D + lane] = (__bf16)(o[0] * inv);
   } else {
     typedef __attribute__((ext_vector_type(kPer))) __bf16 bvec;
     bvec y;
-    if constexpr (kPer == 1) {
-      ((__bf16*)p.out)[row * D + lane] = (__bf16)(o[0] * inv);
-    } else {
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) y[i] = (__bf16)(o[i] * inv);
-      *(bvec*)((uint16_t*)p.out + row * D + lane * kPer) = y;
-    }
+    for (int i = 0; i < kPer; ++i) y[i] = (__bf16)(o[i] * inv);
+    *(bvec*)((uint16_t*)p.out + row * D + lane * kPer) = y;
   }
   if (lane == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + __log2f(l) - kLift) * 0.69314718055994531f;
 }
@@ -622,17 +770,18 @@ hipError_t allow_lds() {
 
 GqaShape gqa_shape(int batch, int num_queries, int group, int head_dim) {
   const int64_t rows = (int64_t)((num_queries + batch - 1) / batch) * group;
-  int rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  if (head_dim == 256 && rt > 2) rt = 2;
-  return GqaShape{rt, rt * head_dim <= 128 ? 2 : 1};
+  const int rt = (int)std::min<int64_t>((rows + 15) / 16, head_dim == 256 ? 2 : 4);
+  return GqaShape{std::max(rt, 1), groups_per_cu(head_dim, std::max(rt, 1))};
 }
 
 hipError_t init_gqa_kernels() {
   hipError_t e = allow_lds<64, 1>();
   if (e == hipSuccess) e = allow_lds<64, 2>();
+  if (e == hipSuccess) e = allow_lds<64, 3>();
   if (e == hipSuccess) e = allow_lds<64, 4>();
   if (e == hipSuccess) e = allow_lds<128, 1>();
   if (e == hipSuccess) e = allow_lds<128, 2>();
+  if (e == hipSuccess) e = allow_lds<128, 3>();
   if (e == hipSuccess) e = allow_lds<128, 4>();
   if (e == hipSuccess) e = allow_lds<256, 1>();
   if (e == hipSuccess) e = allow_lds<256, 2>();
@@ -651,9 +800,12 @@ hipError_t launch_gqa_decode(const GqaDecodeParams& p, const GqaShape& shape, in
     if constexpr (decltype(rt)::value <= 2) return with(integral_constant<int, 256>{}, rt);
     else return hipErrorInvalidValue;
   };
-  if (shape.row_tiles == 1) return dims(integral_constant<int, 1>{});
-  if (shape.row_tiles == 2) return dims(integral_constant<int, 2>{});
-  return dims(integral_constant<int, 4>{});
+  switch (shape.row_tiles) {
+    case 1: return dims(integral_constant<int, 1>{});
+    case 2: return dims(integral_constant<int, 2>{});
+    case 3: return dims(integral_constant<int, 3>{});
+    default: return dims(integral_constant<int, 4>{});
+  }
 }
 
 }  // namespace omniattn
