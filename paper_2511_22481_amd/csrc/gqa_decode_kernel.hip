@@ -34,7 +34,7 @@ typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 constexpr int kThreads = 256;
 constexpr int kWaveTokens = 32;
 // Work groups of a compute unit, as far as their registers allow.
-constexpr int groups_per_cu(int head_dim, int row_tiles) { return head_dim * row_tiles <= 64 ? 4 : head_dim * row_tiles <= 128 ? 2 : 1; }
+constexpr int groups_per_cu(int head_dim, int row_tiles) { return head_dim * row_tiles <= 64 ? 4 : head_dim * row_tiles <= 128 ? 2 : head_dim * row_tiles <= 256 ? 2 : 1; }
 // Weights are 2^(s - m + kLift) for the reference m, which a logit (log2) may exceed by kSlack before it is raised: the largest
 // weight is at most 2^15 (f16 holds 65504), and weights keep full precision down to 2^-25 of the largest.
 constexpr float kLift = 11.f, kSlack = 4.f;
@@ -100,11 +100,16 @@ __device__ __forceinline__ float row_sum(float x) {
   return x + y;
 }
 
+// 2^(ref - top); 1 where both are -inf (no tokens)
+__device__ __forceinline__ float factor(float ref, float top) { return ref == top ? 1.f : exp2_fast(ref - top); }
+
 // Two tokens' codes of four columns (a word each) as f16 pairs, one column's two tokens to a word.
 __device__ __forceinline__ uint32_t f16_pair(uint32_t w, bool upper) {
   return upper ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, true))
                : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, false));
 }
+// The lower or upper two columns' codes of two tokens (four columns each), a column's two tokens side by side.
+__device__ __forceinline__ uint32_t token_pair(uint32_t a, uint32_t b, bool upper) { return __builtin_amdgcn_perm(b, a, upper ? 0x07030602 : 0x05010400); }
 __device__ __forceinline__ uint32_t bf16_pair(uint32_t w, bool upper) {
   return upper ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.0f, true))
                : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.0f, false));
@@ -116,13 +121,24 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t codes_at(const uint8_t* base, 
   return __builtin_amdgcn_make_buffer_rsrc((void*)(uintptr_t)a, 0, (int)__builtin_amdgcn_readfirstlane(bytes), 0x00027000);
 }
 
-template <int D, int RT, bool OUT32>
+// What a variant of the kernel keeps where.
+template <int D, int RT>
 struct Gqa {
   static constexpr int kRows = 16 * RT;
   static constexpr int kCols = D / 16;    // columns of V per lane
   static constexpr int kWords = D / 64;   // 64-byte pieces of a K row; also words of V per lane and token
-  static constexpr int kOStride = D + 4;  // floats of a row in LDS
-  static constexpr size_t kLds = (size_t)4 * kRows * kOStride * 4 + 2 * 4 * kRows * 16;
+  static constexpr int kGroups = groups_per_cu(D, RT);
+  // The query block: registers, or LDS (two buffers, one for the next block) where they are needed for the output
+  static constexpr bool kQLds = D == 256 || D * RT > 256;
+  static constexpr size_t kQBytes = kQLds ? (size_t)kRows * D * 2 : 0;
+  static constexpr size_t kMlBytes = (size_t)4 * kRows * 16;
+  // Columns of the output that meet at a time, 1 / kParts of them, as far as LDS holds them for all four waves
+  static constexpr size_t o_bytes(int parts) { return (size_t)4 * kRows * (D / parts + 4) * 4; }
+  static constexpr size_t kRoom = 160 * 1024 / kGroups - 8 * 1024 - 2 * kQBytes - 2 * kMlBytes;
+  static constexpr int kParts = o_bytes(1) <= kRoom ? 1 : o_bytes(2) <= kRoom ? 2 : 4;
+  static_assert(o_bytes(kParts) <= kRoom, "the waves' outputs have to fit LDS");
+  static constexpr int kOStride = D / kParts + 4;  // floats of a row in LDS
+  static constexpr size_t kLds = o_bytes(kParts) + 2 * kMlBytes + 2 * kQBytes;
 };
 
 template <int WORDS>
@@ -167,8 +183,30 @@ __device__ __forceinline__ void load_v(Tile<D>& t, __amdgpu_buffer_rsrc_t rsrc, 
 // Whether one of four codes is NaN (0x7f or 0xff).
 __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
+// NaN codes as 0.
+__device__ __forceinline__ uint32_t without_nan(uint32_t w) {
+  const uint32_t high = nan_codes(w);  // 0x80 in the bytes that are NaN
+  return w & ~(high | (high - (high >> 7)));
+}
+template <int WORDS>
+__device__ __forceinline__ typename VWord<WORDS>::type without_nan(typename VWord<WORDS>::type v) {
+  if constexpr (WORDS == 1) return without_nan((uint32_t)v);
+  else {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) v[i] = without_nan((uint32_t)v[i]);
+    return v;
+  }
+}
+
 // Orders LDS between the waves of a work group without waiting for the loads of the next block, which are under way.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// The kernel's arguments, to be read again where they are used: kept in scalar registers through the loop they push others out.
+__device__ __forceinline__ const GqaDecodeParams* late_arguments() {
+  uint64_t at = (uint64_t)(uintptr_t)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(at));
+  return (const GqaDecodeParams*)(const __attribute__((address_space(4))) GqaDecodeParams*)(uintptr_t)at;
+}
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
@@ -188,11 +226,12 @@ struct Shares {
 
 template <int D, int RT, bool OUT32>
 __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_kernel(GqaDecodeParams p) {
-  using C = Gqa<D, RT, OUT32>;
+  using C = Gqa<D, RT>;
   constexpr int R = C::kRows, kCols = C::kCols, kWords = C::kWords;
   extern __shared__ __align__(16) float lds[];
   float* const o_lds = lds;                                    // [4 waves][R][kOStride]
   float4* const ml_lds = (float4*)(lds + 4 * R * C::kOStride); // [2][4 waves][R]
+  bf16x8* const q_lds = (bf16x8*)(ml_lds + 2 * 4 * R);         // [2][operands of the products][64 lanes]
   __shared__ int64_t wave_tot[4];
   __shared__ int4 requests[kThreads];  // (batches of up to 256: L, begin, n, units of one KV head)
   __shared__ int64_t found_off;
@@ -329,7 +368,8 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
   };
   // Query rows of a block: lane n16 of every group of 16 holds one row of each row tile, the columns that its K loads
   // bring.  Rows past the last hold zeros.  reach: tokens that the row's query sees.
-  bf16x8 q[RT][2 * kWords];
+  constexpr int kQs = C::kQLds ? RT * kWords / 2 : RT * 2 * kWords;  // operands that the wave reads: its share, or all
+  bf16x8 q[kQs];
   int reach[RT];
   auto rows_of = [&](const Piece& w) { return (int)min((int64_t)w.rq.n * p.group - (int64_t)w.rb * R, (int64_t)R); };
   auto load_q = [&](const Piece& w) {
@@ -341,12 +381,29 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
       const bool valid = row < rows;
       reach[rt] = valid ? w.rq.L - w.rq.n + (int)t + 1 : 0;
       const uint16_t* src = p.q + (int64_t)(w.rq.begin + (int)t) * p.q_stride + (size_t)(w.h * p.group + (int)gi) * D + g * 16;
+      if constexpr (C::kQLds) {
+        // (operand 2 c + u holds columns 64 c + 16 g + 8 u on; the wave reads those with the remainder `wave` by 4)
 #pragma unroll
-      for (int c = 0; c < kWords; ++c) {
-        q[rt][2 * c] = valid ? *(const bf16x8*)(src + c * 64) : bf16x8{};
-        q[rt][2 * c + 1] = valid ? *(const bf16x8*)(src + c * 64 + 8) : bf16x8{};
+        for (int i = 0; i < kWords / 2; ++i) q[rt * kWords / 2 + i] = valid ? *(const bf16x8*)(src + (2 * i + wave / 2) * 64 + wave % 2 * 8) : bf16x8{};
+      } else {
+#pragma unroll
+        for (int i = 0; i < 2 * kWords; ++i) q[rt * 2 * kWords + i] = valid ? *(const bf16x8*)(src + i / 2 * 64 + i % 2 * 8) : bf16x8{};
       }
     }
+  };
+  // The operands that the wave has read go to LDS, where all waves find them behind the next barrier.
+  int q_side = 0;
+  auto store_q = [&](int side) {
+    if constexpr (C::kQLds) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int i = 0; i < kWords / 2; ++i) q_lds[((side * RT + rt) * 2 * kWords + 4 * i + wave) * 64 + lane] = q[rt * kWords / 2 + i];
+    }
+  };
+  auto query = [&](int rt, int i) {
+    if constexpr (C::kQLds) return q_lds[((q_side * RT + rt) * 2 * kWords + i) * 64 + lane];
+    else return q[rt * 2 * kWords + i];
   };
   // What a page's loads need: where its codes are, and the wave's two scales.
   __amdgpu_buffer_rsrc_t rk, rv;
@@ -370,18 +427,17 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
     load_k<D>(t, rk, k_at);
     load_v<D>(t, rv, v_at);
   }
+  if constexpr (C::kQLds) {
+    store_q(0);
+    lds_barrier();
+  }
   // Entries of the next request's first block, asked for as soon as the one before it begins: short requests come and go faster
   // than a chain of loads from the table to the codes.
   int ahead_b = -1, ahead_ids = 0;
 
   while (true) {
     Piece next = now;
-    const bool more_blocks = follow(next);
-    const bool next_loads = more_blocks && next.tile_lo < next.tile_hi;
-    // (its entries: the same as this block's for another KV head; asked for before; or asked for now)
-    const bool same_ids = next.b == now.b && next.rb == now.rb, have_ids = next.b == ahead_b && next.rb == 0 && next.tile_lo < 64;
-    int next_ids = ahead_ids;
-    if (next_loads && !same_ids && !have_ids) next_ids = entries(next.b, next.bk.pages, next.tile_lo);
+    bool more_blocks = false, next_loads = false;
     if (ahead_b <= now.b) {
       ahead_b = now.b + 1;
       if (ahead_b < p.batch) {
@@ -391,15 +447,15 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
     }
     const int reach_lo = now.rq.L - now.rq.n + now.bk.t0 + 1, reach_hi = now.rq.L - now.rq.n + now.bk.t1 + 1;
 
+    // What the next block is (asked late, so that its description need not be kept through the loop), and where its first page is: its
+    // entries are the same as this block's for another KV head, or were asked for before, or are asked for now.
     auto turn_to_next = [&] {
-      if (same_ids) {
-        if (next.tile_lo < held || next.tile_lo - held >= 64) {
-          held = next.tile_lo;
-          ids = entries(next.b, next.bk.pages, held);
-        }
-      } else {
-        held = have_ids ? 0 : next.tile_lo;
-        ids = next_ids;
+      more_blocks = follow(next);
+      next_loads = more_blocks && next.tile_lo < next.tile_hi;
+      if (!next_loads) return;
+      if (!(next.b == now.b && next.rb == now.rb && held == 0)) {
+        held = 0;
+        ids = next.b == ahead_b && next.rb == 0 ? ahead_ids : entries(next.b, next.bk.pages, 0);
       }
       aim(next, next.tile_lo, ids, held);
     };
@@ -416,6 +472,7 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
       for (int c = 0; c < kCols; ++c) o[rt][c] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
+    float saw_nan = 0.f;
     for (int tile = now.tile_lo; tile < now.tile_hi; ++tile) {
       const int pos0 = now.bk.pages.logical(tile) * kPage + wave * kWaveTokens;
       // every query sees and keeps all 32 tokens
@@ -423,23 +480,26 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
       // S^T of the wave's tokens: lane (n16, g) has tokens 16 h2 + 4 g + i of row n16
       f32x4 s[RT][2];
 #pragma unroll
-      for (int h2 = 0; h2 < 2; ++h2) {
+      for (int rt = 0; rt < RT; ++rt) s[rt][0] = s[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) s[rt][h2] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < 2 * kWords; ++i) {
+        bf16x8 k[2];
 #pragma unroll
-        for (int c = 0; c < kWords; ++c)
+        for (int h2 = 0; h2 < 2; ++h2) {
+          u32x4 w;
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            u32x4 w;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              w[2 * i] = bf16_pair(t.k[h2][c][2 * u + i], false);
-              w[2 * i + 1] = bf16_pair(t.k[h2][c][2 * u + i], true);
-            }
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-              s[rt][h2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), q[rt][2 * c + u], s[rt][h2], 0, 0, 0);
+          for (int j = 0; j < 2; ++j) {
+            w[2 * j] = bf16_pair(t.k[h2][i / 2][i % 2 * 2 + j], false);
+            w[2 * j + 1] = bf16_pair(t.k[h2][i / 2][i % 2 * 2 + j], true);
           }
+          k[h2] = __builtin_bit_cast(bf16x8, w);
+        }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          const bf16x8 x = query(rt, i);
+#pragma unroll
+          for (int h2 = 0; h2 < 2; ++h2) s[rt][h2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[h2], x, s[rt][h2], 0, 0, 0);
+        }
       }
       // (the scale of a block without kept tokens may be anything)
       const bool some = pos0 < reach_hi && (pos0 < p.S || (p.W > 0 && pos0 + kWaveTokens > reach_lo - p.W));
@@ -457,16 +517,14 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
           ids = entries(now.b, now.bk.pages, held);
         }
         aim(now, tile + 1, ids, held);
-      } else if (next_loads) {
-        turn_to_next();
       } else {
-        more = false;
+        turn_to_next();
+        more = next_loads;
+        if (more_blocks) load_q(next);
       }
       if (more) load_k<D>(t, rk, k_at);
-      if (tile + 1 == now.tile_hi && more_blocks) load_q(next);
 
       f16x8 w_hi[RT], w_lo[RT];
-      uint32_t keep_bits = 0;  // tokens (of the lane's 8) that its row tile's row keeps, 8 bits a row tile
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         float x[8];
@@ -476,9 +534,7 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int pos = pos0 + 16 * (i / 4) + 4 * g + i % 4;
-            const bool keep = retained(pos, seen[rt], p.S, p.W);
-            x[i] = keep ? x[i] : -INFINITY;
-            keep_bits |= (keep ? 1u : 0u) << (8 * rt + i);
+            x[i] = retained(pos, seen[rt], p.S, p.W) ? x[i] : -INFINITY;
           }
         }
         float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
@@ -511,7 +567,6 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
         }
         l[rt] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
       }
-      uint32_t seen_nan = 0;
       if (!full) {
         // tokens that no row of the block keeps may hold anything
         uint32_t any_nan = 0;
@@ -523,59 +578,43 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
 #pragma unroll
           for (int i = 0; i < kWords; ++i) any_nan |= nan_codes(word<kWords>(t.v[j], i));
         }
-        if (now.bk.t1 > now.bk.t0) seen_nan = __ballot(any_nan != 0) != 0;
+        // NaN in a value row is for the rows that keep the token, and only for those, but a weight of 0 would not stop it in the
+        // product: it goes on as 0, and the block's end sees to it.
+        if (now.bk.t1 > now.bk.t0 && __ballot(any_nan != 0) != 0) {
+          saw_nan = 1.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) t.v[j] = without_nan<kWords>(t.v[j]);
+        }
       }
 #pragma unroll
       for (int wd = 0; wd < kWords; ++wd) {
-        uint32_t pair[2][4];  // [lower or upper two columns][tokens 2 j, 2 j + 1]
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t a = word<kWords>(t.v[2 * j], wd), c = word<kWords>(t.v[2 * j + 1], wd);
-          pair[0][j] = __builtin_amdgcn_perm(c, a, 0x05010400);
-          pair[1][j] = __builtin_amdgcn_perm(c, a, 0x07030602);
-        }
 #pragma unroll
         for (int col = 0; col < 4; ++col) {
           u32x4 f;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) f[j] = f16_pair(pair[col / 2][j], col % 2);
-          f16x8 vt = __builtin_bit_cast(f16x8, f);
-          f16x8 bad = {};
-          if (seen_nan) {
-            // NaN in a value row reaches the rows that keep the token, and only those
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const bool is = vt[j] != vt[j];
-              bad[j] = is ? (_Float16)1.f : (_Float16)0.f;
-              vt[j] = is ? (_Float16)0.f : vt[j];
-            }
-          }
+          for (int j = 0; j < 4; ++j) f[j] = f16_pair(token_pair(word<kWords>(t.v[2 * j], wd), word<kWords>(t.v[2 * j + 1], wd), col / 2), col % 2);
+          const f16x8 vt = __builtin_bit_cast(f16x8, f);
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) {
             f32x4& acc = o[rt][4 * wd + col];
             acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, w_hi[rt], acc, 0, 0, 0);
             if constexpr (OUT32) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, w_lo[rt], acc, 0, 0, 0);
-            if (seen_nan) {
-              f16x8 kept;
-#pragma unroll
-              for (int j = 0; j < 8; ++j) kept[j] = (keep_bits >> (8 * rt + j)) & 1 ? (_Float16)1.f : (_Float16)0.f;
-              const f32x4 hits = __builtin_amdgcn_mfma_f32_16x16x32_f16(bad, kept, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) acc[i] = hits[i] > 0.f ? NAN : acc[i];
-            }
           }
         }
       }
       if (more) load_v<D>(t, rv, v_at);
     }
-    if (now.tile_lo >= now.tile_hi && more_blocks) {  // (nothing kept: the next block's loads have not been asked for yet)
-      load_q(next);
+    if (now.tile_lo >= now.tile_hi) {  // (nothing kept: the next block has not been asked for yet)
+      turn_to_next();
+      if (more_blocks) load_q(next);
       if (next_loads) {
-        turn_to_next();
         load_k<D>(t, rk, k_at);
         load_v<D>(t, rv, v_at);
       }
     }
+
+    if (more_blocks) store_q(q_side ^ 1);
+    q_side ^= 1;
 
     // The waves' shares meet: references and sum first, then the outputs at the common reference.
     float4* const ml = ml_lds + parity * 4 * R;
@@ -583,52 +622,82 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       l[rt] = row_sum(l[rt]);
-      if (g == 0) ml[wave * R + rt * 16 + n16] = make_float4(m[rt], l[rt], n[rt], 0.f);
+      if (g == 0) ml[wave * R + rt * 16 + n16] = make_float4(m[rt], l[rt], n[rt], saw_nan);
     }
     lds_barrier();
+    float shrink[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       float top = -INFINITY;
 #pragma unroll
       for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w * R + rt * 16 + n16].z);
       // (a wave that kept nothing has zeros, or NaN that has to stay: nothing is skipped)
-      const float shrink = n[rt] == top ? 1.f : exp2_fast(n[rt] - top);
-      float* const dst = o_lds + (wave * R + rt * 16 + n16) * C::kOStride;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int c = 0; c < kCols; c += 4)
-          *(f32x4*)(dst + (4 * g + i) * kCols + c) =
-              f32x4{o[rt][c][i] * shrink, o[rt][c + 1][i] * shrink, o[rt][c + 2][i] * shrink, o[rt][c + 3][i] * shrink};
+      shrink[rt] = factor(n[rt], top);
     }
-    lds_barrier();
     const int slot = 2 * blockIdx.x + first_partial;
-    constexpr int kChunks = D / 8;
+    const GqaDecodeParams& end = *late_arguments();
+    constexpr int kChunks = D / 8 / C::kParts;
     const int rows = rows_of(now);
     const bool whole = now.tile_lo == 0 && now.tile_hi == now.bk.pages.count();
+#pragma unroll
+    for (int part = 0; part < C::kParts; ++part) {
+    if (part) lds_barrier();  // (the part before has been read)
+    if (C::kParts == 1 || g / (4 / C::kParts) == part) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        float* const dst = o_lds + (wave * R + rt * 16 + n16) * C::kOStride + (4 * g % (16 / C::kParts)) * kCols;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int c = 0; c < kCols; c += 4)
+            *(f32x4*)(dst + i * kCols + c) = f32x4{o[rt][c][i] * shrink[rt], o[rt][c + 1][i] * shrink[rt], o[rt][c + 2][i] * shrink[rt], o[rt][c + 3][i] * shrink[rt]};
+      }
+    }
+    lds_barrier();
     for (int k = tid; k < rows * kChunks; k += kThreads) {
-      const int row = k / kChunks, col = k % kChunks * 8;
+      const int row = k / kChunks, in_part = k % kChunks * 8, col = part * (D / C::kParts) + in_part;
       f32x4 a = {0.f, 0.f, 0.f, 0.f}, c = a;
-      float top = -INFINITY, vtop = -INFINITY, sum = 0.f;
+      float top = -INFINITY, vtop = -INFINITY, sum = 0.f, nans = 0.f;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         top = fmaxf(top, ml[w * R + row].x);
         vtop = fmaxf(vtop, ml[w * R + row].z);
+        nans += ml[w * R + row].w;
       }
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         const float4 e = ml[w * R + row];
         sum += e.y * (e.x == top ? 1.f : exp2_fast(e.x - top));
-        const f32x4* src = (const f32x4*)(o_lds + (w * R + row) * C::kOStride + col);
+        const f32x4* src = (const f32x4*)(o_lds + (w * R + row) * C::kOStride + in_part);
         a += src[0];
         c += src[1];
       }
-      const uint32_t qt = (uint32_t)(now.rb * R + row) / (uint32_t)p.group, gi = (uint32_t)(now.rb * R + row) - qt * p.group;
-      const int64_t out_row = (int64_t)(now.rq.begin + (int)qt) * p.q_heads + now.h * p.group + (int)gi;
+      const uint32_t qt = (uint32_t)(now.rb * R + row) / (uint32_t)end.group, gi = (uint32_t)(now.rb * R + row) - qt * end.group;
+      if (__builtin_expect(nans != 0.f, 0)) {
+        // NaN that the loop has taken for 0: the columns of the tokens that this row keeps are looked through again
+        const int sees = now.rq.L - now.rq.n + (int)qt + 1;
+#pragma unroll 1
+        for (int tile = now.tile_lo; tile < now.tile_hi; ++tile) {
+          const int lp = now.bk.pages.logical(tile);
+          const size_t ph = (size_t)p.page_table[now.b * p.table_stride + lp] * p.kv_heads + now.h;
+#pragma unroll 1
+          for (int j = 0; j < kPage; ++j) {
+            if (!retained(lp * kPage + j, sees, p.S, p.W)) continue;
+            const u32x2 codes = *(const u32x2*)(p.v_cache + ph * head_bytes + (size_t)j * D + col);
+            const uint32_t lo = nan_codes(codes[0]), hi = nan_codes(codes[1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if ((lo >> (8 * i)) & 0x80u) a[i] = NAN;
+              if ((hi >> (8 * i)) & 0x80u) c[i] = NAN;
+            }
+          }
+        }
+      }
+      const int64_t out_row = (int64_t)(now.rq.begin + (int)qt) * end.q_heads + now.h * end.group + (int)gi;
       if (whole) {
         const float inv = sum == 0.f ? 0.f : exp2_fast(vtop - top) / sum;  // (nothing kept: 0 and -inf)
         if constexpr (OUT32) {
-          f32x4* dst = (f32x4*)((float*)p.out + out_row * D + col);
+          f32x4* dst = (f32x4*)((float*)end.out + out_row * D + col);
           dst[0] = a * inv;
           dst[1] = c * inv;
         } else {
@@ -638,31 +707,29 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
             y[i] = (__bf16)(a[i] * inv);
             y[4 + i] = (__bf16)(c[i] * inv);
           }
-          *(bf16x8*)((uint16_t*)p.out + out_row * D + col) = y;
+          *(bf16x8*)((uint16_t*)end.out + out_row * D + col) = y;
         }
         if (col == 0) {
-          p.lse[out_row] = sum == 0.f ? -INFINITY : (top + __log2f(sum) - kLift) * 0.69314718055994531f;
-          p.rows[out_row] = make_int2(0, 0);
+          end.lse[out_row] = sum == 0.f ? -INFINITY : (top + __log2f(sum) - kLift) * 0.69314718055994531f;
+          end.rows[out_row] = make_int2(0, 0);
         }
       } else {
-        float* dst = p.part_o + ((size_t)slot * R + row) * D + col;
+        float* dst = end.part_o + ((size_t)slot * R + row) * D + col;
         ((f32x4*)dst)[0] = a;
         ((f32x4*)dst)[1] = c;
         if (col == 0) {
-          p.part_ml[(size_t)slot * R + row] = make_float4(top, sum, vtop, 0.f);
+          end.part_ml[(size_t)slot * R + row] = make_float4(top, sum, vtop, 0.f);
           // the work group that takes a block's first page knows which ones take the others
-          if (now.tile_lo == 0) p.rows[out_row] = make_int2(slot, (shares.owner(stop - now.left - now.off + now.bk.units() - 1) - (int)blockIdx.x + 1) * 64 + row);
+          if (now.tile_lo == 0) end.rows[out_row] = make_int2(slot, (shares.owner(stop - now.left - now.off + now.bk.units() - 1) - (int)blockIdx.x + 1) * 64 + row);
         }
       }
+    }
     }
     first_partial = 1;
     if (!more_blocks) break;
     now = next;
   }
 }
-
-// 2^(ref - top); 1 where both are -inf (no tokens)
-__device__ __forceinline__ float factor(float ref, float top) { return ref == top ? 1.f : exp2_fast(ref - top); }
 
 // Joins the partial rows of blocks whose pages went to several work groups: o = sum_i 2^(n_i - n) o_i, l = sum_i 2^(m_i - m) l_i.  Partial i of a
 // row lies in the slot of the i-th work group: the first one may have had another block before (slot 2 u + 1), the others
@@ -748,7 +815,7 @@ __global__ __launch_bounds__(256) void gqa_combine_kernel(GqaDecodeParams p, int
 
 template <int D, int RT, bool OUT32>
 hipError_t start(const GqaDecodeParams& p, int units, hipStream_t stream) {
-  constexpr size_t lds = Gqa<D, RT, OUT32>::kLds;
+  constexpr size_t lds = Gqa<D, RT>::kLds;
   hipLaunchKernelGGL((gqa_decode_kernel<D, RT, OUT32>), dim3(units), dim3(kThreads), lds, stream, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -761,8 +828,8 @@ hipError_t start(const GqaDecodeParams& p, int units, hipStream_t stream) {
 
 template <int D, int RT>
 hipError_t allow_lds() {
-  hipError_t e = hipFuncSetAttribute((const void*)gqa_decode_kernel<D, RT, false>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)Gqa<D, RT, false>::kLds);
-  if (e == hipSuccess) e = hipFuncSetAttribute((const void*)gqa_decode_kernel<D, RT, true>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)Gqa<D, RT, true>::kLds);
+  hipError_t e = hipFuncSetAttribute((const void*)gqa_decode_kernel<D, RT, false>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)Gqa<D, RT>::kLds);
+  if (e == hipSuccess) e = hipFuncSetAttribute((const void*)gqa_decode_kernel<D, RT, true>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)Gqa<D, RT>::kLds);
   return e;
 }
 
