@@ -7,8 +7,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libomniattn.so")
 SOURCES = ["decode_kernels.hip", "decode_mid_kernel.hip", "decode_narrow_kernel.hip", "append_kernels.hip",
-           "table_kernels.hip", "gqa_append_kernel.hip", "gqa_decode_kernel.hip", "api.cpp", "api_gqa.cpp", "plan.cpp"]
-HEADERS = ["kernels.h", "gqa.h", "plan.h", "decode_common.h", os.path.join("..", "..", "include", "omniattn.h")]
+           "table_kernels.hip", "gqa_append_kernel.hip", "gqa_decode_kernel.hip",
+           "gqa_wide_kernel.hip", "api.cpp", "api_gqa.cpp", "plan.cpp"]
+HEADERS = ["kernels.h", "gqa.h", "gqa_common.h", "plan.h", "decode_common.h", os.path.join("..", "..", "include", "omniattn.h")]
 
 
 def hipcc():
@@ -75,7 +76,8 @@ def check_generated_code(verbose=False):
         for src, kernel, builtins in (("decode_kernels.hip", "decode_kernel", False),
                                       ("decode_mid_kernel.hip", "decode_mid_kernel", True),
                                       ("decode_narrow_kernel.hip", "decode_narrow_kernel", False),
-                                      ("gqa_decode_kernel.hip", "gqa_decode_kernel", True)):
+                                      ("gqa_decode_kernel.hip", "gqa_decode_kernel", True),
+                                      ("gqa_wide_kernel.hip", "gqa_wide_kernel", True)):
             out = os.path.join(tmp, src + ".s")
             cmd = [hipcc(), "--offload-arch=gfx950", "-O3", "-std=c++20",
                    "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -72,7 +72,7 @@ struct Workspace {
 };
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 Workspace workspace_of(const omniattn_gqa_t* g, const GqaShape& shape, int units) {
-  const size_t slots = (size_t)2 * units * shape.block_rows();
+  const size_t slots = (size_t)2 * units * shape.block_rows;
   Workspace w;
   w.rows = 0;
   w.ml = align256((size_t)g->num_queries * g->num_q_heads * sizeof(int2));
@@ -218,8 +218,8 @@ int omniattn_gqa_decode(const omniattn_gqa_t* gqa, const void* q, int64_t q_stri
   p.out_fp32 = gqa->out_dtype == OMNIATTN_FP32;
   p.scale_log2 = gqa->softmax_scale * 1.4426950408889634f;
   // Not more work groups than there can be units of work (each block counts 2 beside its pages).
-  const int64_t blocks = ((int64_t)p.num_queries * p.group + shape.block_rows() - 1) / shape.block_rows() + p.batch;
-  const int64_t pages = std::min<int64_t>(p.max_pages, ((int64_t)p.S + kPage - 1) / kPage + ((int64_t)p.W + shape.block_rows() + kPage - 1) / kPage + 1);
+  const int64_t blocks = ((int64_t)p.num_queries * p.group + shape.block_rows - 1) / shape.block_rows + p.batch;
+  const int64_t pages = std::min<int64_t>(p.max_pages, ((int64_t)p.S + kPage - 1) / kPage + ((int64_t)p.W + shape.block_rows + kPage - 1) / kPage + 1);
   units = (int)std::min<int64_t>(units, blocks * p.kv_heads * (pages + 2));
   OA_HIP(launch_gqa_decode(p, shape, units, (hipStream_t)hip_stream));
   return OMNIATTN_OK;

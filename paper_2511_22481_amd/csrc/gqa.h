@@ -70,13 +70,17 @@ struct GqaDecodeParams {
   int out_fp32;
   float scale_log2;         // softmax_scale * log2(e)
 };
-// Rows of a block (16, 32, 48 or 64) and work groups a compute unit holds, for the average number of query rows per request.
+// How a call is computed: by which kernel (gqa_decode_kernel.hip or gqa_wide_kernel.hip), tiles of 16 query rows per wave, rows of a
+// block, and work groups that a compute unit holds.
 struct GqaShape {
-  int row_tiles, groups_per_cu;
-  int block_rows() const { return 16 * row_tiles; }
+  bool wide;
+  int row_tiles, block_rows, groups_per_cu;
 };
 GqaShape gqa_shape(int batch, int num_queries, int group, int head_dim);
 hipError_t init_gqa_kernels();
+hipError_t init_gqa_wide_kernels();
+// The kernel of the shape, and the one that joins partial rows.
 hipError_t launch_gqa_decode(const GqaDecodeParams& p, const GqaShape& shape, int units, hipStream_t stream);
+hipError_t launch_gqa_wide(const GqaDecodeParams& p, const GqaShape& shape, int units, hipStream_t stream);
 
 }  // namespace omniattn

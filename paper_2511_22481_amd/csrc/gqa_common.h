@@ -1,0 +1,544 @@
+// What the two attention kernels of the grouped-query part share: how the work is dealt out, the arithmetic of a tile's
+// softmax, and the end of a block, where the waves' shares meet.  See gqa_decode_kernel.hip for the whole.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "decode_common.h"
+#include "gqa.h"
+
+namespace omniattn {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+
+constexpr int kWaveTokens = 32;
+// Weights are 2^(s - m + kLift) for the reference m, which a logit (log2) may exceed by kSlack before it is raised: the largest
+// weight is at most 2^15 (f16 holds 65504), and weights keep full precision down to 2^-25 of the largest.
+constexpr float kLift = 11.f, kSlack = 4.f;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// What a block costs beside its pages, in pages: its query, the meeting of the waves, its results.
+constexpr int kStart = 2;
+
+// What a request brings: its tokens, its first query token and how many it has.
+struct Request {
+  int L, begin, n;
+};
+__device__ __forceinline__ Request request_of(const GqaDecodeParams& p, int b) {
+  Request r;
+  r.L = min(max(p.seq_lens[b], 0), p.max_pages * kPage);
+  const int lo = p.q_start ? p.q_start[b] : b, hi = p.q_start ? p.q_start[b + 1] : b + 1;
+  r.begin = min(max(lo, 0), p.num_queries);
+  r.n = min(max(hi, r.begin), p.num_queries) - r.begin;
+  return r;
+}
+// Pages of a block of query rows: the union of its queries' kept sets.
+struct Block {
+  int t0, t1;  // its query tokens, both included
+  TileLayout pages;
+  __device__ __forceinline__ int units() const { return kStart + pages.count(); }
+};
+template <int ROWS>
+__device__ __forceinline__ Block block_of(const GqaDecodeParams& p, const Request& r, int rb) {
+  Block k;
+  k.t0 = rb * ROWS / p.group;
+  k.t1 = min(r.n - 1, ((rb + 1) * ROWS - 1) / p.group);
+  k.pages = tile_layout(r.L - r.n + k.t1 + 1, p.S, p.W > 0 ? p.W + (k.t1 - k.t0) : 0, kPage);
+  return k;
+}
+template <int ROWS>
+__device__ __forceinline__ int blocks_of(const GqaDecodeParams& p, const Request& r) {
+  return (int)(((int64_t)r.n * p.group + ROWS - 1) / ROWS);
+}
+// Units of work (pages, and kStart for each block) of one KV head of a request
+template <int ROWS>
+__device__ __forceinline__ int64_t cost_of(const GqaDecodeParams& p, const Request& r) {
+  const int blocks = blocks_of<ROWS>(p, r);
+  int64_t sum = 0;
+  for (int rb = 0; rb < blocks; ++rb) sum += block_of<ROWS>(p, r, rb).units();
+  return sum;
+}
+
+__device__ __forceinline__ float row_max(float x) {  // over the four lanes that hold tokens of the same row
+  float y = x;
+  swap16(x, y);
+  x = fmaxf(x, y);
+  y = x;
+  swap32(x, y);
+  return fmaxf(x, y);
+}
+__device__ __forceinline__ float row_sum(float x) {
+  float y = x;
+  swap16(x, y);
+  x += y;
+  y = x;
+  swap32(x, y);
+  return x + y;
+}
+
+// 2^(ref - top); 1 where both are -inf (no tokens)
+__device__ __forceinline__ float factor(float ref, float top) { return ref == top ? 1.f : exp2_fast(ref - top); }
+
+// Two tokens' codes of four columns (a word each) as f16 pairs, one column's two tokens to a word.
+__device__ __forceinline__ uint32_t f16_pair(uint32_t w, bool upper) {
+  return upper ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, true))
+               : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, false));
+}
+// The lower or upper two columns' codes of two tokens (four columns each), a column's two tokens side by side.
+__device__ __forceinline__ uint32_t token_pair(uint32_t a, uint32_t b, bool upper) { return __builtin_amdgcn_perm(b, a, upper ? 0x07030602 : 0x05010400); }
+__device__ __forceinline__ uint32_t bf16_pair(uint32_t w, bool upper) {
+  return upper ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.0f, true))
+               : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.0f, false));
+}
+
+template <int WORDS>
+struct VWord { typedef u32x4 type; };
+template <>
+struct VWord<1> { typedef uint32_t type; };
+template <>
+struct VWord<2> { typedef u32x2 type; };
+
+template <int WORDS>
+__device__ __forceinline__ uint32_t word(const typename VWord<WORDS>::type& v, int i) {
+  if constexpr (WORDS == 1) return v;
+  else return v[i];
+}
+
+// Whether one of four codes is NaN (0x7f or 0xff).
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
+// NaN codes as 0.
+__device__ __forceinline__ uint32_t without_nan(uint32_t w) {
+  const uint32_t high = nan_codes(w);  // 0x80 in the bytes that are NaN
+  return w & ~(high | (high - (high >> 7)));
+}
+template <int WORDS>
+__device__ __forceinline__ typename VWord<WORDS>::type without_nan(typename VWord<WORDS>::type v) {
+  if constexpr (WORDS == 1) return without_nan((uint32_t)v);
+  else {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) v[i] = without_nan((uint32_t)v[i]);
+    return v;
+  }
+}
+
+// Orders LDS between the waves of a work group without waiting for the loads of the next block, which are under way.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// The kernel's arguments, to be read again where they are used: kept in scalar registers through the loop they push others out.
+__device__ __forceinline__ const GqaDecodeParams* late_arguments() {
+  uint64_t at = (uint64_t)(uintptr_t)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(at));
+  return (const GqaDecodeParams*)(const __attribute__((address_space(4))) GqaDecodeParams*)(uintptr_t)at;
+}
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// The share of work group u of U: units [bound(u), bound(u + 1)), bound(u) = floor(u T / U).
+struct Shares {
+  int64_t T, each;  // each = T / U
+  int U, rest;      // rest = T % U
+  __device__ __forceinline__ int64_t bound(int u) const { return u * each + u * rest / U; }  // (U is at most 2^12)
+  // the work group that has unit x
+  __device__ __forceinline__ int owner(int64_t x) const {
+    int u = min((int)((double)x * U / (double)T), U - 1);
+    while (bound(u) > x) --u;
+    while (bound(u + 1) <= x) ++u;
+    return u;
+  }
+};
+
+// The part of a block that a work group computes.
+struct Piece {
+  int b, h, rb;
+  Request rq;
+  Block bk;
+  int off;               // the block's units before it
+  int tile_lo, tile_hi;  // its pages, by their number among the block's
+  int64_t left;          // units of the share from its first one on
+  __device__ __forceinline__ bool whole() const { return tile_lo == 0 && tile_hi == bk.pages.count(); }
+  // tokens that the block's first and last query see
+  __device__ __forceinline__ int reach_lo() const { return rq.L - rq.n + bk.t0 + 1; }
+  __device__ __forceinline__ int reach_hi() const { return rq.L - rq.n + bk.t1 + 1; }
+};
+
+// Finds a work group's share and walks through its blocks.  R: rows of a block.  All threads call everything.
+template <int R, int THREADS>
+struct Dealer {
+  struct Lds {
+    int64_t wave_tot[THREADS / 64], off;
+    int4 requests[THREADS];  // (batches of up to THREADS: L, begin, n, units of one KV head)
+    int at;
+  };
+  const GqaDecodeParams& p;
+  Lds& lds;
+  int per;       // requests per thread
+  Shares shares;
+  int64_t stop;  // end of the share
+
+  __device__ __forceinline__ Dealer(const GqaDecodeParams& params, Lds& memory) : p(params), lds(memory) {}
+
+  __device__ __forceinline__ Request request(int b) const {
+    if (per == 1) {
+      const int4 r = lds.requests[b];
+      return Request{uniform(r.x), uniform(r.y), uniform(r.z)};
+    }
+    const Request r = request_of(p, b);
+    return Request{uniform(r.L), uniform(r.begin), uniform(r.n)};
+  }
+  __device__ __forceinline__ void cut(Piece& w) const {
+    w.bk = block_of<R>(p, w.rq, w.rb);
+    w.tile_lo = max(w.off - kStart, 0);
+    w.tile_hi = (int)min(max(w.left + w.off - kStart, (int64_t)0), (int64_t)w.bk.pages.count());
+  }
+  // Whether there is something to do: pages, or the empty result of a block that keeps nothing, which is whose share has its first unit.
+  __device__ __forceinline__ static bool counts(const Piece& w) { return w.tile_lo < w.tile_hi || (w.bk.pages.count() == 0 && w.off == 0); }
+  // The next block with something to do for this work group; false if there is none.
+  __device__ __forceinline__ bool follow(Piece& w) const {
+    do {
+      w.left -= w.bk.units() - w.off;
+      w.off = 0;
+      if (w.left <= 0) return false;
+      if (++w.rb >= blocks_of<R>(p, w.rq)) {
+        w.rb = 0;
+        if (++w.h == p.kv_heads) {
+          w.h = 0;
+          do w.rq = request(++w.b);
+          while (w.rq.n == 0);
+        }
+      }
+      cut(w);
+    } while (!counts(w));
+    return true;
+  }
+  // Running sum of the units over the batch, a run of requests per thread; the thread whose requests hold the share's first unit
+  // says so.  False: nothing to do for this work group.
+  __device__ __forceinline__ bool begin(Piece& now) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    per = (p.batch + THREADS - 1) / THREADS;
+    int64_t mine = 0;
+    for (int i = 0; i < per; ++i) {
+      const int b = tid * per + i;
+      if (b < p.batch) {
+        const Request r = request_of(p, b);
+        const int64_t cost = cost_of<R>(p, r);
+        mine += cost * p.kv_heads;
+        if (per == 1) lds.requests[tid] = make_int4(r.L, r.begin, r.n, (int)cost);
+      }
+    }
+    int64_t sum = mine;
+    for (int d = 1; d < 64; d *= 2) {
+      const int64_t y = __shfl_up(sum, d);
+      if (lane >= d) sum += y;
+    }
+    if (lane == 63) lds.wave_tot[wave] = sum;
+    __syncthreads();
+    shares.T = 0;
+    for (int w = 0; w < THREADS / 64; ++w) {
+      if (w == wave) sum += shares.T;
+      shares.T += (int64_t)uniform64(lds.wave_tot[w]);
+    }
+    shares.U = (int)min((int64_t)gridDim.x, shares.T);
+    if ((int)blockIdx.x >= shares.U) return false;
+    if (shares.T >> 31) shares.each = shares.T / shares.U;
+    else shares.each = (uint32_t)shares.T / (uint32_t)shares.U;
+    shares.rest = (int)(shares.T - shares.each * shares.U);
+    const int64_t first = shares.bound(blockIdx.x);
+    if (sum - mine <= first && first < sum) {
+      lds.at = tid;
+      lds.off = first - (sum - mine);
+    }
+    __syncthreads();
+    const int at = uniform(lds.at) * per;
+    int64_t off = (int64_t)uniform64(lds.off);
+    stop = shares.bound(blockIdx.x + 1);
+    now.left = stop - first;
+    if (per == 1) {
+      now.b = at;
+      const int4 r = lds.requests[at];
+      now.rq = Request{uniform(r.x), uniform(r.y), uniform(r.z)};
+      const uint32_t cost = uniform(r.w);
+      now.h = (int)((uint32_t)off / cost);  // (one request's units are below 2^31)
+      off -= (int64_t)now.h * cost;
+    } else {
+      int64_t cost;
+      for (now.b = at;; ++now.b) {
+        now.rq = request(now.b);
+        cost = cost_of<R>(p, now.rq);
+        if (off < cost * p.kv_heads) break;
+        off -= cost * p.kv_heads;
+      }
+      now.h = (int)((uint32_t)off / (uint32_t)cost);
+      off -= now.h * cost;
+    }
+    for (now.rb = 0;; ++now.rb) {
+      const int units = block_of<R>(p, now.rq, now.rb).units();
+      if (off < units) break;
+      off -= units;
+    }
+    now.off = (int)off;
+    cut(now);
+    return counts(now) || follow(now);
+  }
+  __device__ __forceinline__ int rows_of(const Piece& w) const { return (int)min((int64_t)w.rq.n * p.group - (int64_t)w.rb * R, (int64_t)R); }
+  // Work groups that share the block of w, from this one on (which has its first page).
+  __device__ __forceinline__ int partners(const Piece& w) const { return shares.owner(stop - w.left - w.off + w.bk.units() - 1) - (int)blockIdx.x + 1; }
+};
+
+// A wave's share of the output rows: O holds sum 2^(x - n + kLift) v_scale v_code and l sum 2^(x - m + kLift) for the row's logits x
+// (log2).  Two references, so that neither a small nor a large scale of a block of values costs the weights their range.  Lane (n16,
+// g) has row n16 of each row tile, and of O columns (4 g + i) D / 16 + c.
+template <int D, int RT>
+struct Rows {
+  static constexpr int kCols = D / 16;
+  f32x4 o[RT][kCols];
+  float m[RT], n[RT], l[RT], ratio[RT];  // ratio = 2^(m - n)
+  float saw_nan;                         // 1: value codes that are NaN have been taken for 0
+  __device__ __forceinline__ void clear() {
+    saw_nan = 0.f;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      m[rt] = n[rt] = -INFINITY;
+      l[rt] = ratio[rt] = 0.f;
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) o[rt][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+};
+
+// Weights of a tile of 32 tokens from its S^T (lane (n16, g) has tokens 16 h + 4 g + i of row n16), rounded to f16 (`low`: and what
+// that leaves), references, sums and, where a reference rises, the output.  reach: tokens that the row's query sees; full: every
+// row keeps all 32 tokens, which begin at pos0.
+template <int D, int RT, bool OUT32>
+__device__ __forceinline__ void weigh(const GqaDecodeParams& p, Rows<D, RT>& a, const f32x4 (&s)[RT][2], const int (&reach)[RT], bool full, int pos0,
+                                      int g, float k_factor, float v_scale, f16x8 (&high)[RT], f16x8 (&low)[RT]) {
+  // (at least 2^-100: ratio stays finite)
+  const float v_log = fmaxf(__log2f(v_scale), -100.f);
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = s[rt][i / 4][i % 4] * k_factor;
+    if (!full) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int pos = pos0 + 16 * (i / 4) + 4 * g + i % 4;
+        x[i] = retained(pos, reach[rt], p.S, p.W) ? x[i] : -INFINITY;
+      }
+    }
+    float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+    if (__any(top > fminf(a.m[rt], a.n[rt] - v_log) + kSlack)) {
+      top = row_max(top);
+      const float next_m = top > a.m[rt] + kSlack ? top : a.m[rt];
+      const float next_n = top + v_log > a.n[rt] + kSlack ? top + v_log : a.n[rt];
+      a.l[rt] *= factor(a.m[rt], next_m);
+      const float shrink = factor(a.n[rt], next_n);
+      a.m[rt] = next_m;
+      a.n[rt] = next_n;
+      a.ratio[rt] = next_n == -INFINITY ? 0.f : exp2_fast(next_m - next_n);
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a.o[rt][c][i] *= shrink;
+    }
+    // (a row that has kept nothing so far has reference -inf, and only masked logits)
+    const float ref = a.m[rt] == -INFINITY ? 0.f : a.m[rt] - kLift, value = a.ratio[rt] * v_scale;
+    float w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      w[i] = exp2_fast(x[i] - ref);
+      float y = w[i] * value;
+      // (fixed here: the compiler may fuse the product with one of its two uses and round the other in two steps, which
+      // near a tie of f16 leaves the second term for another first term)
+      if constexpr (OUT32) asm("" : "+v"(y));
+      high[rt][i] = (_Float16)y;
+      if constexpr (OUT32) low[rt][i] = (_Float16)(y - (float)high[rt][i]);
+    }
+    a.l[rt] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+  }
+}
+
+// A partial tile's value codes: tokens that no row of the block keeps may hold anything and become 0.  NaN in a kept one is for the rows
+// that keep the token, and only for those, but a weight of 0 would not stop it in the product: it goes on as 0 too, and the block's end
+// sees to it.  Lane (n16, g) has tokens 4 g + j % 4 (+ 16 from j = 4 on).
+template <int D, int RT>
+__device__ __forceinline__ void sanitize(const GqaDecodeParams& p, Rows<D, RT>& a, typename VWord<D / 64>::type (&v)[8], const Piece& now, int pos0, int g) {
+  constexpr int kWords = D / 64;
+  const int lo = now.reach_lo(), hi = now.reach_hi();
+  uint32_t any_nan = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int pos = pos0 + (j < 4 ? 0 : 16) + 4 * g + j % 4;
+    const bool keep = pos < hi && (pos < p.S || (p.W > 0 && pos >= lo - p.W));
+    if (!keep) v[j] = typename VWord<kWords>::type{};
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) any_nan |= nan_codes(word<kWords>(v[j], i));
+  }
+  if (now.bk.t1 > now.bk.t0 && __ballot(any_nan != 0) != 0) {
+    a.saw_nan = 1.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = without_nan<kWords>(v[j]);
+  }
+}
+
+// O^T += V^T P^T
+template <int D, int RT, bool OUT32>
+__device__ __forceinline__ void add_values(Rows<D, RT>& a, const typename VWord<D / 64>::type (&v)[8], const f16x8 (&high)[RT], const f16x8 (&low)[RT]) {
+  constexpr int kWords = D / 64;
+#pragma unroll
+  for (int wd = 0; wd < kWords; ++wd) {
+#pragma unroll
+    for (int col = 0; col < 4; ++col) {
+      u32x4 f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[j] = f16_pair(token_pair(word<kWords>(v[2 * j], wd), word<kWords>(v[2 * j + 1], wd), col / 2), col % 2);
+      const f16x8 vt = __builtin_bit_cast(f16x8, f);
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        f32x4& acc = a.o[rt][4 * wd + col];
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, high[rt], acc, 0, 0, 0);
+        if constexpr (OUT32) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, low[rt], acc, 0, 0, 0);
+      }
+    }
+  }
+}
+
+// A K operand of S^T from its codes: 8 columns of one token.
+__device__ __forceinline__ bf16x8 k_operand(uint32_t lo, uint32_t hi) {
+  const u32x4 w = {bf16_pair(lo, false), bf16_pair(lo, true), bf16_pair(hi, false), bf16_pair(hi, true)};
+  return __builtin_bit_cast(bf16x8, w);
+}
+
+// Whether a block's query rows keep any of the 32 tokens from pos0 on, and all of them.
+struct Kept {
+  bool some, full;
+};
+__device__ __forceinline__ Kept kept_of(const GqaDecodeParams& p, const Piece& now, int pos0) {
+  const int lo = now.reach_lo(), hi = now.reach_hi();
+  return Kept{pos0 < hi && (pos0 < p.S || (p.W > 0 && pos0 + kWaveTokens > lo - p.W)),
+              pos0 + kWaveTokens <= lo && (pos0 + kWaveTokens <= p.S || pos0 >= hi - p.W)};
+}
+
+// End of a block: the shares of the TG waves that hold the same rows (tokens apart) meet in LDS, references and sums first (ml: [TG][R]),
+// then the outputs at the common reference, 1 / PARTS of the columns at a time (o_lds: [TG][R][D / PARTS + 4]).  tg: which of the TG
+// the wave is; row0: its first row.  Blocks that other work groups share too leave partial rows in `slot`.
+template <int D, int RT, int R, int TG, int PARTS, int THREADS, bool OUT32>
+__device__ __forceinline__ void finish(const GqaDecodeParams& p, const Dealer<R, THREADS>& dealer, const Piece& now, Rows<D, RT>& a, float* o_lds, float4* ml,
+                                       int tg, int row0, int slot) {
+  constexpr int kCols = D / 16, kOStride = D / PARTS + 4;
+  const int tid = threadIdx.x, lane = tid & 63, n16 = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    a.l[rt] = row_sum(a.l[rt]);
+    if (g == 0) ml[tg * R + row0 + rt * 16 + n16] = make_float4(a.m[rt], a.l[rt], a.n[rt], a.saw_nan);
+  }
+  lds_barrier();
+  float shrink[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < TG; ++w) top = fmaxf(top, ml[w * R + row0 + rt * 16 + n16].z);
+    // (a wave that kept nothing has zeros, or NaN that has to stay: nothing is skipped)
+    shrink[rt] = factor(a.n[rt], top);
+  }
+  const GqaDecodeParams& end = *late_arguments();
+  constexpr int kChunks = D / 8 / PARTS;
+  const int rows = dealer.rows_of(now);
+  const bool whole = now.whole();
+#pragma unroll
+  for (int part = 0; part < PARTS; ++part) {
+    if (part) lds_barrier();  // (the part before has been read)
+    if (PARTS == 1 || g / (4 / PARTS) == part) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        float* const dst = o_lds + (tg * R + row0 + rt * 16 + n16) * kOStride + (4 * g % (16 / PARTS)) * kCols;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int c = 0; c < kCols; c += 4)
+            *(f32x4*)(dst + i * kCols + c) = f32x4{a.o[rt][c][i] * shrink[rt], a.o[rt][c + 1][i] * shrink[rt], a.o[rt][c + 2][i] * shrink[rt], a.o[rt][c + 3][i] * shrink[rt]};
+      }
+    }
+    lds_barrier();
+    for (int k = tid; k < rows * kChunks; k += THREADS) {
+      const int row = k / kChunks, in_part = k % kChunks * 8, col = part * (D / PARTS) + in_part;
+      f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+      float top = -INFINITY, vtop = -INFINITY, sum = 0.f, nans = 0.f;
+#pragma unroll
+      for (int w = 0; w < TG; ++w) {
+        top = fmaxf(top, ml[w * R + row].x);
+        vtop = fmaxf(vtop, ml[w * R + row].z);
+        nans += ml[w * R + row].w;
+      }
+#pragma unroll
+      for (int w = 0; w < TG; ++w) {
+        const float4 e = ml[w * R + row];
+        sum += e.y * factor(e.x, top);
+        const f32x4* src = (const f32x4*)(o_lds + (w * R + row) * kOStride + in_part);
+        lo += src[0];
+        hi += src[1];
+      }
+      const uint32_t qt = (uint32_t)(now.rb * R + row) / (uint32_t)end.group, gi = (uint32_t)(now.rb * R + row) - qt * end.group;
+      if (__builtin_expect(nans != 0.f, 0)) {
+        // NaN that the loop has taken for 0: the columns of the tokens that this row keeps are looked through again
+        const int sees = now.rq.L - now.rq.n + (int)qt + 1;
+#pragma unroll 1
+        for (int tile = now.tile_lo; tile < now.tile_hi; ++tile) {
+          const int lp = now.bk.pages.logical(tile);
+          const size_t ph = (size_t)end.page_table[now.b * end.table_stride + lp] * end.kv_heads + now.h;
+#pragma unroll 1
+          for (int j = 0; j < kPage; ++j) {
+            if (!retained(lp * kPage + j, sees, end.S, end.W)) continue;
+            const u32x2 codes = *(const u32x2*)(end.v_cache + (ph * kPage + j) * D + col);
+            const uint32_t nan_lo = nan_codes(codes[0]), nan_hi = nan_codes(codes[1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if ((nan_lo >> (8 * i)) & 0x80u) lo[i] = NAN;
+              if ((nan_hi >> (8 * i)) & 0x80u) hi[i] = NAN;
+            }
+          }
+        }
+      }
+      const int64_t out_row = (int64_t)(now.rq.begin + (int)qt) * end.q_heads + now.h * end.group + (int)gi;
+      if (whole) {
+        const float inv = sum == 0.f ? 0.f : exp2_fast(vtop - top) / sum;  // (nothing kept: 0 and -inf)
+        if constexpr (OUT32) {
+          f32x4* dst = (f32x4*)((float*)end.out + out_row * D + col);
+          dst[0] = lo * inv;
+          dst[1] = hi * inv;
+        } else {
+          bf16x8 y;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            y[i] = (__bf16)(lo[i] * inv);
+            y[4 + i] = (__bf16)(hi[i] * inv);
+          }
+          *(bf16x8*)((uint16_t*)end.out + out_row * D + col) = y;
+        }
+        if (col == 0) {
+          end.lse[out_row] = sum == 0.f ? -INFINITY : (top + __log2f(sum) - kLift) * 0.69314718055994531f;
+          end.rows[out_row] = make_int2(0, 0);
+        }
+      } else {
+        float* dst = end.part_o + ((size_t)slot * R + row) * D + col;
+        ((f32x4*)dst)[0] = lo;
+        ((f32x4*)dst)[1] = hi;
+        if (col == 0) {
+          end.part_ml[(size_t)slot * R + row] = make_float4(top, sum, vtop, 0.f);
+          // the work group that takes a block's first page knows which ones take the others
+          if (now.tile_lo == 0) end.rows[out_row] = make_int2(slot, dealer.partners(now) * 64 + row);
+        }
+      }
+    }
+  }
+}
+
+}  // namespace
+}  // namespace omniattn

@@ -1,0 +1,281 @@
+// Attention of grouped-query layers over the paged 8-bit cache for requests with more than 16 query rows (several new tokens, or many
+// query heads to a KV head).  The same work as gqa_decode_kernel.hip, dealt out the same way; what differs is how a tile is shared.
+//
+// One work group of eight waves per compute unit.  A tile (32 TG tokens) is brought to LDS once by direct loads and read by RG = 8 / TG
+// waves for each 32 of its tokens, each with other query rows, so a block has RG * 16 * RT rows: the codes come from memory once for
+// all of them.  The tiles pass through a ring of stages, kStages - 1 of them requested ahead, over the ends of blocks too; one barrier per
+// tile.  (With the tile in registers, as in the other kernel, two waves per SIMD leave room for one tile ahead, and the products of
+// 32 rows take as long as that tile needs to arrive: 4.4 TB/s at 32 rows of width 128, 2.0 at 64.)
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "gqa_common.h"
+
+namespace omniattn {
+namespace {
+
+constexpr int kThreads = 512, kWaves = 8;
+
+template <int D, int RT>
+struct Wide {
+  static constexpr int kTokenGroups = D == 256 ? 2 : 4;       // TG
+  static constexpr int kRowGroups = kWaves / kTokenGroups;    // RG
+  static constexpr int kRows = kRowGroups * 16 * RT;
+  static constexpr int kTokens = kWaveTokens * kTokenGroups;  // of a tile
+  static constexpr int kTilesPerPage = kPage / kTokens;
+  static constexpr int kHalf = kTokens * D;                   // bytes of a tile's K codes; V's follow
+  static constexpr int kStages = D == 64 ? 5 : 3;
+  static constexpr int kLoads = 2 * kHalf / 1024 / kWaves;    // direct loads of a wave and tile (1 KB each), and one of the scales
+  static constexpr int kParts = D == 64 ? 2 : 4;              // the output's columns meet 1 / kParts at a time
+  static constexpr int kScaleBytes = 256;                     // of a wave and stage: K's and V's scale in turn, 32 times
+  static constexpr size_t kRing = (size_t)kStages * (2 * kHalf + kWaves * kScaleBytes);
+  static constexpr size_t kOBytes = (size_t)kTokenGroups * kRows * (D / kParts + 4) * 4;
+  static constexpr size_t kLds = kRing + kOBytes + 2 * kTokenGroups * kRows * 16;
+  static_assert(kLds + 8192 <= 160 * 1024, "LDS of a compute unit");
+};
+
+// Where a row's 16-byte chunks lie in LDS.  Rows stand in groups of 16 (tokens 16 i ..): row r at place(r), its chunk c at c ^ twist(r), so
+// that neither the 16 rows of a K operand nor the rows of a V operand meet in the same banks.  (A row is 4, 8 or 16 chunks, 64 banks
+// are 16 chunks.)
+template <int D>
+__device__ __forceinline__ int place(int r) {
+  if constexpr (D == 64) return r ^ ((r >> 2) & 3);
+  else if constexpr (D == 128) return r ^ ((r >> 2) & 1);
+  else return r;
+}
+template <int D>
+__device__ __forceinline__ int twist(int r) {
+  const int at = place<D>(r);
+  if constexpr (D == 64) return (at >> 2) & 3;
+  else if constexpr (D == 128) return (at >> 1) & 7;
+  else return at & 15;
+}
+
+// The same value from memory for every lane, through the scalar cache.
+__device__ __forceinline__ int scalar_load(const int32_t* at) {
+  return *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)uniform64((uint64_t)(uintptr_t)at);
+}
+
+// Four bytes per lane from an address of its own to LDS (see load_lds16 in decode_common.h).
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void load_lds4_each(uint32_t lds, const void* at) {
+  const uint32_t m = __builtin_amdgcn_readfirstlane(lds);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dword %1, off" : : "s"(m), "v"((uint64_t)(uintptr_t)at) : "m0", "memory");
+}
+#pragma clang diagnostic pop
+
+// Waits until the loads of the oldest tile are done, with `behind` tiles requested after it, and for all waves to get here.  (Other
+// loads and stores in between only make it wait for more than it has to.)
+template <int LOADS, int MOST>
+__device__ __forceinline__ void wait_tile(int behind) {
+  if constexpr (MOST >= 4) {
+    if (behind >= 4) {
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(4 * LOADS) : "memory");
+      return;
+    }
+  }
+  if constexpr (MOST >= 3) {
+    if (behind == 3) {
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(3 * LOADS) : "memory");
+      return;
+    }
+  }
+  if (behind >= 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(2 * LOADS) : "memory");
+  else if (behind == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(LOADS) : "memory");
+  else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
+}
+
+template <int D, int RT, bool OUT32>
+__global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p) {
+  using C = Wide<D, RT>;
+  constexpr int R = C::kRows, TG = C::kTokenGroups, kWords = D / 64, kCols = D / 16, kStages = C::kStages;
+  extern __shared__ __align__(1024) uint8_t ring[];   // [stages][K codes, V codes], [stages][waves][scales], output, references
+  uint8_t* const scale_ring = ring + kStages * 2 * C::kHalf;
+  float* const o_lds = (float*)(ring + C::kRing);
+  float4* const ml_lds = (float4*)(ring + C::kRing + C::kOBytes);
+  __shared__ typename Dealer<R, kThreads>::Lds dealt;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int n16 = lane & 15, g = lane >> 4;
+  const int tg = wave % TG, row0 = wave / TG * 16 * RT;
+  Dealer<R, kThreads> dealer(p, dealt);
+  Piece now;
+  if (!dealer.begin(now)) return;
+  const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)ring;
+
+  const int blocks_per_page = kPage >> p.scale_shift;
+  // Direct loads: the wave brings kLoads KB, one after the other, of K (waves 0 to 3) or V.  Lane l's 16 bytes of a KB are those of
+  // chunk l % chunks ^ twist of the row that belongs to place l / chunks: whole rows of it, in another order.
+  constexpr int kChunks = D / 16, kRowsPerKb = 64 / kChunks;
+  uint32_t from[C::kLoads];
+#pragma unroll
+  for (int i = 0; i < C::kLoads; ++i) {
+    const int at = (wave % 4 * C::kLoads + i) * kRowsPerKb + lane / kChunks;  // place among the tile's rows
+    const int r = at % 16;
+    from[i] = (at / 16 * 16 + place<D>(r)) * D + ((lane % kChunks) ^ twist<D>(place<D>(r))) * 16;  // (place is its own inverse)
+  }
+  const uint8_t* const codes = wave < 4 ? p.k_cache : p.v_cache;
+
+  // The tile that is asked for next: a page of a block, or a half of one.
+  Piece ahead = now;
+  int ahead_tile = now.tile_lo, ahead_half = 0, ahead_stage = 0, issued = 0;
+  auto skip_empty = [&] {  // false: no more tiles
+    while (ahead_tile >= ahead.tile_hi) {
+      if (!dealer.follow(ahead)) return false;
+      ahead_tile = ahead.tile_lo;
+    }
+    return true;
+  };
+  bool ahead_any = skip_empty();
+  int ahead_page = ahead_any ? scalar_load(p.page_table + ahead.b * p.table_stride + ahead.bk.pages.logical(ahead_tile)) : 0;
+  auto issue = [&] {
+    if (!ahead_any) return;
+    const size_t ph = (size_t)ahead_page * p.kv_heads + ahead.h;
+    const uint8_t* const base = codes + (ph * kPage + ahead_half * C::kTokens) * D;
+    const uint32_t to = ring_at + ahead_stage * 2 * C::kHalf + wave * C::kLoads * 1024;
+#pragma unroll
+    for (int i = 0; i < C::kLoads; ++i) load_lds16<false>(to + i * 1024, base, from[i]);
+    const float* const scales = (lane & 1 ? p.v_scales : p.k_scales) + ph * blocks_per_page + ((ahead_half * C::kTokens + tg * kWaveTokens) >> p.scale_shift);
+    load_lds4_each(ring_at + kStages * 2 * C::kHalf + (ahead_stage * kWaves + wave) * C::kScaleBytes, scales);
+    ++issued;
+    if (++ahead_stage == kStages) ahead_stage = 0;
+    if (++ahead_half == C::kTilesPerPage) {
+      ahead_half = 0;
+      ++ahead_tile;
+      ahead_any = skip_empty();
+      if (ahead_any) ahead_page = scalar_load(p.page_table + ahead.b * p.table_stride + ahead.bk.pages.logical(ahead_tile));
+    }
+  };
+  for (int i = 0; i < kStages - 1; ++i) issue();
+
+  bf16x8 q[RT][2 * kWords];
+  int reach[RT];
+  auto load_q = [&](const Piece& w) {
+    const int rows = dealer.rows_of(w);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int row = row0 + rt * 16 + n16;
+      const uint32_t t = (uint32_t)(w.rb * R + row) / (uint32_t)p.group, gi = (uint32_t)(w.rb * R + row) - t * p.group;
+      const bool valid = row < rows;
+      reach[rt] = valid ? w.rq.L - w.rq.n + (int)t + 1 : 0;
+      const uint16_t* src = p.q + (int64_t)(w.rq.begin + (int)t) * p.q_stride + (size_t)(w.h * p.group + (int)gi) * D + g * 16;
+#pragma unroll
+      for (int i = 0; i < 2 * kWords; ++i) q[rt][i] = valid ? *(const bf16x8*)(src + i / 2 * 64 + i % 2 * 8) : bf16x8{};
+    }
+  };
+  load_q(now);
+
+  // Operands in LDS, from the start of a stage on: rows of the wave's 32 tokens
+  const int k_row = (tg * kWaveTokens + place<D>(n16)) * D, k_twist = twist<D>(n16);
+  int v_at[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int r = 4 * g + j;
+    v_at[j] = C::kHalf + (tg * kWaveTokens + place<D>(r)) * D + ((n16 * kCols / 16) ^ twist<D>(r)) * 16 + n16 * kCols % 16;
+  }
+
+  int parity = 0, first_partial = 0, stage = 0, used = 0;
+  while (true) {
+    Rows<D, RT> a;
+    a.clear();
+    Piece next = now;
+    bool more_blocks = false;
+    if (now.tile_lo >= now.tile_hi) more_blocks = dealer.follow(next);
+    const bool mine = row0 < dealer.rows_of(now);  // (a short block: waves without rows only bring their part of the tiles)
+    for (int tile = now.tile_lo; tile < now.tile_hi; ++tile) {
+#pragma unroll 1
+      for (int half = 0; half < C::kTilesPerPage; ++half) {
+        wait_tile<C::kLoads + 1, kStages - 2>(issued - used - 1);
+        issue();  // (into the stage that every wave has left behind at the barrier)
+        ++used;
+        const bool last = tile + 1 == now.tile_hi && half + 1 == C::kTilesPerPage;
+        const uint8_t* const from_stage = ring + stage * 2 * C::kHalf;
+        const float2 scale = *(const float2*)(scale_ring + (stage * kWaves + wave) * C::kScaleBytes);
+        if (++stage == kStages) stage = 0;
+        const int pos0 = now.bk.pages.logical(tile) * kPage + half * C::kTokens + tg * kWaveTokens;
+        const Kept kept = kept_of(p, now, pos0);
+        f32x4 s[RT][2];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) s[rt][0] = s[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const bool work = mine && kept.some;
+        if (work) {
+#pragma unroll
+          for (int c = 0; c < kWords; ++c) {
+            u32x4 k[2];
+#pragma unroll
+            for (int h2 = 0; h2 < 2; ++h2) k[h2] = *(const u32x4*)(from_stage + k_row + h2 * 16 * D + ((4 * c + g) ^ k_twist) * 16);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int h2 = 0; h2 < 2; ++h2) {
+                const bf16x8 x = k_operand(k[h2][2 * u], k[h2][2 * u + 1]);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) s[rt][h2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[rt][2 * c + u], s[rt][h2], 0, 0, 0);
+              }
+          }
+        }
+        int seen[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) seen[rt] = reach[rt];
+        if (last) {
+          more_blocks = dealer.follow(next);
+          if (more_blocks) load_q(next);
+        }
+        if (work) {
+          f16x8 high[RT], low[RT];
+          weigh<D, RT, OUT32>(p, a, s, seen, kept.full, pos0, g, p.scale_log2 * scale.x, scale.y, high, low);
+          typename VWord<kWords>::type v[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = *(const typename VWord<kWords>::type*)(from_stage + v_at[j % 4] + j / 4 * 16 * D);
+          if (!kept.full) sanitize<D, RT>(p, a, v, now, pos0, g);
+          add_values<D, RT, OUT32>(a, v, high, low);
+        }
+      }
+    }
+    if (now.tile_lo >= now.tile_hi && more_blocks) load_q(next);
+    finish<D, RT, R, TG, C::kParts, kThreads, OUT32>(p, dealer, now, a, o_lds, ml_lds + parity * TG * R, tg, row0, 2 * blockIdx.x + first_partial);
+    parity ^= 1;
+    first_partial = 1;
+    if (!more_blocks) break;
+    now = next;
+  }
+}
+
+template <int D, int RT, bool OUT32>
+hipError_t start(const GqaDecodeParams& p, int units, hipStream_t stream) {
+  constexpr size_t lds = Wide<D, RT>::kLds;
+  hipLaunchKernelGGL((gqa_wide_kernel<D, RT, OUT32>), dim3(units), dim3(kThreads), lds, stream, p);
+  return hipGetLastError();
+}
+template <int D, int RT>
+hipError_t allow_lds() {
+  constexpr int lds = (int)Wide<D, RT>::kLds;
+  hipError_t e = hipFuncSetAttribute((const void*)gqa_wide_kernel<D, RT, false>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e == hipSuccess) e = hipFuncSetAttribute((const void*)gqa_wide_kernel<D, RT, true>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  return e;
+}
+
+}  // namespace
+
+hipError_t init_gqa_wide_kernels() {
+  hipError_t e = allow_lds<64, 1>();
+  if (e == hipSuccess) e = allow_lds<64, 2>();
+  if (e == hipSuccess) e = allow_lds<128, 1>();
+  if (e == hipSuccess) e = allow_lds<128, 2>();
+  if (e == hipSuccess) e = allow_lds<256, 1>();
+  return e;
+}
+
+hipError_t launch_gqa_wide(const GqaDecodeParams& p, const GqaShape& shape, int units, hipStream_t stream) {
+  auto with = [&](auto d, auto rt) {
+    return p.out_fp32 ? start<decltype(d)::value, decltype(rt)::value, true>(p, units, stream)
+                      : start<decltype(d)::value, decltype(rt)::value, false>(p, units, stream);
+  };
+  using std::integral_constant;
+  const bool one = shape.row_tiles == 1;
+  if (p.head_dim == 64) return one ? with(integral_constant<int, 64>{}, integral_constant<int, 1>{}) : with(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+  if (p.head_dim == 128) return one ? with(integral_constant<int, 128>{}, integral_constant<int, 1>{}) : with(integral_constant<int, 128>{}, integral_constant<int, 2>{});
+  return with(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+}
+
+}  // namespace omniattn
