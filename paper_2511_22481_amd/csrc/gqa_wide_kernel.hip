@@ -127,7 +127,7 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
     return true;
   };
   bool ahead_any = skip_empty();
-  int ahead_page = ahead_any ? scalar_load(p.page_table + ahead.b * p.table_stride + ahead.bk.pages.logical(ahead_tile)) : 0;
+  int ahead_page = 0;
   auto issue = [&] {
     if (!ahead_any) return;
     const size_t ph = (size_t)ahead_page * p.kv_heads + ahead.h;
@@ -143,10 +143,15 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
       ahead_half = 0;
       ++ahead_tile;
       ahead_any = skip_empty();
-      if (ahead_any) ahead_page = scalar_load(p.page_table + ahead.b * p.table_stride + ahead.bk.pages.logical(ahead_tile));
     }
   };
-  for (int i = 0; i < kStages - 1; ++i) issue();
+  auto ask_page = [&] {
+    if (ahead_any && ahead_half == 0) ahead_page = scalar_load(p.page_table + ahead.b * p.table_stride + ahead.bk.pages.logical(ahead_tile));
+  };
+  for (int i = 0; i < kStages - 1; ++i) {
+    ask_page();
+    issue();
+  }
 
   bf16x8 q[RT][2 * kWords];
   int reach[RT];
@@ -176,19 +181,22 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
 
   int parity = 0, first_partial = 0, stage = 0, used = 0;
   while (true) {
+    // The query is waited for here, and asked for behind the loop.  If its loads could be under way at its use in the loop, the wait
+    // would stand there in every pass, and as the compiler does not count the direct loads, it would be for all tiles.
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int i = 0; i < 2 * kWords; ++i) asm volatile("" : "+v"(q[rt][i]));
     Rows<D, RT> a;
     a.clear();
-    Piece next = now;
-    bool more_blocks = false;
-    if (now.tile_lo >= now.tile_hi) more_blocks = dealer.follow(next);
     const bool mine = row0 < dealer.rows_of(now);  // (a short block: waves without rows only bring their part of the tiles)
     for (int tile = now.tile_lo; tile < now.tile_hi; ++tile) {
 #pragma unroll 1
       for (int half = 0; half < C::kTilesPerPage; ++half) {
+        ask_page();  // (back behind the wait, which is for scalar loads too)
         wait_tile<C::kLoads + 1, kStages - 2>(issued - used - 1);
         issue();  // (into the stage that every wave has left behind at the barrier)
         ++used;
-        const bool last = tile + 1 == now.tile_hi && half + 1 == C::kTilesPerPage;
         const uint8_t* const from_stage = ring + stage * 2 * C::kHalf;
         const float2 scale = *(const float2*)(scale_ring + (stage * kWaves + wave) * C::kScaleBytes);
         if (++stage == kStages) stage = 0;
@@ -214,16 +222,9 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
               }
           }
         }
-        int seen[RT];
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) seen[rt] = reach[rt];
-        if (last) {
-          more_blocks = dealer.follow(next);
-          if (more_blocks) load_q(next);
-        }
         if (work) {
           f16x8 high[RT], low[RT];
-          weigh<D, RT, OUT32>(p, a, s, seen, kept.full, pos0, g, p.scale_log2 * scale.x, scale.y, high, low);
+          weigh<D, RT, OUT32>(p, a, s, reach, kept.full, pos0, g, p.scale_log2 * scale.x, scale.y, high, low);
           typename VWord<kWords>::type v[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[j] = *(const typename VWord<kWords>::type*)(from_stage + v_at[j % 4] + j / 4 * 16 * D);
@@ -232,7 +233,10 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
         }
       }
     }
-    if (now.tile_lo >= now.tile_hi && more_blocks) load_q(next);
+    // (behind the loop: see above)
+    Piece next = now;
+    const bool more_blocks = dealer.follow(next);
+    if (more_blocks) load_q(next);
     finish<D, RT, R, TG, C::kParts, kThreads, OUT32>(p, dealer, now, a, o_lds, ml_lds + parity * TG * R, tg, row0, 2 * blockIdx.x + first_partial);
     parity ^= 1;
     first_partial = 1;
