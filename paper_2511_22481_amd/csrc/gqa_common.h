@@ -168,19 +168,30 @@ struct Piece {
   __device__ __forceinline__ int reach_hi() const { return rq.L - rq.n + bk.t1 + 1; }
 };
 
+// What a loop over a block's pages needs of it.
+struct Span {
+  TileLayout pages;
+  int lo, hi;            // tokens that the block's first and last query see
+  int tile_hi;
+  bool several;          // several queries
+  __device__ __forceinline__ explicit Span(const Piece& w) : pages(w.bk.pages), lo(w.reach_lo()), hi(w.reach_hi()), tile_hi(w.tile_hi), several(w.bk.t1 > w.bk.t0) {}
+};
+
 // Finds a work group's share and walks through its blocks.  R: rows of a block.  All threads call everything.
 template <int R, int THREADS>
 struct Dealer {
+  // What is needed only from block to block stays here: in scalar registers it would push the loop's own out.
   struct Lds {
     int64_t wave_tot[THREADS / 64], off;
     int4 requests[THREADS];  // (batches of up to THREADS: L, begin, n, units of one KV head)
     int at;
+    Shares shares;
+    int64_t stop;            // end of the share
+    int pieces[THREADS / 64][3][16];
   };
   const GqaDecodeParams& p;
   Lds& lds;
-  int per;       // requests per thread
-  Shares shares;
-  int64_t stop;  // end of the share
+  int per;  // requests per thread
 
   __device__ __forceinline__ Dealer(const GqaDecodeParams& params, Lds& memory) : p(params), lds(memory) {}
 
@@ -239,6 +250,7 @@ struct Dealer {
     }
     if (lane == 63) lds.wave_tot[wave] = sum;
     __syncthreads();
+    Shares shares;
     shares.T = 0;
     for (int w = 0; w < THREADS / 64; ++w) {
       if (w == wave) sum += shares.T;
@@ -253,12 +265,13 @@ struct Dealer {
     if (sum - mine <= first && first < sum) {
       lds.at = tid;
       lds.off = first - (sum - mine);
+      lds.shares = shares;
+      lds.stop = shares.bound(blockIdx.x + 1);
     }
     __syncthreads();
     const int at = uniform(lds.at) * per;
     int64_t off = (int64_t)uniform64(lds.off);
-    stop = shares.bound(blockIdx.x + 1);
-    now.left = stop - first;
+    now.left = shares.bound(blockIdx.x + 1) - first;
     if (per == 1) {
       now.b = at;
       const int4 r = lds.requests[at];
@@ -288,7 +301,31 @@ struct Dealer {
   }
   __device__ __forceinline__ int rows_of(const Piece& w) const { return (int)min((int64_t)w.rq.n * p.group - (int64_t)w.rb * R, (int64_t)R); }
   // Work groups that share the block of w, from this one on (which has its first page).
-  __device__ __forceinline__ int partners(const Piece& w) const { return shares.owner(stop - w.left - w.off + w.bk.units() - 1) - (int)blockIdx.x + 1; }
+  __device__ __forceinline__ int partners(const Piece& w) const {
+    const Shares shares = lds.shares;
+    return shares.owner(lds.stop - w.left - w.off + w.bk.units() - 1) - (int)blockIdx.x + 1;
+  }
+  // A wave's notes of blocks, in one of three places.
+  __device__ __forceinline__ void keep(int place, const Piece& w) const {
+    const int v[16] = {w.b, w.h, w.rb, w.rq.L, w.rq.begin, w.rq.n, w.bk.t0, w.bk.t1, w.bk.pages.ns, w.bk.pages.w0, w.bk.pages.w1, w.off, w.tile_lo, w.tile_hi,
+                       (int)w.left, (int)(w.left >> 32)};
+    int4* const at = (int4*)lds.pieces[uniform(threadIdx.x >> 6)][place];
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) at[i] = make_int4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+    }
+  }
+  __device__ __forceinline__ Piece kept(int place) const {
+    const int4* const at = (const int4*)lds.pieces[uniform(threadIdx.x >> 6)][place];
+    const int4 a = at[0], b = at[1], c = at[2], d = at[3];
+    Piece w;
+    w.b = uniform(a.x), w.h = uniform(a.y), w.rb = uniform(a.z), w.rq.L = uniform(a.w);
+    w.rq.begin = uniform(b.x), w.rq.n = uniform(b.y), w.bk.t0 = uniform(b.z), w.bk.t1 = uniform(b.w);
+    w.bk.pages.ns = uniform(c.x), w.bk.pages.w0 = uniform(c.y), w.bk.pages.w1 = uniform(c.z), w.off = uniform(c.w);
+    w.tile_lo = uniform(d.x), w.tile_hi = uniform(d.y);
+    w.left = (int64_t)(((uint64_t)(uint32_t)uniform(d.w) << 32) | (uint32_t)uniform(d.z));
+    return w;
+  }
 };
 
 // A wave's share of the output rows: O holds sum 2^(x - n + kLift) v_scale v_code and l sum 2^(x - m + kLift) for the row's logits x
@@ -368,9 +405,9 @@ __device__ __forceinline__ void weigh(const GqaDecodeParams& p, Rows<D, RT>& a, 
 // that keep the token, and only for those, but a weight of 0 would not stop it in the product: it goes on as 0 too, and the block's end
 // sees to it.  Lane (n16, g) has tokens 4 g + j % 4 (+ 16 from j = 4 on).
 template <int D, int RT>
-__device__ __forceinline__ void sanitize(const GqaDecodeParams& p, Rows<D, RT>& a, typename VWord<D / 64>::type (&v)[8], const Piece& now, int pos0, int g) {
+__device__ __forceinline__ void sanitize(const GqaDecodeParams& p, Rows<D, RT>& a, typename VWord<D / 64>::type (&v)[8], const Span& now, int pos0, int g) {
   constexpr int kWords = D / 64;
-  const int lo = now.reach_lo(), hi = now.reach_hi();
+  const int lo = now.lo, hi = now.hi;
   uint32_t any_nan = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -380,7 +417,7 @@ __device__ __forceinline__ void sanitize(const GqaDecodeParams& p, Rows<D, RT>& 
 #pragma unroll
     for (int i = 0; i < kWords; ++i) any_nan |= nan_codes(word<kWords>(v[j], i));
   }
-  if (now.bk.t1 > now.bk.t0 && __ballot(any_nan != 0) != 0) {
+  if (now.several && __ballot(any_nan != 0) != 0) {
     a.saw_nan = 1.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = without_nan<kWords>(v[j]);
@@ -419,8 +456,8 @@ __device__ __forceinline__ bf16x8 k_operand(uint32_t lo, uint32_t hi) {
 struct Kept {
   bool some, full;
 };
-__device__ __forceinline__ Kept kept_of(const GqaDecodeParams& p, const Piece& now, int pos0) {
-  const int lo = now.reach_lo(), hi = now.reach_hi();
+__device__ __forceinline__ Kept kept_of(const GqaDecodeParams& p, const Span& now, int pos0) {
+  const int lo = now.lo, hi = now.hi;
   return Kept{pos0 < hi && (pos0 < p.S || (p.W > 0 && pos0 + kWaveTokens > lo - p.W)),
               pos0 + kWaveTokens <= lo && (pos0 + kWaveTokens <= p.S || pos0 >= hi - p.W)};
 }

@@ -131,10 +131,10 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D)) void gqa_decode_kernel(
   // What a page's loads need: where its codes are, and the wave's two scales.
   __amdgpu_buffer_rsrc_t rk, rv;
   float ks = 0.f, vs = 0.f;
-  auto aim = [&](const Piece& w, int tile, int ids, int held) {
+  auto aim = [&](const TileLayout& pages, int h, int seen, int tile, int ids, int held) {
     const int page = __builtin_amdgcn_readlane(ids, tile - held);
-    const size_t ph = (size_t)page * p.kv_heads + w.h;
-    const int live = min(w.reach_hi() - w.bk.pages.logical(tile) * kPage, kPage);
+    const size_t ph = (size_t)page * p.kv_heads + h;
+    const int live = min(seen - pages.logical(tile) * kPage, kPage);
     rk = codes_at(p.k_cache + ph * head_bytes, live * D);
     rv = codes_at(p.v_cache + ph * head_bytes, live * D);
     ks = p.k_scales[ph * blocks_per_page + my_block];
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D)) void gqa_decode_kernel(
   int held = now.tile_lo, ids = entries(now.b, now.bk.pages, held);
   load_q(now);
   if (now.tile_lo < now.tile_hi) {
-    aim(now, now.tile_lo, ids, held);
+    aim(now.bk.pages, now.h, now.reach_hi(), now.tile_lo, ids, held);
     load_k<D>(t, rk, k_at);
     load_v<D>(t, rv, v_at);
   }
@@ -156,35 +156,45 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D)) void gqa_decode_kernel(
   // Entries of the next request's first block, asked for as soon as the one before it begins: short requests come and go faster
   // than a chain of loads from the table to the codes.
   int ahead_b = -1, ahead_ids = 0;
+  // Of the block that is computed, what the loop needs; the rest is the wave's note 0, and the next block's note 1.
+  dealer.keep(0, now);
+  int b = now.b, h = now.h, tile = now.tile_lo;
+  Span span(now);
 
   while (true) {
-    Piece next = now;
     bool more_blocks = false, next_loads = false;
-    if (ahead_b <= now.b) {
-      ahead_b = now.b + 1;
+    if (ahead_b <= b) {
+      ahead_b = b + 1;
       if (ahead_b < p.batch) {
         const Request r = dealer.request(ahead_b);
         if (r.n > 0) ahead_ids = entries(ahead_b, block_of<R>(p, r, 0).pages, 0);
       }
     }
-    // What the next block is (asked late, so that its description need not be kept through the loop), and where its first page is: its
-    // entries are the same as this block's for another KV head, or were asked for before, or are asked for now.
+    // What the next block is (asked late, so that its description need not be kept through the loop), its query, and where its first page
+    // is: its entries are the same as this block's for another KV head, or were asked for before, or are asked for now.
     auto turn_to_next = [&] {
+      const Piece was = dealer.kept(0);
+      Piece next = was;
       more_blocks = dealer.follow(next);
-      next_loads = more_blocks && next.tile_lo < next.tile_hi;
-      if (!next_loads) return;
-      if (!(next.b == now.b && next.rb == now.rb && held == 0)) {
-        held = 0;
-        ids = next.b == ahead_b && next.rb == 0 ? ahead_ids : entries(next.b, next.bk.pages, 0);
+      if (!more_blocks) return;
+      dealer.keep(1, next);
+      next_loads = next.tile_lo < next.tile_hi;
+      if (next_loads) {
+        if (!(next.b == was.b && next.rb == was.rb && held == 0)) {
+          held = 0;
+          ids = next.b == ahead_b && next.rb == 0 ? ahead_ids : entries(next.b, next.bk.pages, 0);
+        }
+        aim(next.bk.pages, next.h, next.reach_hi(), next.tile_lo, ids, held);
       }
-      aim(next, next.tile_lo, ids, held);
+      load_q(next);
     };
     Rows<D, 1> a;
     a.clear();
 
-    for (int tile = now.tile_lo; tile < now.tile_hi; ++tile) {
-      const int pos0 = now.bk.pages.logical(tile) * kPage + wave * kWaveTokens;
-      const Kept kept = kept_of(p, now, pos0);
+    const bool nothing = tile >= span.tile_hi;
+    for (; tile < span.tile_hi; ++tile) {
+      const int pos0 = span.pages.logical(tile) * kPage + wave * kWaveTokens;
+      const Kept kept = kept_of(p, span, pos0);
       f32x4 s[1][2] = {{f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}};
 #pragma unroll
       for (int i = 0; i < 2 * kWords; ++i) {
@@ -200,28 +210,26 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D)) void gqa_decode_kernel(
       const int seen[1] = {reach[0]};
       // the next page's loads, of this block or the next one, as soon as their registers are free
       bool more = true;
-      if (tile + 1 < now.tile_hi) {
+      if (tile + 1 < span.tile_hi) {
         if (tile + 1 - held >= 64) {
           held = tile + 1;
-          ids = entries(now.b, now.bk.pages, held);
+          ids = entries(b, span.pages, held);
         }
-        aim(now, tile + 1, ids, held);
+        aim(span.pages, h, span.hi, tile + 1, ids, held);
       } else {
         turn_to_next();
         more = next_loads;
-        if (more_blocks) load_q(next);
       }
       if (more) load_k<D>(t, rk, k_at);
 
       f16x8 high[1], low[1];
       weigh<D, 1, OUT32>(p, a, s, seen, kept.full, pos0, g, k_factor, v_scale, high, low);
-      if (!kept.full) sanitize<D, 1>(p, a, t.v, now, pos0, g);
+      if (!kept.full) sanitize<D, 1>(p, a, t.v, span, pos0, g);
       add_values<D, 1, OUT32>(a, t.v, high, low);
       if (more) load_v<D>(t, rv, v_at);
     }
-    if (now.tile_lo >= now.tile_hi) {  // (nothing kept: the next block has not been asked for yet)
+    if (nothing) {  // (the next block has not been asked for yet)
       turn_to_next();
-      if (more_blocks) load_q(next);
       if (next_loads) {
         load_k<D>(t, rk, k_at);
         load_v<D>(t, rv, v_at);
@@ -229,11 +237,16 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D)) void gqa_decode_kernel(
     }
     if (more_blocks) store_q(q_side ^ 1);
     q_side ^= 1;
-    finish<D, 1, R, 4, C::kParts, kThreads, OUT32>(p, dealer, now, a, o_lds, ml_lds + parity * 4 * R, wave, 0, 2 * blockIdx.x + first_partial);
+    finish<D, 1, R, 4, C::kParts, kThreads, OUT32>(p, dealer, dealer.kept(0), a, o_lds, ml_lds + parity * 4 * R, wave, 0, 2 * blockIdx.x + first_partial);
     parity ^= 1;
     first_partial = 1;
     if (!more_blocks) break;
-    now = next;
+    const Piece next = dealer.kept(1);
+    dealer.keep(0, next);
+    b = next.b;
+    h = next.h;
+    tile = next.tile_lo;
+    span = Span(next);
   }
 }
 

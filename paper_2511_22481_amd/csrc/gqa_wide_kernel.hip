@@ -56,6 +56,16 @@ __device__ __forceinline__ int scalar_load(const int32_t* at) {
   return *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)uniform64((uint64_t)(uintptr_t)at);
 }
 
+// Sixteen bytes per lane at the LDS base set before, from a scalar address that went through settle_address.  (As load_lds16_at, but
+// the rows may stay in L2: other blocks of query rows read them too.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+template <int IMM>
+__device__ __forceinline__ void load_lds16_here(uint64_t base, uint32_t off) {
+  asm volatile("global_load_lds_dwordx4 %0, %1 offset:%2" : : "v"(off), "s"(base), "n"(IMM) : "m0", "memory");
+}
+#pragma clang diagnostic pop
+
 // Four bytes per lane from an address of its own to LDS (see load_lds16 in decode_common.h).
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
@@ -107,46 +117,61 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
   // Direct loads: the wave brings kLoads KB, one after the other, of K (waves 0 to 3) or V.  Lane l's 16 bytes of a KB are those of
   // chunk l % chunks ^ twist of the row that belongs to place l / chunks: whole rows of it, in another order.
   constexpr int kChunks = D / 16, kRowsPerKb = 64 / kChunks;
+  // (The KB's own offset is the instruction's, on both sides.)
   uint32_t from[C::kLoads];
 #pragma unroll
   for (int i = 0; i < C::kLoads; ++i) {
     const int at = (wave % 4 * C::kLoads + i) * kRowsPerKb + lane / kChunks;  // place among the tile's rows
     const int r = at % 16;
-    from[i] = (at / 16 * 16 + place<D>(r)) * D + ((lane % kChunks) ^ twist<D>(place<D>(r))) * 16;  // (place is its own inverse)
+    from[i] = (at / 16 * 16 + place<D>(r)) * D + ((lane % kChunks) ^ twist<D>(place<D>(r))) * 16 - i * 1024;  // (place is its own inverse)
   }
   const uint8_t* const codes = wave < 4 ? p.k_cache : p.v_cache;
 
-  // The tile that is asked for next: a page of a block, or a half of one.
-  Piece ahead = now;
-  int ahead_tile = now.tile_lo, ahead_half = 0, ahead_stage = 0, issued = 0;
-  auto skip_empty = [&] {  // false: no more tiles
-    while (ahead_tile >= ahead.tile_hi) {
-      if (!dealer.follow(ahead)) return false;
-      ahead_tile = ahead.tile_lo;
-    }
-    return true;
+  // The tile that is asked for next: a page of a block, or a half of one.  The block's description is the wave's note 0.
+  int ahead_tile = now.tile_lo, ahead_hi = now.tile_hi, ahead_half = 0, ahead_stage = 0, issued = 0, ahead_h = now.h, ahead_page = 0;
+  TileLayout ahead_pages = now.bk.pages;
+  const int32_t* ahead_table = p.page_table + now.b * p.table_stride;
+  bool ahead_any = true;
+  dealer.keep(0, now);
+  auto skip_empty = [&] {
+    if (ahead_tile < ahead_hi) return;
+    Piece w = dealer.kept(0);
+    do ahead_any = dealer.follow(w);
+    while (ahead_any && w.tile_lo >= w.tile_hi);
+    if (!ahead_any) return;
+    dealer.keep(0, w);
+    ahead_tile = w.tile_lo;
+    ahead_hi = w.tile_hi;
+    ahead_h = w.h;
+    ahead_pages = w.bk.pages;
+    ahead_table = p.page_table + w.b * p.table_stride;
   };
-  bool ahead_any = skip_empty();
-  int ahead_page = 0;
+  skip_empty();
+  const float* const my_scales = lane & 1 ? p.v_scales : p.k_scales;
+  auto ask_page = [&] {
+    if (ahead_any && ahead_half == 0) ahead_page = scalar_load(ahead_table + ahead_pages.logical(ahead_tile));
+  };
   auto issue = [&] {
     if (!ahead_any) return;
-    const size_t ph = (size_t)ahead_page * p.kv_heads + ahead.h;
-    const uint8_t* const base = codes + (ph * kPage + ahead_half * C::kTokens) * D;
-    const uint32_t to = ring_at + ahead_stage * 2 * C::kHalf + wave * C::kLoads * 1024;
-#pragma unroll
-    for (int i = 0; i < C::kLoads; ++i) load_lds16<false>(to + i * 1024, base, from[i]);
-    const float* const scales = (lane & 1 ? p.v_scales : p.k_scales) + ph * blocks_per_page + ((ahead_half * C::kTokens + tg * kWaveTokens) >> p.scale_shift);
-    load_lds4_each(ring_at + kStages * 2 * C::kHalf + (ahead_stage * kWaves + wave) * C::kScaleBytes, scales);
+    const size_t ph = (size_t)ahead_page * p.kv_heads + ahead_h;
+    uint64_t base = (uint64_t)(uintptr_t)(codes + (ph * kPage + ahead_half * C::kTokens) * D), same = base;
+    set_lds_base(ring_at + ahead_stage * 2 * C::kHalf + wave * C::kLoads * 1024);
+    settle_address(base, same);
+    load_lds16_here<0>(base, from[0]);
+    load_lds16_here<1024>(base, from[1]);
+    if constexpr (C::kLoads > 2) {
+      load_lds16_here<2048>(base, from[2]);
+      load_lds16_here<3072>(base, from[3]);
+    }
+    load_lds4_each(ring_at + kStages * 2 * C::kHalf + (ahead_stage * kWaves + wave) * C::kScaleBytes,
+                   my_scales + ph * blocks_per_page + ((ahead_half * C::kTokens + tg * kWaveTokens) >> p.scale_shift));
     ++issued;
     if (++ahead_stage == kStages) ahead_stage = 0;
     if (++ahead_half == C::kTilesPerPage) {
       ahead_half = 0;
       ++ahead_tile;
-      ahead_any = skip_empty();
+      skip_empty();
     }
-  };
-  auto ask_page = [&] {
-    if (ahead_any && ahead_half == 0) ahead_page = scalar_load(p.page_table + ahead.b * p.table_stride + ahead.bk.pages.logical(ahead_tile));
   };
   for (int i = 0; i < kStages - 1; ++i) {
     ask_page();
@@ -180,6 +205,10 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
   }
 
   int parity = 0, first_partial = 0, stage = 0, used = 0;
+  dealer.keep(1, now);  // (notes 1 and 2: the block that is computed, and the one behind it)
+  int tile = now.tile_lo;
+  bool mine = row0 < dealer.rows_of(now);  // (a short block: waves without rows only bring their part of the tiles)
+  Span span(now);
   while (true) {
     // The query is waited for here, and asked for behind the loop.  If its loads could be under way at its use in the loop, the wait
     // would stand there in every pass, and as the compiler does not count the direct loads, it would be for all tiles.
@@ -189,8 +218,7 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
       for (int i = 0; i < 2 * kWords; ++i) asm volatile("" : "+v"(q[rt][i]));
     Rows<D, RT> a;
     a.clear();
-    const bool mine = row0 < dealer.rows_of(now);  // (a short block: waves without rows only bring their part of the tiles)
-    for (int tile = now.tile_lo; tile < now.tile_hi; ++tile) {
+    for (; tile < span.tile_hi; ++tile) {
 #pragma unroll 1
       for (int half = 0; half < C::kTilesPerPage; ++half) {
         ask_page();  // (back behind the wait, which is for scalar loads too)
@@ -200,8 +228,8 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
         const uint8_t* const from_stage = ring + stage * 2 * C::kHalf;
         const float2 scale = *(const float2*)(scale_ring + (stage * kWaves + wave) * C::kScaleBytes);
         if (++stage == kStages) stage = 0;
-        const int pos0 = now.bk.pages.logical(tile) * kPage + half * C::kTokens + tg * kWaveTokens;
-        const Kept kept = kept_of(p, now, pos0);
+        const int pos0 = span.pages.logical(tile) * kPage + half * C::kTokens + tg * kWaveTokens;
+        const Kept kept = kept_of(p, span, pos0);
         f32x4 s[RT][2];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) s[rt][0] = s[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -228,20 +256,28 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
           typename VWord<kWords>::type v[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[j] = *(const typename VWord<kWords>::type*)(from_stage + v_at[j % 4] + j / 4 * 16 * D);
-          if (!kept.full) sanitize<D, RT>(p, a, v, now, pos0, g);
+          if (!kept.full) sanitize<D, RT>(p, a, v, span, pos0, g);
           add_values<D, RT, OUT32>(a, v, high, low);
         }
       }
     }
     // (behind the loop: see above)
-    Piece next = now;
+    const Piece done = dealer.kept(1);
+    Piece next = done;
     const bool more_blocks = dealer.follow(next);
-    if (more_blocks) load_q(next);
-    finish<D, RT, R, TG, C::kParts, kThreads, OUT32>(p, dealer, now, a, o_lds, ml_lds + parity * TG * R, tg, row0, 2 * blockIdx.x + first_partial);
+    if (more_blocks) {
+      load_q(next);
+      dealer.keep(2, next);
+    }
+    finish<D, RT, R, TG, C::kParts, kThreads, OUT32>(p, dealer, done, a, o_lds, ml_lds + parity * TG * R, tg, row0, 2 * blockIdx.x + first_partial);
     parity ^= 1;
     first_partial = 1;
     if (!more_blocks) break;
-    now = next;
+    next = dealer.kept(2);
+    dealer.keep(1, next);
+    tile = next.tile_lo;
+    mine = row0 < dealer.rows_of(next);
+    span = Span(next);
   }
 }
 
