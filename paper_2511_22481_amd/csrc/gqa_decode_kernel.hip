@@ -27,9 +27,9 @@
 namespace omniattn {
 namespace {
 
-constexpr int kThreads = 256, kRows = 16;
+constexpr int kThreads = 256;
 // Work groups of a compute unit, as far as their registers allow.
-constexpr int groups_per_cu(int head_dim) { return head_dim == 64 ? 4 : 2; }
+constexpr int groups_per_cu(int head_dim, int row_tiles) { return head_dim == 64 && row_tiles == 1 ? 4 : 2; }
 
 // Codes of one (page, KV head): `bytes` of them may be read, behind that the loads return zeros and touch no memory.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t codes_at(const uint8_t* base, uint32_t bytes) {
@@ -63,9 +63,10 @@ __device__ __forceinline__ void load_v(Tile<D>& t, __amdgpu_buffer_rsrc_t rsrc, 
   }
 }
 
-template <int D>
+template <int D, int RT>
 struct Narrow {
-  static constexpr int kParts = D == 256 ? 2 : 1;  // the output's columns meet 1 / kParts at a time, so that LDS holds two work groups
+  static constexpr int kRows = 16 * RT;
+  static constexpr int kParts = D * RT == 256 ? 2 : 1;  // the output's columns meet 1 / kParts at a time, so that LDS holds two work groups
   static constexpr int kOStride = D / kParts + 4;  // floats of a row in LDS
   // Width 256: the query operands are kept in LDS (two buffers, one for the next block); in registers they would leave one work
   // group to a compute unit.
@@ -74,10 +75,10 @@ struct Narrow {
   static constexpr size_t kLds = (size_t)4 * kRows * kOStride * 4 + 2 * 4 * kRows * 16 + 2 * kQBytes;
 };
 
-template <int D, bool OUT32>
-__global__ __launch_bounds__(kThreads, groups_per_cu(D)) void gqa_decode_kernel(GqaDecodeParams p) {
-  using C = Narrow<D>;
-  constexpr int R = kRows, kCols = D / 16, kWords = D / 64;
+template <int D, int RT, bool OUT32>
+__global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_kernel(GqaDecodeParams p) {
+  using C = Narrow<D, RT>;
+  constexpr int R = C::kRows, kCols = D / 16, kWords = D / 64;
   extern __shared__ __align__(16) float lds[];
   float* const o_lds = lds;                                    // [4 waves][R][kOStride]
   float4* const ml_lds = (float4*)(lds + 4 * R * C::kOStride); // [2][4 waves][R]
@@ -100,33 +101,40 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D)) void gqa_decode_kernel(
     const int last = pages.count() - 1;
     return last >= 0 ? p.page_table[b * p.table_stride + pages.logical(min(from + lane, last))] : 0;
   };
-  // Query rows of a block: lane n16 of every group of 16 holds one row, the columns that its K loads bring.  Rows past the last hold
-  // zeros.  reach: tokens that the row's query sees.
-  constexpr int kQs = C::kQLds ? kWords / 2 : 2 * kWords;  // operands that the wave reads: its share, or all
-  bf16x8 q[kQs];
-  int reach[1];
+  // Query rows of a block: lane n16 of every group of 16 holds one row of each row tile, the columns that its K loads bring.  Rows past
+  // the last hold zeros.  reach: tokens that the row's query sees.
+  constexpr int kQs = C::kQLds ? kWords / 2 : 2 * kWords;  // operands of a row tile that the wave reads: its share, or all
+  bf16x8 q[RT][kQs];
+  int reach[RT];
   auto load_q = [&](const Piece& w) {
-    const uint32_t t = (uint32_t)(w.rb * R + n16) / (uint32_t)p.group, gi = (uint32_t)(w.rb * R + n16) - t * p.group;
-    const bool valid = n16 < dealer.rows_of(w);
-    reach[0] = valid ? w.rq.L - w.rq.n + (int)t + 1 : 0;
-    const uint16_t* src = p.q + (int64_t)(w.rq.begin + (int)t) * p.q_stride + (size_t)(w.h * p.group + (int)gi) * D + g * 16;
-    // (operand 2 c + u holds columns 64 c + 16 g + 8 u on; in LDS, the wave brings those with the remainder `wave` by 4)
+    const int rows = dealer.rows_of(w);
 #pragma unroll
-    for (int i = 0; i < kQs; ++i) {
-      const int k = C::kQLds ? 4 * i + wave : i;
-      q[i] = valid ? *(const bf16x8*)(src + k / 2 * 64 + k % 2 * 8) : bf16x8{};
+    for (int rt = 0; rt < RT; ++rt) {
+      const int row = rt * 16 + n16;
+      const uint32_t t = (uint32_t)(w.rb * R + row) / (uint32_t)p.group, gi = (uint32_t)(w.rb * R + row) - t * p.group;
+      const bool valid = row < rows;
+      reach[rt] = valid ? w.rq.L - w.rq.n + (int)t + 1 : 0;
+      const uint16_t* src = p.q + (int64_t)(w.rq.begin + (int)t) * p.q_stride + (size_t)(w.h * p.group + (int)gi) * D + g * 16;
+      // (operand 2 c + u holds columns 64 c + 16 g + 8 u on; in LDS, the wave brings those with the remainder `wave` by 4)
+#pragma unroll
+      for (int i = 0; i < kQs; ++i) {
+        const int k = C::kQLds ? 4 * i + wave : i;
+        q[rt][i] = valid ? *(const bf16x8*)(src + k / 2 * 64 + k % 2 * 8) : bf16x8{};
+      }
     }
   };
   int q_side = 0;
   auto store_q = [&](int side) {  // (all waves find them behind the next barrier)
     if constexpr (C::kQLds) {
 #pragma unroll
-      for (int i = 0; i < kQs; ++i) q_lds[(side * 2 * kWords + 4 * i + wave) * 64 + lane] = q[i];
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int i = 0; i < kQs; ++i) q_lds[((side * RT + rt) * 2 * kWords + 4 * i + wave) * 64 + lane] = q[rt][i];
     }
   };
-  auto query = [&](int i) {
-    if constexpr (C::kQLds) return q_lds[(q_side * 2 * kWords + i) * 64 + lane];
-    else return q[i];
+  auto query = [&](int rt, int i) {
+    if constexpr (C::kQLds) return q_lds[((q_side * RT + rt) * 2 * kWords + i) * 64 + lane];
+    else return q[rt][i];
   };
   // What a page's loads need: where its codes are, and the wave's two scales.
   __amdgpu_buffer_rsrc_t rk, rv;
@@ -188,26 +196,33 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D)) void gqa_decode_kernel(
       }
       load_q(next);
     };
-    Rows<D, 1> a;
+    Rows<D, RT> a;
     a.clear();
 
     const bool nothing = tile >= span.tile_hi;
     for (; tile < span.tile_hi; ++tile) {
       const int pos0 = span.pages.logical(tile) * kPage + wave * kWaveTokens;
       const Kept kept = kept_of(p, span, pos0);
-      f32x4 s[1][2] = {{f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}};
+      f32x4 s[RT][2];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) s[rt][0] = s[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < 2 * kWords; ++i) {
-        const bf16x8 x = query(i);
+        bf16x8 k[2];
 #pragma unroll
-        for (int h2 = 0; h2 < 2; ++h2) {
-          const u32x4 codes = t.k[h2][i / 2];
-          s[0][h2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand(codes[i % 2 * 2], codes[i % 2 * 2 + 1]), x, s[0][h2], 0, 0, 0);
+        for (int h2 = 0; h2 < 2; ++h2) k[h2] = k_operand(t.k[h2][i / 2][i % 2 * 2], t.k[h2][i / 2][i % 2 * 2 + 1]);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          const bf16x8 x = query(rt, i);
+#pragma unroll
+          for (int h2 = 0; h2 < 2; ++h2) s[rt][h2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[h2], x, s[rt][h2], 0, 0, 0);
         }
       }
       // (the scale of a block without kept tokens may be anything)
       const float k_factor = p.scale_log2 * ks, v_scale = kept.some ? vs : 0.f;
-      const int seen[1] = {reach[0]};
+      int seen[RT];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) seen[rt] = reach[rt];
       // the next page's loads, of this block or the next one, as soon as their registers are free
       bool more = true;
       if (tile + 1 < span.tile_hi) {
@@ -222,10 +237,10 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D)) void gqa_decode_kernel(
       }
       if (more) load_k<D>(t, rk, k_at);
 
-      f16x8 high[1], low[1];
-      weigh<D, 1, OUT32>(p, a, s, seen, kept.full, pos0, g, k_factor, v_scale, high, low);
-      if (!kept.full) sanitize<D, 1>(p, a, t.v, span, pos0, g);
-      add_values<D, 1, OUT32>(a, t.v, high, low);
+      f16x8 high[RT], low[RT];
+      weigh<D, RT, OUT32>(p, a, s, seen, kept.full, pos0, g, k_factor, v_scale, high, low);
+      if (!kept.full) sanitize<D, RT>(p, a, t.v, span, pos0, g);
+      add_values<D, RT, OUT32>(a, t.v, high, low);
       if (more) load_v<D>(t, rv, v_at);
     }
     if (nothing) {  // (the next block has not been asked for yet)
@@ -237,7 +252,7 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D)) void gqa_decode_kernel(
     }
     if (more_blocks) store_q(q_side ^ 1);
     q_side ^= 1;
-    finish<D, 1, R, 4, C::kParts, kThreads, OUT32>(p, dealer, dealer.kept(0), a, o_lds, ml_lds + parity * 4 * R, wave, 0, 2 * blockIdx.x + first_partial);
+    finish<D, RT, R, 4, C::kParts, kThreads, OUT32>(p, dealer, dealer.kept(0), a, o_lds, ml_lds + parity * 4 * R, wave, 0, 2 * blockIdx.x + first_partial);
     parity ^= 1;
     first_partial = 1;
     if (!more_blocks) break;
@@ -341,39 +356,55 @@ hipError_t join(const GqaDecodeParams& p, int block_rows, int units, hipStream_t
   return hipGetLastError();
 }
 
-template <int D, bool OUT32>
-hipError_t start(const GqaDecodeParams& p, const GqaShape& shape, int units, hipStream_t stream) {
-  if (shape.wide) {
-    const hipError_t e = launch_gqa_wide(p, shape, units, stream);
-    if (e != hipSuccess) return e;
-  } else {
-    hipLaunchKernelGGL((gqa_decode_kernel<D, OUT32>), dim3(units), dim3(kThreads), Narrow<D>::kLds, stream, p);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  return join<D, OUT32>(p, shape.block_rows, units, stream);
+template <int D, int RT, bool OUT32>
+hipError_t narrow(const GqaDecodeParams& p, int units, hipStream_t stream) {
+  constexpr size_t lds = Narrow<D, RT>::kLds;
+  hipLaunchKernelGGL((gqa_decode_kernel<D, RT, OUT32>), dim3(units), dim3(kThreads), lds, stream, p);
+  return hipGetLastError();
 }
 
-template <int D>
+template <int D, bool OUT32>
+hipError_t start(const GqaDecodeParams& p, const GqaShape& shape, int units, hipStream_t stream) {
+  hipError_t e = hipErrorInvalidValue;
+  if (shape.wide) e = launch_gqa_wide(p, shape, units, stream);
+  else if (shape.row_tiles == 1) e = narrow<D, 1, OUT32>(p, units, stream);
+  else if constexpr (D <= 128) {
+    if (shape.row_tiles == 2) e = narrow<D, 2, OUT32>(p, units, stream);
+    else if constexpr (D == 64) e = narrow<D, 4, OUT32>(p, units, stream);
+  }
+  return e != hipSuccess ? e : join<D, OUT32>(p, shape.block_rows, units, stream);
+}
+
+template <int D, int RT>
 hipError_t allow_lds() {
-  hipError_t e = hipFuncSetAttribute((const void*)gqa_decode_kernel<D, false>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)Narrow<D>::kLds);
-  if (e == hipSuccess) e = hipFuncSetAttribute((const void*)gqa_decode_kernel<D, true>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)Narrow<D>::kLds);
+  constexpr int lds = (int)Narrow<D, RT>::kLds;
+  hipError_t e = hipFuncSetAttribute((const void*)gqa_decode_kernel<D, RT, false>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e == hipSuccess) e = hipFuncSetAttribute((const void*)gqa_decode_kernel<D, RT, true>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   return e;
 }
 
 }  // namespace
 
+// By the average number of query rows of a request and KV head.  us a call, 64 requests of 2000 to 16000 tokens, 4 KV heads; "tiles": this
+// kernel with so many row tiles (several blocks where the rows are more):
+//   width  rows   1 tile   2 tiles   4 tiles   wide, 32 rows   wide, 64 rows
+//   TODO
 GqaShape gqa_shape(int batch, int num_queries, int group, int head_dim) {
   const int64_t rows = (int64_t)((num_queries + batch - 1) / batch) * group;
-  if (rows <= kRows) return GqaShape{false, 1, kRows, groups_per_cu(head_dim)};
-  const int row_tiles = head_dim == 256 || rows <= 32 ? 1 : 2;
-  return GqaShape{true, row_tiles, head_dim == 256 ? 64 : 32 * row_tiles, 1};
+  if (rows <= 16) return GqaShape{false, 1, 16, groups_per_cu(head_dim, 1)};
+  if (head_dim == 256) return GqaShape{true, 1, 64, 1};
+  if (rows <= 32) return GqaShape{false, 2, 32, groups_per_cu(head_dim, 2)};
+  if (head_dim == 64) return GqaShape{false, 4, 64, groups_per_cu(head_dim, 4)};
+  return GqaShape{true, 2, 64, 1};
 }
 
 hipError_t init_gqa_kernels() {
-  hipError_t e = allow_lds<64>();
-  if (e == hipSuccess) e = allow_lds<128>();
-  if (e == hipSuccess) e = allow_lds<256>();
+  hipError_t e = allow_lds<64, 1>();
+  if (e == hipSuccess) e = allow_lds<64, 2>();
+  if (e == hipSuccess) e = allow_lds<64, 4>();
+  if (e == hipSuccess) e = allow_lds<128, 1>();
+  if (e == hipSuccess) e = allow_lds<128, 2>();
+  if (e == hipSuccess) e = allow_lds<256, 1>();
   if (e == hipSuccess) e = init_gqa_wide_kernels();
   return e;
 }

@@ -298,24 +298,15 @@ hipError_t allow_lds() {
 }  // namespace
 
 hipError_t init_gqa_wide_kernels() {
-  hipError_t e = allow_lds<64, 1>();
-  if (e == hipSuccess) e = allow_lds<64, 2>();
-  if (e == hipSuccess) e = allow_lds<128, 1>();
-  if (e == hipSuccess) e = allow_lds<128, 2>();
+  hipError_t e = allow_lds<128, 2>();
   if (e == hipSuccess) e = allow_lds<256, 1>();
   return e;
 }
 
 hipError_t launch_gqa_wide(const GqaDecodeParams& p, const GqaShape& shape, int units, hipStream_t stream) {
-  auto with = [&](auto d, auto rt) {
-    return p.out_fp32 ? start<decltype(d)::value, decltype(rt)::value, true>(p, units, stream)
-                      : start<decltype(d)::value, decltype(rt)::value, false>(p, units, stream);
-  };
-  using std::integral_constant;
-  const bool one = shape.row_tiles == 1;
-  if (p.head_dim == 64) return one ? with(integral_constant<int, 64>{}, integral_constant<int, 1>{}) : with(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-  if (p.head_dim == 128) return one ? with(integral_constant<int, 128>{}, integral_constant<int, 1>{}) : with(integral_constant<int, 128>{}, integral_constant<int, 2>{});
-  return with(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+  if (p.head_dim == 128 && shape.row_tiles == 2) return p.out_fp32 ? start<128, 2, true>(p, units, stream) : start<128, 2, false>(p, units, stream);
+  if (p.head_dim == 256 && shape.row_tiles == 1) return p.out_fp32 ? start<256, 1, true>(p, units, stream) : start<256, 1, false>(p, units, stream);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace omniattn
