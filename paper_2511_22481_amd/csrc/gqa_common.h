@@ -174,7 +174,9 @@ struct Span {
   int lo, hi;            // tokens that the block's first and last query see
   int tile_hi;
   bool several;          // several queries
-  __device__ __forceinline__ explicit Span(const Piece& w) : pages(w.bk.pages), lo(w.reach_lo()), hi(w.reach_hi()), tile_hi(w.tile_hi), several(w.bk.t1 > w.bk.t0) {}
+  __device__ __forceinline__ explicit Span(const Piece& w)
+      : pages{uniform(w.bk.pages.ns), uniform(w.bk.pages.w0), uniform(w.bk.pages.w1)}, lo(uniform(w.reach_lo())), hi(uniform(w.reach_hi())),
+        tile_hi(uniform(w.tile_hi)), several(uniform(w.bk.t1 - w.bk.t0) > 0) {}
 };
 
 // Finds a work group's share and walks through its blocks.  R: rows of a block.  All threads call everything.

@@ -63,6 +63,10 @@ __device__ __forceinline__ void load_v(Tile<D>& t, __amdgpu_buffer_rsrc_t rsrc, 
   }
 }
 
+// Waits for a load's result here, where it has just been asked for, and not where it is used on other ways too: there the wait would be
+// for everything that has been asked for since.
+__device__ __forceinline__ void settle(int& x) { asm volatile("" : "+v"(x)); }
+
 template <int D, int RT>
 struct Narrow {
   static constexpr int kRows = 16 * RT;
@@ -136,26 +140,30 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
     if constexpr (C::kQLds) return q_lds[((q_side * RT + rt) * 2 * kWords + i) * 64 + lane];
     else return q[rt][i];
   };
-  // What a page's loads need: where its codes are, and the wave's two scales.
-  __amdgpu_buffer_rsrc_t rk, rv;
+  // A page's loads: where its codes are (scalar registers, made where they are used), and the wave's two scales.
+  struct Codes {
+    __amdgpu_buffer_rsrc_t k, v;
+  };
+  const Codes none = {codes_at(p.k_cache, 0), codes_at(p.v_cache, 0)};
   float ks = 0.f, vs = 0.f;
   auto aim = [&](const TileLayout& pages, int h, int seen, int tile, int ids, int held) {
     const int page = __builtin_amdgcn_readlane(ids, tile - held);
     const size_t ph = (size_t)page * p.kv_heads + h;
-    const int live = min(seen - pages.logical(tile) * kPage, kPage);
-    rk = codes_at(p.k_cache + ph * head_bytes, live * D);
-    rv = codes_at(p.v_cache + ph * head_bytes, live * D);
+    const int live = max(min(seen - pages.logical(tile) * kPage, kPage), 0);
     ks = p.k_scales[ph * blocks_per_page + my_block];
     vs = p.v_scales[ph * blocks_per_page + my_block];
+    return Codes{codes_at(p.k_cache + ph * head_bytes, live * D), codes_at(p.v_cache + ph * head_bytes, live * D)};
   };
 
   Tile<D> t;
   int held = now.tile_lo, ids = entries(now.b, now.bk.pages, held);
+  settle(ids);
   load_q(now);
-  if (now.tile_lo < now.tile_hi) {
-    aim(now.bk.pages, now.h, now.reach_hi(), now.tile_lo, ids, held);
-    load_k<D>(t, rk, k_at);
-    load_v<D>(t, rv, v_at);
+  // (a share that begins with a block that keeps nothing: entry 0, none of whose tokens is read)
+  {
+    const Codes c = aim(now.bk.pages, now.h, now.tile_lo < now.tile_hi ? now.reach_hi() : 0, now.tile_lo, ids, held);
+    load_k<D>(t, c.k, k_at);
+    load_v<D>(t, c.v, v_at);
   }
   if constexpr (C::kQLds) {
     store_q(0);
@@ -166,11 +174,11 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
   int ahead_b = -1, ahead_ids = 0;
   // Of the block that is computed, what the loop needs; the rest is the wave's note 0, and the next block's note 1.
   dealer.keep(0, now);
-  int b = now.b, h = now.h, tile = now.tile_lo;
+  int b = uniform(now.b), h = uniform(now.h), tile = uniform(now.tile_lo);
   Span span(now);
 
   while (true) {
-    bool more_blocks = false, next_loads = false;
+    bool more_blocks = false;
     if (ahead_b <= b) {
       ahead_b = b + 1;
       if (ahead_b < p.batch) {
@@ -184,23 +192,24 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
       const Piece was = dealer.kept(0);
       Piece next = was;
       more_blocks = dealer.follow(next);
-      if (!more_blocks) return;
+      if (!more_blocks) return none;
       dealer.keep(1, next);
-      next_loads = next.tile_lo < next.tile_hi;
-      if (next_loads) {
-        if (!(next.b == was.b && next.rb == was.rb && held == 0)) {
-          held = 0;
-          ids = next.b == ahead_b && next.rb == 0 ? ahead_ids : entries(next.b, next.bk.pages, 0);
-        }
-        aim(next.bk.pages, next.h, next.reach_hi(), next.tile_lo, ids, held);
-      }
       load_q(next);
+      if (next.tile_lo >= next.tile_hi) return none;
+      if (!(next.b == was.b && next.rb == was.rb && held == 0)) {
+        held = 0;
+        ids = next.b == ahead_b && next.rb == 0 ? ahead_ids : entries(next.b, next.bk.pages, 0);
+        settle(ids);
+      }
+      return aim(next.bk.pages, next.h, next.reach_hi(), next.tile_lo, ids, held);
     };
     Rows<D, RT> a;
     a.clear();
 
-    const bool nothing = tile >= span.tile_hi;
-    for (; tile < span.tile_hi; ++tile) {
+    // A page; the loads of the one behind it go out as soon as their registers are free.  (They go out in any case, behind the share's last
+    // page with nothing to read: were they conditional, the wait for K in the next pass would have to be for V's too.  And the last page
+    // of a block is a copy of its own: what it has to find out would otherwise be carried through every pass.)
+    auto step = [&](auto last) {
       const int pos0 = span.pages.logical(tile) * kPage + wave * kWaveTokens;
       const Kept kept = kept_of(p, span, pos0);
       f32x4 s[RT][2];
@@ -223,32 +232,36 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
       int seen[RT];
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) seen[rt] = reach[rt];
-      // the next page's loads, of this block or the next one, as soon as their registers are free
-      bool more = true;
-      if (tile + 1 < span.tile_hi) {
+      Codes c;
+      if constexpr (decltype(last)::value) {
+        c = turn_to_next();
+      } else {
         if (tile + 1 - held >= 64) {
           held = tile + 1;
           ids = entries(b, span.pages, held);
+          settle(ids);
         }
-        aim(span.pages, h, span.hi, tile + 1, ids, held);
-      } else {
-        turn_to_next();
-        more = next_loads;
+        c = aim(span.pages, h, span.hi, tile + 1, ids, held);
       }
-      if (more) load_k<D>(t, rk, k_at);
+      load_k<D>(t, c.k, k_at);
 
       f16x8 high[RT], low[RT];
       weigh<D, RT, OUT32>(p, a, s, seen, kept.full, pos0, g, k_factor, v_scale, high, low);
       if (!kept.full) sanitize<D, RT>(p, a, t.v, span, pos0, g);
       add_values<D, RT, OUT32>(a, t.v, high, low);
-      if (more) load_v<D>(t, rv, v_at);
-    }
-    if (nothing) {  // (the next block has not been asked for yet)
-      turn_to_next();
-      if (next_loads) {
-        load_k<D>(t, rk, k_at);
-        load_v<D>(t, rv, v_at);
-      }
+      load_v<D>(t, c.v, v_at);
+    };
+    if (tile < span.tile_hi) {
+      for (; tile + 1 < span.tile_hi; ++tile) step(std::false_type{});
+      step(std::true_type{});
+    } else {  // (nothing kept; the loads are waited for here, so that this rare way does not count where the waits of the others are set)
+      const Codes c = turn_to_next();
+      load_k<D>(t, c.k, k_at);
+      load_v<D>(t, c.v, v_at);
+#pragma unroll
+      for (int i = 0; i < 2 * kWords; ++i) asm volatile("" : "+v"(t.k[i / kWords][i % kWords]));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(t.v[j]));
     }
     if (more_blocks) store_q(q_side ^ 1);
     q_side ^= 1;
