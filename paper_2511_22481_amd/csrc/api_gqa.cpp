@@ -67,12 +67,17 @@ int check_gqa(const omniattn_gqa_t* g) {
   return OMNIATTN_OK;
 }
 
+GqaShape shape_of(const omniattn_gqa_t* g, int cus) {
+  const int64_t pages = std::min<int64_t>(g->max_pages_per_seq, ((int64_t)g->sink + kPage - 1) / kPage + ((int64_t)g->window + kPage - 1) / kPage + 1);
+  return gqa_shape(g->batch, g->num_queries, g->num_q_heads / g->num_kv_heads, g->num_kv_heads, g->head_dim, pages, cus);
+}
+
 struct Workspace {
   size_t rows, ml, o, bytes;  // offsets, and the whole
 };
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
-Workspace workspace_of(const omniattn_gqa_t* g, const GqaShape& shape, int units) {
-  const size_t slots = (size_t)2 * units * shape.block_rows;
+Workspace workspace_of(const omniattn_gqa_t* g, const GqaShape& shape) {
+  const size_t slots = (size_t)2 * shape.groups * shape.shares * shape.block_rows;
   Workspace w;
   w.rows = 0;
   w.ml = align256((size_t)g->num_queries * g->num_q_heads * sizeof(int2));
@@ -165,8 +170,10 @@ int omniattn_gqa_append(const omniattn_gqa_t* gqa, int32_t num_tokens, const voi
 size_t omniattn_gqa_workspace_bytes(const omniattn_gqa_t* gqa) {
   int cus = 0;
   if (check_gqa(gqa) != OMNIATTN_OK || device_cus(&cus) != OMNIATTN_OK) return 0;
-  const GqaShape shape = gqa_shape(gqa->batch, gqa->num_queries, gqa->num_q_heads / gqa->num_kv_heads, gqa->head_dim);
-  return workspace_of(gqa, shape, cus * shape.groups_per_cu).bytes;
+  // (enough for any kept set and table width: those with few pages have the most shares)
+  omniattn_gqa_t short_ones = *gqa;
+  short_ones.sink = short_ones.window = 0;
+  return std::max(workspace_of(gqa, shape_of(gqa, cus)).bytes, workspace_of(gqa, shape_of(&short_ones, cus)).bytes);
 }
 
 int omniattn_gqa_decode(const omniattn_gqa_t* gqa, const void* q, int64_t q_stride, const void* k_cache, const void* v_cache, const float* k_scales,
@@ -186,9 +193,8 @@ int omniattn_gqa_decode(const omniattn_gqa_t* gqa, const void* q, int64_t q_stri
   if (rc != OMNIATTN_OK) return rc;
   GqaDecodeParams p;
   p.group = gqa->num_q_heads / gqa->num_kv_heads;
-  const GqaShape shape = gqa_shape(gqa->batch, gqa->num_queries, p.group, gqa->head_dim);
-  int units = cus * shape.groups_per_cu;
-  const Workspace w = workspace_of(gqa, shape, units);
+  const GqaShape shape = shape_of(gqa, cus);
+  const Workspace w = workspace_of(gqa, shape);
   if (!workspace || workspace_bytes < w.bytes || !aligned(workspace, 256)) return OMNIATTN_EWORKSPACE;
   p.q = (const uint16_t*)q;
   p.q_stride = q_stride;
@@ -217,11 +223,11 @@ int omniattn_gqa_decode(const omniattn_gqa_t* gqa, const void* q, int64_t q_stri
   p.scale_shift = gqa->scale_tokens == 32 ? 5 : gqa->scale_tokens == 64 ? 6 : 7;
   p.out_fp32 = gqa->out_dtype == OMNIATTN_FP32;
   p.scale_log2 = gqa->softmax_scale * 1.4426950408889634f;
-  // Not more work groups than there can be units of work (each block counts 2 beside its pages).
+  // Not more shares than there can be units of work (each block counts up to 2 beside its pages).
   const int64_t blocks = ((int64_t)p.num_queries * p.group + shape.block_rows - 1) / shape.block_rows + p.batch;
   const int64_t pages = std::min<int64_t>(p.max_pages, ((int64_t)p.S + kPage - 1) / kPage + ((int64_t)p.W + shape.block_rows + kPage - 1) / kPage + 1);
-  units = (int)std::min<int64_t>(units, blocks * p.kv_heads * (pages + 2));
-  OA_HIP(launch_gqa_decode(p, shape, units, (hipStream_t)hip_stream));
+  const int groups = (int)std::min<int64_t>(shape.groups, (blocks * p.kv_heads * (pages + 2) + shape.shares - 1) / shape.shares);
+  OA_HIP(launch_gqa_decode(p, shape, groups * shape.shares, (hipStream_t)hip_stream));
   return OMNIATTN_OK;
 }
 

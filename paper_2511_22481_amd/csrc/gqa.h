@@ -71,16 +71,17 @@ struct GqaDecodeParams {
   float scale_log2;         // softmax_scale * log2(e)
 };
 // How a call is computed: by which kernel (gqa_decode_kernel.hip or gqa_wide_kernel.hip), tiles of 16 query rows per wave, rows of a
-// block, and work groups that a compute unit holds.
+// block, work groups at most, and shares of the work to each.
 struct GqaShape {
   bool wide;
-  int row_tiles, block_rows, groups_per_cu;
+  int row_tiles, block_rows, groups, shares;
 };
-GqaShape gqa_shape(int batch, int num_queries, int group, int head_dim);
+// pages: those that a query's kept tokens can lie in.
+GqaShape gqa_shape(int batch, int num_queries, int group, int kv_heads, int head_dim, int64_t pages, int cus);
 hipError_t init_gqa_kernels();
 hipError_t init_gqa_wide_kernels();
 // The kernel of the shape, and the one that joins partial rows.
-hipError_t launch_gqa_decode(const GqaDecodeParams& p, const GqaShape& shape, int units, hipStream_t stream);
-hipError_t launch_gqa_wide(const GqaDecodeParams& p, const GqaShape& shape, int units, hipStream_t stream);
+hipError_t launch_gqa_decode(const GqaDecodeParams& p, const GqaShape& shape, int shares, hipStream_t stream);
+hipError_t launch_gqa_wide(const GqaDecodeParams& p, const GqaShape& shape, int shares, hipStream_t stream);
 
 }  // namespace omniattn

@@ -23,8 +23,6 @@ constexpr float kLift = 11.f, kSlack = 4.f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// What a block costs beside its pages, in pages: its query, the meeting of the waves, its results.
-constexpr int kStart = 2;
 
 // What a request brings: its tokens, its first query token and how many it has.
 struct Request {
@@ -42,7 +40,6 @@ __device__ __forceinline__ Request request_of(const GqaDecodeParams& p, int b) {
 struct Block {
   int t0, t1;  // its query tokens, both included
   TileLayout pages;
-  __device__ __forceinline__ int units() const { return kStart + pages.count(); }
 };
 template <int ROWS>
 __device__ __forceinline__ Block block_of(const GqaDecodeParams& p, const Request& r, int rb) {
@@ -56,15 +53,6 @@ template <int ROWS>
 __device__ __forceinline__ int blocks_of(const GqaDecodeParams& p, const Request& r) {
   return (int)(((int64_t)r.n * p.group + ROWS - 1) / ROWS);
 }
-// Units of work (pages, and kStart for each block) of one KV head of a request
-template <int ROWS>
-__device__ __forceinline__ int64_t cost_of(const GqaDecodeParams& p, const Request& r) {
-  const int blocks = blocks_of<ROWS>(p, r);
-  int64_t sum = 0;
-  for (int rb = 0; rb < blocks; ++rb) sum += block_of<ROWS>(p, r, rb).units();
-  return sum;
-}
-
 __device__ __forceinline__ float row_max(float x) {  // over the four lanes that hold tokens of the same row
   float y = x;
   swap16(x, y);
@@ -140,12 +128,12 @@ __device__ __forceinline__ const GqaDecodeParams* late_arguments() {
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// The share of work group u of U: units [bound(u), bound(u + 1)), bound(u) = floor(u T / U).
+// Share u of U: units [bound(u), bound(u + 1)), bound(u) = floor(u T / U).
 struct Shares {
   int64_t T, each;  // each = T / U
   int U, rest;      // rest = T % U
   __device__ __forceinline__ int64_t bound(int u) const { return u * each + u * rest / U; }  // (U is at most 2^12)
-  // the work group that has unit x
+  // the share that has unit x
   __device__ __forceinline__ int owner(int64_t x) const {
     int u = min((int)((double)x * U / (double)T), U - 1);
     while (bound(u) > x) --u;
@@ -154,7 +142,7 @@ struct Shares {
   }
 };
 
-// The part of a block that a work group computes.
+// The part of a block that belongs to a share.
 struct Piece {
   int b, h, rb;
   Request rq;
@@ -179,16 +167,16 @@ struct Span {
         tile_hi(uniform(w.tile_hi)), several(uniform(w.bk.t1 - w.bk.t0) > 0) {}
 };
 
-// Finds a work group's share and walks through its blocks.  R: rows of a block.  All threads call everything.
-template <int R, int THREADS>
+// Finds shares and walks through their blocks.  R: rows of a block.  START: what a block costs beside its pages (its query, the
+// meeting of the waves, its results), in pages.  SHARES: of a work group, 1 or one for each wave.  All threads call begin.
+template <int R, int THREADS, int START, int SHARES = 1>
 struct Dealer {
   // What is needed only from block to block stays here: in scalar registers it would push the loop's own out.
   struct Lds {
-    int64_t wave_tot[THREADS / 64], off;
+    int64_t wave_tot[THREADS / 64], off[SHARES], stop[SHARES];  // the share's first unit among the units of request `at`; its end
     int4 requests[THREADS];  // (batches of up to THREADS: L, begin, n, units of one KV head)
-    int at;
+    int at[SHARES];
     Shares shares;
-    int64_t stop;            // end of the share
     int pieces[THREADS / 64][3][16];
   };
   const GqaDecodeParams& p;
@@ -196,6 +184,17 @@ struct Dealer {
   int per;  // requests per thread
 
   __device__ __forceinline__ Dealer(const GqaDecodeParams& params, Lds& memory) : p(params), lds(memory) {}
+
+  __device__ __forceinline__ static int which() { return SHARES > 1 ? uniform(threadIdx.x >> 6) : 0; }
+  __device__ __forceinline__ static int share() { return (int)blockIdx.x * SHARES + which(); }
+  __device__ __forceinline__ static int units(const Block& k) { return START + k.pages.count(); }
+  // Units of one KV head of a request
+  __device__ __forceinline__ int64_t cost_of(const Request& r) const {
+    const int blocks = blocks_of<R>(p, r);
+    int64_t sum = 0;
+    for (int rb = 0; rb < blocks; ++rb) sum += units(block_of<R>(p, r, rb));
+    return sum;
+  }
 
   __device__ __forceinline__ Request request(int b) const {
     if (per == 1) {
@@ -207,15 +206,15 @@ struct Dealer {
   }
   __device__ __forceinline__ void cut(Piece& w) const {
     w.bk = block_of<R>(p, w.rq, w.rb);
-    w.tile_lo = max(w.off - kStart, 0);
-    w.tile_hi = (int)min(max(w.left + w.off - kStart, (int64_t)0), (int64_t)w.bk.pages.count());
+    w.tile_lo = max(w.off - START, 0);
+    w.tile_hi = (int)min(max(w.left + w.off - START, (int64_t)0), (int64_t)w.bk.pages.count());
   }
   // Whether there is something to do: pages, or the empty result of a block that keeps nothing, which is whose share has its first unit.
   __device__ __forceinline__ static bool counts(const Piece& w) { return w.tile_lo < w.tile_hi || (w.bk.pages.count() == 0 && w.off == 0); }
-  // The next block with something to do for this work group; false if there is none.
+  // The next block of the share with something to do; false if there is none.
   __device__ __forceinline__ bool follow(Piece& w) const {
     do {
-      w.left -= w.bk.units() - w.off;
+      w.left -= units(w.bk) - w.off;
       w.off = 0;
       if (w.left <= 0) return false;
       if (++w.rb >= blocks_of<R>(p, w.rq)) {
@@ -230,8 +229,8 @@ struct Dealer {
     } while (!counts(w));
     return true;
   }
-  // Running sum of the units over the batch, a run of requests per thread; the thread whose requests hold the share's first unit
-  // says so.  False: nothing to do for this work group.
+  // Running sum of the units over the batch, a run of requests per thread; the thread whose requests hold a share's first unit
+  // says so.  False: nothing to do for this wave.
   __device__ __forceinline__ bool begin(Piece& now) {
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     per = (p.batch + THREADS - 1) / THREADS;
@@ -240,7 +239,7 @@ struct Dealer {
       const int b = tid * per + i;
       if (b < p.batch) {
         const Request r = request_of(p, b);
-        const int64_t cost = cost_of<R>(p, r);
+        const int64_t cost = cost_of(r);
         mine += cost * p.kv_heads;
         if (per == 1) lds.requests[tid] = make_int4(r.L, r.begin, r.n, (int)cost);
       }
@@ -258,22 +257,29 @@ struct Dealer {
       if (w == wave) sum += shares.T;
       shares.T += (int64_t)uniform64(lds.wave_tot[w]);
     }
-    shares.U = (int)min((int64_t)gridDim.x, shares.T);
-    if ((int)blockIdx.x >= shares.U) return false;
+    shares.U = (int)min((int64_t)gridDim.x * SHARES, shares.T);
+    if ((int)blockIdx.x * SHARES >= shares.U) return false;
     if (shares.T >> 31) shares.each = shares.T / shares.U;
     else shares.each = (uint32_t)shares.T / (uint32_t)shares.U;
     shares.rest = (int)(shares.T - shares.each * shares.U);
-    const int64_t first = shares.bound(blockIdx.x);
-    if (sum - mine <= first && first < sum) {
-      lds.at = tid;
-      lds.off = first - (sum - mine);
-      lds.shares = shares;
-      lds.stop = shares.bound(blockIdx.x + 1);
+    int64_t first = shares.bound(blockIdx.x * SHARES);
+#pragma unroll
+    for (int i = 0; i < SHARES; ++i) {
+      const int u = blockIdx.x * SHARES + i;
+      const int64_t stop = shares.bound(u + 1);
+      if (u < shares.U && sum - mine <= first && first < sum) {
+        lds.at[i] = tid;
+        lds.off[i] = first - (sum - mine);
+        lds.stop[i] = stop;
+        lds.shares = shares;
+      }
+      first = stop;
     }
     __syncthreads();
-    const int at = uniform(lds.at) * per;
-    int64_t off = (int64_t)uniform64(lds.off);
-    now.left = shares.bound(blockIdx.x + 1) - first;
+    if (share() >= shares.U) return false;
+    const int at = uniform(lds.at[which()]) * per;
+    int64_t off = (int64_t)uniform64(lds.off[which()]);
+    now.left = shares.bound(share() + 1) - shares.bound(share());
     if (per == 1) {
       now.b = at;
       const int4 r = lds.requests[at];
@@ -285,7 +291,7 @@ struct Dealer {
       int64_t cost;
       for (now.b = at;; ++now.b) {
         now.rq = request(now.b);
-        cost = cost_of<R>(p, now.rq);
+        cost = cost_of(now.rq);
         if (off < cost * p.kv_heads) break;
         off -= cost * p.kv_heads;
       }
@@ -293,19 +299,19 @@ struct Dealer {
       off -= now.h * cost;
     }
     for (now.rb = 0;; ++now.rb) {
-      const int units = block_of<R>(p, now.rq, now.rb).units();
-      if (off < units) break;
-      off -= units;
+      const int of_block = units(block_of<R>(p, now.rq, now.rb));
+      if (off < of_block) break;
+      off -= of_block;
     }
     now.off = (int)off;
     cut(now);
     return counts(now) || follow(now);
   }
   __device__ __forceinline__ int rows_of(const Piece& w) const { return (int)min((int64_t)w.rq.n * p.group - (int64_t)w.rb * R, (int64_t)R); }
-  // Work groups that share the block of w, from this one on (which has its first page).
+  // Shares that have a part of the block of w, from this one on (which has its first page).
   __device__ __forceinline__ int partners(const Piece& w) const {
     const Shares shares = lds.shares;
-    return shares.owner(lds.stop - w.left - w.off + w.bk.units() - 1) - (int)blockIdx.x + 1;
+    return shares.owner(lds.stop[which()] - w.left - w.off + units(w.bk) - 1) - share() + 1;
   }
   // A wave's notes of blocks, in one of three places.
   __device__ __forceinline__ void keep(int place, const Piece& w) const {
@@ -467,8 +473,8 @@ __device__ __forceinline__ Kept kept_of(const GqaDecodeParams& p, const Span& no
 // End of a block: the shares of the TG waves that hold the same rows (tokens apart) meet in LDS, references and sums first (ml: [TG][R]),
 // then the outputs at the common reference, 1 / PARTS of the columns at a time (o_lds: [TG][R][D / PARTS + 4]).  tg: which of the TG
 // the wave is; row0: its first row.  Blocks that other work groups share too leave partial rows in `slot`.
-template <int D, int RT, int R, int TG, int PARTS, int THREADS, bool OUT32>
-__device__ __forceinline__ void finish(const GqaDecodeParams& p, const Dealer<R, THREADS>& dealer, const Piece& now, Rows<D, RT>& a, float* o_lds, float4* ml,
+template <int D, int RT, int R, int TG, int PARTS, int THREADS, bool OUT32, int START>
+__device__ __forceinline__ void finish(const GqaDecodeParams& p, const Dealer<R, THREADS, START>& dealer, const Piece& now, Rows<D, RT>& a, float* o_lds, float4* ml,
                                        int tg, int row0, int slot) {
   constexpr int kCols = D / 16, kOStride = D / PARTS + 4;
   const int tid = threadIdx.x, lane = tid & 63, n16 = lane & 15, g = lane >> 4;
@@ -571,10 +577,78 @@ __device__ __forceinline__ void finish(const GqaDecodeParams& p, const Dealer<R,
         ((f32x4*)dst)[1] = hi;
         if (col == 0) {
           end.part_ml[(size_t)slot * R + row] = make_float4(top, sum, vtop, 0.f);
-          // the work group that takes a block's first page knows which ones take the others
+          // the share that has a block's first page knows which ones have the others
           if (now.tile_lo == 0) end.rows[out_row] = make_int2(slot, dealer.partners(now) * 64 + row);
         }
       }
+    }
+  }
+}
+
+// End of a block that one wave computes by itself, one row tile: every lane has D / 4 adjacent columns of its row, and writes them.
+template <int D, int THREADS, bool OUT32, int START, int SHARES>
+__device__ __forceinline__ void finish_alone(const Dealer<16, THREADS, START, SHARES>& dealer, const Piece& now, Rows<D, 1>& a, int slot) {
+  constexpr int kCols = D / 16;
+  const int lane = threadIdx.x & 63, row = lane & 15, g = lane >> 4, col = 4 * g * kCols;
+  const float sum = row_sum(a.l[0]);
+  if (row >= dealer.rows_of(now)) return;
+  const GqaDecodeParams& end = *late_arguments();
+  const uint32_t qt = (uint32_t)(now.rb * 16 + row) / (uint32_t)end.group, gi = (uint32_t)(now.rb * 16 + row) - qt * end.group;
+  if (__builtin_expect(a.saw_nan != 0.f, 0)) {  // (as in finish)
+    const int sees = now.rq.L - now.rq.n + (int)qt + 1;
+    uint32_t nans = 0;  // of the lane's columns
+#pragma unroll 1
+    for (int tile = now.tile_lo; tile < now.tile_hi; ++tile) {
+      const int lp = now.bk.pages.logical(tile);
+      const size_t ph = (size_t)end.page_table[now.b * end.table_stride + lp] * end.kv_heads + now.h;
+#pragma unroll 1
+      for (int j = 0; j < kPage; ++j) {
+        if (!retained(lp * kPage + j, sees, end.S, end.W)) continue;
+        const uint32_t* codes = (const uint32_t*)(end.v_cache + (ph * kPage + j) * D + col);
+#pragma unroll 1
+        for (int i = 0; i < kCols; ++i) {
+          const uint32_t n = nan_codes(codes[i]);
+          nans |= ((n >> 7 & 1) | (n >> 14 & 2) | (n >> 21 & 4) | (n >> 28 & 8)) << (4 * i);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < kCols; ++c)
+        if (nans >> (i * kCols + c) & 1) a.o[0][c][i] = NAN;
+  }
+  const int64_t out_row = (int64_t)(now.rq.begin + (int)qt) * end.q_heads + now.h * end.group + (int)gi;
+  if (now.whole()) {
+    const float inv = sum == 0.f ? 0.f : exp2_fast(a.n[0] - a.m[0]) / sum;  // (nothing kept: 0 and -inf)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < kCols; c += 4) {
+        const int64_t at = out_row * D + col + i * kCols + c;
+        if constexpr (OUT32) {
+          *(f32x4*)((float*)end.out + at) = f32x4{a.o[0][c][i] * inv, a.o[0][c + 1][i] * inv, a.o[0][c + 2][i] * inv, a.o[0][c + 3][i] * inv};
+        } else {
+          typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+          bf16x4 y;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) y[k] = (__bf16)(a.o[0][c + k][i] * inv);
+          *(bf16x4*)((uint16_t*)end.out + at) = y;
+        }
+      }
+    if (g == 0) {
+      end.lse[out_row] = sum == 0.f ? -INFINITY : (a.m[0] + __log2f(sum) - kLift) * 0.69314718055994531f;
+      end.rows[out_row] = make_int2(0, 0);
+    }
+  } else {
+    float* const dst = end.part_o + ((size_t)slot * 16 + row) * D + col;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < kCols; c += 4) *(f32x4*)(dst + i * kCols + c) = f32x4{a.o[0][c][i], a.o[0][c + 1][i], a.o[0][c + 2][i], a.o[0][c + 3][i]};
+    if (g == 0) {
+      end.part_ml[(size_t)slot * 16 + row] = make_float4(a.m[0], sum, a.n[0], 0.f);
+      if (now.tile_lo == 0) end.rows[out_row] = make_int2(slot, dealer.partners(now) * 64 + row);
     }
   }
 }

@@ -79,25 +79,25 @@ struct Narrow {
   static constexpr size_t kLds = (size_t)4 * kRows * kOStride * 4 + 2 * 4 * kRows * 16 + 2 * kQBytes;
 };
 
-template <int D, int RT, bool OUT32>
+template <int D, int RT, bool OUT32, bool ALONE>
 __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_kernel(GqaDecodeParams p) {
   using C = Narrow<D, RT>;
+  using Deal = Dealer<C::kRows, kThreads, ALONE ? 1 : 2, ALONE ? 4 : 1>;
+  static_assert(!ALONE || (D == 64 && RT == 1));
   constexpr int R = C::kRows, kCols = D / 16, kWords = D / 64;
   extern __shared__ __align__(16) float lds[];
   float* const o_lds = lds;                                    // [4 waves][R][kOStride]
   float4* const ml_lds = (float4*)(lds + 4 * R * C::kOStride); // [2][4 waves][R]
   bf16x8* const q_lds = (bf16x8*)(ml_lds + 2 * 4 * R);         // [2][operands of the products][64 lanes]
-  __shared__ typename Dealer<R, kThreads>::Lds dealt;
+  __shared__ typename Deal::Lds dealt;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int n16 = lane & 15, g = lane >> 4;
-  Dealer<R, kThreads> dealer(p, dealt);
+  Deal dealer(p, dealt);
   Piece now;
   if (!dealer.begin(now)) return;
 
-  const size_t head_bytes = (size_t)kPage * D;
-  const int k_at = (wave * kWaveTokens + n16) * D + g * 16;
-  const int v_at = (wave * kWaveTokens + 4 * g) * D + n16 * kCols;
-  const int blocks_per_page = kPage >> p.scale_shift, my_block = (wave * kWaveTokens) >> p.scale_shift;
+  const int k_at = n16 * D + g * 16, v_at = 4 * g * D + n16 * kCols;
+  const int blocks_per_page = kPage >> p.scale_shift;
   int parity = 0, first_partial = 0;  // first_partial: 1 once this work group has left its first block behind
 
   // Page-table entries of up to 64 of a block's pages from number `from` on, one per lane.
@@ -140,28 +140,49 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
     if constexpr (C::kQLds) return q_lds[((q_side * RT + rt) * 2 * kWords + i) * 64 + lane];
     else return q[rt][i];
   };
-  // A page's loads: where its codes are (scalar registers, made where they are used), and the wave's two scales.
+  // A tile: 32 tokens of a page, the wave's quarter of it, or the four in turn if the wave is alone.  The next one with tokens that the
+  // block keeps, from `at` on; page `hi` if there is none before it.
+  struct At {
+    int page, quarter;
+  };
+  auto from = [&](const Span& span, At at, int hi) {
+    if constexpr (ALONE) {
+      while (at.page < hi && !kept_of(p, span, span.pages.logical(at.page) * kPage + at.quarter * kWaveTokens).some) {
+        at.quarter = (at.quarter + 1) & 3;
+        at.page += at.quarter == 0;
+      }
+    }
+    return at;
+  };
+  auto behind = [&](const Span& span, At at) {
+    if constexpr (ALONE) return from(span, At{at.page + (at.quarter == 3), (at.quarter + 1) & 3}, span.tile_hi);
+    else return At{at.page + 1, at.quarter};
+  };
+  const int first_quarter = ALONE ? 0 : wave;
+  // A tile's loads: where its codes are (scalar registers, made where they are used), and the two scales.
   struct Codes {
     __amdgpu_buffer_rsrc_t k, v;
   };
   const Codes none = {codes_at(p.k_cache, 0), codes_at(p.v_cache, 0)};
   float ks = 0.f, vs = 0.f;
-  auto aim = [&](const TileLayout& pages, int h, int seen, int tile, int ids, int held) {
-    const int page = __builtin_amdgcn_readlane(ids, tile - held);
-    const size_t ph = (size_t)page * p.kv_heads + h;
-    const int live = max(min(seen - pages.logical(tile) * kPage, kPage), 0);
-    ks = p.k_scales[ph * blocks_per_page + my_block];
-    vs = p.v_scales[ph * blocks_per_page + my_block];
-    return Codes{codes_at(p.k_cache + ph * head_bytes, live * D), codes_at(p.v_cache + ph * head_bytes, live * D)};
+  auto aim = [&](const TileLayout& pages, int h, int seen, At at, int ids, int held) {
+    const int page = __builtin_amdgcn_readlane(ids, at.page - held);
+    const int first = at.quarter * kWaveTokens, live = max(min(seen - pages.logical(at.page) * kPage - first, kWaveTokens), 0);
+    const size_t ph = (size_t)page * p.kv_heads + h, block = ph * blocks_per_page + (first >> p.scale_shift), code = (ph * kPage + first) * D;
+    ks = p.k_scales[block];
+    vs = p.v_scales[block];
+    return Codes{codes_at(p.k_cache + code, live * D), codes_at(p.v_cache + code, live * D)};
   };
 
   Tile<D> t;
   int held = now.tile_lo, ids = entries(now.b, now.bk.pages, held);
   settle(ids);
   load_q(now);
-  // (a share that begins with a block that keeps nothing: entry 0, none of whose tokens is read)
+  Span span(now);
+  At at = from(span, At{uniform(now.tile_lo), first_quarter}, span.tile_hi);
   {
-    const Codes c = aim(now.bk.pages, now.h, now.tile_lo < now.tile_hi ? now.reach_hi() : 0, now.tile_lo, ids, held);
+    Codes c = none;
+    if (at.page < span.tile_hi) c = aim(span.pages, now.h, span.hi, at, ids, held);
     load_k<D>(t, c.k, k_at);
     load_v<D>(t, c.v, v_at);
   }
@@ -174,8 +195,7 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
   int ahead_b = -1, ahead_ids = 0;
   // Of the block that is computed, what the loop needs; the rest is the wave's note 0, and the next block's note 1.
   dealer.keep(0, now);
-  int b = uniform(now.b), h = uniform(now.h), tile = uniform(now.tile_lo);
-  Span span(now);
+  int b = uniform(now.b), h = uniform(now.h);
 
   while (true) {
     bool more_blocks = false;
@@ -195,13 +215,15 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
       if (!more_blocks) return none;
       dealer.keep(1, next);
       load_q(next);
-      if (next.tile_lo >= next.tile_hi) return none;
+      const Span its(next);
+      const At first = from(its, At{uniform(next.tile_lo), first_quarter}, its.tile_hi);
+      if (first.page >= its.tile_hi) return none;
       if (!(next.b == was.b && next.rb == was.rb && held == 0)) {
         held = 0;
         ids = next.b == ahead_b && next.rb == 0 ? ahead_ids : entries(next.b, next.bk.pages, 0);
         settle(ids);
       }
-      return aim(next.bk.pages, next.h, next.reach_hi(), next.tile_lo, ids, held);
+      return aim(its.pages, next.h, its.hi, first, ids, held);
     };
     Rows<D, RT> a;
     a.clear();
@@ -209,8 +231,8 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
     // A page; the loads of the one behind it go out as soon as their registers are free.  (They go out in any case, behind the share's last
     // page with nothing to read: were they conditional, the wait for K in the next pass would have to be for V's too.  And the last page
     // of a block is a copy of its own: what it has to find out would otherwise be carried through every pass.)
-    auto step = [&](auto last) {
-      const int pos0 = span.pages.logical(tile) * kPage + wave * kWaveTokens;
+    auto step = [&](auto last, At then) {
+      const int pos0 = span.pages.logical(at.page) * kPage + at.quarter * kWaveTokens;
       const Kept kept = kept_of(p, span, pos0);
       f32x4 s[RT][2];
 #pragma unroll
@@ -236,12 +258,12 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
       if constexpr (decltype(last)::value) {
         c = turn_to_next();
       } else {
-        if (tile + 1 - held >= 64) {
-          held = tile + 1;
+        if (then.page - held >= 64) {
+          held = then.page;
           ids = entries(b, span.pages, held);
           settle(ids);
         }
-        c = aim(span.pages, h, span.hi, tile + 1, ids, held);
+        c = aim(span.pages, h, span.hi, then, ids, held);
       }
       load_k<D>(t, c.k, k_at);
 
@@ -251,9 +273,14 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
       add_values<D, RT, OUT32>(a, t.v, high, low);
       load_v<D>(t, c.v, v_at);
     };
-    if (tile < span.tile_hi) {
-      for (; tile + 1 < span.tile_hi; ++tile) step(std::false_type{});
-      step(std::true_type{});
+    if (at.page < span.tile_hi) {
+      while (true) {
+        const At then = behind(span, at);
+        if (then.page >= span.tile_hi) break;
+        step(std::false_type{}, then);
+        at = then;
+      }
+      step(std::true_type{}, at);
     } else {  // (nothing kept; the loads are waited for here, so that this rare way does not count where the waits of the others are set)
       const Codes c = turn_to_next();
       load_k<D>(t, c.k, k_at);
@@ -265,16 +292,21 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
     }
     if (more_blocks) store_q(q_side ^ 1);
     q_side ^= 1;
-    finish<D, RT, R, 4, C::kParts, kThreads, OUT32>(p, dealer, dealer.kept(0), a, o_lds, ml_lds + parity * 4 * R, wave, 0, 2 * blockIdx.x + first_partial);
-    parity ^= 1;
+    const int slot = 2 * dealer.share() + first_partial;
+    if constexpr (ALONE) {
+      finish_alone<D, kThreads, OUT32>(dealer, dealer.kept(0), a, slot);
+    } else {
+      finish<D, RT, R, 4, C::kParts, kThreads, OUT32>(p, dealer, dealer.kept(0), a, o_lds, ml_lds + parity * 4 * R, wave, 0, slot);
+      parity ^= 1;
+    }
     first_partial = 1;
     if (!more_blocks) break;
     const Piece next = dealer.kept(1);
     dealer.keep(0, next);
     b = next.b;
     h = next.h;
-    tile = next.tile_lo;
     span = Span(next);
+    at = from(span, At{uniform(next.tile_lo), first_quarter}, span.tile_hi);
   }
 }
 
@@ -282,7 +314,7 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
 // row lies in the slot of the i-th work group: the first one may have had another block before (slot 2 u + 1), the others
 // begin with this one (2 u).  WAVES waves share a row, each every WAVES-th partial.
 template <int D, bool OUT32, int WAVES>
-__global__ __launch_bounds__(256) void gqa_combine_kernel(GqaDecodeParams p, int block_rows, int units) {
+__global__ __launch_bounds__(256) void gqa_combine_kernel(GqaDecodeParams p, int block_rows, int shares) {
   constexpr int kPer = D / 64;  // columns per lane
   typedef __attribute__((ext_vector_type(kPer))) float vec;
   __shared__ float sh_o[WAVES > 1 ? 4 : 1][WAVES > 1 ? D : 1];
@@ -294,7 +326,7 @@ __global__ __launch_bounds__(256) void gqa_combine_kernel(GqaDecodeParams p, int
   if (p.q_start && (row / p.q_heads < p.q_start[0] || row / p.q_heads >= p.q_start[p.batch])) return;
   const int2 d = p.rows[row];
   const int count = __builtin_amdgcn_readfirstlane(d.y / 64), in_block = d.y % 64;
-  if (count <= 0 || d.x < 0 || d.x / 2 + count > units) return;
+  if (count <= 0 || d.x < 0 || d.x / 2 + count > shares) return;
   const int u0 = d.x / 2;
   float m = -INFINITY, n = -INFINITY, l = 0.f;
   vec o = {};
@@ -361,38 +393,41 @@ __global__ __launch_bounds__(256) void gqa_combine_kernel(GqaDecodeParams p, int
 }
 
 template <int D, bool OUT32>
-hipError_t join(const GqaDecodeParams& p, int block_rows, int units, hipStream_t stream) {
+hipError_t join(const GqaDecodeParams& p, int block_rows, int shares, hipStream_t stream) {
   const int64_t rows = (int64_t)p.num_queries * p.q_heads;
   // Few rows: four waves to a row.
-  if (rows <= 2048) hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 4>), dim3((uint32_t)rows), dim3(256), 0, stream, p, block_rows, units);
-  else hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 1>), dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, stream, p, block_rows, units);
+  if (rows <= 2048) hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 4>), dim3((uint32_t)rows), dim3(256), 0, stream, p, block_rows, shares);
+  else hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 1>), dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, stream, p, block_rows, shares);
   return hipGetLastError();
 }
 
-template <int D, int RT, bool OUT32>
-hipError_t narrow(const GqaDecodeParams& p, int units, hipStream_t stream) {
-  constexpr size_t lds = Narrow<D, RT>::kLds;
-  hipLaunchKernelGGL((gqa_decode_kernel<D, RT, OUT32>), dim3(units), dim3(kThreads), lds, stream, p);
+template <int D, int RT, bool OUT32, bool ALONE = false>
+hipError_t narrow(const GqaDecodeParams& p, int shares, hipStream_t stream) {
+  constexpr size_t lds = ALONE ? 0 : Narrow<D, RT>::kLds;
+  hipLaunchKernelGGL((gqa_decode_kernel<D, RT, OUT32, ALONE>), dim3(ALONE ? shares / 4 : shares), dim3(kThreads), lds, stream, p);
   return hipGetLastError();
 }
 
 template <int D, bool OUT32>
-hipError_t start(const GqaDecodeParams& p, const GqaShape& shape, int units, hipStream_t stream) {
+hipError_t start(const GqaDecodeParams& p, const GqaShape& shape, int shares, hipStream_t stream) {
   hipError_t e = hipErrorInvalidValue;
-  if (shape.wide) e = launch_gqa_wide(p, shape, units, stream);
-  else if (shape.row_tiles == 1) e = narrow<D, 1, OUT32>(p, units, stream);
-  else if constexpr (D <= 128) {
-    if (shape.row_tiles == 2) e = narrow<D, 2, OUT32>(p, units, stream);
-    else if constexpr (D == 64) e = narrow<D, 4, OUT32>(p, units, stream);
+  if (shape.wide) e = launch_gqa_wide(p, shape, shares, stream);
+  else if (shape.shares == 4) {
+    if constexpr (D == 64) e = narrow<D, 1, OUT32, true>(p, shares, stream);
   }
-  return e != hipSuccess ? e : join<D, OUT32>(p, shape.block_rows, units, stream);
+  else if (shape.row_tiles == 1) e = narrow<D, 1, OUT32>(p, shares, stream);
+  else if constexpr (D <= 128) {
+    if (shape.row_tiles == 2) e = narrow<D, 2, OUT32>(p, shares, stream);
+    else if constexpr (D == 64) e = narrow<D, 4, OUT32>(p, shares, stream);
+  }
+  return e != hipSuccess ? e : join<D, OUT32>(p, shape.block_rows, shares, stream);
 }
 
 template <int D, int RT>
 hipError_t allow_lds() {
   constexpr int lds = (int)Narrow<D, RT>::kLds;
-  hipError_t e = hipFuncSetAttribute((const void*)gqa_decode_kernel<D, RT, false>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  if (e == hipSuccess) e = hipFuncSetAttribute((const void*)gqa_decode_kernel<D, RT, true>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  hipError_t e = hipFuncSetAttribute((const void*)gqa_decode_kernel<D, RT, false, false>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e == hipSuccess) e = hipFuncSetAttribute((const void*)gqa_decode_kernel<D, RT, true, false>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   return e;
 }
 
@@ -402,13 +437,21 @@ hipError_t allow_lds() {
 // kernel with so many row tiles (several blocks where the rows are more):
 //   width  rows   1 tile   2 tiles   4 tiles   wide, 32 rows   wide, 64 rows
 //   TODO
-GqaShape gqa_shape(int batch, int num_queries, int group, int head_dim) {
+// Waves that work alone: a block costs them 3 us less, as they need not meet, but they leave more partial rows, and what is left uneven
+// weighs four times as much.  256 requests, 12 KV heads of width 64, us with them and without: 128 tokens each 19.6 / 26.3, 1 to 2000
+// (window 1024) 34 / 40.5, 1024 each 87 / 83, 2048 each 156 / 153; 128 requests of 500 to 8000 tokens, 8 KV heads 85 / 83.5.  At width 128
+// they lose from 50 to 1000 tokens on (200 requests, 8 KV heads: 44 / 41.5), and so they are for many short blocks of width 64.
+GqaShape gqa_shape(int batch, int num_queries, int group, int kv_heads, int head_dim, int64_t pages, int cus) {
   const int64_t rows = (int64_t)((num_queries + batch - 1) / batch) * group;
-  if (rows <= 16) return GqaShape{false, 1, 16, groups_per_cu(head_dim, 1)};
-  if (head_dim == 256) return GqaShape{true, 1, 64, 1};
-  if (rows <= 32) return GqaShape{false, 2, 32, groups_per_cu(head_dim, 2)};
-  if (head_dim == 64) return GqaShape{false, 4, 64, groups_per_cu(head_dim, 4)};
-  return GqaShape{true, 2, 64, 1};
+  if (rows <= 16) {
+    const int groups = cus * groups_per_cu(head_dim, 1);
+    const bool alone = head_dim == 64 && (int64_t)batch * kv_heads >= 2 * groups && pages <= 16;
+    return GqaShape{false, 1, 16, groups, alone ? 4 : 1};
+  }
+  if (head_dim == 256) return GqaShape{true, 1, 64, cus, 1};
+  if (rows <= 32) return GqaShape{false, 2, 32, cus * groups_per_cu(head_dim, 2), 1};
+  if (head_dim == 64) return GqaShape{false, 4, 64, cus * groups_per_cu(head_dim, 4), 1};
+  return GqaShape{true, 2, 64, cus, 1};
 }
 
 hipError_t init_gqa_kernels() {
@@ -422,9 +465,9 @@ hipError_t init_gqa_kernels() {
   return e;
 }
 
-hipError_t launch_gqa_decode(const GqaDecodeParams& p, const GqaShape& shape, int units, hipStream_t stream) {
+hipError_t launch_gqa_decode(const GqaDecodeParams& p, const GqaShape& shape, int shares, hipStream_t stream) {
   auto with = [&](auto d) {
-    return p.out_fp32 ? start<decltype(d)::value, true>(p, shape, units, stream) : start<decltype(d)::value, false>(p, shape, units, stream);
+    return p.out_fp32 ? start<decltype(d)::value, true>(p, shape, shares, stream) : start<decltype(d)::value, false>(p, shape, shares, stream);
   };
   if (p.head_dim == 64) return with(std::integral_constant<int, 64>{});
   if (p.head_dim == 128) return with(std::integral_constant<int, 128>{});

@@ -14,7 +14,7 @@
 namespace omniattn {
 namespace {
 
-constexpr int kThreads = 512, kWaves = 8;
+constexpr int kThreads = 512, kWaves = 8, kStart = 2;
 
 template <int D, int RT>
 struct Wide {
@@ -104,11 +104,11 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
   uint8_t* const scale_ring = ring + kStages * 2 * C::kHalf;
   float* const o_lds = (float*)(ring + C::kRing);
   float4* const ml_lds = (float4*)(ring + C::kRing + C::kOBytes);
-  __shared__ typename Dealer<R, kThreads>::Lds dealt;
+  __shared__ typename Dealer<R, kThreads, kStart>::Lds dealt;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int n16 = lane & 15, g = lane >> 4;
   const int tg = wave % TG, row0 = wave / TG * 16 * RT;
-  Dealer<R, kThreads> dealer(p, dealt);
+  Dealer<R, kThreads, kStart> dealer(p, dealt);
   Piece now;
   if (!dealer.begin(now)) return;
   const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)ring;
@@ -282,9 +282,9 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
 }
 
 template <int D, int RT, bool OUT32>
-hipError_t start(const GqaDecodeParams& p, int units, hipStream_t stream) {
+hipError_t start(const GqaDecodeParams& p, int shares, hipStream_t stream) {
   constexpr size_t lds = Wide<D, RT>::kLds;
-  hipLaunchKernelGGL((gqa_wide_kernel<D, RT, OUT32>), dim3(units), dim3(kThreads), lds, stream, p);
+  hipLaunchKernelGGL((gqa_wide_kernel<D, RT, OUT32>), dim3(shares), dim3(kThreads), lds, stream, p);
   return hipGetLastError();
 }
 template <int D, int RT>
@@ -303,9 +303,9 @@ hipError_t init_gqa_wide_kernels() {
   return e;
 }
 
-hipError_t launch_gqa_wide(const GqaDecodeParams& p, const GqaShape& shape, int units, hipStream_t stream) {
-  if (p.head_dim == 128 && shape.row_tiles == 2) return p.out_fp32 ? start<128, 2, true>(p, units, stream) : start<128, 2, false>(p, units, stream);
-  if (p.head_dim == 256 && shape.row_tiles == 1) return p.out_fp32 ? start<256, 1, true>(p, units, stream) : start<256, 1, false>(p, units, stream);
+hipError_t launch_gqa_wide(const GqaDecodeParams& p, const GqaShape& shape, int shares, hipStream_t stream) {
+  if (p.head_dim == 128 && shape.row_tiles == 2) return p.out_fp32 ? start<128, 2, true>(p, shares, stream) : start<128, 2, false>(p, shares, stream);
+  if (p.head_dim == 256 && shape.row_tiles == 1) return p.out_fp32 ? start<256, 1, true>(p, shares, stream) : start<256, 1, false>(p, shares, stream);
   return hipErrorInvalidValue;
 }
 

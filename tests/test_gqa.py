@@ -359,6 +359,34 @@ def test_many_requests_fill_every_work_group_several_times():
 
 
 @gpu
+@pytest.mark.parametrize("out_dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("group,most,sink,window", [(1, 1, 4, 150), (1, 3, 0, 10 ** 6), (3, 3, 2, 40), (16, 1, 0, 1), (1, 20, 130, 60)])
+def test_many_short_requests_of_narrow_heads(group, most, sink, window, out_dtype):
+    """2048 blocks and more, of one wave each: empty ones, parts of a page, blocks cut between waves, requests of more rows than a block."""
+    rng = random.Random(group + most)
+    lens = [rng.choice([0, 1, 31, 32, 33, 65, 128, 129, 200, 290]) for _ in range(256)]
+    news = [min(n, rng.choice([0, 1, most]) if most > 1 else 1) for n in lens]
+    Problem(lens, news, 8 * group, 8, 64, 32, sink, window, seed=group, extra_pages=0).check(out_dtype)
+
+
+@gpu
+def test_nan_among_many_short_requests():
+    lens, news = [150] * 256, [3] * 256
+    clean = Problem(lens, news, 8, 8, 64, 64, 1, 30, seed=9, poison=False)
+    p = Problem(lens, news, 8, 8, 64, 64, 1, 30, seed=9, poison=False)
+    for b, at, head, column in ((3, 149, 0, 63), (3, 148, 7, 0), (100, 119, 4, 17), (255, 0, 5, 40), (200, 60, 2, 9)):
+        p.codes[1].view(torch.uint8)[p.table[b][at // PAGE], head, at % PAGE, column] = 0x7f
+    (want, want_lse), (out, lse) = clean.run(torch.float32), p.run(torch.float32)
+    bad = torch.zeros(want.shape, dtype=torch.bool)
+    bad[3 * 3 + 2, 0, 63] = True           # token 149: the last query's
+    bad[3 * 3 + 1:3 * 3 + 3, 7, 0] = True  # token 148: the last two queries'
+    bad[100 * 3:100 * 3 + 2, 4, 17] = True  # token 119 has left the last query's window
+    bad[255 * 3:255 * 3 + 3, 5, 40] = True  # token 0 is a sink
+    assert torch.equal(out.isnan().cpu(), bad) and torch.equal(lse, want_lse)
+    assert torch.equal(out.cpu()[~bad], want.cpu()[~bad])
+
+
+@gpu
 def test_peaked_and_shifted_logits():
     """Large logits that grow along the request (the reference is raised again and again) and shrink (it never is)."""
     for sign in (1, -1):
