@@ -401,77 +401,101 @@ def _want(ok, what):
         raise OmniAttnError(-1, what)
 
 
+# (The checks below cost as much as a short kernel takes, so each is one test that fails as a whole, and builds its message only then.)
+
 def _ints(t, n, name):
-    """A contiguous int32 CUDA tensor of n elements."""
+    """Address of a contiguous int32 CUDA tensor of n elements."""
     import torch
-    _want(t.dtype is torch.int32 and t.is_cuda and t.is_contiguous() and t.numel() == n, f"{name}: int32 CUDA tensor of {n} elements wanted")
+    if t.dtype is not torch.int32 or t.numel() != n or not t.is_cuda or not t.is_contiguous():
+        raise OmniAttnError(-1, f"{name}: int32 CUDA tensor of {n} elements wanted")
     return t.data_ptr()
 
 
-def _table(page_table, batch, num_pages, max_tokens):
+def _table_of(page_table, batch):
+    """(columns, row stride) of a page table."""
     import torch
-    _want(page_table.dtype is torch.int32 and page_table.is_cuda and page_table.dim() == 2 and page_table.shape[0] == batch
-          and page_table.stride(1) == 1, "page_table: int32 CUDA tensor [batch, pages] wanted, its rows contiguous")
-    return _table_record(batch, page_table.shape[1], page_table.stride(0), max_tokens, num_pages)
+    if page_table.dtype is torch.int32 and page_table.is_cuda and page_table.dim() == 2:
+        rows, columns = page_table.shape
+        stride, step = page_table.stride()
+        if rows == batch and step == 1:
+            return columns, stride
+    raise OmniAttnError(-1, "page_table: int32 CUDA tensor [batch, pages] wanted, its rows contiguous")
+
+
+def _handle(stream):
+    """Of the given stream, or of torch's current one, for calls whose tensors are CUDA tensors already (torch's CUDA part is running)."""
+    if stream is not None:
+        return stream.cuda_stream
+    from torch import _C
+    return _C._cuda_getCurrentRawStream(_C._cuda_getDevice())
 
 
 def omniattn_table_extend(seq_lens, new_lens, free_pages, free_count, page_table, seq_lens_out, free_count_out, q_start, slot_map, stream=None):
     """Tables of one step on the GPU: every request grows by its new tokens and takes pages from the stack of free ones (all int32
     CUDA tensors; page_table, seq_lens_out, free_count_out, q_start [batch + 1] and slot_map are written).  seq_lens_out may be
     seq_lens, free_count_out may be free_count.  A request that does not fit keeps its length and gets slots -1."""
-    batch, tokens = seq_lens.shape[0], slot_map.shape[0]
-    rec = _table(page_table, batch, free_pages.shape[0], tokens)
+    batch, tokens, pages = seq_lens.numel(), slot_map.numel(), free_pages.numel()
+    columns, stride = _table_of(page_table, batch)
     _check(load_library().omniattn_table_extend(
-        rec, _ints(seq_lens, batch, "seq_lens"), _ints(new_lens, batch, "new_lens"), _ints(free_pages, free_pages.shape[0], "free_pages"),
+        _table_record(batch, columns, stride, tokens, pages), _ints(seq_lens, batch, "seq_lens"), _ints(new_lens, batch, "new_lens"),
+        _ints(free_pages, pages, "free_pages"),
         _ints(free_count, 1, "free_count"), page_table.data_ptr(), _ints(seq_lens_out, batch, "seq_lens_out"),
         _ints(free_count_out, 1, "free_count_out"), _ints(q_start, batch + 1, "q_start"), _ints(slot_map, tokens, "slot_map"),
-        _current_stream() if stream is None else stream.cuda_stream))
+        _handle(stream)))
 
 
 def omniattn_table_release(seq_lens, done, page_table, free_pages, free_count, stream=None):
     """Pages of the requests with done[b] != 0 go back on the stack, their lengths become 0 (seq_lens, free_pages and free_count
     change in place)."""
-    batch = seq_lens.shape[0]
-    rec = _table(page_table, batch, free_pages.shape[0], 0)
+    batch, pages = seq_lens.numel(), free_pages.numel()
+    columns, stride = _table_of(page_table, batch)
     _check(load_library().omniattn_table_release(
-        rec, _ints(done, batch, "done"), _ints(seq_lens, batch, "seq_lens"), page_table.data_ptr(), _ints(free_pages, free_pages.shape[0], "free_pages"),
-        _ints(free_count, 1, "free_count"), _current_stream() if stream is None else stream.cuda_stream))
+        _table_record(batch, columns, stride, 0, pages), _ints(done, batch, "done"), _ints(seq_lens, batch, "seq_lens"), page_table.data_ptr(),
+        _ints(free_pages, pages, "free_pages"), _ints(free_count, 1, "free_count"), _handle(stream)))
 
 
 def _cache_shape(k_cache, v_cache, k_scales, v_scales):
     """(pages, KV heads, page size, head width, tokens to a scale) of a layer's cache."""
     import torch
+    codes, numbers = torch.float8_e4m3fn, torch.float32
     shape, scales = k_cache.shape, k_scales.shape
-    _want(len(shape) == 4 and len(scales) == 3 and scales[:2] == shape[:2] and v_cache.shape == shape and v_scales.shape == scales,
-          "cache [pages, KV heads, 128, head width] with scales [pages, KV heads, 128 / tokens] wanted, for K and V alike")
-    _want(k_cache.dtype is torch.float8_e4m3fn and v_cache.dtype is torch.float8_e4m3fn and k_scales.dtype is torch.float32
-          and v_scales.dtype is torch.float32, "cache of float8_e4m3fn with scales of float32 wanted")
-    _want(k_cache.is_contiguous() and v_cache.is_contiguous() and k_scales.is_contiguous() and v_scales.is_contiguous()
-          and k_cache.is_cuda and v_cache.is_cuda and k_scales.is_cuda and v_scales.is_cuda, "cache and scales: contiguous CUDA tensors wanted")
-    _want(scales[2] > 0 and shape[2] % scales[2] == 0, "scales: they divide a page")
-    return shape[0], shape[1], shape[2], shape[3], shape[2] // scales[2]
+    if (k_cache.dtype is not codes or v_cache.dtype is not codes or k_scales.dtype is not numbers or v_scales.dtype is not numbers
+            or len(shape) != 4 or len(scales) != 3 or v_cache.shape != shape or v_scales.shape != scales):
+        raise OmniAttnError(-1, "cache (float8_e4m3fn) [pages, KV heads, 128, head width] with scales (float32) [pages, KV heads, 128 / tokens] "
+                                "wanted, for K and V alike")
+    if not (k_cache.is_contiguous() and v_cache.is_contiguous() and k_scales.is_contiguous() and v_scales.is_contiguous()
+            and k_cache.is_cuda and v_cache.is_cuda and k_scales.is_cuda and v_scales.is_cuda):
+        raise OmniAttnError(-1, "cache and scales: contiguous CUDA tensors wanted")
+    pages, heads, page, dim = shape
+    per_page = scales[2]
+    if scales[0] != pages or scales[1] != heads or per_page <= 0 or page % per_page:
+        raise OmniAttnError(-1, "scales: for every page and KV head of the cache wanted, their number a divisor of a page's tokens")
+    return pages, heads, page, dim, page // per_page
 
 
 def _rows_of(t, heads, dim, name):
-    """Address and token stride of bf16 rows [tokens, heads, dim]."""
+    """(tokens, address, token stride) of bf16 rows [tokens, heads, dim]."""
     import torch
-    _want(t.dtype is torch.bfloat16 and t.is_cuda and t.dim() == 3 and t.shape[1] == heads and t.shape[2] == dim
-          and t.stride(2) == 1 and (t.stride(1) == dim or heads == 1), f"{name}: bf16 CUDA tensor [tokens, {heads}, {dim}] wanted, a token's rows contiguous")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else heads * dim)
+    if t.dtype is torch.bfloat16 and t.is_cuda and t.dim() == 3:
+        n, h, d = t.shape
+        stride, head, step = t.stride()
+        if h == heads and d == dim and step == 1 and (head == dim or heads == 1):
+            return n, t.data_ptr(), stride if n > 1 else heads * dim
+    raise OmniAttnError(-1, f"{name}: bf16 CUDA tensor [tokens, {heads}, {dim}] wanted, a token's rows contiguous")
 
 
 def omniattn_gqa_append(k_new, v_new, slot_map, k_cache, v_cache, k_scales, v_scales, stream=None):
     """New K and V rows (bf16 [tokens, KV heads, head width], any token stride) to their slots in a layer's cache, rounded to e4m3
     with a scale for each block of tokens and head.  k_cache, v_cache, k_scales and v_scales are written."""
     pages, heads, page, dim, tokens = _cache_shape(k_cache, v_cache, k_scales, v_scales)
-    n = slot_map.shape[0]
-    _want(k_new.shape[0] == n and v_new.shape[0] == n, "k_new, v_new and slot_map: as many tokens wanted")
-    k, k_stride = _rows_of(k_new, heads, dim, "k_new")
-    v, v_stride = _rows_of(v_new, heads, dim, "v_new")
+    n, k, k_stride = _rows_of(k_new, heads, dim, "k_new")
+    n_v, v, v_stride = _rows_of(v_new, heads, dim, "v_new")
+    if n_v != n:
+        raise OmniAttnError(-1, "k_new and v_new: as many tokens wanted")
     rec = _gqa_record(1, 0, heads, heads, dim, page, tokens, 1, 1, pages, 0, 0, 1.0, BF16)
     _check(load_library().omniattn_gqa_append(
         rec, n, k, k_stride, v, v_stride, _ints(slot_map, n, "slot_map"), k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(),
-        v_scales.data_ptr(), _current_stream() if stream is None else stream.cuda_stream))
+        v_scales.data_ptr(), _handle(stream)))
 
 
 def omniattn_gqa_workspace_bytes(batch, num_queries, num_q_heads, num_kv_heads, head_dim):
@@ -489,20 +513,21 @@ def omniattn_gqa_decode(q, k_cache, v_cache, k_scales, v_scales, page_table, seq
     out (bf16 or fp32, shaped like q) and lse (fp32 [tokens, query heads]) are written."""
     import torch
     pages, heads, page, dim, tokens = _cache_shape(k_cache, v_cache, k_scales, v_scales)
-    batch, n, q_heads = seq_lens.shape[0], q.shape[0], q.shape[1]
-    src, q_stride = _rows_of(q, q_heads, dim, "q")
-    _want(page_table.dtype is torch.int32 and page_table.is_cuda and page_table.dim() == 2 and page_table.shape[0] == batch
-          and page_table.stride(1) == 1, "page_table: int32 CUDA tensor [batch, pages] wanted, its rows contiguous")
-    _want((out.dtype is torch.bfloat16 or out.dtype is torch.float32) and out.shape == q.shape and out.is_contiguous() and out.is_cuda,
-          "out: contiguous bf16 or fp32 CUDA tensor shaped like q wanted")
-    _want(lse.dtype is torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous() and lse.is_cuda, "lse: contiguous fp32 CUDA tensor [tokens, query heads] wanted")
-    rec = _gqa_record(batch, n, q_heads, heads, dim, page, tokens, page_table.shape[1], page_table.stride(0), pages, operator.index(sink),
-                      operator.index(window), float(softmax_scale), FP32 if out.dtype is torch.float32 else BF16)
+    shape = q.shape
+    batch, q_heads = seq_lens.numel(), shape[1] if len(shape) == 3 else 0
+    n, src, q_stride = _rows_of(q, q_heads, dim, "q")
+    columns, stride = _table_of(page_table, batch)
+    fp32 = out.dtype is torch.float32
+    if not (fp32 or out.dtype is torch.bfloat16) or out.shape != shape or not out.is_contiguous() or not out.is_cuda:
+        raise OmniAttnError(-1, "out: contiguous bf16 or fp32 CUDA tensor shaped like q wanted")
+    if lse.dtype is not torch.float32 or lse.shape != (n, q_heads) or not lse.is_contiguous() or not lse.is_cuda:
+        raise OmniAttnError(-1, "lse: contiguous fp32 CUDA tensor [tokens, query heads] wanted")
+    rec = _gqa_record(batch, n, q_heads, heads, dim, page, tokens, columns, stride, pages, operator.index(sink), operator.index(window),
+                      float(softmax_scale), FP32 if fp32 else BF16)
     _check(load_library().omniattn_gqa_decode(
         rec, src, q_stride, k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), page_table.data_ptr(),
         _ints(seq_lens, batch, "seq_lens"), _ints(q_start, batch + 1, "q_start") if q_start is not None else None, out.data_ptr(), lse.data_ptr(),
-        _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0,
-        _current_stream() if stream is None else stream.cuda_stream))
+        _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0, _handle(stream)))
 
 
 def gqa_decode(q, k_cache, v_cache, k_scales, v_scales, page_table, seq_lens, sink, window, softmax_scale, q_start=None, out_dtype=None):
