@@ -8,8 +8,8 @@
 //
 // A work group looks through C consecutive tokens of the call for runs (tokens that follow one another in one block) that begin
 // there, for one head and K or V.  A long run is the work of all its waves: the rows stay in registers between the maximum
-// and the rounding, so they are read once.  Runs that fit one pass of a wave (a decode step's single tokens) are dealt out to
-// the waves.
+// and the rounding, so they are read once.  Runs that fit one pass of a wave are dealt out to the waves, and single tokens (a
+// decode step's) to the groups of lanes that hold a row, so that the 32 of a mixed step's C are two passes and not eight.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -73,10 +73,14 @@ template <int D>
 __device__ __forceinline__ void regrow(const Run& run, float old, float scale, int row, int rows) {
   if (run.off > 0 && scale > old) {
     const float ratio = old / scale;
-    for (int k = row - run.off; k < 0; k += rows) {
-      u32x2* at = (u32x2*)(run.codes + (ptrdiff_t)k * D);
-      const u32x2 c = *at;
-      *at = u32x2{recode(c[0], ratio), recode(c[1], ratio)};
+    constexpr int kBatch = 8;  // rows under way: one at a time, a single token late in its block would wait for each of them in turn
+    for (int k0 = row - run.off; k0 < 0; k0 += kBatch * rows) {
+      u32x2 c[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) c[i] = *(const u32x2*)(run.codes + (ptrdiff_t)min(k0 + i * rows, -1) * D);
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        if (k0 + i * rows < 0) *(u32x2*)(run.codes + (ptrdiff_t)(k0 + i * rows) * D) = u32x2{recode(c[i][0], ratio), recode(c[i][1], ratio)};
     }
   }
 }
@@ -87,8 +91,10 @@ __device__ __forceinline__ uint32_t largest(const u32x4& x) {
   for (int j = 0; j < 4; ++j) top = max(top, max(finite_bits(x[j]), finite_bits(x[j] >> 16)));
   return top;
 }
-__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
-  for (int d = 1; d < 64; d *= 2) x = max(x, (uint32_t)__shfl_xor(x, d));
+template <int LANES>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t x) {
+#pragma unroll
+  for (int d = 1; d < LANES; d *= 2) x = max(x, (uint32_t)__shfl_xor(x, d));
   return x;
 }
 
@@ -141,12 +147,46 @@ __global__ __launch_bounds__(kThreads) void gqa_append_kernel(GqaAppendParams p,
     return min(r, each - off);
   };
   auto slot_of = [&](int i) { return __builtin_amdgcn_readlane(i < 64 ? slot[0] : slot[1], i & 63); };
+  uint64_t begins[2], single[2];
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    begins[w] = valid[w] & ~next[w];
+    single[w] = begins[w] & ~(next[w] >> 1 | next[w + 1] << 63);
+    begins[w] &= ~single[w];
+  }
+
+  // single tokens, kRows at a time
+  int count = 0, my_token = -1, my_slot = 0;
+  auto append_singles = [&] {
+    if (my_token >= 0) {
+      const u32x4 x = *(const u32x4*)(rows + (int64_t)my_token * stride);
+      const Run run = run_at<D>(p, kv, head, my_slot, col);
+      const float old = run.off > 0 ? *run.scale : 0.f;
+      const float scale = fmaxf(old, block_scale(lanes_max<kPer>(largest(x)))), inv = scale > 0.f ? 1.f / scale : 0.f;
+      *(u32x2*)run.codes = u32x2{encode_words(x[0], x[1], inv), encode_words(x[2], x[3], inv)};
+      regrow<D>(run, old, scale, 0, 1);
+      if (col == 0) *run.scale = scale;
+    }
+    my_token = -1;
+  };
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    for (uint64_t rest = single[w]; rest; rest &= rest - 1) {
+      const int i = w * 64 + __builtin_ctzll(rest), s0 = slot_of(i);
+      if (count % kRows == row) {
+        my_token = i0 + i;
+        my_slot = s0;
+      }
+      if (++count % kRows == 0) append_singles();
+    }
+  }
+  if (count % kRows) append_singles();
 
   // long runs
   int parity = 0, turn = 0;
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
-    for (uint64_t begin = valid[w] & ~next[w]; begin; begin &= begin - 1) {
+    for (uint64_t begin = begins[w]; begin; begin &= begin - 1) {
       const int i = w * 64 + __builtin_ctzll(begin), s0 = slot_of(i);
       const int r = length(i, s0 % each);
       if (r <= kWaveRows) continue;
@@ -162,7 +202,7 @@ __global__ __launch_bounds__(kThreads) void gqa_append_kernel(GqaAppendParams p,
 #pragma unroll
       for (int s = 0; s < kPasses; ++s)
         if (s * kRows < r) top = max(top, largest(x[s]));
-      top = wave_max(top);
+      top = lanes_max<64>(top);
       if (lane == 0) tot[parity][wave] = top;
       __syncthreads();  // (also: every thread has read the old scale)
       top = max(max(tot[parity][0], tot[parity][1]), max(tot[parity][2], tot[parity][3]));
@@ -181,14 +221,14 @@ __global__ __launch_bounds__(kThreads) void gqa_append_kernel(GqaAppendParams p,
   const int wrow = lane / kPer;
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
-    for (uint64_t begin = valid[w] & ~next[w]; begin; begin &= begin - 1) {
+    for (uint64_t begin = begins[w]; begin; begin &= begin - 1) {
       const int i = w * 64 + __builtin_ctzll(begin), s0 = slot_of(i);
       const int r = length(i, s0 % each);
       if (r > kWaveRows || (turn++ & 3) != wave) continue;
       const u32x4 x = wrow < r ? *(const u32x4*)(rows + (int64_t)(i0 + i + wrow) * stride) : u32x4{0, 0, 0, 0};
       const Run run = run_at<D>(p, kv, head, s0, col);
       const float old = run.off > 0 ? *run.scale : 0.f;
-      const float scale = fmaxf(old, block_scale(wave_max(largest(x)))), inv = scale > 0.f ? 1.f / scale : 0.f;
+      const float scale = fmaxf(old, block_scale(lanes_max<64>(largest(x)))), inv = scale > 0.f ? 1.f / scale : 0.f;
       if (wrow < r) *(u32x2*)(run.codes + (size_t)wrow * D) = u32x2{encode_words(x[0], x[1], inv), encode_words(x[2], x[3], inv)};
       regrow<D>(run, old, scale, wrow, kWaveRows);
       if (lane == 0) *run.scale = scale;
@@ -200,9 +240,10 @@ __global__ __launch_bounds__(kThreads) void gqa_append_kernel(GqaAppendParams p,
 
 hipError_t launch_gqa_append(const GqaAppendParams& p, hipStream_t stream) {
   if (p.num_tokens <= 0) return hipSuccess;
-  // About 2048 work groups, or fewer; no more tokens to one than its scale's block has.
+  // 1024 to 2048 work groups (looking through the slots costs each of them more than its rows do), of no more tokens than their scale's block
+  // has.  us, 133 requests with chunks, 7 heads / 65536 tokens, 8 heads: at least 1024 groups 8.0 / 66.3, 2048 9.4 / 66.3, 4096 12.3 / 66.4.
   int C = 1;
-  while (C < p.scale_tokens && (int64_t)p.num_tokens * p.kv_heads * 2 > (int64_t)2048 * C) C *= 2;
+  while (C < p.scale_tokens && (int64_t)p.num_tokens * p.kv_heads * 2 > (int64_t)1024 * C) C *= 2;
   const dim3 grid((uint32_t)(((int64_t)p.num_tokens + C - 1) / C * p.kv_heads * 2));
   if (p.head_dim == 64) hipLaunchKernelGGL(gqa_append_kernel<64>, grid, dim3(kThreads), 0, stream, p, C);
   else if (p.head_dim == 128) hipLaunchKernelGGL(gqa_append_kernel<128>, grid, dim3(kThreads), 0, stream, p, C);

@@ -177,6 +177,30 @@ def test_append(dim, each, heads, runs, seed):
 
 
 @gpu
+@pytest.mark.parametrize("dim,heads", [(64, 2), (128, 7), (256, 1)])
+@pytest.mark.parametrize("each", [32, 128])
+def test_append_single_tokens_beside_prompts(dim, heads, each):
+    """A mixed step: hundreds of single tokens, pairs and threes, whole chunks between them, in the places of their blocks that the others leave."""
+    rng = random.Random(dim + each)
+    runs = [rng.choice([1] * 12 + [2, 3, 5, 9, 150]) for _ in range(400)]
+    slots, pages = [], 0
+    for n in runs:
+        first = rng.choice([0, 1, 31, 32, 77, 126, 127])
+        at = [pages * PAGE + first + i for i in range(n)]
+        pages += (first + n + PAGE - 1) // PAGE
+        slots += at
+    codes, scales = _cache(pages, heads, dim, each, dim)
+    new = torch.randn((2, len(slots), heads, dim), generator=_gen(dim)) * 2.0 ** torch.randint(-20, 8, (2, len(slots), heads, 1), generator=_gen(each)).float()
+    new = new.bfloat16()
+    k, v = codes.cuda()
+    ks, vs = scales.cuda()
+    on_gpu = new.cuda()
+    oa.omniattn_gqa_append(on_gpu[0], on_gpu[1], ints(slots), k, v, ks, vs)
+    _check_append(new[0], slots, codes[0], scales[0], k, ks)
+    _check_append(new[1], slots, codes[1], scales[1], v, vs)
+
+
+@gpu
 def test_append_strided_rows_unknown_slots_and_special_numbers():
     """K and V as slices of one tensor, tokens without a slot among them, infinities, NaN, subnormal and the largest numbers."""
     g = _gen(5)
