@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "gqa.h"
 
@@ -22,8 +23,8 @@ __device__ __forceinline__ uint32_t sat(uint32_t a, uint32_t b) { return min(a +
 
 __device__ __forceinline__ int pages_of(int64_t tokens) { return (int)((tokens + kPage - 1) / kPage); }
 
-// Inclusive running sum over the work group's threads.  `tot`: one word per wave; two barriers.
-__device__ __forceinline__ uint32_t group_sum(uint32_t x, uint32_t* tot) {
+// Sum over the work group's threads before this one.  `tot`: one word per wave; two barriers.
+__device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t* tot) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int d = 1; d < 64; d *= 2) {
     const uint32_t y = __shfl_up(x, d);
@@ -34,7 +35,8 @@ __device__ __forceinline__ uint32_t group_sum(uint32_t x, uint32_t* tot) {
   __syncthreads();
   uint32_t before = 0;
   for (int w = 0; w < wave; ++w) before = sat(before, tot[w]);
-  return sat(x, before);
+  x = __shfl_up(x, 1);
+  return lane ? sat(x, before) : before;
 }
 
 // First index whose running sum is above i (n entries, the last one is).
@@ -51,57 +53,82 @@ __device__ __forceinline__ int owner(const uint32_t* ends, int n, uint32_t i) {
 // WHAT: 1 table, first tokens and slots; 2 lengths and the stack's height; 3 both.  Every work group sums over the whole
 // batch by itself (its lengths are a few KB in L2) and writes its share of the slots and table entries, so one launch
 // does it and no group waits for another.  Only where the new lengths replace the old ones in place must the writing of
-// them come behind all reading: a launch of its own, or the only work group.
-template <int WHAT>
+// them come behind all reading: a launch of its own, or the only work group.  PER: neighbouring requests to a thread; batches of
+// more than PER work groups' threads take several turns, one behind the other.
+template <int WHAT, int PER>
 __global__ __launch_bounds__(kThreads) void extend_kernel(TableParams p) {
+  constexpr int kMany = PER * kThreads;
   __shared__ uint32_t tot[kThreads / 64];
-  __shared__ uint32_t token_end[kThreads], page_end[kThreads];
-  __shared__ int had[kThreads], len[kThreads];  // had: -1 where the request is refused
+  __shared__ uint32_t token_end[kMany], page_end[kMany];
+  __shared__ int had[kMany], len[kMany];  // had: -1 where the request is refused
   const int tid = threadIdx.x, threads = blockDim.x;
   const bool first_group = blockIdx.x == 0;
   const int count = *p.free_count;
   const uint32_t free = (uint32_t)max(count, 0);
   uint32_t tokens = 0, pages = 0, used = 0;  // sums over the chunks before; pages granted
-  for (int b0 = 0; b0 < p.batch; b0 += threads) {
-    const int b = b0 + tid;
-    const bool mine = b < p.batch;
-    const int L = mine ? p.seq_lens[b] : 0, n = mine ? p.new_lens[b] : 0;
-    const int start_page = mine && L >= 0 && L / kPage < p.max_pages && n > 0 ? p.page_table[b * p.stride + L / kPage] : 0;
-    const uint32_t t_end = sat(tokens, group_sum((uint32_t)max(n, 0), tot));
-    const uint32_t t_start = t_end - (uint32_t)max(n, 0);  // (not where the sum has stopped: refused below)
-    const int64_t after = (int64_t)L + n;
-    const int before_pages = L >= 0 ? pages_of(L) : 0;
-    bool fine = mine && L >= 0 && n >= 0 && pages_of(after) <= p.max_pages && t_end <= (uint32_t)p.max_tokens && t_end < kMost;
-    const uint32_t need = fine ? (uint32_t)(pages_of(after) - before_pages) : 0;
-    const uint32_t p_end = sat(pages, group_sum(need, tot));
-    fine = fine && (need == 0 || p_end <= free);
-    const uint32_t granted = fine ? need : 0;
-    if constexpr (WHAT & 2) {
-      if (first_group && mine) p.seq_lens_out[b] = fine ? (int)after : L;
+  for (int b0 = 0; b0 < p.batch; b0 += PER * threads) {
+    int L[PER], n[PER], start_page[PER];
+    uint32_t sum = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int b = b0 + tid * PER + j;
+      L[j] = b < p.batch ? p.seq_lens[b] : 0;
+      n[j] = b < p.batch ? p.new_lens[b] : 0;
     }
-    if constexpr (WHAT & 1) {
-      if (first_group && mine) {
-        p.q_start[b + 1] = (int)t_end;
-        if (b == 0) p.q_start[0] = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int b = b0 + tid * PER + j;
+      if constexpr (PER == 1) start_page[j] = b < p.batch && L[j] >= 0 && L[j] / kPage < p.max_pages && n[j] > 0 ? p.page_table[b * p.stride + L[j] / kPage] : 0;
+      sum = sat(sum, (uint32_t)max(n[j], 0));
+    }
+    // (a sum that has stopped is no request's first token: refused below)
+    uint32_t t_end[PER], p_end[PER], need[PER];
+    bool fine[PER];
+    uint32_t run = sat(tokens, sum_before(sum, tot));
+    sum = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const bool mine = b0 + tid * PER + j < p.batch;
+      const int64_t after = (int64_t)L[j] + n[j];
+      t_end[j] = run = sat(run, (uint32_t)max(n[j], 0));
+      fine[j] = mine && L[j] >= 0 && n[j] >= 0 && pages_of(after) <= p.max_pages && t_end[j] <= (uint32_t)p.max_tokens && t_end[j] < kMost;
+      need[j] = fine[j] ? (uint32_t)(pages_of(after) - pages_of(L[j])) : 0;
+      sum = sat(sum, need[j]);
+    }
+    run = sat(pages, sum_before(sum, tot));
+    bool more = false;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int at = tid * PER + j, b = b0 + at;
+      p_end[j] = run = sat(run, need[j]);
+      fine[j] = fine[j] && (need[j] == 0 || p_end[j] <= free);
+      if (first_group && b < p.batch) {
+        if constexpr (WHAT & 2) p.seq_lens_out[b] = fine[j] ? L[j] + n[j] : L[j];
+        if constexpr (WHAT & 1) {
+          p.q_start[b + 1] = (int)t_end[j];
+          if (b == 0) p.q_start[0] = 0;
+        }
       }
+      token_end[at] = t_end[j];
+      page_end[at] = p_end[j];
+      had[at] = fine[j] ? pages_of(L[j]) : -1;
+      len[at] = L[j];
+      more = more || n[j] > 1;
     }
-    token_end[tid] = t_end;
-    page_end[tid] = p_end;
-    had[tid] = fine ? before_pages : -1;
-    len[tid] = L;
     // (whether all of the chunk's requests bring one token at most: a decode step)
-    const bool chunky = __syncthreads_or(n > 1);
-    const int last = min(threads, p.batch - b0) - 1;
+    const bool chunky = __syncthreads_or(more) || PER > 1;
+    const int last = min(PER * threads, p.batch - b0) - 1;
     if constexpr (WHAT & 1) {
       if (!chunky) {
-        if (first_group && mine && n == 1 && t_end <= (uint32_t)p.max_tokens) {
+        const int b = b0 + tid;
+        if (first_group && b < p.batch && n[0] == 1 && t_end[0] <= (uint32_t)p.max_tokens) {
           int slot = -1;
-          if (fine) {
-            const int page = granted ? p.free_pages[free - p_end] : start_page;
-            if (granted) p.page_table[b * p.stride + before_pages] = page;
-            slot = page * kPage + L % kPage;
+          if (fine[0]) {
+            const int page = need[0] ? p.free_pages[free - p_end[0]] : start_page[0];
+            if (need[0]) p.page_table[b * p.stride + pages_of(L[0])] = page;
+            slot = page * kPage + L[0] % kPage;
           }
-          p.slot_map[t_start] = slot;
+          p.slot_map[t_end[0] - 1] = slot;
         }
       } else {
         const uint32_t step = gridDim.x * threads, at = blockIdx.x * threads + tid;
@@ -169,7 +196,7 @@ __global__ __launch_bounds__(kThreads) void release_kernel(ReleaseParams p) {
     const int b = b0 + tid;
     const bool gone = b < p.batch && p.done[b] != 0;
     const int L = gone ? p.seq_lens[b] : 0;
-    const uint32_t end = sat(pages, group_sum((uint32_t)min(pages_of(max(L, 0)), p.max_pages), tot));
+    const uint32_t many = (uint32_t)min(pages_of(max(L, 0)), p.max_pages), end = sat(sat(pages, sum_before(many, tot)), many);
     page_end[tid] = end;
     if (gone) p.seq_lens[b] = 0;
     __syncthreads();
@@ -188,20 +215,21 @@ __global__ __launch_bounds__(kThreads) void release_kernel(ReleaseParams p) {
 }  // namespace
 
 hipError_t launch_table_extend(const TableParams& p, hipStream_t stream) {
-  // Work groups: one for each 1024 slots.
+  // Work groups: one for each 1024 slots.  Two requests to a thread where there are more than threads (1500 requests: 11.7 us in two turns).
+  const bool pairs = p.batch > kThreads;
   const int want = std::max(p.batch, std::min(p.max_tokens, kThreads));
   const int threads = std::min(kThreads, (want + 63) / 64 * 64);
   const int groups = std::max(1, std::min(256, (p.max_tokens + threads - 1) / threads));
   const bool in_place = p.seq_lens_out == p.seq_lens || p.free_count_out == p.free_count;
-  if (in_place && groups > 1) {
-    hipLaunchKernelGGL(extend_kernel<1>, dim3(groups), dim3(threads), 0, stream, p);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(extend_kernel<2>, dim3(1), dim3(threads), 0, stream, p);
-  } else {
-    hipLaunchKernelGGL(extend_kernel<3>, dim3(groups), dim3(threads), 0, stream, p);
-  }
-  return hipGetLastError();
+  auto launch = [&](auto what, int grid) {
+    constexpr int kWhat = decltype(what)::value;
+    if (pairs) hipLaunchKernelGGL((extend_kernel<kWhat, 2>), dim3(grid), dim3(threads), 0, stream, p);
+    else hipLaunchKernelGGL((extend_kernel<kWhat, 1>), dim3(grid), dim3(threads), 0, stream, p);
+    return hipGetLastError();
+  };
+  if (!in_place || groups == 1) return launch(std::integral_constant<int, 3>{}, groups);
+  const hipError_t e = launch(std::integral_constant<int, 1>{}, groups);
+  return e != hipSuccess ? e : launch(std::integral_constant<int, 2>{}, 1);
 }
 
 hipError_t launch_table_release(const ReleaseParams& p, hipStream_t stream) {
