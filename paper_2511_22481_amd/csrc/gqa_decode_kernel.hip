@@ -313,25 +313,26 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
 // Joins the partial rows of blocks whose pages went to several work groups: o = sum_i 2^(n_i - n) o_i, l = sum_i 2^(m_i - m) l_i.  Partial i of a
 // row lies in the slot of the i-th work group: the first one may have had another block before (slot 2 u + 1), the others
 // begin with this one (2 u).  WAVES waves share a row, each every WAVES-th partial.
-template <int D, bool OUT32, int WAVES>
-__global__ __launch_bounds__(256) void gqa_combine_kernel(GqaDecodeParams p, int block_rows, int shares) {
+template <int D, bool OUT32, int WAVES, int BATCH>
+__global__ __launch_bounds__(64 * (WAVES > 4 ? WAVES : 4)) void gqa_combine_kernel(GqaDecodeParams p, int block_rows, int shares) {
   constexpr int kPer = D / 64;  // columns per lane
   typedef __attribute__((ext_vector_type(kPer))) float vec;
-  __shared__ float sh_o[WAVES > 1 ? 4 : 1][WAVES > 1 ? D : 1];
-  __shared__ float4 sh_ml[4];
+  __shared__ float sh_o[WAVES > 1 ? WAVES : 1][WAVES > 1 ? D : 1];
+  __shared__ float4 sh_ml[WAVES];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * (4 / WAVES) + wave / WAVES;
+  const int64_t row = WAVES > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
   if (row >= (int64_t)p.num_queries * p.q_heads) return;
-  // (rows of no request: nothing was written for them)
-  if (p.q_start && (row / p.q_heads < p.q_start[0] || row / p.q_heads >= p.q_start[p.batch])) return;
+  // (all three are asked for together)
   const int2 d = p.rows[row];
+  const int token = (int)((uint32_t)row / (uint32_t)p.q_heads), first = p.q_start ? p.q_start[0] : 0, stop = p.q_start ? p.q_start[p.batch] : p.num_queries;
+  if (token < first || token >= stop) return;  // (rows of no request: nothing was written for them)
   const int count = __builtin_amdgcn_readfirstlane(d.y / 64), in_block = d.y % 64;
   if (count <= 0 || d.x < 0 || d.x / 2 + count > shares) return;
   const int u0 = d.x / 2;
   float m = -INFINITY, n = -INFINITY, l = 0.f;
   vec o = {};
-  constexpr int kBatch = 8;
-  for (int i0 = wave % WAVES; i0 < count; i0 += kBatch * WAVES) {
+  constexpr int kBatch = BATCH;
+  for (int i0 = WAVES > 1 ? wave : 0; i0 < count; i0 += kBatch * WAVES) {
     float4 e[kBatch];
     vec x[kBatch];
 #pragma unroll
@@ -396,8 +397,8 @@ template <int D, bool OUT32>
 hipError_t join(const GqaDecodeParams& p, int block_rows, int shares, hipStream_t stream) {
   const int64_t rows = (int64_t)p.num_queries * p.q_heads;
   // Few rows: four waves to a row.
-  if (rows <= 2048) hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 4>), dim3((uint32_t)rows), dim3(256), 0, stream, p, block_rows, shares);
-  else hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 1>), dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, stream, p, block_rows, shares);
+  if (rows <= 2048) hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 8, 4>), dim3((uint32_t)rows), dim3(512), 0, stream, p, block_rows, shares);
+  else hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 1, 4>), dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, stream, p, block_rows, shares);
   return hipGetLastError();
 }
 
