@@ -471,7 +471,7 @@ __device__ __forceinline__ Kept kept_of(const GqaDecodeParams& p, const Span& no
 }
 
 // End of a block: the shares of the TG waves that hold the same rows (tokens apart) meet in LDS, references and sums first (ml: [TG][R]),
-// then the outputs at the common reference, 1 / PARTS of the columns at a time (o_lds: [TG][R][D / PARTS + 4]).  tg: which of the TG
+// then the outputs at the common reference, 1 / PARTS of every lane's columns at a time (o_lds: [TG][R][D / PARTS + 4]).  tg: which of the TG
 // the wave is; row0: its first row.  Blocks that other work groups share too leave partial rows in `slot`.
 template <int D, int RT, int R, int TG, int PARTS, int THREADS, bool OUT32, int START>
 __device__ __forceinline__ void finish(const GqaDecodeParams& p, const Dealer<R, THREADS, START>& dealer, const Piece& now, Rows<D, RT>& a, float* o_lds, float4* ml,
@@ -494,26 +494,27 @@ __device__ __forceinline__ void finish(const GqaDecodeParams& p, const Dealer<R,
     shrink[rt] = factor(a.n[rt], top);
   }
   const GqaDecodeParams& end = *late_arguments();
-  constexpr int kChunks = D / 8 / PARTS;
+  constexpr int kChunks = D / 8 / PARTS, kEach = 4 / PARTS;
   const int rows = dealer.rows_of(now);
   const bool whole = now.whole();
 #pragma unroll
   for (int part = 0; part < PARTS; ++part) {
     if (part) lds_barrier();  // (the part before has been read)
-    if (PARTS == 1 || g / (4 / PARTS) == part) {
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        float* const dst = o_lds + (tg * R + row0 + rt * 16 + n16) * kOStride + (4 * g % (16 / PARTS)) * kCols;
+    for (int rt = 0; rt < RT; ++rt) {
+      float* const dst = o_lds + (tg * R + row0 + rt * 16 + n16) * kOStride + g * kEach * kCols;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+      for (int j = 0; j < kEach; ++j) {
+        const int i = part * kEach + j;
 #pragma unroll
-          for (int c = 0; c < kCols; c += 4)
-            *(f32x4*)(dst + i * kCols + c) = f32x4{a.o[rt][c][i] * shrink[rt], a.o[rt][c + 1][i] * shrink[rt], a.o[rt][c + 2][i] * shrink[rt], a.o[rt][c + 3][i] * shrink[rt]};
+        for (int c = 0; c < kCols; c += 4)
+          *(f32x4*)(dst + j * kCols + c) = f32x4{a.o[rt][c][i] * shrink[rt], a.o[rt][c + 1][i] * shrink[rt], a.o[rt][c + 2][i] * shrink[rt], a.o[rt][c + 3][i] * shrink[rt]};
       }
     }
     lds_barrier();
     for (int k = tid; k < rows * kChunks; k += THREADS) {
-      const int row = k / kChunks, in_part = k % kChunks * 8, col = part * (D / PARTS) + in_part;
+      const int row = k / kChunks, in_part = k % kChunks * 8;
+      const int col = in_part / (kEach * kCols) * 4 * kCols + part * kEach * kCols + in_part % (kEach * kCols);
       f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
       float top = -INFINITY, vtop = -INFINITY, sum = 0.f, nans = 0.f;
 #pragma unroll
