@@ -223,7 +223,9 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
       for (int half = 0; half < C::kTilesPerPage; ++half) {
         ask_page();  // (back behind the wait, which is for scalar loads too)
         wait_tile<C::kLoads + 1, kStages - 2>(issued - used - 1);
-        issue();  // (into the stage that every wave has left behind at the barrier)
+        // (into the stage that every wave has left behind at the barrier; half of the waves later, so that one of a SIMD's two is
+        // computing while the other one asks)
+        if (wave < 4) issue();
         ++used;
         const uint8_t* const from_stage = ring + stage * 2 * C::kHalf;
         const float2 scale = *(const float2*)(scale_ring + (stage * kWaves + wave) * C::kScaleBytes);
@@ -250,6 +252,7 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
               }
           }
         }
+        if (wave >= 4) issue();
         if (work) {
           f16x8 high[RT], low[RT];
           weigh<D, RT, OUT32>(p, a, s, reach, kept.full, pos0, g, p.scale_log2 * scale.x, scale.y, high, low);
