@@ -132,10 +132,11 @@ __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirs
 struct Shares {
   int64_t T, each;  // each = T / U
   int U, rest;      // rest = T % U
-  __device__ __forceinline__ int64_t bound(int u) const { return u * each + u * rest / U; }  // (U is at most 2^12)
+  // (U is at most 2^14: the product stays in 32 bits)
+  __device__ __forceinline__ int64_t bound(int u) const { return u * each + (uint32_t)u * (uint32_t)rest / (uint32_t)U; }
   // the share that has unit x
   __device__ __forceinline__ int owner(int64_t x) const {
-    int u = min((int)((double)x * U / (double)T), U - 1);
+    int u = min((int)((float)x * U / (float)T), U - 1);
     while (bound(u) > x) --u;
     while (bound(u + 1) <= x) ++u;
     return u;
