@@ -371,7 +371,8 @@ int omniattn_gqa_append(const omniattn_gqa_t* gqa, int32_t num_tokens, const voi
  *   q_start     device, int32 [B + 1], ascending, at most N; NULL: one query for each request (N = B)
  *   out         device, out_dtype [N, num_q_heads, head_dim]; rows of no request are left as they are
  *   lse         device, fp32 [N, num_q_heads], natural logarithm.  A query that keeps nothing gives 0 and -inf.
- *   workspace   device, omniattn_gqa_workspace_bytes(gqa) bytes, 256-byte aligned; calls in flight at once need one each
+ *   workspace   device, omniattn_gqa_workspace_bytes(gqa) bytes, 256-byte aligned (enough for calls of fewer queries, and of any kept
+ *               set and table width, too); calls in flight at once need one each
  * Tokens that a query does not keep may hold anything (NaN too) without effect on it; a kept NaN makes the row NaN.
  * Same inputs give bitwise identical results.  Arithmetic: codes and queries enter the matrix instructions exactly (bf16),
  * logits, sums and outputs are held in fp32; the weights are rounded to f16 (relative 2^-11, down to 2^-25 of a

@@ -170,10 +170,19 @@ int omniattn_gqa_append(const omniattn_gqa_t* gqa, int32_t num_tokens, const voi
 size_t omniattn_gqa_workspace_bytes(const omniattn_gqa_t* gqa) {
   int cus = 0;
   if (check_gqa(gqa) != OMNIATTN_OK || device_cus(&cus) != OMNIATTN_OK) return 0;
-  // (enough for any kept set and table width: those with few pages have the most shares)
-  omniattn_gqa_t short_ones = *gqa;
-  short_ones.sink = short_ones.window = 0;
-  return std::max(workspace_of(gqa, shape_of(gqa, cus)).bytes, workspace_of(gqa, shape_of(&short_ones, cus)).bytes);
+  // Enough for fewer queries too, and for any kept set and table width: the calls of a server share one.  (The number of queries decides
+  // by its rows to a request and KV head, up to 16, up to 32 or more; those that keep few pages have the most shares.)
+  size_t bytes = 0;
+  omniattn_gqa_t g = *gqa;
+  g.sink = g.window = 0;
+  const int64_t group = gqa->num_q_heads / gqa->num_kv_heads;
+  for (int rows : {16, 32, INT32_MAX}) {
+    g.num_queries = (int32_t)std::min<int64_t>(gqa->num_queries, std::max<int64_t>(rows / group, 1) * gqa->batch);
+    GqaShape shape = shape_of(&g, cus);
+    g.num_queries = gqa->num_queries;
+    bytes = std::max(bytes, workspace_of(&g, shape).bytes);
+  }
+  return bytes;
 }
 
 int omniattn_gqa_decode(const omniattn_gqa_t* gqa, const void* q, int64_t q_stride, const void* k_cache, const void* v_cache, const float* k_scales,

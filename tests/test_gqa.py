@@ -708,6 +708,29 @@ def test_workspace_is_checked():
 
 
 @gpu
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("batch,q_heads,kv_heads", [(1, 1, 1), (200, 12, 12), (64, 32, 4), (300, 40, 2), (2048, 1, 1)])
+def test_a_workspace_is_enough_for_fewer_queries(batch, q_heads, kv_heads, dim):
+    sizes = [oa.omniattn_gqa_workspace_bytes(batch, n, q_heads, kv_heads, dim) for n in (1, batch, 3 * batch, 10 * batch, 17 * batch, 40 * batch, 100 * batch)]
+    assert sizes == sorted(sizes)
+
+
+@gpu
+def test_a_server_keeps_one_workspace():
+    """Prompts and single tokens in turn, with the workspace of the most tokens."""
+    batch, heads, dim = 200, 12, 64
+    ws = torch.full((oa.omniattn_gqa_workspace_bytes(batch, 10 * batch, heads, heads, dim),), 0xff, dtype=torch.uint8, device="cuda")
+    for news in ([1] * batch, [10] * batch, [30] * 60 + [1] * 140):
+        p = Problem([n + 20 for n in news], news, heads, heads, dim, 64, 4, 30, seed=len(news) + news[0], extra_pages=0)
+        want, want_lse = p.run(torch.bfloat16)
+        k, v = p.codes.cuda()
+        ks, vs = p.scales.cuda()
+        out, lse = torch.empty_like(want), torch.empty_like(want_lse)
+        oa.omniattn_gqa_decode(p.q.cuda(), k, v, ks, vs, ints(p.table), ints(p.lens), ints(p.q_start), out, lse, ws, sink=4, window=30, softmax_scale=p.scale)
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+@gpu
 def test_the_binding_refuses_wrong_tensors():
     p = Problem([200], [1], 4, 2, 128, 64, 0, 1000, seed=1)
     k, v = p.codes.cuda()
