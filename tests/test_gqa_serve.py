@@ -1,0 +1,60 @@
+"""The three calls of a grouped-query step together, as a server makes them: requests come, grow, finish and give their pages back."""
+import numpy as np
+import pytest
+import torch
+
+import gqa_reference as ref
+from paper_2511_22481_amd.gqa_serve import PAGE, Pool, serve
+
+gpu = pytest.mark.gpu
+PROMPTS, ANSWERS = [300, 1, 40, 129, 256], [7, 9, 0, 3, 5]
+Q_HEADS, HEADS, DIM, LAYERS, SINK, WINDOW = 6, 2, 64, 2, 4, 200
+
+
+def _rows(step, buffer):
+    """The same rows for the same step, whichever way it is called."""
+    g = torch.Generator().manual_seed(step)
+    full = torch.randn((LAYERS, 500, Q_HEADS + 2 * HEADS, DIM), generator=g).bfloat16()
+    buffer.copy_(full[:, :buffer.shape[1]])
+
+
+def _run(graph):
+    pool = Pool(len(PROMPTS), LAYERS, 12, HEADS, DIM, 5)
+    seen = []
+
+    def observe(step, news, out, lse):
+        n = sum(news)
+        seen.append((news, out[:, :n].clone(), lse[:, :n].clone(), pool.lens.tolist(), pool.table.tolist(), pool.q_start.tolist(),
+                     [t.cpu() for t in (pool.k, pool.v, pool.k_scales, pool.v_scales)]))
+    return serve(pool, PROMPTS, ANSWERS, Q_HEADS, SINK, WINDOW, _rows, chunk=128, graph=graph, observe=observe), seen
+
+
+@gpu
+def test_steps_follow_the_reference_and_pages_come_back():
+    what, seen = _run(graph=False)
+    assert what["tokens"] == sum(PROMPTS) + sum(ANSWERS) and what["free_at_the_end"] == 12 and what["pages"] <= 12
+    grown = [0] * len(PROMPTS)
+    for step, (news, out, lse, lens, table, q_start, (k, v, ks, vs)) in enumerate(seen):
+        grown = [g + n for g, n in zip(grown, news)]
+        assert all(length == g for length, g, n in zip(lens, grown, news) if n)  # (finished requests have given theirs up)
+        full = torch.empty((LAYERS, sum(news), Q_HEADS + 2 * HEADS, DIM), dtype=torch.bfloat16)
+        _rows(step, full)
+        for i in range(LAYERS):
+            cache = [ref.as_double(t[i]) for t in (k, v, ks, vs)]
+            want, want_lse, tol, lse_tol = ref.attend_bf16(ref.as_double(full[i, :, :Q_HEADS]), *cache, table, lens, q_start, SINK, WINDOW, DIM ** -0.5)
+            assert (np.abs(ref.as_double(out[i]) - want) <= tol).all(), (step, i)
+            assert (np.abs(ref.as_double(lse[i]) - want_lse) <= lse_tol).all(), (step, i)
+
+
+@gpu
+def test_replayed_steps_are_the_called_ones():
+    called, replayed = _run(graph=False)[1], _run(graph=True)[1]
+    assert len(called) == len(replayed)
+    for step, (a, b) in enumerate(zip(called, replayed)):
+        assert a[0] == b[0] and a[3:6] == b[3:6], step
+        assert torch.equal(a[1], b[1]) and torch.equal(a[2], b[2]), step
+
+
+def test_a_pool_has_room_for_every_scale():
+    pool = Pool(3, 2, 4, 1, 64, 2, scale_tokens=32, device="cpu")
+    assert pool.k.shape == (2, 4, 1, PAGE, 64) and pool.k_scales.shape == (2, 4, 1, 4) and pool.free.tolist() == [0, 1, 2, 3]
