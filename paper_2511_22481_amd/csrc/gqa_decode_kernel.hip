@@ -4,18 +4,29 @@
 // keeps (j < S, or among the last W of them): out = sum_j p_j v_j / sum_j p_j, p_j = exp(scale q.k_j), lse = ln sum p_j.
 //
 // Work.  The query rows (t, head of the group) of one (request, KV head) are cut into blocks of 16, 32 or 64; a block
-// reads the pages that hold kept tokens.  A block counts as many units as it has pages, and kStart.  All units of the call, in
-// order of request, KV head and block, are dealt out evenly: work group u of U takes units [u T / U, (u + 1) T / U).  Every work group finds its share by
-// itself from the lengths on the device, so the host needs to know nothing but the sizes of the arrays.  A block whose
-// pages went to several groups leaves one partial row each, which gqa_combine_kernel joins.
+// reads the pages that hold kept tokens.  A block counts as many units as it has pages, and two for its start (its query, the
+// meeting of the waves, its results).  All units of the call, in order of request, KV head and block, are dealt out evenly: work
+// group u of U takes units [u T / U, (u + 1) T / U).  Every work group finds its share by itself from the lengths on the device, so
+// the host needs to know nothing but the sizes of the arrays.  A block whose pages went to several groups leaves one partial row
+// each, which gqa_combine_kernel joins.
 //
 // A page.  The four waves take 32 of its 128 tokens each and keep a running maximum, sum and output of their own; they meet
 // only at the end of a block's share.  K rows come from memory in the operand order of S^T = K Q^T (16x16x32 bf16 matrix
 // instructions; an e4m3 code is exact in bf16), V rows as 8 tokens x D/16 columns per lane, which a byte permutation turns
 // into the operand of O^T += V^T P^T (f16: exact for the codes, and 2^-11 relative for the weights, which the reference
 // scales into [0, 2^15]).  The contraction's order of tokens is free, so P^T is what S^T's layout already gives each lane.
-// No LDS and no barrier in the loop.  A block's scale is one number per wave and page: K's goes into the softmax factor,
-// V's multiplies the page's product when it is added.
+// No LDS and no barrier in the loop (width 256: the query's operands come from LDS).  A block's scale is one number per wave and
+// page: K's goes into the softmax factor, V's into the weights.
+//
+// Many short blocks of width 64: every wave has a share of its own and takes the four tiles of a page in turn, so that the waves
+// need not meet.
+//
+// What bounds it: up to 32 rows (64 at width 64), memory.  A work group has one tile of each wave under way (16 to 64 KB a compute
+// unit), asked for as soon as the registers of the tile before are free; the loads are without conditions and every wait is for as
+// many as are needed, no more.  64 requests of 32768 tokens, 8 KV heads of width 128 (4.30 GB): 739 us, 5.8 TB/s, where nothing but
+// reading them in this order reaches 6.25.  One request of 131072 (268 MB): 52 us, of which 6 pass before the first product (a chain
+// of four loads: lengths, table, codes, query) and 3 at the end.  93 ragged requests of 200 to 20000, 4 KV heads: 78 us, 5 TB/s.
+// 64 requests of 2000 to 16000, 4 KV heads of width 128, 32 rows: 103 us, 4.6 TB/s; above, gqa_wide_kernel.hip is faster.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -436,8 +447,11 @@ hipError_t allow_lds() {
 
 // By the average number of query rows of a request and KV head.  us a call, 64 requests of 2000 to 16000 tokens, 4 KV heads; "tiles": this
 // kernel with so many row tiles (several blocks where the rows are more):
-//   width  rows   1 tile   2 tiles   4 tiles   wide, 32 rows   wide, 64 rows
-//   TODO
+//   width 64   rows 16  24  32  40  64 128    width 128  rows 16  24  32  40  64 128    width 256  rows 16  24  32  40  64 128
+//   1 tile          55  86  79 104 141 296    1 tile          93 148 157 219 275 556    1 tile         181 281 287 409 523 977
+//   2 tiles         53  60  57  82  88 171    2 tiles         95 101 108 156 159 301    wide           179 180 182 217 247 423
+//   4 tiles         67  79  70  69  75 142    wide           102 107 115 136 139 265
+// (Up to 16 rows of width 256 the two are alike at these lengths; short requests end and begin faster with this kernel.)
 // Waves that work alone: a block costs them 3 us less, as they need not meet, but they leave more partial rows, and what is left uneven
 // weighs four times as much.  256 requests, 12 KV heads of width 64, us with them and without: 128 tokens each 19.6 / 26.3, 1 to 2000
 // (window 1024) 34 / 40.5, 1024 each 87 / 83, 2048 each 156 / 153; 128 requests of 500 to 8000 tokens, 8 KV heads 85 / 83.5.  At width 128

@@ -1,11 +1,17 @@
-// Attention of grouped-query layers over the paged 8-bit cache for requests with more than 16 query rows (several new tokens, or many
-// query heads to a KV head).  The same work as gqa_decode_kernel.hip, dealt out the same way; what differs is how a tile is shared.
+// Attention of grouped-query layers over the paged 8-bit cache for requests with many query rows: more than 32 at width 128, more than 16
+// at width 256 (several new tokens, or many query heads to a KV head).  The same work as gqa_decode_kernel.hip, dealt out the same way;
+// what differs is how a tile is shared.
 //
 // One work group of eight waves per compute unit.  A tile (32 TG tokens) is brought to LDS once by direct loads and read by RG = 8 / TG
-// waves for each 32 of its tokens, each with other query rows, so a block has RG * 16 * RT rows: the codes come from memory once for
+// waves for each 32 of its tokens, each with other query rows, so a block has RG * 16 * RT = 64 rows: the codes come from memory once for
 // all of them.  The tiles pass through a ring of stages, kStages - 1 of them requested ahead, over the ends of blocks too; one barrier per
-// tile.  (With the tile in registers, as in the other kernel, two waves per SIMD leave room for one tile ahead, and the products of
-// 32 rows take as long as that tile needs to arrive: 4.4 TB/s at 32 rows of width 128, 2.0 at 64.)
+// tile.
+//
+// What bounds it: the vector unit.  A tile of 32 tokens and 16 rows of width 256 costs a wave 192 conversions and permutations of
+// codes and 130 instructions of softmax beside 32 to 48 matrix instructions, and the two waves of a SIMD take 4600 cycles for it where
+// the codes would arrive in 2600.  64 requests of 2000 to 16000 tokens, 4 KV heads: width 128 139 us at 64 rows and 136 at 40 (3.3
+// TB/s, 420 TFLOP/s at 64), width 256 182 at 32 rows, 217 at 40, 247 at 64.  (More row tiles to a wave would share the conversions, but
+// at width 256 two leave no registers, and at width 128 four leave one wave to a SIMD.)
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
