@@ -401,19 +401,19 @@ def _want(ok, what):
         raise OmniAttnError(-1, what)
 
 
-# (The checks below cost as much as a short kernel takes, so each is one test that fails as a whole, and builds its message only then.)
+# (The checks below cost as much as a short kernel takes: each is one test that fails as a whole and builds its message only then, and
+# torch is looked up once a call.)
 
-def _ints(t, n, name):
-    """Address of a contiguous int32 CUDA tensor of n elements."""
-    import torch
-    if t.dtype is not torch.int32 or t.numel() != n or not t.is_cuda or not t.is_contiguous():
-        raise OmniAttnError(-1, f"{name}: int32 CUDA tensor of {n} elements wanted")
-    return t.data_ptr()
+def _ints(torch, tensors):
+    """Checks (tensor, elements, name)s: contiguous int32 CUDA tensors wanted."""
+    int32 = torch.int32
+    for t, n, name in tensors:
+        if t.dtype is not int32 or t.numel() != n or not t.is_cuda or not t.is_contiguous():
+            raise OmniAttnError(-1, f"{name}: int32 CUDA tensor of {n} elements wanted")
 
 
-def _table_of(page_table, batch):
+def _table_of(torch, page_table, batch):
     """(columns, row stride) of a page table."""
-    import torch
     if page_table.dtype is torch.int32 and page_table.is_cuda and page_table.dim() == 2:
         rows, columns = page_table.shape
         stride, step = page_table.stride()
@@ -422,41 +422,44 @@ def _table_of(page_table, batch):
     raise OmniAttnError(-1, "page_table: int32 CUDA tensor [batch, pages] wanted, its rows contiguous")
 
 
-def _handle(stream):
+def _handle(torch, stream):
     """Of the given stream, or of torch's current one, for calls whose tensors are CUDA tensors already (torch's CUDA part is running)."""
     if stream is not None:
         return stream.cuda_stream
-    from torch import _C
-    return _C._cuda_getCurrentRawStream(_C._cuda_getDevice())
+    c = torch._C
+    return c._cuda_getCurrentRawStream(c._cuda_getDevice())
 
 
 def omniattn_table_extend(seq_lens, new_lens, free_pages, free_count, page_table, seq_lens_out, free_count_out, q_start, slot_map, stream=None):
     """Tables of one step on the GPU: every request grows by its new tokens and takes pages from the stack of free ones (all int32
     CUDA tensors; page_table, seq_lens_out, free_count_out, q_start [batch + 1] and slot_map are written).  seq_lens_out may be
     seq_lens, free_count_out may be free_count.  A request that does not fit keeps its length and gets slots -1."""
+    import torch
     batch, tokens, pages = seq_lens.numel(), slot_map.numel(), free_pages.numel()
-    columns, stride = _table_of(page_table, batch)
+    columns, stride = _table_of(torch, page_table, batch)
+    _ints(torch, ((seq_lens, batch, "seq_lens"), (new_lens, batch, "new_lens"), (free_pages, pages, "free_pages"), (free_count, 1, "free_count"),
+                  (seq_lens_out, batch, "seq_lens_out"), (free_count_out, 1, "free_count_out"), (q_start, batch + 1, "q_start"),
+                  (slot_map, tokens, "slot_map")))
     _check(load_library().omniattn_table_extend(
-        _table_record(batch, columns, stride, tokens, pages), _ints(seq_lens, batch, "seq_lens"), _ints(new_lens, batch, "new_lens"),
-        _ints(free_pages, pages, "free_pages"),
-        _ints(free_count, 1, "free_count"), page_table.data_ptr(), _ints(seq_lens_out, batch, "seq_lens_out"),
-        _ints(free_count_out, 1, "free_count_out"), _ints(q_start, batch + 1, "q_start"), _ints(slot_map, tokens, "slot_map"),
-        _handle(stream)))
+        _table_record(batch, columns, stride, tokens, pages), seq_lens.data_ptr(), new_lens.data_ptr(), free_pages.data_ptr(),
+        free_count.data_ptr(), page_table.data_ptr(), seq_lens_out.data_ptr(), free_count_out.data_ptr(), q_start.data_ptr(),
+        slot_map.data_ptr(), _handle(torch, stream)))
 
 
 def omniattn_table_release(seq_lens, done, page_table, free_pages, free_count, stream=None):
     """Pages of the requests with done[b] != 0 go back on the stack, their lengths become 0 (seq_lens, free_pages and free_count
     change in place)."""
-    batch, pages = seq_lens.numel(), free_pages.numel()
-    columns, stride = _table_of(page_table, batch)
-    _check(load_library().omniattn_table_release(
-        _table_record(batch, columns, stride, 0, pages), _ints(done, batch, "done"), _ints(seq_lens, batch, "seq_lens"), page_table.data_ptr(),
-        _ints(free_pages, pages, "free_pages"), _ints(free_count, 1, "free_count"), _handle(stream)))
-
-
-def _cache_shape(k_cache, v_cache, k_scales, v_scales):
-    """(pages, KV heads, page size, head width, tokens to a scale) of a layer's cache."""
     import torch
+    batch, pages = seq_lens.numel(), free_pages.numel()
+    columns, stride = _table_of(torch, page_table, batch)
+    _ints(torch, ((done, batch, "done"), (seq_lens, batch, "seq_lens"), (free_pages, pages, "free_pages"), (free_count, 1, "free_count")))
+    _check(load_library().omniattn_table_release(
+        _table_record(batch, columns, stride, 0, pages), done.data_ptr(), seq_lens.data_ptr(), page_table.data_ptr(), free_pages.data_ptr(),
+        free_count.data_ptr(), _handle(torch, stream)))
+
+
+def _cache_shape(torch, k_cache, v_cache, k_scales, v_scales):
+    """(pages, KV heads, page size, head width, tokens to a scale) of a layer's cache."""
     codes, numbers = torch.float8_e4m3fn, torch.float32
     shape, scales = k_cache.shape, k_scales.shape
     if (k_cache.dtype is not codes or v_cache.dtype is not codes or k_scales.dtype is not numbers or v_scales.dtype is not numbers
@@ -473,9 +476,8 @@ def _cache_shape(k_cache, v_cache, k_scales, v_scales):
     return pages, heads, page, dim, page // per_page
 
 
-def _rows_of(t, heads, dim, name):
+def _rows_of(torch, t, heads, dim, name):
     """(tokens, address, token stride) of bf16 rows [tokens, heads, dim]."""
-    import torch
     if t.dtype is torch.bfloat16 and t.is_cuda and t.dim() == 3:
         n, h, d = t.shape
         stride, head, step = t.stride()
@@ -487,15 +489,17 @@ def _rows_of(t, heads, dim, name):
 def omniattn_gqa_append(k_new, v_new, slot_map, k_cache, v_cache, k_scales, v_scales, stream=None):
     """New K and V rows (bf16 [tokens, KV heads, head width], any token stride) to their slots in a layer's cache, rounded to e4m3
     with a scale for each block of tokens and head.  k_cache, v_cache, k_scales and v_scales are written."""
-    pages, heads, page, dim, tokens = _cache_shape(k_cache, v_cache, k_scales, v_scales)
-    n, k, k_stride = _rows_of(k_new, heads, dim, "k_new")
-    n_v, v, v_stride = _rows_of(v_new, heads, dim, "v_new")
+    import torch
+    pages, heads, page, dim, tokens = _cache_shape(torch, k_cache, v_cache, k_scales, v_scales)
+    n, k, k_stride = _rows_of(torch, k_new, heads, dim, "k_new")
+    n_v, v, v_stride = _rows_of(torch, v_new, heads, dim, "v_new")
     if n_v != n:
         raise OmniAttnError(-1, "k_new and v_new: as many tokens wanted")
+    _ints(torch, ((slot_map, n, "slot_map"),))
     rec = _gqa_record(1, 0, heads, heads, dim, page, tokens, 1, 1, pages, 0, 0, 1.0, BF16)
     _check(load_library().omniattn_gqa_append(
-        rec, n, k, k_stride, v, v_stride, _ints(slot_map, n, "slot_map"), k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(),
-        v_scales.data_ptr(), _handle(stream)))
+        rec, n, k, k_stride, v, v_stride, slot_map.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(),
+        v_scales.data_ptr(), _handle(torch, stream)))
 
 
 def omniattn_gqa_workspace_bytes(batch, num_queries, num_q_heads, num_kv_heads, head_dim):
@@ -512,11 +516,12 @@ def omniattn_gqa_decode(q, k_cache, v_cache, k_scales, v_scales, page_table, seq
     [batch + 1]): request b's queries are tokens q_start[b] .. q_start[b + 1], the last ones of its seq_lens[b]; None: one each.
     out (bf16 or fp32, shaped like q) and lse (fp32 [tokens, query heads]) are written."""
     import torch
-    pages, heads, page, dim, tokens = _cache_shape(k_cache, v_cache, k_scales, v_scales)
+    pages, heads, page, dim, tokens = _cache_shape(torch, k_cache, v_cache, k_scales, v_scales)
     shape = q.shape
     batch, q_heads = seq_lens.numel(), shape[1] if len(shape) == 3 else 0
-    n, src, q_stride = _rows_of(q, q_heads, dim, "q")
-    columns, stride = _table_of(page_table, batch)
+    n, src, q_stride = _rows_of(torch, q, q_heads, dim, "q")
+    columns, stride = _table_of(torch, page_table, batch)
+    _ints(torch, ((seq_lens, batch, "seq_lens"),) if q_start is None else ((seq_lens, batch, "seq_lens"), (q_start, batch + 1, "q_start")))
     fp32 = out.dtype is torch.float32
     if not (fp32 or out.dtype is torch.bfloat16) or out.shape != shape or not out.is_contiguous() or not out.is_cuda:
         raise OmniAttnError(-1, "out: contiguous bf16 or fp32 CUDA tensor shaped like q wanted")
@@ -526,8 +531,8 @@ def omniattn_gqa_decode(q, k_cache, v_cache, k_scales, v_scales, page_table, seq
                       float(softmax_scale), FP32 if fp32 else BF16)
     _check(load_library().omniattn_gqa_decode(
         rec, src, q_stride, k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), page_table.data_ptr(),
-        _ints(seq_lens, batch, "seq_lens"), _ints(q_start, batch + 1, "q_start") if q_start is not None else None, out.data_ptr(), lse.data_ptr(),
-        _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0, _handle(stream)))
+        seq_lens.data_ptr(), _ptr(q_start), out.data_ptr(), lse.data_ptr(), _ptr(workspace),
+        workspace.numel() * workspace.element_size() if workspace is not None else 0, _handle(torch, stream)))
 
 
 def gqa_decode(q, k_cache, v_cache, k_scales, v_scales, page_table, seq_lens, sink, window, softmax_scale, q_start=None, out_dtype=None):
