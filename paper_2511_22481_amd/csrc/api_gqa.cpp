@@ -231,6 +231,7 @@ int omniattn_gqa_decode(const omniattn_gqa_t* gqa, const void* q, int64_t q_stri
   p.W = std::min(gqa->window, (int)kMaxPages * kPage / 2);
   p.scale_shift = gqa->scale_tokens == 32 ? 5 : gqa->scale_tokens == 64 ? 6 : 7;
   p.out_fp32 = gqa->out_dtype == OMNIATTN_FP32;
+  p.uncut = shape.uncut;
   p.scale_log2 = gqa->softmax_scale * 1.4426950408889634f;
   // Not more shares than there can be units of work (each block counts up to 2 beside its pages).
   const int64_t blocks = ((int64_t)p.num_queries * p.group + shape.block_rows - 1) / shape.block_rows + p.batch;

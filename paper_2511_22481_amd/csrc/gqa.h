@@ -68,6 +68,7 @@ struct GqaDecodeParams {
   int batch, num_queries, q_heads, kv_heads, group, head_dim;
   int max_pages, S, W, scale_shift;  // scale_shift: log2 of the tokens that share a scale
   int out_fp32;
+  int uncut;                // blocks go whole to the share that has their first unit: no partial rows
   float scale_log2;         // softmax_scale * log2(e)
 };
 // How a call is computed: by which kernel (gqa_decode_kernel.hip or gqa_wide_kernel.hip), tiles of 16 query rows per wave, rows of a
@@ -75,6 +76,7 @@ struct GqaDecodeParams {
 struct GqaShape {
   bool wide;
   int row_tiles, block_rows, groups, shares;
+  bool uncut;               // see GqaDecodeParams
 };
 // pages: those that a query's kept tokens can lie in.
 GqaShape gqa_shape(int batch, int num_queries, int group, int kv_heads, int head_dim, int64_t pages, int cus);

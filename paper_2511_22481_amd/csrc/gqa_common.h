@@ -208,7 +208,7 @@ struct Dealer {
   __device__ __forceinline__ void cut(Piece& w) const {
     w.bk = block_of<R>(p, w.rq, w.rb);
     w.tile_lo = max(w.off - START, 0);
-    w.tile_hi = (int)min(max(w.left + w.off - START, (int64_t)0), (int64_t)w.bk.pages.count());
+    w.tile_hi = p.uncut ? w.bk.pages.count() : (int)min(max(w.left + w.off - START, (int64_t)0), (int64_t)w.bk.pages.count());
   }
   // Whether there is something to do: pages, or the empty result of a block that keeps nothing, which is whose share has its first unit.
   __device__ __forceinline__ static bool counts(const Piece& w) { return w.tile_lo < w.tile_hi || (w.bk.pages.count() == 0 && w.off == 0); }
@@ -306,7 +306,7 @@ struct Dealer {
     }
     now.off = (int)off;
     cut(now);
-    return counts(now) || follow(now);
+    return (counts(now) && !(p.uncut && now.off > 0)) || follow(now);
   }
   __device__ __forceinline__ int rows_of(const Piece& w) const { return (int)min((int64_t)w.rq.n * p.group - (int64_t)w.rb * R, (int64_t)R); }
   // Shares that have a part of the block of w, from this one on (which has its first page).

@@ -432,7 +432,7 @@ hipError_t start(const GqaDecodeParams& p, const GqaShape& shape, int shares, hi
     if (shape.row_tiles == 2) e = narrow<D, 2, OUT32>(p, shares, stream);
     else if constexpr (D == 64) e = narrow<D, 4, OUT32>(p, shares, stream);
   }
-  return e != hipSuccess ? e : join<D, OUT32>(p, shape.block_rows, shares, stream);
+  return e != hipSuccess || p.uncut ? e : join<D, OUT32>(p, shape.block_rows, shares, stream);
 }
 
 template <int D, int RT>
@@ -456,17 +456,28 @@ hipError_t allow_lds() {
 // weighs four times as much.  256 requests, 12 KV heads of width 64, us with them and without: 128 tokens each 19.6 / 26.3, 1 to 2000
 // (window 1024) 34 / 40.5, 1024 each 87 / 83, 2048 each 156 / 153; 128 requests of 500 to 8000 tokens, 8 KV heads 85 / 83.5.  At width 128
 // they lose from 50 to 1000 tokens on (200 requests, 8 KV heads: 44 / 41.5), and so they are for many short blocks of width 64.
+// Blocks that cannot have more than a few pages go whole to a share: nothing has to be joined, which saves the second launch (2 to 3 us,
+// and 3 us of the host's time).  us cut / uncut, all requests of so many pages (4 query heads to a KV head but for width 64; "wide": 40 rows):
+//   requests x heads     1 page      2            3            4            6            8
+//   width 128   1 x 8     8.6/7.0   10.1/7.8     10.1/8.5     10.1/9.2     10.1/10.5    10.3/11.9
+//              16 x 8     9.6/7.7   12.7/10.6    14.0/11.8    14.1/13.3    14.6/16.6    15.7/19.7
+//             256 x 8    25.3/22.9  31.0/28.6    47.4/44.7    58.7/56.0    81.4/78.6   104.9/102.2
+//   width 64   16 x 12    9.6/7.9   12.3/10.4    12.6/9.6     14.6/14.1    15.1/17.0    15.1/19.4
+//   alone     256 x 12   15.3/13.3  19.1/17.0    20.6/19.7    22.2/24.7    23.2/28.7    26.4/34.9   (lengths up to so many pages)
+//   width 256   1 x 2    10.4/8.9   11.8/10.1    11.7/11.3    11.8/12.3    11.8/14.6    11.8/17.0
+//   wide        1 x 2    15.9/14.4  16.8/17.8    16.9/21.3    16.9/24.6    16.8/31.4    17.0/38.3
+//              64 x 2    18.8/16.6  22.7/20.3    26.1/23.7    29.2/27.0    32.8/33.7    36.6/41.0
 GqaShape gqa_shape(int batch, int num_queries, int group, int kv_heads, int head_dim, int64_t pages, int cus) {
   const int64_t rows = (int64_t)((num_queries + batch - 1) / batch) * group;
   if (rows <= 16) {
     const int groups = cus * groups_per_cu(head_dim, 1);
     const bool alone = head_dim == 64 && (int64_t)batch * kv_heads >= 2 * groups && pages <= 16;
-    return GqaShape{false, 1, 16, groups, alone ? 4 : 1};
+    return GqaShape{false, 1, 16, groups, alone ? 4 : 1, pages <= (alone || head_dim == 256 ? 3 : 4)};
   }
-  if (head_dim == 256) return GqaShape{true, 1, 64, cus, 1};
-  if (rows <= 32) return GqaShape{false, 2, 32, cus * groups_per_cu(head_dim, 2), 1};
-  if (head_dim == 64) return GqaShape{false, 4, 64, cus * groups_per_cu(head_dim, 4), 1};
-  return GqaShape{true, 2, 64, cus, 1};
+  if (head_dim == 256) return GqaShape{true, 1, 64, cus, 1, pages <= 2};
+  if (rows <= 32) return GqaShape{false, 2, 32, cus * groups_per_cu(head_dim, 2), 1, pages <= 4};
+  if (head_dim == 64) return GqaShape{false, 4, 64, cus * groups_per_cu(head_dim, 4), 1, pages <= 4};
+  return GqaShape{true, 2, 64, cus, 1, pages <= 2};
 }
 
 hipError_t init_gqa_kernels() {

@@ -394,6 +394,23 @@ def test_many_short_requests_of_narrow_heads(group, most, sink, window, out_dtyp
 
 
 @gpu
+@pytest.mark.parametrize("dim,q_heads,kv_heads,most", [(64, 3, 3, 1), (64, 8, 8, 1), (128, 8, 2, 1), (128, 4, 1, 8), (128, 8, 1, 12), (256, 2, 1, 1), (256, 8, 1, 5)])
+@pytest.mark.parametrize("columns,sink,window", [(1, 0, 10 ** 6), (2, 0, 10 ** 6), (4, 0, 10 ** 6), (12, 4, 128), (12, 0, 200)])
+def test_blocks_of_few_pages_are_not_cut(dim, q_heads, kv_heads, most, columns, sink, window):
+    """Narrow tables and small windows: from one request to many more blocks than work groups, empty ones among them."""
+    rng = random.Random(columns + dim)
+    for batch in (1, 7, 300):
+        lens = [min(rng.choice([0, 1, 127, 128, 129, 400, 1500]), columns * PAGE) for _ in range(batch)]
+        news = [min(n, rng.randint(0, most) if most > 1 else 1) for n in lens]
+        news[0] = min(lens[0], most)
+        if sum(news) == 0:
+            lens[0], news[0] = 100, most
+        p = Problem(lens, news, q_heads, kv_heads, dim, 64, sink, window, seed=batch, poison=batch < 100, extra_pages=1)
+        p.table = [row[:columns] + [0] * (columns - len(row)) for row in p.table]
+        p.check(torch.float32 if columns == 2 else torch.bfloat16)
+
+
+@gpu
 def test_nan_among_many_short_requests():
     lens, news = [150] * 256, [3] * 256
     clean = Problem(lens, news, 8, 8, 64, 64, 1, 30, seed=9, poison=False)
