@@ -68,6 +68,7 @@ struct GqaDecodeParams {
   int batch, num_queries, q_heads, kv_heads, group, head_dim;
   int max_pages, S, W, scale_shift;  // scale_shift: log2 of the tokens that share a scale
   int out_fp32;
+  int few_units;            // a call's units of work (pages and blocks) are counted in 32 bits
   int uncut;                // blocks go whole to the share that has their first unit: no partial rows
   float scale_log2;         // softmax_scale * log2(e)
 };

@@ -44,14 +44,15 @@ struct Block {
 template <int ROWS>
 __device__ __forceinline__ Block block_of(const GqaDecodeParams& p, const Request& r, int rb) {
   Block k;
-  k.t0 = rb * ROWS / p.group;
-  k.t1 = min(r.n - 1, ((rb + 1) * ROWS - 1) / p.group);
+  // (rows of a call are counted in 32 bits; most requests have one block, and divisions are what a share's finding consists of)
+  k.t0 = rb ? (int)((uint32_t)(rb * ROWS) / (uint32_t)p.group) : 0;
+  k.t1 = (rb + 1) * ROWS >= r.n * p.group ? r.n - 1 : (int)((uint32_t)((rb + 1) * ROWS - 1) / (uint32_t)p.group);
   k.pages = tile_layout(r.L - r.n + k.t1 + 1, p.S, p.W > 0 ? p.W + (k.t1 - k.t0) : 0, kPage);
   return k;
 }
 template <int ROWS>
 __device__ __forceinline__ int blocks_of(const GqaDecodeParams& p, const Request& r) {
-  return (int)(((int64_t)r.n * p.group + ROWS - 1) / ROWS);
+  return (r.n * p.group + ROWS - 1) / ROWS;
 }
 __device__ __forceinline__ float row_max(float x) {  // over the four lanes that hold tokens of the same row
   float y = x;
@@ -128,12 +129,18 @@ __device__ __forceinline__ const GqaDecodeParams* late_arguments() {
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// Share u of U: units [bound(u), bound(u + 1)), bound(u) = floor(u T / U).
+// Share u of U: units [bound(u), bound(u + 1)), about u T / U.  Every share has T / U or one more; those with more are spread evenly (the
+// neighbours in a compute unit would have a fifth more to read than others: 256 requests of 12 heads 33 us, in one run 40).
 struct Shares {
   int64_t T, each;  // each = T / U
-  int U, rest;      // rest = T % U
-  // (U is at most 2^14: the product stays in 32 bits)
-  __device__ __forceinline__ int64_t bound(int u) const { return u * each + (uint32_t)u * (uint32_t)rest / (uint32_t)U; }
+  int U;            // at most 2^14
+  uint32_t more;    // (T % U) 2^17 / U, rounded up
+  __device__ __forceinline__ Shares(int64_t total, int most) : T(total), U((int)min((int64_t)most, total)) {
+    each = T >> 31 ? T / max(U, 1) : (uint32_t)T / (uint32_t)max(U, 1);
+    more = ((uint32_t)(T - each * U) << 17) / (uint32_t)max(U, 1) + 1;
+  }
+  __device__ __forceinline__ Shares() {}
+  __device__ __forceinline__ int64_t bound(int u) const { return u * each + ((uint32_t)u * more >> 17); }
   // the share that has unit x
   __device__ __forceinline__ int owner(int64_t x) const {
     int u = min((int)((float)x * U / (float)T), U - 1);
@@ -142,6 +149,19 @@ struct Shares {
     return u;
   }
 };
+
+// Running sum over a wave.
+__device__ __forceinline__ int wave_sum_up_to(int x) {
+#define OMNIATTN_ADD(ctrl, rows) x += __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xf, true)
+  OMNIATTN_ADD(0x111, 0xf);  // from the lane one, two, four, eight before, in rows of 16
+  OMNIATTN_ADD(0x112, 0xf);
+  OMNIATTN_ADD(0x114, 0xf);
+  OMNIATTN_ADD(0x118, 0xf);
+  OMNIATTN_ADD(0x142, 0xa);  // a row's last lane to the row behind it
+  OMNIATTN_ADD(0x143, 0xc);  // lane 31 to the upper half
+#undef OMNIATTN_ADD
+  return x;
+}
 
 // The part of a block that belongs to a share.
 struct Piece {
@@ -246,23 +266,23 @@ struct Dealer {
       }
     }
     int64_t sum = mine;
-    for (int d = 1; d < 64; d *= 2) {
-      const int64_t y = __shfl_up(sum, d);
-      if (lane >= d) sum += y;
+    if (p.few_units) {
+      sum = wave_sum_up_to((int)mine);
+    } else {
+      for (int d = 1; d < 64; d *= 2) {
+        const int64_t y = __shfl_up(sum, d);
+        if (lane >= d) sum += y;
+      }
     }
     if (lane == 63) lds.wave_tot[wave] = sum;
     __syncthreads();
-    Shares shares;
-    shares.T = 0;
+    int64_t total = 0;
     for (int w = 0; w < THREADS / 64; ++w) {
-      if (w == wave) sum += shares.T;
-      shares.T += (int64_t)uniform64(lds.wave_tot[w]);
+      if (w == wave) sum += total;
+      total += (int64_t)uniform64(lds.wave_tot[w]);
     }
-    shares.U = (int)min((int64_t)gridDim.x * SHARES, shares.T);
+    const Shares shares(total, gridDim.x * SHARES);
     if ((int)blockIdx.x * SHARES >= shares.U) return false;
-    if (shares.T >> 31) shares.each = shares.T / shares.U;
-    else shares.each = (uint32_t)shares.T / (uint32_t)shares.U;
-    shares.rest = (int)(shares.T - shares.each * shares.U);
     int64_t first = shares.bound(blockIdx.x * SHARES);
 #pragma unroll
     for (int i = 0; i < SHARES; ++i) {
@@ -308,7 +328,7 @@ struct Dealer {
     cut(now);
     return (counts(now) && !(p.uncut && now.off > 0)) || follow(now);
   }
-  __device__ __forceinline__ int rows_of(const Piece& w) const { return (int)min((int64_t)w.rq.n * p.group - (int64_t)w.rb * R, (int64_t)R); }
+  __device__ __forceinline__ int rows_of(const Piece& w) const { return min(w.rq.n * p.group - w.rb * R, R); }
   // Shares that have a part of the block of w, from this one on (which has its first page).
   __device__ __forceinline__ int partners(const Piece& w) const {
     const Shares shares = lds.shares;
