@@ -236,7 +236,7 @@ int omniattn_gqa_decode(const omniattn_gqa_t* gqa, const void* q, int64_t q_stri
   // Not more shares than there can be units of work (each block counts up to 2 beside its pages).
   const int64_t blocks = ((int64_t)p.num_queries * p.group + shape.block_rows - 1) / shape.block_rows + p.batch;
   const int64_t pages = std::min<int64_t>(p.max_pages, ((int64_t)p.S + kPage - 1) / kPage + ((int64_t)p.W + shape.block_rows + kPage - 1) / kPage + 1);
-  const int64_t units = blocks * p.kv_heads * (pages + 2);
+  const int64_t units = blocks * p.kv_heads * (shape.shares > 1 ? 4 * pages + 4 : pages + 2);
   p.few_units = units <= INT32_MAX;
   const int groups = (int)std::min<int64_t>(shape.groups, (units + shape.shares - 1) / shape.shares);
   OA_HIP(launch_gqa_decode(p, shape, groups * shape.shares, (hipStream_t)hip_stream));

@@ -36,18 +36,18 @@ __device__ __forceinline__ Request request_of(const GqaDecodeParams& p, int b) {
   r.n = min(max(hi, r.begin), p.num_queries) - r.begin;
   return r;
 }
-// Pages of a block of query rows: the union of its queries' kept sets.
+// Pages of a block of query rows (GRAIN 32: their quarters): the union of its queries' kept sets.
 struct Block {
   int t0, t1;  // its query tokens, both included
   TileLayout pages;
 };
-template <int ROWS>
+template <int ROWS, int GRAIN>
 __device__ __forceinline__ Block block_of(const GqaDecodeParams& p, const Request& r, int rb) {
   Block k;
   // (rows of a call are counted in 32 bits; most requests have one block, and divisions are what a share's finding consists of)
   k.t0 = rb ? (int)((uint32_t)(rb * ROWS) / (uint32_t)p.group) : 0;
   k.t1 = (rb + 1) * ROWS >= r.n * p.group ? r.n - 1 : (int)((uint32_t)((rb + 1) * ROWS - 1) / (uint32_t)p.group);
-  k.pages = tile_layout(r.L - r.n + k.t1 + 1, p.S, p.W > 0 ? p.W + (k.t1 - k.t0) : 0, kPage);
+  k.pages = tile_layout(r.L - r.n + k.t1 + 1, p.S, p.W > 0 ? p.W + (k.t1 - k.t0) : 0, GRAIN);
   return k;
 }
 template <int ROWS>
@@ -189,9 +189,12 @@ struct Span {
 };
 
 // Finds shares and walks through their blocks.  R: rows of a block.  START: what a block costs beside its pages (its query, the
-// meeting of the waves, its results), in pages.  SHARES: of a work group, 1 or one for each wave.  All threads call begin.
+// meeting of the waves, its results), in pages.  SHARES: of a work group, 1 or one for each wave, which counts quarters of pages.  All
+// threads call begin.
 template <int R, int THREADS, int START, int SHARES = 1>
 struct Dealer {
+  static constexpr int kGrain = SHARES > 1 ? kWaveTokens : kPage;
+
   // What is needed only from block to block stays here: in scalar registers it would push the loop's own out.
   struct Lds {
     int64_t wave_tot[THREADS / 64], off[SHARES], stop[SHARES];  // the share's first unit among the units of request `at`; its end
@@ -213,7 +216,7 @@ struct Dealer {
   __device__ __forceinline__ int64_t cost_of(const Request& r) const {
     const int blocks = blocks_of<R>(p, r);
     int64_t sum = 0;
-    for (int rb = 0; rb < blocks; ++rb) sum += units(block_of<R>(p, r, rb));
+    for (int rb = 0; rb < blocks; ++rb) sum += units(block_of<R, kGrain>(p, r, rb));
     return sum;
   }
 
@@ -226,7 +229,7 @@ struct Dealer {
     return Request{uniform(r.L), uniform(r.begin), uniform(r.n)};
   }
   __device__ __forceinline__ void cut(Piece& w) const {
-    w.bk = block_of<R>(p, w.rq, w.rb);
+    w.bk = block_of<R, kGrain>(p, w.rq, w.rb);
     w.tile_lo = max(w.off - START, 0);
     w.tile_hi = p.uncut ? w.bk.pages.count() : (int)min(max(w.left + w.off - START, (int64_t)0), (int64_t)w.bk.pages.count());
   }
@@ -320,7 +323,7 @@ struct Dealer {
       off -= now.h * cost;
     }
     for (now.rb = 0;; ++now.rb) {
-      const int of_block = units(block_of<R>(p, now.rq, now.rb));
+      const int of_block = units(block_of<R, kGrain>(p, now.rq, now.rb));
       if (off < of_block) break;
       off -= of_block;
     }
@@ -610,7 +613,7 @@ __device__ __forceinline__ void finish(const GqaDecodeParams& p, const Dealer<R,
 // End of a block that one wave computes by itself, one row tile: every lane has D / 4 adjacent columns of its row, and writes them.
 template <int D, int THREADS, bool OUT32, int START, int SHARES>
 __device__ __forceinline__ void finish_alone(const Dealer<16, THREADS, START, SHARES>& dealer, const Piece& now, Rows<D, 1>& a, int slot) {
-  constexpr int kCols = D / 16;
+  constexpr int kCols = D / 16, kQuarters = kPage / kWaveTokens;
   const int lane = threadIdx.x & 63, row = lane & 15, g = lane >> 4, col = 4 * g * kCols;
   const float sum = row_sum(a.l[0]);
   if (row >= dealer.rows_of(now)) return;
@@ -622,11 +625,11 @@ __device__ __forceinline__ void finish_alone(const Dealer<16, THREADS, START, SH
 #pragma unroll 1
     for (int tile = now.tile_lo; tile < now.tile_hi; ++tile) {
       const int lp = now.bk.pages.logical(tile);
-      const size_t ph = (size_t)end.page_table[now.b * end.table_stride + lp] * end.kv_heads + now.h;
+      const size_t ph = (size_t)end.page_table[now.b * end.table_stride + lp / kQuarters] * end.kv_heads + now.h;
 #pragma unroll 1
-      for (int j = 0; j < kPage; ++j) {
-        if (!retained(lp * kPage + j, sees, end.S, end.W)) continue;
-        const uint32_t* codes = (const uint32_t*)(end.v_cache + (ph * kPage + j) * D + col);
+      for (int j = 0; j < kWaveTokens; ++j) {
+        if (!retained(lp * kWaveTokens + j, sees, end.S, end.W)) continue;
+        const uint32_t* codes = (const uint32_t*)(end.v_cache + (ph * kPage + lp % kQuarters * kWaveTokens + j) * D + col);
 #pragma unroll 1
         for (int i = 0; i < kCols; ++i) {
           const uint32_t n = nan_codes(codes[i]);

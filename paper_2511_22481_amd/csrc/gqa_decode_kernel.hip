@@ -93,7 +93,8 @@ struct Narrow {
 template <int D, int RT, bool OUT32, bool ALONE>
 __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_kernel(GqaDecodeParams p) {
   using C = Narrow<D, RT>;
-  using Deal = Dealer<C::kRows, kThreads, ALONE ? 1 : 2, ALONE ? 4 : 1>;
+  using Deal = Dealer<C::kRows, kThreads, ALONE ? 4 : 2, ALONE ? 4 : 1>;
+  constexpr int kGrain = Deal::kGrain;
   static_assert(!ALONE || (D == 64 && RT == 1));
   constexpr int R = C::kRows, kCols = D / 16, kWords = D / 64;
   extern __shared__ __align__(16) float lds[];
@@ -111,10 +112,10 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
   const int blocks_per_page = kPage >> p.scale_shift;
   int parity = 0, first_partial = 0;  // first_partial: 1 once this work group has left its first block behind
 
-  // Page-table entries of up to 64 of a block's pages from number `from` on, one per lane.
+  // Page-table entries of up to 64 of a block's pages (or quarters, if the wave is alone) from number `from` on, one per lane.
   auto entries = [&](int b, const TileLayout& pages, int from) {
     const int last = pages.count() - 1;
-    return last >= 0 ? p.page_table[b * p.table_stride + pages.logical(min(from + lane, last))] : 0;
+    return last >= 0 ? p.page_table[b * p.table_stride + pages.logical(min(from + lane, last)) / (kPage / kGrain)] : 0;
   };
   // Query rows of a block: lane n16 of every group of 16 holds one row of each row tile, the columns that its K loads bring.  Rows past
   // the last hold zeros.  reach: tokens that the row's query sees.
@@ -151,34 +152,17 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
     if constexpr (C::kQLds) return q_lds[((q_side * RT + rt) * 2 * kWords + i) * 64 + lane];
     else return q[rt][i];
   };
-  // A tile: 32 tokens of a page, the wave's quarter of it, or the four in turn if the wave is alone.  The next one with tokens that the
-  // block keeps, from `at` on; page `hi` if there is none before it.
-  struct At {
-    int page, quarter;
-  };
-  auto from = [&](const Span& span, At at, int hi) {
-    if constexpr (ALONE) {
-      while (at.page < hi && !kept_of(p, span, span.pages.logical(at.page) * kPage + at.quarter * kWaveTokens).some) {
-        at.quarter = (at.quarter + 1) & 3;
-        at.page += at.quarter == 0;
-      }
-    }
-    return at;
-  };
-  auto behind = [&](const Span& span, At at) {
-    if constexpr (ALONE) return from(span, At{at.page + (at.quarter == 3), (at.quarter + 1) & 3}, span.tile_hi);
-    else return At{at.page + 1, at.quarter};
-  };
-  const int first_quarter = ALONE ? 0 : wave;
+  // A tile: the wave's quarter of a page, or the next quarter if the wave is alone.  Its first token:
+  auto first_of = [&](const TileLayout& pages, int tile) { return pages.logical(tile) * kGrain + (ALONE ? 0 : wave * kWaveTokens); };
   // A tile's loads: where its codes are (scalar registers, made where they are used), and the two scales.
   struct Codes {
     __amdgpu_buffer_rsrc_t k, v;
   };
   const Codes none = {codes_at(p.k_cache, 0), codes_at(p.v_cache, 0)};
   float ks = 0.f, vs = 0.f;
-  auto aim = [&](const TileLayout& pages, int h, int seen, At at, int ids, int held) {
-    const int page = __builtin_amdgcn_readlane(ids, at.page - held);
-    const int first = at.quarter * kWaveTokens, live = max(min(seen - pages.logical(at.page) * kPage - first, kWaveTokens), 0);
+  auto aim = [&](const TileLayout& pages, int h, int seen, int tile, int ids, int held) {
+    const int page = __builtin_amdgcn_readlane(ids, tile - held);
+    const int pos = first_of(pages, tile), first = pos % kPage, live = max(min(seen - pos, kWaveTokens), 0);
     const size_t ph = (size_t)page * p.kv_heads + h, block = ph * blocks_per_page + (first >> p.scale_shift), code = (ph * kPage + first) * D;
     ks = p.k_scales[block];
     vs = p.v_scales[block];
@@ -190,10 +174,10 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
   settle(ids);
   load_q(now);
   Span span(now);
-  At at = from(span, At{uniform(now.tile_lo), first_quarter}, span.tile_hi);
+  int tile = uniform(now.tile_lo);
   {
     Codes c = none;
-    if (at.page < span.tile_hi) c = aim(span.pages, now.h, span.hi, at, ids, held);
+    if (tile < span.tile_hi) c = aim(span.pages, now.h, span.hi, tile, ids, held);
     load_k<D>(t, c.k, k_at);
     load_v<D>(t, c.v, v_at);
   }
@@ -214,7 +198,7 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
       ahead_b = b + 1;
       if (ahead_b < p.batch) {
         const Request r = dealer.request(ahead_b);
-        if (r.n > 0) ahead_ids = entries(ahead_b, block_of<R>(p, r, 0).pages, 0);
+        if (r.n > 0) ahead_ids = entries(ahead_b, block_of<R, kGrain>(p, r, 0).pages, 0);
       }
     }
     // What the next block is (asked late, so that its description need not be kept through the loop), its query, and where its first page
@@ -226,15 +210,13 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
       if (!more_blocks) return none;
       dealer.keep(1, next);
       load_q(next);
-      const Span its(next);
-      const At first = from(its, At{uniform(next.tile_lo), first_quarter}, its.tile_hi);
-      if (first.page >= its.tile_hi) return none;
+      if (next.tile_lo >= next.tile_hi) return none;
       if (!(next.b == was.b && next.rb == was.rb && held == 0)) {
         held = 0;
         ids = next.b == ahead_b && next.rb == 0 ? ahead_ids : entries(next.b, next.bk.pages, 0);
         settle(ids);
       }
-      return aim(its.pages, next.h, its.hi, first, ids, held);
+      return aim(next.bk.pages, next.h, next.reach_hi(), next.tile_lo, ids, held);
     };
     Rows<D, RT> a;
     a.clear();
@@ -242,8 +224,8 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
     // A page; the loads of the one behind it go out as soon as their registers are free.  (They go out in any case, behind the share's last
     // page with nothing to read: were they conditional, the wait for K in the next pass would have to be for V's too.  And the last page
     // of a block is a copy of its own: what it has to find out would otherwise be carried through every pass.)
-    auto step = [&](auto last, At then) {
-      const int pos0 = span.pages.logical(at.page) * kPage + at.quarter * kWaveTokens;
+    auto step = [&](auto last) {
+      const int pos0 = first_of(span.pages, tile);
       const Kept kept = kept_of(p, span, pos0);
       f32x4 s[RT][2];
 #pragma unroll
@@ -269,12 +251,12 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
       if constexpr (decltype(last)::value) {
         c = turn_to_next();
       } else {
-        if (then.page - held >= 64) {
-          held = then.page;
+        if (tile + 1 - held >= 64) {
+          held = tile + 1;
           ids = entries(b, span.pages, held);
           settle(ids);
         }
-        c = aim(span.pages, h, span.hi, then, ids, held);
+        c = aim(span.pages, h, span.hi, tile + 1, ids, held);
       }
       load_k<D>(t, c.k, k_at);
 
@@ -284,14 +266,9 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
       add_values<D, RT, OUT32>(a, t.v, high, low);
       load_v<D>(t, c.v, v_at);
     };
-    if (at.page < span.tile_hi) {
-      while (true) {
-        const At then = behind(span, at);
-        if (then.page >= span.tile_hi) break;
-        step(std::false_type{}, then);
-        at = then;
-      }
-      step(std::true_type{}, at);
+    if (tile < span.tile_hi) {
+      for (; tile + 1 < span.tile_hi; ++tile) step(std::false_type{});
+      step(std::true_type{});
     } else {  // (nothing kept; the loads are waited for here, so that this rare way does not count where the waits of the others are set)
       const Codes c = turn_to_next();
       load_k<D>(t, c.k, k_at);
@@ -317,7 +294,7 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
     b = next.b;
     h = next.h;
     span = Span(next);
-    at = from(span, At{uniform(next.tile_lo), first_quarter}, span.tile_hi);
+    tile = next.tile_lo;
   }
 }
 
@@ -452,10 +429,10 @@ hipError_t allow_lds() {
 //   2 tiles         53  60  57  82  88 171    2 tiles         95 101 108 156 159 301    wide           179 180 182 217 247 423
 //   4 tiles         67  79  70  69  75 142    wide           102 107 115 136 139 265
 // (Up to 16 rows of width 256 the two are alike at these lengths; short requests end and begin faster with this kernel.)
-// Waves that work alone: a block costs them 3 us less, as they need not meet, but they leave more partial rows, and what is left uneven
-// weighs four times as much.  256 requests, 12 KV heads of width 64, us with them and without: 128 tokens each 19.6 / 26.3, 1 to 2000
-// (window 1024) 34 / 40.5, 1024 each 87 / 83, 2048 each 156 / 153; 128 requests of 500 to 8000 tokens, 8 KV heads 85 / 83.5.  At width 128
-// they lose from 50 to 1000 tokens on (200 requests, 8 KV heads: 44 / 41.5), and so they are for many short blocks of width 64.
+// Waves that work alone: a block costs them 3 us less, as they need not meet, but they leave more partial rows and have less under way where
+// blocks are long.  256 requests, 12 KV heads of width 64, us with them and without: 128 tokens each 13.4 / 18.1, 1 to 2000 (window 1024)
+// 29.9 / 35.1, 1024 each 84 / 80, 2048 each 154 / 149; 128 requests of 500 to 8000 tokens, 8 KV heads 85 / 83.5.  At width 128 they lose from
+// 50 to 1000 tokens on (200 requests, 8 KV heads: 44 / 41.5), and so they are for many short blocks of width 64.
 // Blocks that cannot have more than a few pages go whole to a share: nothing has to be joined, which saves the second launch (2 to 3 us,
 // and 3 us of the host's time).  us cut / uncut, all requests of so many pages (4 query heads to a KV head but for width 64; "wide": 40 rows):
 //   requests x heads     1 page      2            3            4            6            8
