@@ -302,21 +302,10 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
 // row lies in the slot of the i-th work group: the first one may have had another block before (slot 2 u + 1), the others
 // begin with this one (2 u).  WAVES waves share a row, each every WAVES-th partial.
 template <int D, bool OUT32, int WAVES, int BATCH>
-__global__ __launch_bounds__(64 * (WAVES > 4 ? WAVES : 4)) void gqa_combine_kernel(GqaDecodeParams p, int block_rows, int shares) {
+__device__ __forceinline__ void join_row(const GqaDecodeParams& p, int64_t row, int first, int count, int in_block, int block_rows, float (*sh_o)[D], float4* sh_ml) {
   constexpr int kPer = D / 64;  // columns per lane
   typedef __attribute__((ext_vector_type(kPer))) float vec;
-  __shared__ float sh_o[WAVES > 1 ? WAVES : 1][WAVES > 1 ? D : 1];
-  __shared__ float4 sh_ml[WAVES];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int64_t row = WAVES > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
-  if (row >= (int64_t)p.num_queries * p.q_heads) return;
-  // (all three are asked for together)
-  const int2 d = p.rows[row];
-  const int token = (int)((uint32_t)row / (uint32_t)p.q_heads), first = p.q_start ? p.q_start[0] : 0, stop = p.q_start ? p.q_start[p.batch] : p.num_queries;
-  if (token < first || token >= stop) return;  // (rows of no request: nothing was written for them)
-  const int count = __builtin_amdgcn_readfirstlane(d.y / 64), in_block = d.y % 64;
-  if (count <= 0 || d.x < 0 || d.x / 2 + count > shares) return;
-  const int u0 = d.x / 2;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, u0 = first / 2;
   float m = -INFINITY, n = -INFINITY, l = 0.f;
   vec o = {};
   constexpr int kBatch = BATCH;
@@ -326,7 +315,7 @@ __global__ __launch_bounds__(64 * (WAVES > 4 ? WAVES : 4)) void gqa_combine_kern
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       const int i = min(i0 + k * WAVES, count - 1);
-      const size_t slot = i == 0 ? d.x : 2 * (u0 + i);
+      const size_t slot = i == 0 ? first : 2 * (u0 + i);
       e[k] = p.part_ml[slot * block_rows + in_block];
       x[k] = *(const vec*)(p.part_o + (slot * block_rows + in_block) * D + lane * kPer);
     }
@@ -381,12 +370,44 @@ __global__ __launch_bounds__(64 * (WAVES > 4 ? WAVES : 4)) void gqa_combine_kern
   if (lane == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + __log2f(l) - kLift) * 0.69314718055994531f;
 }
 
+// ROWS: to a wave (with one wave to a row), of which it joins those that are in parts.
+template <int D, bool OUT32, int WAVES, int BATCH, int ROWS>
+__global__ __launch_bounds__(64 * (WAVES > 4 ? WAVES : 4)) void gqa_combine_kernel(GqaDecodeParams p, int block_rows, int shares) {
+  static_assert(WAVES == 1 || ROWS == 1);
+  __shared__ float sh_o[WAVES > 1 ? WAVES : 1][D];
+  __shared__ float4 sh_ml[WAVES];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int64_t row0 = WAVES > 1 ? (int64_t)blockIdx.x : ((int64_t)blockIdx.x * 4 + wave) * ROWS, row = row0 + (ROWS > 1 ? lane : 0);
+  int2 d = {0, 0};
+  if (lane < ROWS || ROWS == 1) {
+    if (row < (int64_t)p.num_queries * p.q_heads) {
+      // (all three are asked for together)
+      d = p.rows[row];
+      const int token = (int)((uint32_t)row / (uint32_t)p.q_heads), first = p.q_start ? p.q_start[0] : 0, stop = p.q_start ? p.q_start[p.batch] : p.num_queries;
+      const int count = d.y / 64;
+      // (rows of no request: nothing was written for them)
+      if (token < first || token >= stop || count <= 0 || d.x < 0 || d.x / 2 + count > shares) d.y = 0;
+    }
+  }
+  if constexpr (ROWS == 1) {
+    const int y = __builtin_amdgcn_readfirstlane(d.y);
+    if (y >= 64) join_row<D, OUT32, WAVES, BATCH>(p, row, d.x, y / 64, y % 64, block_rows, sh_o, sh_ml);
+  } else {
+    for (uint64_t rest = __ballot(d.y >= 64); rest; rest &= rest - 1) {
+      const int k = __builtin_ctzll(rest), y = __builtin_amdgcn_readlane(d.y, k);
+      join_row<D, OUT32, 1, BATCH>(p, row0 + k, __builtin_amdgcn_readlane(d.x, k), y / 64, y % 64, block_rows, sh_o, sh_ml);
+    }
+  }
+}
+
 template <int D, bool OUT32>
 hipError_t join(const GqaDecodeParams& p, int block_rows, int shares, hipStream_t stream) {
   const int64_t rows = (int64_t)p.num_queries * p.q_heads;
-  // Few rows: four waves to a row.
-  if (rows <= 2048) hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 8, 4>), dim3((uint32_t)rows), dim3(512), 0, stream, p, block_rows, shares);
-  else hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 1, 4>), dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, stream, p, block_rows, shares);
+  // Few rows: eight waves to each.  Very many, of which few are in parts (prompts): a wave looks at 16 (524288 rows: 34 us less
+  // than one to a wave).
+  if (rows <= 2048) hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 8, 4, 1>), dim3((uint32_t)rows), dim3(512), 0, stream, p, block_rows, shares);
+  else if (rows <= 65536) hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 1, 4, 1>), dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, stream, p, block_rows, shares);
+  else hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 1, 4, 16>), dim3((uint32_t)((rows + 63) / 64)), dim3(256), 0, stream, p, block_rows, shares);
   return hipGetLastError();
 }
 

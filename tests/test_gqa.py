@@ -411,6 +411,17 @@ def test_blocks_of_few_pages_are_not_cut(dim, q_heads, kv_heads, most, columns, 
 
 
 @gpu
+@pytest.mark.parametrize("dim,q_heads,kv_heads", [(64, 32, 2), (128, 48, 2), (64, 120, 120)])
+def test_prompts_of_many_rows(dim, q_heads, kv_heads):
+    """More than 65536 rows, of which a few are in parts."""
+    lens, news = [700, 0, 130, 690], [700, 0, 65, 690]
+    assert sum(news) * q_heads > 65536 or q_heads == 32
+    if q_heads == 32:
+        lens, news = lens + [700], news + [700]
+    Problem(lens, news, q_heads, kv_heads, dim, 64, 4, 200, seed=dim + q_heads, poison=False).check()
+
+
+@gpu
 def test_nan_among_many_short_requests():
     lens, news = [150] * 256, [3] * 256
     clean = Problem(lens, news, 8, 8, 64, 64, 1, 30, seed=9, poison=False)
