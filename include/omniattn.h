@@ -313,7 +313,7 @@ typedef struct {
  * A request that does not fit is refused as a whole: its row of page_table would be too short, a length is negative,
  * its tokens reach past max_tokens, or the sum of the pages that requests up to it lack exceeds the stack (requests
  * that lack no page are not affected by that).  Its length stays, its tokens' slots are -1; q_start counts them all the
- * same, since they have their places among the call's rows.
+ * same, since they have their places among the call's rows (attention for them means nothing: their keys are not in the cache).
  *
  * omniattn_table_release puts the pages of the requests with done[b] != 0 back on the stack, in their order, and sets
  * their lengths to 0.  (seq_lens, free_pages and free_count change in place.)

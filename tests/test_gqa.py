@@ -422,6 +422,29 @@ def test_prompts_of_many_rows(dim, q_heads, kv_heads):
 
 
 @gpu
+@pytest.mark.parametrize("dim,q_heads,kv_heads", [(64, 2, 2), (128, 8, 2), (128, 5, 1), (256, 4, 1)])
+def test_more_queries_than_tokens(dim, q_heads, kv_heads):
+    """Requests whose new tokens found no pages: queries before the first token keep nothing."""
+    Problem([0, 3, 200, 40, 0], [40, 20, 20, 41, 1], q_heads, kv_heads, dim, 64, 2, 30, seed=dim).check()
+    Problem([0, 3], [1, 4], q_heads, kv_heads, dim, 64, 0, 10 ** 6, seed=dim).check(torch.float32)
+
+
+@gpu
+@pytest.mark.parametrize("dim,kv_heads", [(64, 8), (128, 8), (256, 16)])
+def test_tables_for_very_long_requests(dim, kv_heads):
+    """Columns for 2^29 tokens: units of work are counted in 64 bits.  The same blocks, the same bits as with a table of few columns."""
+    lens = [random.Random(b).choice([0, 1, 100, 700, 1500]) for b in range(70)]
+    p = Problem(lens, [min(1, n) for n in lens], kv_heads, kv_heads, dim, 64, 0, 10 ** 6, seed=dim, poison=False)
+    want, want_lse = p.check()
+    k, v = p.codes.cuda()
+    ks, vs = p.scales.cuda()
+    table = torch.zeros((70, 2 ** 22), dtype=torch.int32, device="cuda")
+    table[:, :len(p.table[0])] = ints(p.table)
+    out, lse = oa.gqa_decode(p.q.cuda(), k, v, ks, vs, table, ints(p.lens), 0, 2 ** 29, p.scale, q_start=ints(p.q_start))
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+@gpu
 def test_nan_among_many_short_requests():
     lens, news = [150] * 256, [3] * 256
     clean = Problem(lens, news, 8, 8, 64, 64, 1, 30, seed=9, poison=False)
