@@ -383,13 +383,6 @@ def decode(q, kv_cache, kv_scales, page_table, seq_lens_host, sink, window, soft
     return out, lse, plan
 
 
-@functools.lru_cache(maxsize=64)
-def _table_record(batch, max_pages, stride, max_tokens, num_pages):
-    """The record that the library reads (and does not keep or change) on every call for a pool and its tables."""
-    return ctypes.pointer(Table(batch, 128, max_pages, max_tokens, stride, num_pages))
-
-
-@functools.lru_cache(maxsize=256)
 def _gqa_record(batch, num_queries, num_q_heads, num_kv_heads, head_dim, page_size, scale_tokens, max_pages, stride, num_pages, sink, window,
                 softmax_scale, out_dtype):
     return ctypes.pointer(Gqa(batch, num_queries, num_q_heads, num_kv_heads, head_dim, page_size, scale_tokens, max_pages, stride, num_pages,
@@ -401,105 +394,43 @@ def _want(ok, what):
         raise OmniAttnError(-1, what)
 
 
-# (The checks below cost as much as a short kernel takes: each is one test that fails as a whole and builds its message only then, and
-# torch is looked up once a call.)
-
-def _ints(torch, tensors):
-    """Checks (tensor, elements, name)s: contiguous int32 CUDA tensors wanted."""
-    int32 = torch.int32
-    for t, n, name in tensors:
-        if t.dtype is not int32 or t.numel() != n or not t.is_cuda or not t.is_contiguous():
-            raise OmniAttnError(-1, f"{name}: int32 CUDA tensor of {n} elements wanted")
+_marshal = None
 
 
-def _table_of(torch, page_table, batch):
-    """(columns, row stride) of a page table."""
-    if page_table.dtype is torch.int32 and page_table.is_cuda and page_table.dim() == 2:
-        rows, columns = page_table.shape
-        stride, step = page_table.stride()
-        if rows == batch and step == 1:
-            return columns, stride
-    raise OmniAttnError(-1, "page_table: int32 CUDA tensor [batch, pages] wanted, its rows contiguous")
-
-
-def _handle(torch, stream):
-    """Of the given stream, or of torch's current one, for calls whose tensors are CUDA tensors already (torch's CUDA part is running)."""
-    if stream is not None:
-        return stream.cuda_stream
-    c = torch._C
-    return c._cuda_getCurrentRawStream(c._cuda_getDevice())
+def _native():
+    """The module that checks a call's tensors and calls the library (csrc/gqa_marshal.cpp)."""
+    global _marshal
+    if _marshal is None:
+        import importlib.util
+        import torch   # (its libraries have to be loaded before the module is)
+        lib = load_library()
+        spec = importlib.util.spec_from_file_location("gqa_marshal", os.path.join(HERE, "gqa_marshal.so"))
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        module.setup(OmniAttnError, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
+                     *(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.omniattn_table_extend, lib.omniattn_table_release,
+                                                                       lib.omniattn_gqa_append, lib.omniattn_gqa_decode)))
+        _marshal = module
+    return _marshal
 
 
 def omniattn_table_extend(seq_lens, new_lens, free_pages, free_count, page_table, seq_lens_out, free_count_out, q_start, slot_map, stream=None):
     """Tables of one step on the GPU: every request grows by its new tokens and takes pages from the stack of free ones (all int32
     CUDA tensors; page_table, seq_lens_out, free_count_out, q_start [batch + 1] and slot_map are written).  seq_lens_out may be
     seq_lens, free_count_out may be free_count.  A request that does not fit keeps its length and gets slots -1."""
-    import torch
-    batch, tokens, pages = seq_lens.numel(), slot_map.numel(), free_pages.numel()
-    columns, stride = _table_of(torch, page_table, batch)
-    _ints(torch, ((seq_lens, batch, "seq_lens"), (new_lens, batch, "new_lens"), (free_pages, pages, "free_pages"), (free_count, 1, "free_count"),
-                  (seq_lens_out, batch, "seq_lens_out"), (free_count_out, 1, "free_count_out"), (q_start, batch + 1, "q_start"),
-                  (slot_map, tokens, "slot_map")))
-    _check(load_library().omniattn_table_extend(
-        _table_record(batch, columns, stride, tokens, pages), seq_lens.data_ptr(), new_lens.data_ptr(), free_pages.data_ptr(),
-        free_count.data_ptr(), page_table.data_ptr(), seq_lens_out.data_ptr(), free_count_out.data_ptr(), q_start.data_ptr(),
-        slot_map.data_ptr(), _handle(torch, stream)))
+    _check((_marshal or _native()).extend(seq_lens, new_lens, free_pages, free_count, page_table, seq_lens_out, free_count_out, q_start, slot_map, stream))
 
 
 def omniattn_table_release(seq_lens, done, page_table, free_pages, free_count, stream=None):
     """Pages of the requests with done[b] != 0 go back on the stack, their lengths become 0 (seq_lens, free_pages and free_count
     change in place)."""
-    import torch
-    batch, pages = seq_lens.numel(), free_pages.numel()
-    columns, stride = _table_of(torch, page_table, batch)
-    _ints(torch, ((done, batch, "done"), (seq_lens, batch, "seq_lens"), (free_pages, pages, "free_pages"), (free_count, 1, "free_count")))
-    _check(load_library().omniattn_table_release(
-        _table_record(batch, columns, stride, 0, pages), done.data_ptr(), seq_lens.data_ptr(), page_table.data_ptr(), free_pages.data_ptr(),
-        free_count.data_ptr(), _handle(torch, stream)))
-
-
-def _cache_shape(torch, k_cache, v_cache, k_scales, v_scales):
-    """(pages, KV heads, page size, head width, tokens to a scale) of a layer's cache."""
-    codes, numbers = torch.float8_e4m3fn, torch.float32
-    shape, scales = k_cache.shape, k_scales.shape
-    if (k_cache.dtype is not codes or v_cache.dtype is not codes or k_scales.dtype is not numbers or v_scales.dtype is not numbers
-            or len(shape) != 4 or len(scales) != 3 or v_cache.shape != shape or v_scales.shape != scales):
-        raise OmniAttnError(-1, "cache (float8_e4m3fn) [pages, KV heads, 128, head width] with scales (float32) [pages, KV heads, 128 / tokens] "
-                                "wanted, for K and V alike")
-    if not (k_cache.is_contiguous() and v_cache.is_contiguous() and k_scales.is_contiguous() and v_scales.is_contiguous()
-            and k_cache.is_cuda and v_cache.is_cuda and k_scales.is_cuda and v_scales.is_cuda):
-        raise OmniAttnError(-1, "cache and scales: contiguous CUDA tensors wanted")
-    pages, heads, page, dim = shape
-    per_page = scales[2]
-    if scales[0] != pages or scales[1] != heads or per_page <= 0 or page % per_page:
-        raise OmniAttnError(-1, "scales: for every page and KV head of the cache wanted, their number a divisor of a page's tokens")
-    return pages, heads, page, dim, page // per_page
-
-
-def _rows_of(torch, t, heads, dim, name):
-    """(tokens, address, token stride) of bf16 rows [tokens, heads, dim]."""
-    if t.dtype is torch.bfloat16 and t.is_cuda and t.dim() == 3:
-        n, h, d = t.shape
-        stride, head, step = t.stride()
-        if h == heads and d == dim and step == 1 and (head == dim or heads == 1):
-            return n, t.data_ptr(), stride if n > 1 else heads * dim
-    raise OmniAttnError(-1, f"{name}: bf16 CUDA tensor [tokens, {heads}, {dim}] wanted, a token's rows contiguous")
+    _check((_marshal or _native()).release(seq_lens, done, page_table, free_pages, free_count, stream))
 
 
 def omniattn_gqa_append(k_new, v_new, slot_map, k_cache, v_cache, k_scales, v_scales, stream=None):
     """New K and V rows (bf16 [tokens, KV heads, head width], any token stride) to their slots in a layer's cache, rounded to e4m3
     with a scale for each block of tokens and head.  k_cache, v_cache, k_scales and v_scales are written."""
-    import torch
-    pages, heads, page, dim, tokens = _cache_shape(torch, k_cache, v_cache, k_scales, v_scales)
-    n, k, k_stride = _rows_of(torch, k_new, heads, dim, "k_new")
-    n_v, v, v_stride = _rows_of(torch, v_new, heads, dim, "v_new")
-    if n_v != n:
-        raise OmniAttnError(-1, "k_new and v_new: as many tokens wanted")
-    _ints(torch, ((slot_map, n, "slot_map"),))
-    rec = _gqa_record(1, 0, heads, heads, dim, page, tokens, 1, 1, pages, 0, 0, 1.0, BF16)
-    _check(load_library().omniattn_gqa_append(
-        rec, n, k, k_stride, v, v_stride, slot_map.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(),
-        v_scales.data_ptr(), _handle(torch, stream)))
+    _check((_marshal or _native()).append(k_new, v_new, slot_map, k_cache, v_cache, k_scales, v_scales, stream))
 
 
 def omniattn_gqa_workspace_bytes(batch, num_queries, num_q_heads, num_kv_heads, head_dim):
@@ -515,24 +446,8 @@ def omniattn_gqa_decode(q, k_cache, v_cache, k_scales, v_scales, page_table, seq
     """Attention of the query tokens q (bf16 [tokens, query heads, head width], any token stride) over a layer's cache.  q_start (int32
     [batch + 1]): request b's queries are tokens q_start[b] .. q_start[b + 1], the last ones of its seq_lens[b]; None: one each.
     out (bf16 or fp32, shaped like q) and lse (fp32 [tokens, query heads]) are written."""
-    import torch
-    pages, heads, page, dim, tokens = _cache_shape(torch, k_cache, v_cache, k_scales, v_scales)
-    shape = q.shape
-    batch, q_heads = seq_lens.numel(), shape[1] if len(shape) == 3 else 0
-    n, src, q_stride = _rows_of(torch, q, q_heads, dim, "q")
-    columns, stride = _table_of(torch, page_table, batch)
-    _ints(torch, ((seq_lens, batch, "seq_lens"),) if q_start is None else ((seq_lens, batch, "seq_lens"), (q_start, batch + 1, "q_start")))
-    fp32 = out.dtype is torch.float32
-    if not (fp32 or out.dtype is torch.bfloat16) or out.shape != shape or not out.is_contiguous() or not out.is_cuda:
-        raise OmniAttnError(-1, "out: contiguous bf16 or fp32 CUDA tensor shaped like q wanted")
-    if lse.dtype is not torch.float32 or lse.shape != (n, q_heads) or not lse.is_contiguous() or not lse.is_cuda:
-        raise OmniAttnError(-1, "lse: contiguous fp32 CUDA tensor [tokens, query heads] wanted")
-    rec = _gqa_record(batch, n, q_heads, heads, dim, page, tokens, columns, stride, pages, operator.index(sink), operator.index(window),
-                      float(softmax_scale), FP32 if fp32 else BF16)
-    _check(load_library().omniattn_gqa_decode(
-        rec, src, q_stride, k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), page_table.data_ptr(),
-        seq_lens.data_ptr(), _ptr(q_start), out.data_ptr(), lse.data_ptr(), _ptr(workspace),
-        workspace.numel() * workspace.element_size() if workspace is not None else 0, _handle(torch, stream)))
+    _check((_marshal or _native()).decode(q, k_cache, v_cache, k_scales, v_scales, page_table, seq_lens, q_start, out, lse, workspace, sink, window,
+                                          softmax_scale, stream))
 
 
 def gqa_decode(q, k_cache, v_cache, k_scales, v_scales, page_table, seq_lens, sink, window, softmax_scale, q_start=None, out_dtype=None):

@@ -1,7 +1,11 @@
-"""Compile the HIP library for gfx950 in-tree (paper_2511_22481_amd/libomniattn.so)."""
+"""Compile the HIP library for gfx950 in-tree (paper_2511_22481_amd/libomniattn.so), and the binding's module that reads torch tensors
+(paper_2511_22481_amd/gqa_marshal.so, host code)."""
 import hashlib
+import importlib.metadata
 import os
 import subprocess
+import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -10,6 +14,9 @@ SOURCES = ["decode_kernels.hip", "decode_mid_kernel.hip", "decode_narrow_kernel.
            "table_kernels.hip", "gqa_append_kernel.hip", "gqa_decode_kernel.hip",
            "gqa_wide_kernel.hip", "api.cpp", "api_gqa.cpp", "plan.cpp"]
 HEADERS = ["kernels.h", "gqa.h", "gqa_common.h", "plan.h", "decode_common.h", os.path.join("..", "..", "include", "omniattn.h")]
+
+MARSHAL = os.path.join(HERE, "gqa_marshal.so")
+MARSHAL_SOURCE = "gqa_marshal.cpp"
 
 
 def hipcc():
@@ -25,7 +32,9 @@ CHECKER = os.path.join(HERE, "check_isa.py")
 
 def source_hash():
     h = hashlib.sha256()
-    for f in sorted(SOURCES + HEADERS):
+    # (the module is built against one interpreter and one torch)
+    h.update(f"{sys.implementation.cache_tag} {importlib.metadata.version('torch')}".encode())
+    for f in sorted(SOURCES + HEADERS + [MARSHAL_SOURCE]):
         h.update(f.encode())
         h.update(open(os.path.join(CSRC, f), "rb").read())
     h.update(open(CHECKER, "rb").read())
@@ -35,7 +44,7 @@ def source_hash():
 def is_stale():
     """True unless the library exists and was built, and its generated code checked, from
     exactly the present sources (content hash, so that file times do not matter)."""
-    if not os.path.exists(LIB) or not os.path.exists(STAMP):
+    if not os.path.exists(LIB) or not os.path.exists(MARSHAL) or not os.path.exists(STAMP):
         return True
     return open(STAMP).read().strip() != source_hash()
 
@@ -52,7 +61,12 @@ def build(force=True, verbose=False):
            "-Wno-unused-command-line-argument", "-parallel-jobs=8", "-x", "hip"]
     cmd += [os.path.join(CSRC, f) for f in SOURCES]
     cmd += ["-o", LIB]
+    marshal = subprocess.Popen(marshal_command(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
+    said = marshal.communicate()[0]
+    if marshal.returncode != 0:
+        print(said)
+        raise RuntimeError("building the binding's module failed")
     if verbose or res.returncode != 0:
         print(res.stdout)
         print("\n".join(l for l in res.stderr.splitlines()
@@ -63,6 +77,14 @@ def build(force=True, verbose=False):
     with open(STAMP, "w") as f:     # only a library whose generated code passed the check is stamped
         f.write(source_hash() + "\n")
     return LIB
+
+
+def marshal_command():
+    import torch
+    root = os.path.dirname(os.path.abspath(torch.__file__))
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(root, "include"), os.path.join(CSRC, MARSHAL_SOURCE),
+            "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-o", MARSHAL]
 
 
 def check_generated_code(verbose=False):

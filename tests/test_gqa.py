@@ -745,6 +745,48 @@ def test_tables_refuse_missing_and_overlapping_arrays():
     assert lib.omniattn_table_extend(None, *spread, None) == -1
 
 
+def test_the_binding_refuses_what_is_no_cuda_tensor():
+    """Before anything reaches the library: host tensors, other types and sizes, and things that are no tensors."""
+    n = lambda *shape: torch.zeros(shape, dtype=torch.int32)
+    good = [n(3), n(3), n(9), n(1), n(3, 4), n(3), n(1), n(4), n(5)]
+    for bad in [good] + [good[:i] + [x] + good[i + 1:] for i in range(9) for x in (None, 7, [1], torch.zeros(3), n(2, 2).t())]:
+        with pytest.raises(oa.OmniAttnError) as e:
+            oa.omniattn_table_extend(*bad)
+        assert e.value.code == -1
+        with pytest.raises(oa.OmniAttnError):
+            oa.omniattn_table_release(bad[0], bad[1], bad[4], bad[2], bad[3])
+    codes, scales = torch.zeros((2, 1, 128, 64), dtype=torch.uint8).view(torch.float8_e4m3fn), torch.zeros((2, 1, 2))
+    rows = torch.zeros((3, 1, 64), dtype=torch.bfloat16)
+    for cache in ([codes, codes, scales, scales], [codes[:1], codes, scales, scales], [codes.view(torch.uint8), codes, scales, scales], [codes, codes, None, scales],
+                  [codes, codes, scales[:, :, :0], scales[:, :, :0]]):
+        with pytest.raises(oa.OmniAttnError):
+            oa.omniattn_gqa_append(rows, rows, n(3), *cache)
+        with pytest.raises(oa.OmniAttnError):
+            oa.omniattn_gqa_decode(rows, *cache, n(3, 4), n(3), None, rows, torch.zeros((3, 1)), None, sink=0, window=1, softmax_scale=1.0)
+    with pytest.raises(TypeError):
+        oa.omniattn_table_extend(*good[:8])
+
+
+@gpu
+def test_the_binding_refuses_numbers_out_of_range():
+    p = Problem([200], [1], 4, 2, 128, 64, 0, 1000, seed=1)
+    k, v = p.codes.cuda()
+    ks, vs = p.scales.cuda()
+    out, lse = torch.empty((1, 4, 128), dtype=torch.bfloat16, device="cuda"), torch.empty((1, 4), device="cuda")
+    ws = torch.empty(oa.omniattn_gqa_workspace_bytes(1, 1, 4, 2, 128), dtype=torch.uint8, device="cuda")
+    call = lambda **kw: oa.omniattn_gqa_decode(p.q.cuda(), k, v, ks, vs, ints(p.table), ints(p.lens), None, out, lse, ws, **{**dict(sink=0, window=1000, softmax_scale=0.1), **kw})
+    call()
+    for bad in (dict(sink=2 ** 31), dict(window=-1), dict(window=2 ** 70), dict(sink=-2 ** 40), dict(softmax_scale=float("nan"))):
+        with pytest.raises(oa.OmniAttnError) as e:
+            call(**bad)
+        assert e.value.code == -1
+    for bad in (dict(sink=1.5), dict(window=None), dict(softmax_scale="1")):
+        with pytest.raises(TypeError):
+            call(**bad)
+    call(stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+
+
 @gpu
 def test_workspace_is_checked():
     p = Problem([200], [1], 4, 2, 128, 64, 0, 1000, seed=1)
