@@ -23,18 +23,30 @@ __device__ __forceinline__ uint32_t sat(uint32_t a, uint32_t b) { return min(a +
 
 __device__ __forceinline__ int pages_of(int64_t tokens) { return (int)((tokens + kPage - 1) / kPage); }
 
-// Sum over the work group's threads before this one.  `tot`: one word per wave; two barriers.
-__device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t* tot) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int d = 1; d < 64; d *= 2) {
-    const uint32_t y = __shfl_up(x, d);
-    if (lane >= d) x = sat(x, y);
+// Running sum over a wave, or (rows of 16 only) over each 16 lanes.
+template <bool WAVE>
+__device__ __forceinline__ uint32_t sum_up_to(uint32_t x) {
+#define OMNIATTN_ADD(ctrl, rows) x = sat(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, true))
+  OMNIATTN_ADD(0x111, 0xf);  // from the lane one, two, four, eight before, in rows of 16
+  OMNIATTN_ADD(0x112, 0xf);
+  OMNIATTN_ADD(0x114, 0xf);
+  OMNIATTN_ADD(0x118, 0xf);
+  if constexpr (WAVE) {
+    OMNIATTN_ADD(0x142, 0xa);  // a row's last lane to the row behind it
+    OMNIATTN_ADD(0x143, 0xc);  // lane 31 to the upper half
   }
-  __syncthreads();
+#undef OMNIATTN_ADD
+  return x;
+}
+
+// Sum over the work group's threads before this one.  `tot`: one word per wave, to be left alone until the caller's next barrier.  One barrier.
+__device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t* tot) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x / 64;
+  x = sum_up_to<true>(x);
   if (lane == 63) tot[wave] = x;
   __syncthreads();
-  uint32_t before = 0;
-  for (int w = 0; w < wave; ++w) before = sat(before, tot[w]);
+  const uint32_t ends = sum_up_to<false>(lane < waves ? tot[lane] : 0);  // (up to 16 waves)
+  const uint32_t before = wave ? (uint32_t)__builtin_amdgcn_readlane((int)ends, wave - 1) : 0;
   x = __shfl_up(x, 1);
   return lane ? sat(x, before) : before;
 }
@@ -58,7 +70,7 @@ __device__ __forceinline__ int owner(const uint32_t* ends, int n, uint32_t i) {
 template <int WHAT, int PER>
 __global__ __launch_bounds__(kThreads) void extend_kernel(TableParams p) {
   constexpr int kMany = PER * kThreads;
-  __shared__ uint32_t tot[kThreads / 64];
+  __shared__ uint32_t tot[2][kThreads / 64];
   __shared__ uint32_t token_end[kMany], page_end[kMany];
   __shared__ int had[kMany], len[kMany];  // had: -1 where the request is refused
   const int tid = threadIdx.x, threads = blockDim.x;
@@ -84,7 +96,7 @@ __global__ __launch_bounds__(kThreads) void extend_kernel(TableParams p) {
     // (a sum that has stopped is no request's first token: refused below)
     uint32_t t_end[PER], p_end[PER], need[PER];
     bool fine[PER];
-    uint32_t run = sat(tokens, sum_before(sum, tot));
+    uint32_t run = sat(tokens, sum_before(sum, tot[0]));
     sum = 0;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
@@ -95,7 +107,7 @@ __global__ __launch_bounds__(kThreads) void extend_kernel(TableParams p) {
       need[j] = fine[j] ? (uint32_t)(pages_of(after) - pages_of(L[j])) : 0;
       sum = sat(sum, need[j]);
     }
-    run = sat(pages, sum_before(sum, tot));
+    run = sat(pages, sum_before(sum, tot[1]));
     bool more = false;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
@@ -166,7 +178,7 @@ __global__ __launch_bounds__(kThreads) void extend_kernel(TableParams p) {
     }
     tokens = token_end[last];
     pages = page_end[last];
-    __syncthreads();  // the sums are read before the next chunk's replace them
+    if (b0 + PER * threads < p.batch) __syncthreads();  // the sums are read before the next chunk's replace them
   }
   if constexpr (WHAT & 1) {
     for (uint32_t i = tokens + blockIdx.x * threads + tid; i < (uint32_t)p.max_tokens; i += gridDim.x * threads) p.slot_map[i] = -1;
@@ -174,10 +186,10 @@ __global__ __launch_bounds__(kThreads) void extend_kernel(TableParams p) {
   if constexpr (WHAT & 2) {
     if (first_group) {
       for (int d = 1; d < 64; d *= 2) used = max(used, (uint32_t)__shfl_xor(used, d));
-      if ((tid & 63) == 0) tot[tid >> 6] = used;
+      if ((tid & 63) == 0) tot[0][tid >> 6] = used;
       __syncthreads();
       if (tid == 0) {
-        for (int w = 1; w < threads / 64; ++w) used = max(used, tot[w]);
+        for (int w = 1; w < threads / 64; ++w) used = max(used, tot[0][w]);
         *p.free_count_out = count - (int)used;
       }
     }
@@ -215,9 +227,10 @@ __global__ __launch_bounds__(kThreads) void release_kernel(ReleaseParams p) {
 }  // namespace
 
 hipError_t launch_table_extend(const TableParams& p, hipStream_t stream) {
-  // Work groups: one for each 1024 slots.  Two requests to a thread where there are more than threads (1500 requests: 11.7 us in two turns).
+  // A thread to a request, or to two where there are more than threads (1500 requests: 11.7 us in two turns), and at least 256; as many work
+  // groups as there are slots for them (256 requests with chunks: 6.8 us with 1024 threads each).
   const bool pairs = p.batch > kThreads;
-  const int want = std::max(p.batch, std::min(p.max_tokens, kThreads));
+  const int want = std::max(pairs ? (p.batch + 1) / 2 : p.batch, std::min(p.max_tokens, 256));
   const int threads = std::min(kThreads, (want + 63) / 64 * 64);
   const int groups = std::max(1, std::min(256, (p.max_tokens + threads - 1) / threads));
   const bool in_place = p.seq_lens_out == p.seq_lens || p.free_count_out == p.free_count;
