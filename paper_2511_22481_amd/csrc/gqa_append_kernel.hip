@@ -91,10 +91,23 @@ __device__ __forceinline__ uint32_t largest(const u32x4& x) {
   for (int j = 0; j < 4; ++j) top = max(top, max(finite_bits(x[j]), finite_bits(x[j] >> 16)));
   return top;
 }
+// Largest of each LANES neighbouring lanes (8, 16, 32 or 64), in all of them.
 template <int LANES>
 __device__ __forceinline__ uint32_t lanes_max(uint32_t x) {
-#pragma unroll
-  for (int d = 1; d < LANES; d *= 2) x = max(x, (uint32_t)__shfl_xor(x, d));
+#define OMNIATTN_MAX(ctrl) x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, 0xf, 0xf, true))
+  OMNIATTN_MAX(0xb1);   // the other of two
+  OMNIATTN_MAX(0x4e);   // the other two of four
+  OMNIATTN_MAX(0x141);  // eight, mirrored
+  if constexpr (LANES >= 16) OMNIATTN_MAX(0x140);  // sixteen, mirrored
+#undef OMNIATTN_MAX
+  if constexpr (LANES >= 32) {
+    const auto y = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = max(y[0], y[1]);
+  }
+  if constexpr (LANES >= 64) {
+    const auto y = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    x = max(y[0], y[1]);
+  }
   return x;
 }
 
