@@ -24,7 +24,7 @@
 // What bounds it: up to 32 rows (64 at width 64), memory.  A work group has one tile of each wave under way (16 to 64 KB a compute
 // unit), asked for as soon as the registers of the tile before are free; the loads are without conditions and every wait is for as
 // many as are needed, no more.  64 requests of 32768 tokens, 8 KV heads of width 128 (4.30 GB): 739 us, 5.8 TB/s, where nothing but
-// reading them in this order reaches 6.25.  One request of 131072 (268 MB): 52 us, of which 6 pass before the first product (a chain
+// reading them in this order reaches 6.25.  One request of 131072 (268 MB): 52 us, of which 5 pass before the first product (a chain
 // of four loads: lengths, table, codes, query) and 3 at the end.  93 ragged requests of 200 to 20000, 4 KV heads: 78 us, 5 TB/s.
 // 64 requests of 2000 to 16000, 4 KV heads of width 128, 32 rows: 103 us, 4.6 TB/s; above, gqa_wide_kernel.hip is faster.
 #include <hip/hip_runtime.h>
