@@ -30,30 +30,29 @@ struct Wide {
   static constexpr int kTokens = kWaveTokens * kTokenGroups;  // of a tile
   static constexpr int kTilesPerPage = kPage / kTokens;
   static constexpr int kHalf = kTokens * D;                   // bytes of a tile's K codes; V's follow
-  static constexpr int kStages = D == 64 ? 5 : 3;
+  static constexpr int kStages = 3;
   static constexpr int kLoads = 2 * kHalf / 1024 / kWaves;    // direct loads of a wave and tile (1 KB each), and one of the scales
-  static constexpr int kParts = D == 64 ? 2 : 4;              // the output's columns meet 1 / kParts at a time
+  static constexpr int kParts = 4;                            // the output's columns meet 1 / kParts at a time
   static constexpr int kScaleBytes = 256;                     // of a wave and stage: K's and V's scale in turn, 32 times
   static constexpr size_t kRing = (size_t)kStages * (2 * kHalf + kWaves * kScaleBytes);
   static constexpr size_t kOBytes = (size_t)kTokenGroups * kRows * (D / kParts + 4) * 4;
   static constexpr size_t kLds = kRing + kOBytes + 2 * kTokenGroups * kRows * 16;
-  static_assert(kLds + 8192 <= 160 * 1024, "LDS of a compute unit");
+  static_assert(kLds + 10240 <= 160 * 1024, "LDS of a compute unit");
+  static_assert((D == 128 || D == 256) && kLoads == 4);
 };
 
 // Where a row's 16-byte chunks lie in LDS.  Rows stand in groups of 16 (tokens 16 i ..): row r at place(r), its chunk c at c ^ twist(r), so
-// that neither the 16 rows of a K operand nor the rows of a V operand meet in the same banks.  (A row is 4, 8 or 16 chunks, 64 banks
-// are 16 chunks.)
+// that neither the 16 rows of a K operand nor the rows of a V operand meet in the same banks.  (A row is 8 or 16 chunks, 64 banks are
+// 16 chunks.)
 template <int D>
 __device__ __forceinline__ int place(int r) {
-  if constexpr (D == 64) return r ^ ((r >> 2) & 3);
-  else if constexpr (D == 128) return r ^ ((r >> 2) & 1);
+  if constexpr (D == 128) return r ^ ((r >> 2) & 1);
   else return r;
 }
 template <int D>
 __device__ __forceinline__ int twist(int r) {
   const int at = place<D>(r);
-  if constexpr (D == 64) return (at >> 2) & 3;
-  else if constexpr (D == 128) return (at >> 1) & 7;
+  if constexpr (D == 128) return (at >> 1) & 7;
   else return at & 15;
 }
 
@@ -81,24 +80,11 @@ __device__ __forceinline__ void load_lds4_each(uint32_t lds, const void* at) {
 }
 #pragma clang diagnostic pop
 
-// Waits until the loads of the oldest tile are done, with `behind` tiles requested after it, and for all waves to get here.  (Other
+// Waits until the loads of the oldest tile are done, with one tile requested after it or none, and for all waves to get here.  (Other
 // loads and stores in between only make it wait for more than it has to.)
-template <int LOADS, int MOST>
-__device__ __forceinline__ void wait_tile(int behind) {
-  if constexpr (MOST >= 4) {
-    if (behind >= 4) {
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(4 * LOADS) : "memory");
-      return;
-    }
-  }
-  if constexpr (MOST >= 3) {
-    if (behind == 3) {
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(3 * LOADS) : "memory");
-      return;
-    }
-  }
-  if (behind >= 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(2 * LOADS) : "memory");
-  else if (behind == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(LOADS) : "memory");
+template <int LOADS>
+__device__ __forceinline__ void wait_tile(bool one_behind) {
+  if (one_behind) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(LOADS) : "memory");
   else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
 }
 
@@ -165,10 +151,8 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
     settle_address(base, same);
     load_lds16_here<0>(base, from[0]);
     load_lds16_here<1024>(base, from[1]);
-    if constexpr (C::kLoads > 2) {
-      load_lds16_here<2048>(base, from[2]);
-      load_lds16_here<3072>(base, from[3]);
-    }
+    load_lds16_here<2048>(base, from[2]);
+    load_lds16_here<3072>(base, from[3]);
     load_lds4_each(ring_at + kStages * 2 * C::kHalf + (ahead_stage * kWaves + wave) * C::kScaleBytes,
                    my_scales + ph * blocks_per_page + ((ahead_half * C::kTokens + tg * kWaveTokens) >> p.scale_shift));
     ++issued;
@@ -228,7 +212,7 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
 #pragma unroll 1
       for (int half = 0; half < C::kTilesPerPage; ++half) {
         ask_page();  // (back behind the wait, which is for scalar loads too)
-        wait_tile<C::kLoads + 1, kStages - 2>(issued - used - 1);
+        wait_tile<C::kLoads + 1>(issued - used > 1);
         // (into the stage that every wave has left behind at the barrier; half of the waves later, so that one of a SIMD's two is
         // computing while the other one asks)
         if (wave < 4) issue();
