@@ -445,6 +445,18 @@ def test_tables_for_very_long_requests(dim, kv_heads):
 
 
 @gpu
+@pytest.mark.parametrize("group,most,sink,window", [(1, 1, 0, 10 ** 6), (3, 5, 0, 10 ** 6), (2, 2, 100, 1500)])
+def test_a_few_long_requests_among_many_short_ones(group, most, sink, window):
+    """Waves that work alone through blocks of 64 quarters of pages and, with several queries, one more."""
+    rng = random.Random(most)
+    lens = [rng.choice([0, 1, 1, 5, 40]) for _ in range(256)]
+    for b in (0, 7, 100, 101, 255):
+        lens[b] = rng.choice([2048, 2047, 2017, 1900])
+    lens[7] = 2048
+    Problem(lens, [min(n, most) for n in lens], 8 * group, 8, 64, 128, sink, window, seed=most, poison=False).check()
+
+
+@gpu
 def test_nan_among_many_short_requests():
     lens, news = [150] * 256, [3] * 256
     clean = Problem(lens, news, 8, 8, 64, 64, 1, 30, seed=9, poison=False)
