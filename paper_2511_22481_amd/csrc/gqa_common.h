@@ -498,7 +498,7 @@ __device__ __forceinline__ Kept kept_of(const GqaDecodeParams& p, const Span& no
 // then the outputs at the common reference, 1 / PARTS of every lane's columns at a time (o_lds: [TG][R][D / PARTS + 4]).  tg: which of the TG
 // the wave is; row0: its first row.  Blocks that other work groups share too leave partial rows in `slot`.
 template <int D, int RT, int R, int TG, int PARTS, int THREADS, bool OUT32, int START>
-__device__ __forceinline__ void finish(const GqaDecodeParams& p, const Dealer<R, THREADS, START>& dealer, const Piece& now, Rows<D, RT>& a, float* o_lds, float4* ml,
+__device__ __forceinline__ void finish(const Dealer<R, THREADS, START>& dealer, const Piece& now, Rows<D, RT>& a, float* o_lds, float4* ml,
                                        int tg, int row0, int slot) {
   constexpr int kCols = D / 16, kOStride = D / PARTS + 4;
   const int tid = threadIdx.x, lane = tid & 63, n16 = lane & 15, g = lane >> 4;

@@ -284,7 +284,7 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
     if constexpr (ALONE) {
       finish_alone<D, kThreads, OUT32>(dealer, dealer.kept(0), a, slot);
     } else {
-      finish<D, RT, R, 4, C::kParts, kThreads, OUT32>(p, dealer, dealer.kept(0), a, o_lds, ml_lds + parity * 4 * R, wave, 0, slot);
+      finish<D, RT, R, 4, C::kParts, kThreads, OUT32>(dealer, dealer.kept(0), a, o_lds, ml_lds + parity * 4 * R, wave, 0, slot);
       parity ^= 1;
     }
     first_partial = 1;

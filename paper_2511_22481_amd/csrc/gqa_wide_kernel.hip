@@ -151,8 +151,8 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
     settle_address(base, same);
     load_lds16_here<0>(base, from[0]);
     load_lds16_here<1024>(base, from[1]);
-    load_lds16_here<2048>(base, from[2]);
-    load_lds16_here<3072>(base, from[3]);
+    load_lds16_here<2 * 1024>(base, from[2]);
+    load_lds16_here<3 * 1024>(base, from[3]);
     load_lds4_each(ring_at + kStages * 2 * C::kHalf + (ahead_stage * kWaves + wave) * C::kScaleBytes,
                    my_scales + ph * blocks_per_page + ((ahead_half * C::kTokens + tg * kWaveTokens) >> p.scale_shift));
     ++issued;
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
       load_q(next);
       dealer.keep(2, next);
     }
-    finish<D, RT, R, TG, C::kParts, kThreads, OUT32>(p, dealer, done, a, o_lds, ml_lds + parity * TG * R, tg, row0, 2 * blockIdx.x + first_partial);
+    finish<D, RT, R, TG, C::kParts, kThreads, OUT32>(dealer, done, a, o_lds, ml_lds + parity * TG * R, tg, row0, 2 * blockIdx.x + first_partial);
     parity ^= 1;
     first_partial = 1;
     if (!more_blocks) break;
