@@ -375,8 +375,8 @@ int omniattn_gqa_append(const omniattn_gqa_t* gqa, int32_t num_tokens, const voi
  *               set and table width, too); calls in flight at once need one each
  * Tokens that a query does not keep may hold anything (NaN too) without effect on it; a kept NaN makes the row NaN.
  * Same inputs give bitwise identical results.  Arithmetic: codes and queries enter the matrix instructions exactly (bf16),
- * logits, sums and outputs are held in fp32; the weights are rounded to f16 (relative 2^-11, down to 2^-25 of a
- * row's largest weight; fp32 results: to two f16 terms, 2^-22 down to 2^-14 and 2^-36 of the largest below that).
+ * logits, sums and outputs are held in fp32; a weight times its value block's scale enters in two f16 terms (relative 2^-22 down to
+ * 2^-14 of the row's largest such product, and 2^-36 of that below).  A bf16 result is the fp32 result rounded.
  *
  * omniattn_gqa_workspace_bytes depends on the current device and on batch, num_queries, the head counts and head_dim;
  * 0 for an invalid problem.

@@ -18,7 +18,7 @@ typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 
 constexpr int kWaveTokens = 32;
 // Weights are 2^(s - m + kLift) for the reference m, which a logit (log2) may exceed by kSlack before it is raised: the largest
-// weight is at most 2^15 (f16 holds 65504), and weights keep full precision down to 2^-25 of the largest.
+// weight is at most 2^15 (f16 holds 65504), and its two f16 terms keep 2^-22 of weights down to 2^-14 of the largest, below that 2^-36 of the largest.
 constexpr float kLift = 11.f, kSlack = 4.f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -381,10 +381,13 @@ struct Rows {
   }
 };
 
-// Weights of a tile of 32 tokens from its S^T (lane (n16, g) has tokens 16 h + 4 g + i of row n16), rounded to f16 (`low`: and what
-// that leaves), references, sums and, where a reference rises, the output.  reach: tokens that the row's query sees; full: every
-// row keeps all 32 tokens, which begin at pos0.
-template <int D, int RT, bool OUT32>
+// Weights of a tile of 32 tokens from its S^T (lane (n16, g) has tokens 16 h + 4 g + i of row n16), in two f16 terms (`low`: what
+// rounding to `high` leaves), references, sums and, where a reference rises, the output.  reach: tokens that the row's query sees; full: every
+// row keeps all 32 tokens, which begin at pos0.  (One term is 2^-11 of a weight: 7 to 9 in a hundred bf16 results then were the neighbour
+// of the right one.  With two a bf16 result is the fp32 result rounded.  us with one / two: 1 request of 131072 56.8 / 56.9, 64 of 32768
+// 713 / 714, 256 short ones of width 64 30.4 / 30.9; 64 requests of 2000 to 16000, 4 KV heads, 64 rows: width 64 75 / 86, 128 132 / 151,
+// 256 238 / 270.)
+template <int D, int RT>
 __device__ __forceinline__ void weigh(const GqaDecodeParams& p, Rows<D, RT>& a, const f32x4 (&s)[RT][2], const int (&reach)[RT], bool full, int pos0,
                                       int g, float k_factor, float v_scale, f16x8 (&high)[RT], f16x8 (&low)[RT]) {
   // (at least 2^-100: ratio stays finite)
@@ -425,9 +428,9 @@ __device__ __forceinline__ void weigh(const GqaDecodeParams& p, Rows<D, RT>& a, 
       float y = w[i] * value;
       // (fixed here: the compiler may fuse the product with one of its two uses and round the other in two steps, which
       // near a tie of f16 leaves the second term for another first term)
-      if constexpr (OUT32) asm("" : "+v"(y));
+      asm("" : "+v"(y));
       high[rt][i] = (_Float16)y;
-      if constexpr (OUT32) low[rt][i] = (_Float16)(y - (float)high[rt][i]);
+      low[rt][i] = (_Float16)(y - (float)high[rt][i]);
     }
     a.l[rt] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
   }
@@ -457,7 +460,7 @@ __device__ __forceinline__ void sanitize(const GqaDecodeParams& p, Rows<D, RT>& 
 }
 
 // O^T += V^T P^T
-template <int D, int RT, bool OUT32>
+template <int D, int RT>
 __device__ __forceinline__ void add_values(Rows<D, RT>& a, const typename VWord<D / 64>::type (&v)[8], const f16x8 (&high)[RT], const f16x8 (&low)[RT]) {
   constexpr int kWords = D / 64;
 #pragma unroll
@@ -472,7 +475,7 @@ __device__ __forceinline__ void add_values(Rows<D, RT>& a, const typename VWord<
       for (int rt = 0; rt < RT; ++rt) {
         f32x4& acc = a.o[rt][4 * wd + col];
         acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, high[rt], acc, 0, 0, 0);
-        if constexpr (OUT32) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, low[rt], acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, low[rt], acc, 0, 0, 0);
       }
     }
   }

@@ -13,7 +13,7 @@
 // A page.  The four waves take 32 of its 128 tokens each and keep a running maximum, sum and output of their own; they meet
 // only at the end of a block's share.  K rows come from memory in the operand order of S^T = K Q^T (16x16x32 bf16 matrix
 // instructions; an e4m3 code is exact in bf16), V rows as 8 tokens x D/16 columns per lane, which a byte permutation turns
-// into the operand of O^T += V^T P^T (f16: exact for the codes, and 2^-11 relative for the weights, which the reference
+// into the operand of O^T += V^T P^T (f16: exact for the codes, two terms and so 2^-22 for the weights, which the reference
 // scales into [0, 2^15]).  The contraction's order of tokens is free, so P^T is what S^T's layout already gives each lane.
 // No LDS and no barrier in the loop (width 256: the query's operands come from LDS).  A block's scale is one number per wave and
 // page: K's goes into the softmax factor, V's into the weights.
@@ -261,9 +261,9 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
       load_k<D>(t, c.k, k_at);
 
       f16x8 high[RT], low[RT];
-      weigh<D, RT, OUT32>(p, a, s, seen, kept.full, pos0, g, k_factor, v_scale, high, low);
+      weigh<D, RT>(p, a, s, seen, kept.full, pos0, g, k_factor, v_scale, high, low);
       if (!kept.full) sanitize<D, RT>(p, a, t.v, span, pos0, g);
-      add_values<D, RT, OUT32>(a, t.v, high, low);
+      add_values<D, RT>(a, t.v, high, low);
       load_v<D>(t, c.v, v_at);
     };
     if (tile < span.tile_hi) {

@@ -245,12 +245,12 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
         if (wave >= 4) issue();
         if (work) {
           f16x8 high[RT], low[RT];
-          weigh<D, RT, OUT32>(p, a, s, reach, kept.full, pos0, g, p.scale_log2 * scale.x, scale.y, high, low);
+          weigh<D, RT>(p, a, s, reach, kept.full, pos0, g, p.scale_log2 * scale.x, scale.y, high, low);
           typename VWord<kWords>::type v[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[j] = *(const typename VWord<kWords>::type*)(from_stage + v_at[j % 4] + j / 4 * 16 * D);
           if (!kept.full) sanitize<D, RT>(p, a, v, span, pos0, g);
-          add_values<D, RT, OUT32>(a, v, high, low);
+          add_values<D, RT>(a, v, high, low);
         }
       }
     }

@@ -853,3 +853,18 @@ def test_the_binding_refuses_wrong_tensors():
         oa.gqa_decode(p.q, k, v, ks, vs, table, lens, 0, 1000, 0.1)
     with pytest.raises(oa.OmniAttnError):
         oa.omniattn_gqa_append(q[:, :2], q[:, :2], ints([1, 2]), k, v, ks, vs)
+
+
+@gpu
+@pytest.mark.parametrize("dim,q_heads,kv_heads,batch,longest,most,window", [
+    (64, 8, 2, 5, 3000, 1, 10 ** 6), (128, 8, 2, 5, 3000, 1, 10 ** 6), (256, 8, 2, 5, 3000, 1, 10 ** 6),      # blocks of 16 rows, cut and joined
+    (64, 8, 2, 3, 900, 7, 10 ** 6), (128, 8, 2, 3, 900, 7, 10 ** 6),                                          # of 32
+    (64, 16, 2, 3, 900, 9, 10 ** 6), (128, 16, 2, 3, 900, 9, 10 ** 6), (256, 16, 2, 3, 900, 9, 10 ** 6),      # of 64
+    (64, 8, 8, 256, 300, 1, 10 ** 6),                                                                         # a wave to a block
+    (128, 8, 2, 5, 3000, 1, 100)])                                                                            # not cut
+def test_bf16_results_are_the_fp32_results_rounded(dim, q_heads, kv_heads, batch, longest, most, window):
+    """Both come from the same sums in fp32, and only the last rounding differs: equal, not only near."""
+    lens = [random.Random(b).randint(most, longest) for b in range(batch)]
+    p = Problem(lens, [most] * batch, q_heads, kv_heads, dim, 64, 4, window, seed=dim + most, poison=False)
+    (want, want_lse), (got, got_lse) = p.run(torch.float32), p.run(torch.bfloat16)
+    assert torch.equal(got, want.bfloat16()) and torch.equal(got_lse, want_lse)
