@@ -13,7 +13,7 @@ LIB = os.path.join(HERE, "libomniattn.so")
 SOURCES = ["decode_kernels.hip", "decode_mid_kernel.hip", "decode_narrow_kernel.hip", "append_kernels.hip",
            "table_kernels.hip", "gqa_append_kernel.hip", "gqa_decode_kernel.hip",
            "gqa_wide_kernel.hip", "api.cpp", "api_gqa.cpp", "plan.cpp"]
-HEADERS = ["kernels.h", "gqa.h", "gqa_common.h", "plan.h", "decode_common.h", os.path.join("..", "..", "include", "omniattn.h")]
+HEADERS = ["kernels.h", "gqa.h", "gqa_common.h", "gqa_deal.h", "plan.h", "decode_common.h", os.path.join("..", "..", "include", "omniattn.h")]
 
 MARSHAL = os.path.join(HERE, "gqa_marshal.so")
 MARSHAL_SOURCE = "gqa_marshal.cpp"

@@ -8,6 +8,7 @@
 
 #include "decode_common.h"
 #include "gqa.h"
+#include "gqa_deal.h"
 
 namespace omniattn {
 namespace {
@@ -24,10 +25,6 @@ constexpr float kLift = 11.f, kSlack = 4.f;
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 
-// What a request brings: its tokens, its first query token and how many it has.
-struct Request {
-  int L, begin, n;
-};
 __device__ __forceinline__ Request request_of(const GqaDecodeParams& p, int b) {
   Request r;
   r.L = min(max(p.seq_lens[b], 0), p.max_pages * kPage);
@@ -35,24 +32,6 @@ __device__ __forceinline__ Request request_of(const GqaDecodeParams& p, int b) {
   r.begin = min(max(lo, 0), p.num_queries);
   r.n = min(max(hi, r.begin), p.num_queries) - r.begin;
   return r;
-}
-// Pages of a block of query rows (GRAIN 32: their quarters): the union of its queries' kept sets.
-struct Block {
-  int t0, t1;  // its query tokens, both included
-  TileLayout pages;
-};
-template <int ROWS, int GRAIN>
-__device__ __forceinline__ Block block_of(const GqaDecodeParams& p, const Request& r, int rb) {
-  Block k;
-  // (rows of a call are counted in 32 bits; most requests have one block, and divisions are what a share's finding consists of)
-  k.t0 = rb ? (int)((uint32_t)(rb * ROWS) / (uint32_t)p.group) : 0;
-  k.t1 = (rb + 1) * ROWS >= r.n * p.group ? r.n - 1 : (int)((uint32_t)((rb + 1) * ROWS - 1) / (uint32_t)p.group);
-  k.pages = tile_layout(r.L - r.n + k.t1 + 1, p.S, p.W > 0 ? p.W + (k.t1 - k.t0) : 0, GRAIN);
-  return k;
-}
-template <int ROWS>
-__device__ __forceinline__ int blocks_of(const GqaDecodeParams& p, const Request& r) {
-  return (r.n * p.group + ROWS - 1) / ROWS;
 }
 __device__ __forceinline__ float row_max(float x) {  // over the four lanes that hold tokens of the same row
   float y = x;
@@ -129,27 +108,6 @@ __device__ __forceinline__ const GqaDecodeParams* late_arguments() {
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// Share u of U: units [bound(u), bound(u + 1)), about u T / U.  Every share has T / U or one more; those with more are spread evenly (the
-// neighbours in a compute unit would have a fifth more to read than others: 256 requests of 12 heads 33 us, in one run 40).
-struct Shares {
-  int64_t T, each;  // each = T / U
-  int U;            // at most 2^14
-  uint32_t more;    // (T % U) 2^17 / U, rounded up
-  __device__ __forceinline__ Shares(int64_t total, int most) : T(total), U((int)min((int64_t)most, total)) {
-    each = T >> 31 ? T / max(U, 1) : (uint32_t)T / (uint32_t)max(U, 1);
-    more = ((uint32_t)(T - each * U) << 17) / (uint32_t)max(U, 1) + 1;
-  }
-  __device__ __forceinline__ Shares() {}
-  __device__ __forceinline__ int64_t bound(int u) const { return u * each + ((uint32_t)u * more >> 17); }
-  // the share that has unit x
-  __device__ __forceinline__ int owner(int64_t x) const {
-    int u = min((int)((float)x * U / (float)T), U - 1);
-    while (bound(u) > x) --u;
-    while (bound(u + 1) <= x) ++u;
-    return u;
-  }
-};
-
 // Running sum over a wave.
 __device__ __forceinline__ int wave_sum_up_to(int x) {
 #define OMNIATTN_ADD(ctrl, rows) x += __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xf, true)
@@ -163,20 +121,6 @@ __device__ __forceinline__ int wave_sum_up_to(int x) {
   return x;
 }
 
-// The part of a block that belongs to a share.
-struct Piece {
-  int b, h, rb;
-  Request rq;
-  Block bk;
-  int off;               // the block's units before it
-  int tile_lo, tile_hi;  // its pages, by their number among the block's
-  int64_t left;          // units of the share from its first one on
-  __device__ __forceinline__ bool whole() const { return tile_lo == 0 && tile_hi == bk.pages.count(); }
-  // tokens that the block's first and last query see
-  __device__ __forceinline__ int reach_lo() const { return rq.L - rq.n + bk.t0 + 1; }
-  __device__ __forceinline__ int reach_hi() const { return rq.L - rq.n + bk.t1 + 1; }
-};
-
 // What a loop over a block's pages needs of it.
 struct Span {
   TileLayout pages;
@@ -188,38 +132,31 @@ struct Span {
         tile_hi(uniform(w.tile_hi)), several(uniform(w.bk.t1 - w.bk.t0) > 0) {}
 };
 
-// Finds shares and walks through their blocks.  R: rows of a block.  START: what a block costs beside its pages (its query, the
-// meeting of the waves, its results), in pages.  SHARES: of a work group, 1 or one for each wave, which counts quarters of pages.  All
-// threads call begin.
+// Finds shares and walks through their blocks (see Walk in gqa_deal.h).  SHARES: of a work group, 1 or one for each wave, which counts quarters of
+// pages.  All threads call begin.
 template <int R, int THREADS, int START, int SHARES = 1>
 struct Dealer {
   static constexpr int kGrain = SHARES > 1 ? kWaveTokens : kPage;
+  using Walker = Walk<R, START, kGrain, GqaDecodeParams>;
 
   // What is needed only from block to block stays here: in scalar registers it would push the loop's own out.
   struct Lds {
     int64_t wave_tot[THREADS / 64], off[SHARES], stop[SHARES];  // the share's first unit among the units of request `at`; its end
-    int4 requests[THREADS];  // (batches of up to THREADS: L, begin, n, units of one KV head)
+    int64_t cost[SHARES];    // (batches of up to THREADS: units of one KV head of that request)
+    int4 requests[THREADS];  // (the same: L, begin, n)
     int at[SHARES];
     Shares shares;
     int pieces[THREADS / 64][3][16];
   };
   const GqaDecodeParams& p;
+  const Walker walk;
   Lds& lds;
   int per;  // requests per thread
 
-  __device__ __forceinline__ Dealer(const GqaDecodeParams& params, Lds& memory) : p(params), lds(memory) {}
+  __device__ __forceinline__ Dealer(const GqaDecodeParams& params, Lds& memory) : p(params), walk(params), lds(memory) {}
 
   __device__ __forceinline__ static int which() { return SHARES > 1 ? uniform(threadIdx.x >> 6) : 0; }
   __device__ __forceinline__ static int share() { return (int)blockIdx.x * SHARES + which(); }
-  __device__ __forceinline__ static int units(const Block& k) { return START + k.pages.count(); }
-  // Units of one KV head of a request
-  __device__ __forceinline__ int64_t cost_of(const Request& r) const {
-    const int blocks = blocks_of<R>(p, r);
-    int64_t sum = 0;
-    for (int rb = 0; rb < blocks; ++rb) sum += units(block_of<R, kGrain>(p, r, rb));
-    return sum;
-  }
-
   __device__ __forceinline__ Request request(int b) const {
     if (per == 1) {
       const int4 r = lds.requests[b];
@@ -228,44 +165,23 @@ struct Dealer {
     const Request r = request_of(p, b);
     return Request{uniform(r.L), uniform(r.begin), uniform(r.n)};
   }
-  __device__ __forceinline__ void cut(Piece& w) const {
-    w.bk = block_of<R, kGrain>(p, w.rq, w.rb);
-    w.tile_lo = max(w.off - START, 0);
-    w.tile_hi = p.uncut ? w.bk.pages.count() : (int)min(max(w.left + w.off - START, (int64_t)0), (int64_t)w.bk.pages.count());
-  }
-  // Whether there is something to do: pages, or the empty result of a block that keeps nothing, which is whose share has its first unit.
-  __device__ __forceinline__ static bool counts(const Piece& w) { return w.tile_lo < w.tile_hi || (w.bk.pages.count() == 0 && w.off == 0); }
   // The next block of the share with something to do; false if there is none.
   __device__ __forceinline__ bool follow(Piece& w) const {
-    do {
-      w.left -= units(w.bk) - w.off;
-      w.off = 0;
-      if (w.left <= 0) return false;
-      if (++w.rb >= blocks_of<R>(p, w.rq)) {
-        w.rb = 0;
-        if (++w.h == p.kv_heads) {
-          w.h = 0;
-          do w.rq = request(++w.b);
-          while (w.rq.n == 0);
-        }
-      }
-      cut(w);
-    } while (!counts(w));
-    return true;
+    return walk.follow(w, [&](int b) { return request(b); });
   }
   // Running sum of the units over the batch, a run of requests per thread; the thread whose requests hold a share's first unit
   // says so.  False: nothing to do for this wave.
   __device__ __forceinline__ bool begin(Piece& now) {
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     per = (p.batch + THREADS - 1) / THREADS;
-    int64_t mine = 0;
+    int64_t mine = 0, cost = 0;
     for (int i = 0; i < per; ++i) {
       const int b = tid * per + i;
       if (b < p.batch) {
         const Request r = request_of(p, b);
-        const int64_t cost = cost_of(r);
+        cost = walk.cost_of(r);
         mine += cost * p.kv_heads;
-        if (per == 1) lds.requests[tid] = make_int4(r.L, r.begin, r.n, (int)cost);
+        if (per == 1) lds.requests[tid] = make_int4(r.L, r.begin, r.n, 0);
       }
     }
     int64_t sum = mine;
@@ -294,6 +210,7 @@ struct Dealer {
       if (u < shares.U && sum - mine <= first && first < sum) {
         lds.at[i] = tid;
         lds.off[i] = first - (sum - mine);
+        lds.cost[i] = cost;
         lds.stop[i] = stop;
         lds.shares = shares;
       }
@@ -304,38 +221,23 @@ struct Dealer {
     const int at = uniform(lds.at[which()]) * per;
     int64_t off = (int64_t)uniform64(lds.off[which()]);
     now.left = shares.bound(share() + 1) - shares.bound(share());
+    now.b = at;
+    now.rq = request(at);
     if (per == 1) {
-      now.b = at;
-      const int4 r = lds.requests[at];
-      now.rq = Request{uniform(r.x), uniform(r.y), uniform(r.z)};
-      const uint32_t cost = uniform(r.w);
-      now.h = (int)((uint32_t)off / cost);  // (one request's units are below 2^31)
-      off -= (int64_t)now.h * cost;
+      cost = (int64_t)uniform64(lds.cost[which()]);
     } else {
-      int64_t cost;
-      for (now.b = at;; ++now.b) {
-        now.rq = request(now.b);
-        cost = cost_of(now.rq);
-        if (off < cost * p.kv_heads) break;
+      while (off >= (cost = walk.cost_of(now.rq)) * p.kv_heads) {
         off -= cost * p.kv_heads;
+        now.rq = request(++now.b);
       }
-      now.h = (int)((uint32_t)off / (uint32_t)cost);
-      off -= now.h * cost;
     }
-    for (now.rb = 0;; ++now.rb) {
-      const int of_block = units(block_of<R, kGrain>(p, now.rq, now.rb));
-      if (off < of_block) break;
-      off -= of_block;
-    }
-    now.off = (int)off;
-    cut(now);
-    return (counts(now) && !(p.uncut && now.off > 0)) || follow(now);
+    return walk.enter(now, off, cost, [&](int b) { return request(b); });
   }
   __device__ __forceinline__ int rows_of(const Piece& w) const { return min(w.rq.n * p.group - w.rb * R, R); }
   // Shares that have a part of the block of w, from this one on (which has its first page).
   __device__ __forceinline__ int partners(const Piece& w) const {
     const Shares shares = lds.shares;
-    return shares.owner(lds.stop[which()] - w.left - w.off + units(w.bk) - 1) - share() + 1;
+    return shares.owner(lds.stop[which()] - w.left - w.off + walk.units(w.bk) - 1) - share() + 1;
   }
   // A wave's notes of blocks, in one of three places.
   __device__ __forceinline__ void keep(int place, const Piece& w) const {
