@@ -57,7 +57,8 @@ def serve(pool, prompts, answers, q_heads, sink, window, rows, chunk=512, graph=
     from . import omniattn_gqa_workspace_bytes
     layers, pages, heads, _, dim = pool.k.shape
     batch, device = len(prompts), pool.k.device
-    most = max(batch, sum(min(n, chunk) for n in prompts))
+    # (a request without a prompt begins with its answer, a token a step)
+    most = max(batch, sum(max(min(p, chunk), min(a, 1)) for p, a in zip(prompts, answers)))
     qkv = torch.empty((layers, most, q_heads + 2 * heads, dim), dtype=torch.bfloat16, device=device)
     out = torch.empty((layers, most, q_heads, dim), dtype=torch.bfloat16, device=device)
     lse = torch.empty((layers, most, q_heads), device=device)

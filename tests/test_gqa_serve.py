@@ -58,3 +58,37 @@ def test_replayed_steps_are_the_called_ones():
 def test_a_pool_has_room_for_every_scale():
     pool = Pool(3, 2, 4, 1, 64, 2, scale_tokens=32, device="cpu")
     assert pool.k.shape == (2, 4, 1, PAGE, 64) and pool.k_scales.shape == (2, 4, 1, 4) and pool.free.tolist() == [0, 1, 2, 3]
+
+
+def _check_step(step, pool, news, granted, out, lse, before):
+    """A step against the reference: lengths, and the results of the requests whose tokens are in the cache."""
+    lens, table, q_start = pool.lens.tolist(), pool.table.tolist(), pool.q_start.tolist()
+    assert lens == [a + n for a, n in zip(before, granted)], step
+    assert q_start == [int(x) for x in np.cumsum([0] + news)], step
+    full = torch.empty((LAYERS, sum(news), Q_HEADS + 2 * HEADS, DIM), dtype=torch.bfloat16)
+    _rows(step, full)
+    rows = np.repeat([n == g for n, g in zip(news, granted)], news)
+    for i in range(LAYERS):
+        cache = [ref.as_double(t[i]) for t in (pool.k, pool.v, pool.k_scales, pool.v_scales)]
+        want, want_lse, tol, lse_tol = ref.attend_bf16(ref.as_double(full[i, :, :Q_HEADS]), *cache, table, lens, q_start, SINK, WINDOW, DIM ** -0.5)
+        assert (np.abs(ref.as_double(out[i, :sum(news)]) - want) <= tol)[rows].all(), (step, i)
+        assert (np.abs(ref.as_double(lse[i, :sum(news)]) - want_lse) <= lse_tol)[rows].all(), (step, i)
+
+
+@gpu
+@pytest.mark.parametrize("graph", [False, True])
+@pytest.mark.parametrize("prompts,answers", [([128, 0], [0, 5]), ([300, 0, 0, 7], [2, 4, 1, 0]), ([0, 0, 0], [3, 1, 2])])
+def test_requests_without_a_prompt(prompts, answers, graph):
+    """Their first tokens come beside whole chunks of the others: the buffers have room for all of them."""
+    pool = Pool(len(prompts), LAYERS, 8, HEADS, DIM, 3)
+    grown = [0] * len(prompts)
+
+    def observe(step, news, out, lse):
+        before = [n if any(w) else 0 for n, w in zip(grown, left)]   # (finished requests have given theirs up)
+        _check_step(step, pool, news, news, out, lse, before)
+        for b, n in enumerate(news):
+            grown[b] += n
+            left[b] = [max(0, left[b][0] - n), left[b][1] - max(0, n - left[b][0])]
+    left = [[p, a] for p, a in zip(prompts, answers)]
+    what = serve(pool, prompts, answers, Q_HEADS, SINK, WINDOW, _rows, chunk=128, graph=graph, observe=observe)
+    assert grown == [p + a for p, a in zip(prompts, answers)] and what["tokens"] == sum(grown) and what["free_at_the_end"] == 8
