@@ -52,7 +52,8 @@ class Pool:
 def serve(pool, prompts, answers, q_heads, sink, window, rows, chunk=512, graph=True, observe=None):
     """Request b brings prompts[b] tokens, `chunk` to a step at most, and then answers[b] more, one to a step.  rows(step, buffer) fills the new
     tokens' rows of all layers, [layers, tokens, query heads + 2 KV heads, head width]; observe(step, new_lens, out, lse) sees what the
-    layers give.  Returns what happened."""
+    layers give.  A request for whose new tokens there are no pages keeps its length (pool.lens; its rows of out and lse mean nothing) and brings
+    them again in the next step, when others may have given pages back.  RuntimeError if a step has pages for none.  Returns what happened."""
     import torch
     from . import omniattn_gqa_workspace_bytes
     layers, pages, heads, _, dim = pool.k.shape
@@ -73,6 +74,7 @@ def serve(pool, prompts, answers, q_heads, sink, window, rows, chunk=512, graph=
             pool.attend(i, qkv[i, :n], slots[:n], out[i, :n], lse[i, :n], workspace, sink, window)
 
     wait, left, captured = list(prompts), list(answers), None
+    held = pool.lens.tolist()
     steps = tokens = used = 0
     decode_us = []
     while any(wait) or any(left):
@@ -99,6 +101,11 @@ def serve(pool, prompts, answers, q_heads, sink, window, rows, chunk=512, graph=
             decode_us.append(begin.elapsed_time(end) * 1000 / layers)
         if observe:
             observe(steps, news, out, lse)
+        # (extend takes a request's tokens as a whole or not at all)
+        lens = pool.lens.tolist()
+        news = [n if after == before + n else 0 for n, before, after in zip(news, held, lens)]
+        if not any(news):
+            raise RuntimeError(f"{int(pool.free_count)} free pages of {pages}, and none of the requests that are left can go on: lengths {lens}, still to come {[w + a for w, a in zip(wait, left)]}")
         steps += 1
         tokens += sum(news)
         used = max(used, pages - int(pool.free_count))
@@ -109,6 +116,7 @@ def serve(pool, prompts, answers, q_heads, sink, window, rows, chunk=512, graph=
         if any(gone):
             done.copy_(torch.tensor(gone, dtype=torch.int32))
             pool.release(done)
+        held = [0 if g else n for g, n in zip(gone, lens)]
     return {"requests": batch, "steps": steps, "tokens": tokens, "pages": used, "free_at_the_end": int(pool.free_count),
             "decode_us_per_layer": sorted(decode_us)[len(decode_us) // 2] if decode_us else None}
 

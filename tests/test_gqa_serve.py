@@ -92,3 +92,37 @@ def test_requests_without_a_prompt(prompts, answers, graph):
     left = [[p, a] for p, a in zip(prompts, answers)]
     what = serve(pool, prompts, answers, Q_HEADS, SINK, WINDOW, _rows, chunk=128, graph=graph, observe=observe)
     assert grown == [p + a for p, a in zip(prompts, answers)] and what["tokens"] == sum(grown) and what["free_at_the_end"] == 8
+
+
+@gpu
+@pytest.mark.parametrize("graph", [False, True])
+@pytest.mark.parametrize("pages", [5, 6, 8])
+def test_a_small_pool_makes_requests_wait(pages, graph):
+    """Fewer pages than the requests have together at the end: those that are refused bring their tokens again, and every token is served once."""
+    pool = Pool(len(PROMPTS), LAYERS, pages, HEADS, DIM, 5)
+    left, grown, refused = [[p, a] for p, a in zip(PROMPTS, ANSWERS)], [0] * len(PROMPTS), 0
+
+    def observe(step, news, out, lse):
+        nonlocal refused
+        before = [n if any(w) else 0 for n, w in zip(grown, left)]
+        granted = [n if now == old + n else 0 for n, old, now in zip(news, before, pool.lens.tolist())]
+        refused += sum(n > g for n, g in zip(news, granted))
+        _check_step(step, pool, news, granted, out, lse, before)
+        for b, n in enumerate(granted):
+            assert n <= (min(left[b][0], 128) or min(left[b][1], 1))
+            grown[b] += n
+            left[b] = [left[b][0] - n, left[b][1]] if left[b][0] else [0, left[b][1] - n]
+    what = serve(pool, PROMPTS, ANSWERS, Q_HEADS, SINK, WINDOW, _rows, chunk=128, graph=graph, observe=observe)
+    assert refused > 0 and grown == [p + a for p, a in zip(PROMPTS, ANSWERS)]
+    assert what["tokens"] == sum(grown) and what["free_at_the_end"] == pages and what["pages"] <= pages
+
+
+@gpu
+@pytest.mark.parametrize("graph", [False, True])
+@pytest.mark.parametrize("pages,columns,prompts,answers", [(2, 5, [300], [7]), (3, 5, [256, 256, 256], [0, 0, 0]), (12, 2, [200, 400], [5, 0]), (1, 1, [128], [1])])
+def test_requests_that_can_never_be_served_are_reported(pages, columns, prompts, answers, graph):
+    """A prompt longer than the pool, requests that hold each other's pages, a table with too few columns: an error, not a count of tokens."""
+    pool = Pool(len(prompts), LAYERS, pages, HEADS, DIM, columns)
+    with pytest.raises(RuntimeError, match="still to come"):
+        serve(pool, prompts, answers, Q_HEADS, SINK, WINDOW, lambda step, buffer: buffer.normal_(), chunk=128, graph=graph)
+    assert int(pool.free_count) == pages - int(((pool.lens + PAGE - 1) // PAGE).sum())
