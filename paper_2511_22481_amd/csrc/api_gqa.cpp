@@ -226,9 +226,9 @@ int omniattn_gqa_decode(const omniattn_gqa_t* gqa, const void* q, int64_t q_stri
   p.kv_heads = gqa->num_kv_heads;
   p.head_dim = gqa->head_dim;
   p.max_pages = gqa->max_pages_per_seq;
-  // (no request is longer than its table: larger numbers mean the same, and sums with them stay in 32 bits)
-  p.S = std::min(gqa->sink, (int)kMaxPages * kPage / 2);
-  p.W = std::min(gqa->window, (int)kMaxPages * kPage / 2);
+  // (no request is longer than its table, 2^31 - 128 tokens at most: larger numbers mean the same, and W + 63 stays in 32 bits)
+  p.S = std::min(gqa->sink, gqa->max_pages_per_seq * kPage);
+  p.W = std::min(gqa->window, gqa->max_pages_per_seq * kPage);
   p.scale_shift = gqa->scale_tokens == 32 ? 5 : gqa->scale_tokens == 64 ? 6 : 7;
   p.out_fp32 = gqa->out_dtype == OMNIATTN_FP32;
   p.uncut = shape.uncut;

@@ -128,7 +128,7 @@ struct Span {
   int tile_hi;
   bool several;          // several queries
   __device__ __forceinline__ explicit Span(const Piece& w)
-      : pages{uniform(w.bk.pages.ns), uniform(w.bk.pages.w0), uniform(w.bk.pages.w1)}, lo(uniform(w.reach_lo())), hi(uniform(w.reach_hi())),
+      : pages{uniform(w.bk.pages.ns), uniform(w.bk.pages.w0), uniform(w.bk.pages.w1)}, lo(uniform(w.reach(w.bk.t0))), hi(uniform(w.reach(w.bk.t1))),
         tile_hi(uniform(w.tile_hi)), several(uniform(w.bk.t1 - w.bk.t0) > 0) {}
 };
 
@@ -463,7 +463,7 @@ __device__ __forceinline__ void finish(const Dealer<R, THREADS, START>& dealer, 
       const uint32_t qt = (uint32_t)(now.rb * R + row) / (uint32_t)end.group, gi = (uint32_t)(now.rb * R + row) - qt * end.group;
       if (__builtin_expect(nans != 0.f, 0)) {
         // NaN that the loop has taken for 0: the columns of the tokens that this row keeps are looked through again
-        const int sees = now.rq.L - now.rq.n + (int)qt + 1;
+        const int sees = now.reach((int)qt);
 #pragma unroll 1
         for (int tile = now.tile_lo; tile < now.tile_hi; ++tile) {
           const int lp = now.bk.pages.logical(tile);
@@ -525,7 +525,7 @@ __device__ __forceinline__ void finish_alone(const Dealer<16, THREADS, START, SH
   const GqaDecodeParams& end = *late_arguments();
   const uint32_t qt = (uint32_t)(now.rb * 16 + row) / (uint32_t)end.group, gi = (uint32_t)(now.rb * 16 + row) - qt * end.group;
   if (__builtin_expect(a.saw_nan != 0.f, 0)) {  // (as in finish)
-    const int sees = now.rq.L - now.rq.n + (int)qt + 1;
+    const int sees = now.reach((int)qt);
     uint32_t nans = 0;  // of the lane's columns
 #pragma unroll 1
     for (int tile = now.tile_lo; tile < now.tile_hi; ++tile) {

@@ -72,9 +72,9 @@ struct Piece {
   int tile_lo, tile_hi;  // its pages, by their number among the block's
   int64_t left;          // units of the share from its first one on
   OA_INLINE bool whole() const { return tile_lo == 0 && tile_hi == bk.pages.count(); }
-  // tokens that the block's first and last query see
-  OA_INLINE int reach_lo() const { return rq.L - rq.n + bk.t0 + 1; }
-  OA_INLINE int reach_hi() const { return rq.L - rq.n + bk.t1 + 1; }
+  // tokens that query t sees: none if it comes before the request's first token (not a negative number, from which a window of nearly 2^31 tokens
+  // could not be subtracted)
+  OA_INLINE int reach(int t) const { return larger(rq.L - rq.n + t + 1, 0); }
 };
 
 // Walks through the blocks of a share.  R: rows of a block.  START: what a block costs beside its pages (its query, the meeting of the waves,

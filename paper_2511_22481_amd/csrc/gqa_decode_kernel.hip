@@ -129,7 +129,7 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
       const int row = rt * 16 + n16;
       const uint32_t t = (uint32_t)(w.rb * R + row) / (uint32_t)p.group, gi = (uint32_t)(w.rb * R + row) - t * p.group;
       const bool valid = row < rows;
-      reach[rt] = valid ? w.rq.L - w.rq.n + (int)t + 1 : 0;
+      reach[rt] = valid ? w.reach((int)t) : 0;
       const uint16_t* src = p.q + (int64_t)(w.rq.begin + (int)t) * p.q_stride + (size_t)(w.h * p.group + (int)gi) * D + g * 16;
       // (operand 2 c + u holds columns 64 c + 16 g + 8 u on; in LDS, the wave brings those with the remainder `wave` by 4)
 #pragma unroll
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
         ids = next.b == ahead_b && next.rb == 0 ? ahead_ids : entries(next.b, next.bk.pages, 0);
         settle(ids);
       }
-      return aim(next.bk.pages, next.h, next.reach_hi(), next.tile_lo, ids, held);
+      return aim(next.bk.pages, next.h, next.reach(next.bk.t1), next.tile_lo, ids, held);
     };
     Rows<D, RT> a;
     a.clear();

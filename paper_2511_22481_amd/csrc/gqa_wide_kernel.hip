@@ -177,7 +177,7 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
       const int row = row0 + rt * 16 + n16;
       const uint32_t t = (uint32_t)(w.rb * R + row) / (uint32_t)p.group, gi = (uint32_t)(w.rb * R + row) - t * p.group;
       const bool valid = row < rows;
-      reach[rt] = valid ? w.rq.L - w.rq.n + (int)t + 1 : 0;
+      reach[rt] = valid ? w.reach((int)t) : 0;
       const uint16_t* src = p.q + (int64_t)(w.rq.begin + (int)t) * p.q_stride + (size_t)(w.h * p.group + (int)gi) * D + g * 16;
 #pragma unroll
       for (int i = 0; i < 2 * kWords; ++i) q[rt][i] = valid ? *(const bf16x8*)(src + i / 2 * 64 + i % 2 * 8) : bf16x8{};

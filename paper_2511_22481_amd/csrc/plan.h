@@ -46,8 +46,8 @@ OA_HD inline TileLayout tile_layout(int L, int S, int W, int tile = kTile) {
   int sink_end = S < L ? S : L;                 // sink range [0, sink_end)
   bool has_recent = W > 0 && L > 0;             // recent range [max(L - W, 0), L)
   int win_lo = L - W > 0 ? L - W : 0;
-  t.ns = (sink_end + tile - 1) / tile;
-  t.w1 = has_recent ? (L + tile - 1) / tile : 0;
+  t.ns = (sink_end + (tile - 1)) / tile;         // (brackets: the longest requests end 128 below 2^31)
+  t.w1 = has_recent ? (L + (tile - 1)) / tile : 0;
   int w0 = has_recent ? win_lo / tile : 0;
   t.w0 = w0 > t.ns ? w0 : t.ns;                 // tiles shared with the sink range count once
   if (t.w0 > t.w1) t.w0 = t.w1;

@@ -868,3 +868,29 @@ def test_bf16_results_are_the_fp32_results_rounded(dim, q_heads, kv_heads, batch
     p = Problem(lens, [most] * batch, q_heads, kv_heads, dim, 64, 4, window, seed=dim + most, poison=False)
     (want, want_lse), (got, got_lse) = p.run(torch.float32), p.run(torch.bfloat16)
     assert torch.equal(got, want.bfloat16()) and torch.equal(got_lse, want_lse)
+
+
+@gpu
+@pytest.mark.parametrize("sink,window", [(0, 2 ** 31 - 1), (2 ** 31 - 1, 0), (0, 2 ** 30 + 1000), (100, 2 ** 30 + 900), (0, 2 ** 30 - 100)])
+@pytest.mark.parametrize("dim,q_heads", [(64, 1), (128, 1), (128, 40)])
+def test_requests_of_more_than_2_30_tokens(dim, q_heads, sink, window):
+    """The first page holds nearly all of the weight, one page of zero keys and values stands for all the others.  Logits are 40 and 0, so the 2^30 others are
+    2^30 exp(-40) / 128 = 4e-11 of the sum, and what the rounding of their own sum does is far below the tolerance: 128 weights and their sum (2^-22, 2^-24
+    each), logits of 40 (2^-20 for the products, the factor and exp2)."""
+    length = 2 ** 30 + 1000
+    columns = -(-length // PAGE)
+    table = torch.zeros((1, columns), dtype=torch.int32, device="cuda")
+    table[0, 0] = 1
+    k, v = torch.zeros((2, 2, 1, PAGE, dim), dtype=torch.float32)
+    k[1], v[1] = 1.0, (torch.arange(PAGE) % 5).float()[None, :, None]
+    k, v = (t.to(torch.float8_e4m3fn).cuda() for t in (k, v))
+    ones = torch.ones((2, 1, 2), device="cuda")
+    q = torch.ones((1, q_heads, dim), dtype=torch.bfloat16, device="cuda")
+    out, lse = oa.gqa_decode(q, k, v, ones, ones, table, ints([length]), sink, window, 40 / dim, out_dtype=torch.float32)
+    kept = [j for j in range(PAGE) if j < sink or j >= length - window]
+    if kept:
+        want, want_lse = sum(j % 5 for j in kept) / len(kept), 40 + np.log(len(kept))
+    else:
+        want, want_lse = 0.0, np.log(window)
+    assert np.abs(ref.as_double(lse) - want_lse).max() <= 40 * 2.0 ** -20 + 128 * 2.0 ** -23 + (0 if kept else 1e-3)
+    assert np.abs(ref.as_double(out) - want).max() <= 4 * (40 * 2.0 ** -20 + 128 * 2.0 ** -22)

@@ -48,3 +48,11 @@ def test_ordinary_calls(driver):
 ])
 def test_prompts_of_more_units_than_32_bits(driver, shape, heads, group, shares, requests):
     driver([(shape, heads, group, 0, 2 ** 30, False, shares, requests)])
+
+
+@pytest.mark.parametrize("shape", SHAPES[:3])
+def test_windows_and_requests_of_nearly_2_31_tokens(driver, shape):
+    """The longest table and whatever keeps all of it; more queries than tokens beside it."""
+    most = 2 ** 31 - 128
+    for sink, window in ((0, most), (most, 0), (most, most), (5, most - 1), (2 ** 30, 2 ** 30)):
+        driver([(shape, 2, 1, sink, window, False, 256, [(most, 64), (3, 70), (most - 77, 1), (0, 5)])])
