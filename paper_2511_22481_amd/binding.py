@@ -403,7 +403,9 @@ def _native():
     if _marshal is None:
         import importlib.util
         import torch   # (its libraries have to be loaded before the module is)
+        from .build import build_marshal
         lib = load_library()
+        build_marshal(force=False)   # (as load_library: never one that is older than its sources)
         spec = importlib.util.spec_from_file_location("gqa_marshal", os.path.join(HERE, "gqa_marshal.so"))
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)

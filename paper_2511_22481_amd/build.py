@@ -1,7 +1,6 @@
-"""Compile the HIP library for gfx950 in-tree (paper_2511_22481_amd/libomniattn.so), and the binding's module that reads torch tensors
-(paper_2511_22481_amd/gqa_marshal.so, host code)."""
+"""Compile the HIP library for gfx950 in-tree (paper_2511_22481_amd/libomniattn.so), which needs hipcc and nothing else, and the binding's
+module that reads torch tensors (paper_2511_22481_amd/gqa_marshal.so, host code), which needs g++ and torch."""
 import hashlib
-import importlib.metadata
 import os
 import subprocess
 import sys
@@ -27,14 +26,13 @@ def hipcc():
 
 
 STAMP = LIB + ".stamp"   # hash of the sources the library was built (and checked) from
+MARSHAL_STAMP = MARSHAL + ".stamp"
 CHECKER = os.path.join(HERE, "check_isa.py")
 
 
 def source_hash():
     h = hashlib.sha256()
-    # (the module is built against one interpreter and one torch)
-    h.update(f"{sys.implementation.cache_tag} {importlib.metadata.version('torch')}".encode())
-    for f in sorted(SOURCES + HEADERS + [MARSHAL_SOURCE]):
+    for f in sorted(SOURCES + HEADERS):
         h.update(f.encode())
         h.update(open(os.path.join(CSRC, f), "rb").read())
     h.update(open(CHECKER, "rb").read())
@@ -44,7 +42,7 @@ def source_hash():
 def is_stale():
     """True unless the library exists and was built, and its generated code checked, from
     exactly the present sources (content hash, so that file times do not matter)."""
-    if not os.path.exists(LIB) or not os.path.exists(MARSHAL) or not os.path.exists(STAMP):
+    if not os.path.exists(LIB) or not os.path.exists(STAMP):
         return True
     return open(STAMP).read().strip() != source_hash()
 
@@ -61,12 +59,7 @@ def build(force=True, verbose=False):
            "-Wno-unused-command-line-argument", "-parallel-jobs=8", "-x", "hip"]
     cmd += [os.path.join(CSRC, f) for f in SOURCES]
     cmd += ["-o", LIB]
-    marshal = subprocess.Popen(marshal_command(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
-    said = marshal.communicate()[0]
-    if marshal.returncode != 0:
-        print(said)
-        raise RuntimeError("building the binding's module failed")
     if verbose or res.returncode != 0:
         print(res.stdout)
         print("\n".join(l for l in res.stderr.splitlines()
@@ -77,6 +70,37 @@ def build(force=True, verbose=False):
     with open(STAMP, "w") as f:     # only a library whose generated code passed the check is stamped
         f.write(source_hash() + "\n")
     return LIB
+
+
+def marshal_hash():
+    """What the module is built from: its sources, one interpreter and one torch."""
+    import torch
+    h = hashlib.sha256(f"{sys.implementation.cache_tag} {torch.__version__}".encode())
+    for f in (MARSHAL_SOURCE, os.path.join("..", "..", "include", "omniattn.h")):
+        h.update(open(os.path.join(CSRC, f), "rb").read())
+    return h.hexdigest()
+
+
+def marshal_is_stale():
+    """is_stale, of the binding's module."""
+    if not os.path.exists(MARSHAL) or not os.path.exists(MARSHAL_STAMP):
+        return True
+    return open(MARSHAL_STAMP).read().strip() != marshal_hash()
+
+
+def build_marshal(force=True):
+    """The binding's module, with g++ against the torch that is installed."""
+    if not force and not marshal_is_stale():
+        return MARSHAL
+    if os.path.exists(MARSHAL_STAMP):
+        os.remove(MARSHAL_STAMP)
+    res = subprocess.run(marshal_command(), capture_output=True, text=True)
+    if res.returncode != 0:
+        print(res.stdout, res.stderr)
+        raise RuntimeError("building the binding's module failed")
+    with open(MARSHAL_STAMP, "w") as f:
+        f.write(marshal_hash() + "\n")
+    return MARSHAL
 
 
 def marshal_command():
@@ -118,5 +142,11 @@ def check_generated_code(verbose=False):
 if __name__ == "__main__":
     import sys
     sys.path.insert(0, os.path.dirname(HERE))
-    from paper_2511_22481_amd.build import build as _b
+    from paper_2511_22481_amd.build import build as _b, build_marshal as _m
     print(_b(verbose=True))
+    try:
+        import torch  # noqa: F401
+    except ImportError:
+        print("no torch: the binding's module for its tensors is not built")
+    else:
+        print(_m())
