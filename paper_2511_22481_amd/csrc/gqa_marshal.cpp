@@ -50,10 +50,10 @@ struct Call {
   int32_t* ints(PyObject* o, int64_t n, const char* name) { return ints(tensor(o, name), n, name); }
   int32_t* table(PyObject* o, int64_t batch, int32_t& columns, int64_t& stride) {
     const at::Tensor& t = tensor(o, "page_table");
-    if (t.scalar_type() != at::kInt || t.dim() != 2 || t.size(0) != batch || t.stride(1) != 1 || t.size(1) > INT32_MAX || !here(t))
+    if (t.scalar_type() != at::kInt || t.dim() != 2 || t.size(0) != batch || (t.stride(1) != 1 && t.size(1) > 1) || t.size(1) > INT32_MAX || !here(t))
       refuse("page_table: int32 CUDA tensor [batch, pages] wanted, its rows contiguous");
     columns = static_cast<int32_t>(t.size(1));
-    stride = t.stride(0);
+    stride = t.size(0) > 1 ? t.stride(0) : columns;  // (of a single row it may be anything)
     return static_cast<int32_t*>(t.data_ptr());
   }
   // bf16 rows [tokens, heads, dim] with any stride from token to token

@@ -894,3 +894,27 @@ def test_requests_of_more_than_2_30_tokens(dim, q_heads, sink, window):
         want, want_lse = 0.0, np.log(window)
     assert np.abs(ref.as_double(lse) - want_lse).max() <= 40 * 2.0 ** -20 + 128 * 2.0 ** -23 + (0 if kept else 1e-3)
     assert np.abs(ref.as_double(out) - want).max() <= 4 * (40 * 2.0 ** -20 + 128 * 2.0 ** -22)
+
+
+@gpu
+@pytest.mark.parametrize("batch,columns", [(1, 4), (3, 1), (1, 1)])
+def test_tables_of_one_row_or_one_column_whatever_their_strides(batch, columns):
+    """A stride that no element is reached by may be any number: a column seen as the only row, a row seen as the only column."""
+    lens = [columns * PAGE - 9 - b for b in range(batch)]
+    p = Problem(lens, [1] * batch, 4, 2, 128, 64, 0, 10 ** 6, seed=batch)
+    (want, want_lse), (k, v), (ks, vs) = p.run(torch.bfloat16), p.codes.cuda(), p.scales.cuda()
+    table = ints(p.table)
+    odd = torch.full((columns, batch), 7, dtype=torch.int32, device="cuda").t().copy_(table)   # strides (1, batch)
+    wide = torch.full((batch, 2 * columns), 7, dtype=torch.int32, device="cuda")[:, ::2]         # strides (2 columns, 2)
+    tables = [odd] + ([wide.copy_(table)] if columns == 1 else [])
+    assert all(t.shape == table.shape and torch.equal(t, table) for t in tables)
+    for t in tables:
+        out, lse = oa.gqa_decode(p.q.cuda(), k, v, ks, vs, t, ints(p.lens), 0, 10 ** 6, p.scale)
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+        before = [n - 1 for n in lens]
+        free, count, q_start, slots = ints([50, 51, 52]), ints([3]), torch.empty(batch + 1, dtype=torch.int32, device="cuda"), torch.empty(batch, dtype=torch.int32, device="cuda")
+        got = torch.empty(batch, dtype=torch.int32, device="cuda")
+        oa.omniattn_table_extend(ints(before), ints([1] * batch), free, count, t, got, torch.empty_like(count), q_start, slots)
+        assert got.tolist() == lens and slots.tolist() == [p.table[b][n // PAGE] * PAGE + n % PAGE for b, n in enumerate(before)]
+        oa.omniattn_table_release(got, ints([1] * batch), t, torch.empty(batch * columns, dtype=torch.int32, device="cuda"), ints([0]))
+        assert got.tolist() == [0] * batch
