@@ -918,3 +918,32 @@ def test_tables_of_one_row_or_one_column_whatever_their_strides(batch, columns):
         assert got.tolist() == lens and slots.tolist() == [p.table[b][n // PAGE] * PAGE + n % PAGE for b, n in enumerate(before)]
         oa.omniattn_table_release(got, ints([1] * batch), t, torch.empty(batch * columns, dtype=torch.int32, device="cuda"), ints([0]))
         assert got.tolist() == [0] * batch
+
+
+@gpu
+def test_the_binding_refuses_wrong_tables():
+    """int32 tables that would be read out of their rows: columns apart, too many or too few rows, rows that overlap, other numbers of dimensions."""
+    p = Problem([200, 77], [1, 1], 4, 2, 128, 64, 0, 1000, seed=1)
+    k, v = p.codes.cuda()
+    ks, vs = p.scales.cuda()
+    q, lens = p.q.cuda(), ints(p.lens)
+    columns = len(p.table[0])
+    assert columns == 2
+    good = torch.full((4, 2 * columns), 1, dtype=torch.int32, device="cuda")
+    good[:2, :columns] = ints(p.table)
+    bad = [good[:2, ::2], good[:3, :columns], good[:1, :columns], good[0, :columns], good[:2, None, :columns], good[:columns, :2].t(), good[:1, :columns].expand(2, columns),
+           torch.as_strided(good, (2, columns), (1, 1)), good[:2, :0]]
+    for t in bad:
+        with pytest.raises(oa.OmniAttnError) as e:
+            oa.gqa_decode(q, k, v, ks, vs, t, lens, 0, 1000, 0.1)
+        assert e.value.code == -1, t.shape
+        n = torch.zeros(3, dtype=torch.int32, device="cuda")
+        with pytest.raises(oa.OmniAttnError) as e:
+            oa.omniattn_table_extend(lens, lens, ints([1]), ints([1]), t, lens, ints([1]), n, n)
+        assert e.value.code == -1
+        with pytest.raises(oa.OmniAttnError) as e:
+            oa.omniattn_table_release(lens, lens, t, ints([1]), ints([1]))
+        assert e.value.code == -1
+    want = oa.gqa_decode(q, k, v, ks, vs, ints(p.table), lens, 0, 1000, 0.1)
+    got = oa.gqa_decode(q, k, v, ks, vs, good[:2, :columns], lens, 0, 1000, 0.1)
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and lens.tolist() == p.lens
