@@ -373,7 +373,8 @@ int omniattn_gqa_append(const omniattn_gqa_t* gqa, int32_t num_tokens, const voi
  *   lse         device, fp32 [N, num_q_heads], natural logarithm.  A query that keeps nothing gives 0 and -inf.
  *   workspace   device, omniattn_gqa_workspace_bytes(gqa) bytes, 256-byte aligned (enough for calls of fewer queries, and of any kept
  *               set and table width, too); calls in flight at once need one each
- * Tokens that a query does not keep may hold anything (NaN too) without effect on it; a kept NaN makes the row NaN.
+ * Tokens that a query does not keep may hold anything (NaN too) without effect on it; a kept NaN in a K row makes the query's row and
+ * its lse NaN, one in a V row the columns in which it stands.
  * Same inputs give bitwise identical results.  Arithmetic: codes and queries enter the matrix instructions exactly (bf16),
  * logits, sums and outputs are held in fp32; a weight times its value block's scale enters in two f16 terms (relative 2^-22 down to
  * 2^-14 of the row's largest such product, and 2^-36 of that below).  A bf16 result is the fp32 result rounded.

@@ -11,8 +11,8 @@
 // and the rounding, so they are read once.  Runs that fit one pass of a wave are dealt out to the waves, and single tokens (a
 // decode step's) to the groups of lanes that hold a row, so that the 32 of a mixed step's C are two passes and not eight.
 //
-// What bounds it: 65536 tokens of 8 heads of 128 (302 MB) 66 us, 4.6 TB/s of the 4.78 that a copy reaches.  A decode step's 64 tokens 4.4 us: a
-// launch, and slots, rows and scales one behind the other.  133 requests with chunks of prompts (5.7 MB) 8.1 us: the same, once for
+// What bounds it: 65536 tokens of 8 heads of 128 (302 MB) 67 us, 4.5 TB/s of the 4.78 that a copy reaches.  A decode step's 64 tokens 4.2 us: a
+// launch, and slots, rows and scales one behind the other.  133 requests with chunks of prompts (5.7 MB) 7.6 us: the same, once for
 // the single tokens and once or twice for long runs.
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -23,10 +23,10 @@
 //
 // What bounds it: up to 32 rows (64 at width 64), memory.  A work group has one tile of each wave under way (16 to 64 KB a compute
 // unit), asked for as soon as the registers of the tile before are free; the loads are without conditions and every wait is for as
-// many as are needed, no more.  64 requests of 32768 tokens, 8 KV heads of width 128 (4.30 GB): 739 us, 5.8 TB/s, where nothing but
-// reading them in this order reaches 6.25.  One request of 131072 (268 MB): 52 us, of which 5 pass before the first product (a chain
+// many as are needed, no more.  64 requests of 32768 tokens, 8 KV heads of width 128 (4.30 GB): 733 us, 5.9 TB/s, where nothing but
+// reading them in this order reaches 6.25.  One request of 131072 (268 MB): 53 us, of which 5 pass before the first product (a chain
 // of four loads: lengths, table, codes, query) and 3 at the end.  93 ragged requests of 200 to 20000, 4 KV heads: 78 us, 5 TB/s.
-// 64 requests of 2000 to 16000, 4 KV heads of width 128, 32 rows: 103 us, 4.6 TB/s; above, gqa_wide_kernel.hip is faster.
+// 64 requests of 2000 to 16000, 4 KV heads of width 128, 32 rows: 108 us, 4.4 TB/s; above, gqa_wide_kernel.hip is faster.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -443,28 +443,30 @@ hipError_t allow_lds() {
 
 }  // namespace
 
-// By the average number of query rows of a request and KV head.  us a call, 64 requests of 2000 to 16000 tokens, 4 KV heads; "tiles": this
-// kernel with so many row tiles (several blocks where the rows are more):
+// By the average number of query rows of a request and KV head.  (The lengths are on the device, so the host knows no more.  All that follows was
+// measured with as many new tokens for every request; a chunk of a prompt among many single tokens is cut into the few-row blocks of
+// their mean, and is not measured.)  us a call, 64 requests of 2000 to 16000 tokens, 4 KV heads; "tiles": this kernel with so many row tiles
+// (several blocks where the rows are more):
 //   width 64   rows 16  24  32  40  64 128    width 128  rows 16  24  32  40  64 128    width 256  rows 16  24  32  40  64 128
-//   1 tile          55  86  79 104 141 296    1 tile          93 148 157 219 275 556    1 tile         181 281 287 409 523 977
-//   2 tiles         53  60  57  82  88 171    2 tiles         95 101 108 156 159 301    wide           179 180 182 217 247 423
-//   4 tiles         67  79  70  69  75 142    wide           102 107 115 136 139 265
+//   1 tile          54  85  79 103 143 300    1 tile          92 149 157 220 274 553    1 tile         181 281 285 411 523 981
+//   2 tiles         54  62  58  89  97 191    2 tiles         96 101 108 160 160 305    wide           178 189 183 232 262 462
+//   4 tiles         80  90  82  81  87 170    wide           106 111 119 144 152 294
 // (Up to 16 rows of width 256 the two are alike at these lengths; short requests end and begin faster with this kernel.)
 // Waves that work alone: a block costs them 3 us less, as they need not meet, but they leave more partial rows and have less under way where
-// blocks are long.  256 requests, 12 KV heads of width 64, us with them and without: 128 tokens each 13.4 / 18.1, 1 to 2000 (window 1024)
-// 29.9 / 35.1, 1024 each 84 / 80, 2048 each 154 / 149; 128 requests of 500 to 8000 tokens, 8 KV heads 85 / 83.5.  At width 128 they lose from
+// blocks are long.  256 requests, 12 KV heads of width 64, us with them and without: 128 tokens each 14.3 / 19.8, 1 to 2000 (window 1024)
+// 29.3 / 36.5, 1024 each 85 / 81, 2048 each 155 / 150; 128 requests of 500 to 8000 tokens, 8 KV heads 82 / 82.  At width 128 they lose from
 // 50 to 1000 tokens on (200 requests, 8 KV heads: 44 / 41.5), and so they are for many short blocks of width 64.
 // Blocks that cannot have more than a few pages go whole to a share: nothing has to be joined, which saves the second launch (2 to 3 us,
 // and 3 us of the host's time).  us cut / uncut, all requests of so many pages (4 query heads to a KV head but for width 64; "wide": 40 rows):
 //   requests x heads     1 page      2            3            4            6            8
-//   width 128   1 x 8     8.6/7.0   10.1/7.8     10.1/8.5     10.1/9.2     10.1/10.5    10.3/11.9
-//              16 x 8     9.6/7.7   12.7/10.6    14.0/11.8    14.1/13.3    14.6/16.6    15.7/19.7
-//             256 x 8    25.3/22.9  31.0/28.6    47.4/44.7    58.7/56.0    81.4/78.6   104.9/102.2
-//   width 64   16 x 12    9.6/7.9   12.3/10.4    12.6/9.6     14.6/14.1    15.1/17.0    15.1/19.4
-//   alone     256 x 12   15.3/13.3  19.1/17.0    20.6/19.7    22.2/24.7    23.2/28.7    26.4/34.9   (lengths up to so many pages)
-//   width 256   1 x 2    10.4/8.9   11.8/10.1    11.7/11.3    11.8/12.3    11.8/14.6    11.8/17.0
-//   wide        1 x 2    15.9/14.4  16.8/17.8    16.9/21.3    16.9/24.6    16.8/31.4    17.0/38.3
-//              64 x 2    18.8/16.6  22.7/20.3    26.1/23.7    29.2/27.0    32.8/33.7    36.6/41.0
+//   width 128   1 x 8     8.0/6.4    9.5/7.2      9.6/8.0      9.5/8.7      9.6/10.1     9.7/11.6
+//              16 x 8     9.0/7.1   12.0/9.6     13.1/11.0    13.3/12.8    13.8/16.4    15.2/19.7
+//             256 x 8    23.0/20.5  29.6/27.1    46.2/43.7    58.0/55.4    81.4/78.6   103.9/101.2
+//   width 64   16 x 12    8.8/7.0   11.6/9.7     11.7/8.9     13.6/13.7    14.5/17.0    14.3/19.6
+//   alone     256 x 12   16.0/13.4  17.3/16.9    18.9/18.9    19.8/24.2    21.6/30.2    23.3/37.9   (lengths up to so many pages)
+//   width 256   1 x 2     9.8/8.3   11.3/9.6     11.3/10.9    11.3/12.1    11.3/14.6    11.4/17.1
+//   wide        1 x 2    14.9/13.4  16.0/17.3    16.1/21.1    16.0/24.7    16.0/32.2    16.3/39.6
+//              64 x 2    18.0/15.9  22.5/19.9    26.2/23.7    29.7/27.5    33.4/34.7    37.3/42.2
 GqaShape gqa_shape(int batch, int num_queries, int group, int kv_heads, int head_dim, int64_t pages, int cus) {
   const int64_t rows = (int64_t)((num_queries + batch - 1) / batch) * group;
   if (rows <= 16) {

@@ -8,9 +8,10 @@
 // tile.
 //
 // What bounds it: the vector unit.  A tile of 32 tokens and 16 rows of width 256 costs a wave 192 conversions and permutations of
-// codes and 130 instructions of softmax beside 32 to 48 matrix instructions, and the two waves of a SIMD take 4600 cycles for it where
-// the codes would arrive in 2600.  64 requests of 2000 to 16000 tokens, 4 KV heads: width 128 139 us at 64 rows and 136 at 40 (3.3
-// TB/s, 420 TFLOP/s at 64), width 256 182 at 32 rows, 217 at 40, 247 at 64.  (More row tiles to a wave would share the conversions, but
+// codes and 130 instructions of softmax beside 48 matrix instructions, and the two waves of a SIMD take 4600 cycles for it where
+// the codes would arrive in 2600.  64 requests of 2000 to 16000 tokens, 4 KV heads: width 128 152 us at 64 rows and 144 at 40 (3.0
+// TB/s, 381 TFLOP/s at 64), width 256 183 at 32 rows, 232 at 40, 262 at 64.  Chunks of 512 tokens of 64 requests' prompts, 32/8 heads of 128:
+// 642 us, 266 TFLOP/s (the codes are converted again for every 64 rows of a chunk).  (More row tiles to a wave would share the conversions, but
 // at width 256 two leave no registers, and at width 128 four leave one wave to a SIMD.)
 #include <hip/hip_runtime.h>
 #include <stdint.h>

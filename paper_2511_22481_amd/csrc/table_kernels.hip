@@ -5,7 +5,7 @@
 // of the pages that requests up to b lack, page k of request b is free[count - 1 - (N_b - need_b) - k].  Everything
 // follows from two running sums over the batch (tokens and pages), so no entry waits for another request's.
 //
-// What bounds it: a launch and a chain of dependent loads.  64 requests of a token 2.4 us, 256 with chunks of up to 512 tokens 4.4, 1500 requests'
+// What bounds it: a launch and a chain of dependent loads.  64 requests of a token 2.4 us, 256 of which 32 bring up to 512 tokens 4.5, 1500 requests'
 // prompts (25000 slots) 5.9.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
