@@ -388,6 +388,112 @@ int omniattn_gqa_decode(const omniattn_gqa_t* gqa, const void* q, int64_t q_stri
                         const int32_t* q_start, void* out, float* lse, void* workspace, size_t workspace_bytes,
                         void* hip_stream);
 
+/*
+ * Speculative decoding on grouped-query layers.  Every request brings a tree of drafted tokens instead of one token: node 0 is the last
+ * token of its text (the one that the step before has chosen), every other node follows its parent, which comes before it.  The nodes are
+ * the request's new tokens: omniattn_table_extend counts them, omniattn_gqa_append puts their rows behind the text, in the nodes'
+ * order.  The rest of a step:
+ *
+ *   1. omniattn_tree_masks      which nodes each node follows, and its position in the text (for a rotation of queries and keys)
+ *   2. omniattn_gqa_tree        attention of the nodes' queries, for every layer
+ *   3. omniattn_tree_verify     which nodes stay, and the tokens that follow them
+ *   4. omniattn_gqa_keep        rows of the nodes that stay move up behind the text, for all layers
+ *   5. omniattn_table_truncate  the other nodes and their pages go
+ *
+ * A request has n = q_start[b + 1] - q_start[b] <= OMNIATTN_TREE_NODES nodes, as omniattn_table_extend numbers them (q_start NULL: one
+ * each).  Like the calls above these are asynchronous, allocate nothing and read no length on the host; arrays of nodes lie behind one another
+ * as the requests do; rows of no request are left as they are.
+ */
+#define OMNIATTN_TREE_NODES 64
+
+/*
+ *   parents    device, int32 [num_tokens]: the parent's number among the request's nodes.  One that does not come before the node (such as -1):
+ *              the node follows the text directly.
+ *   seq_lens   device, int32 [batch]: lengths with the nodes
+ *   masks      device, uint64 [num_tokens]: bit a is set if the node follows node a or is node a.  0 for every node of a request with
+ *              too many.
+ *   positions  device, int32 [num_tokens] or NULL: L - n + (bits of the mask) - 1; -1 in a request with too many nodes
+ */
+int omniattn_tree_masks(int32_t batch, int32_t num_tokens, const int32_t* parents, const int32_t* seq_lens, const int32_t* q_start,
+                        uint64_t* masks, int32_t* positions, void* hip_stream);
+
+/*
+ * Attention of the nodes' queries.  As omniattn_gqa_decode, except for what a query sees: with t the number of bits of its mask among the
+ * request's nodes and P = L - n + t - 1 its position, the tokens j < L - n of the text with j < sink or j > P - window, and the nodes a of its mask
+ * whose own positions L - n + (bits of the mask below a) pass the same test.  (Any set of nodes will do, a tree's or not.)  A query whose mask
+ * has no bit of a node keeps nothing.
+ *   masks       device, uint64 [N].  Bits of nodes that the request does not have do not count; nodes from number 64 on are seen by none.
+ */
+int omniattn_gqa_tree(const omniattn_gqa_t* gqa, const void* q, int64_t q_stride, const void* k_cache, const void* v_cache, const float* k_scales,
+                      const float* v_scales, const int32_t* page_table, const int32_t* seq_lens, const int32_t* q_start,
+                      const uint64_t* masks, void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* What a verification is about. */
+typedef struct {
+  int32_t batch;              /* B >= 1 requests                                                  */
+  int32_t num_tokens;         /* N: all requests' nodes together                                  */
+  int32_t vocab;              /* V >= 1                                                           */
+  int32_t logits_dtype;       /* OMNIATTN_BF16 | OMNIATTN_FP32                                    */
+} omniattn_verify_t;
+
+/*
+ * Which drafted tokens stay.  Row i of `logits` is the target's for the token behind node i; p = softmax(logits / T), T the request's
+ * temperature.  For every node a token y is chosen:
+ *   T not above 0    the first of the largest logits
+ *   no draft_probs   y = the first v with p_0 + .. + p_v > u1 (p_0 + .. + p_V-1)
+ *   draft_probs      row i is the distribution q that the token of the node's first child was drawn from.  That child x is taken if
+ *                    u0 q(x) < p(x).  Otherwise y is chosen as above with max(p - q, 0) in p's place (with p, if that is 0 everywhere).
+ *                    A node without children is treated as without q.
+ * From node 0 on, the first child whose token is y is the path's next node; the path ends where there is none.  So the tokens along the path
+ * and the one behind it are distributed as the target's own, however the drafts were found (other children than a first one must not depend on
+ * u1).  u0, u1 = uniforms[i], in [0, 1).
+ *
+ *   logits       device, logits_dtype [N, V]; logits_stride elements from one row to the next.  NaN counts as -inf.  A row with +inf gives
+ *                the first such token, one of -inf only gives -1, which ends the path.
+ *   draft_probs  device, fp32 [N, V], draft_stride elements from one row to the next; or NULL
+ *   tokens       device, int32 [N]: the nodes' tokens (those outside [0, V) are never taken)
+ *   parents      as for omniattn_tree_masks; nodes that do not descend from node 0 are not reached
+ *   temperature  device, fp32 [B]
+ *   uniforms     device, fp32 [N, 2]
+ *   path         device, int32 [N]: for every request the nodes that stay, in ascending order from node 0 on, then -1
+ *   out_tokens   device, int32 [N]: the token behind each of them; the last one is new; then -1
+ *   logprobs     device, fp32 [N] or NULL: ln p of these tokens (T not above 0: at temperature 1); then 0
+ *   dropped      device, int32 [B]: nodes that do not stay
+ *   workspace    device, omniattn_tree_verify_workspace_bytes(verify) bytes, 256-byte aligned (enough for fewer nodes, too); calls in
+ *                flight at once need one each
+ * A request with too many nodes keeps none.  Probabilities and sums are in 64 bits.  Same inputs give the same results.
+ */
+size_t omniattn_tree_verify_workspace_bytes(const omniattn_verify_t* verify);
+int omniattn_tree_verify(const omniattn_verify_t* verify, const void* logits, int64_t logits_stride, const float* draft_probs, int64_t draft_stride,
+                         const int32_t* tokens, const int32_t* parents, const int32_t* q_start, const float* temperature,
+                         const float* uniforms, int32_t* path, int32_t* out_tokens, float* logprobs, int32_t* dropped,
+                         void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Rows of the nodes that stay move up in the cache: row L - n + path[i] goes to row L - n + i, in num_layers layers that lie behind one
+ * another, for K and V.  (Of `gqa`: batch, num_queries (all requests' nodes together), num_kv_heads, head_dim, page_size, scale_tokens,
+ * max_pages_per_seq, page_table_stride and num_pages, of a layer, count.)
+ *   path        device, int32 [num_queries], as omniattn_tree_verify writes it: a request's path ascends from its first entry on and ends before
+ *               the first entry that does not, or is no node (such as -1)
+ *   seq_lens    device, int32 [B]: lengths with the nodes (before omniattn_table_truncate)
+ *   k_cache, v_cache    device, e4m3 [num_layers, num_pages, num_kv_heads, 128, head_dim]
+ *   k_scales, v_scales  device, fp32 [num_layers, num_pages, num_kv_heads, 128 / scale_tokens], finite, >= 0
+ * The scale of a block that a row moves to becomes the largest of the scales that its rows of the path came with and, where tokens of the
+ * text lie in it, its own; codes of these rows and tokens are multiplied by old / new and rounded (exact for powers of two but for
+ * numbers that become subnormal).  Blocks that no row moves to stay as they are, and so do the codes of nodes that nothing moves to (their tokens
+ * are undefined once the path is taken).  A request with too many nodes, or more than it has tokens, is left alone.
+ */
+int omniattn_gqa_keep(const omniattn_gqa_t* gqa, int32_t num_layers, const int32_t* path, const int32_t* seq_lens, const int32_t* q_start,
+                      const int32_t* page_table, void* k_cache, void* v_cache, float* k_scales, float* v_scales, void* hip_stream);
+
+/*
+ * Requests lose their last tokens: of L, L - min(max(dropped, 0), L) are left, and the pages above them go back on the stack, in the order
+ * of the requests and of their rows.  (max_tokens of `table` does not count.)  seq_lens_out may be seq_lens, free_count_out may be free_count.
+ */
+int omniattn_table_truncate(const omniattn_table_t* table, const int32_t* seq_lens, const int32_t* dropped, const int32_t* page_table,
+                            int32_t* free_pages, const int32_t* free_count, int32_t* seq_lens_out, int32_t* free_count_out,
+                            void* hip_stream);
+
 const char* omniattn_strerror(int code);
 /* Text of the last HIP error seen by the calling thread ("" if none). */
 const char* omniattn_last_hip_error(void);

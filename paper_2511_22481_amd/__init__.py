@@ -25,8 +25,16 @@ from .binding import (  # noqa: F401
     omniattn_gqa_workspace_bytes,
     omniattn_gqa_decode,
     gqa_decode,
+    omniattn_tree_masks,
+    omniattn_gqa_tree,
+    gqa_tree,
+    omniattn_tree_verify_workspace_bytes,
+    omniattn_tree_verify,
+    omniattn_gqa_keep,
+    omniattn_table_truncate,
     Table,
     Gqa,
+    Verify,
     lib_path,
     load_library,
     BF16,

@@ -51,6 +51,11 @@ class Gqa(ctypes.Structure):
     ]
 
 
+class Verify(ctypes.Structure):
+    """omniattn_verify_t"""
+    _fields_ = [("batch", ctypes.c_int32), ("num_tokens", ctypes.c_int32), ("vocab", ctypes.c_int32), ("logits_dtype", ctypes.c_int32)]
+
+
 def lib_path():
     return _LIB_PATH
 
@@ -117,6 +122,18 @@ def load_library():
     lib.omniattn_gqa_workspace_bytes.argtypes = [ctypes.POINTER(Gqa)]
     lib.omniattn_gqa_decode.restype = ctypes.c_int
     lib.omniattn_gqa_decode.argtypes = [ctypes.POINTER(Gqa), P, ctypes.c_int64] + [P] * 10 + [ctypes.c_size_t, P]
+    lib.omniattn_tree_masks.restype = ctypes.c_int
+    lib.omniattn_tree_masks.argtypes = [ctypes.c_int32, ctypes.c_int32] + [P] * 6
+    lib.omniattn_gqa_tree.restype = ctypes.c_int
+    lib.omniattn_gqa_tree.argtypes = [ctypes.POINTER(Gqa), P, ctypes.c_int64] + [P] * 11 + [ctypes.c_size_t, P]
+    lib.omniattn_tree_verify_workspace_bytes.restype = ctypes.c_size_t
+    lib.omniattn_tree_verify_workspace_bytes.argtypes = [ctypes.POINTER(Verify)]
+    lib.omniattn_tree_verify.restype = ctypes.c_int
+    lib.omniattn_tree_verify.argtypes = [ctypes.POINTER(Verify), P, ctypes.c_int64, P, ctypes.c_int64] + [P] * 10 + [ctypes.c_size_t, P]
+    lib.omniattn_gqa_keep.restype = ctypes.c_int
+    lib.omniattn_gqa_keep.argtypes = [ctypes.POINTER(Gqa), ctypes.c_int32] + [P] * 9
+    lib.omniattn_table_truncate.restype = ctypes.c_int
+    lib.omniattn_table_truncate.argtypes = [ctypes.POINTER(Table)] + [P] * 8
     lib.omniattn_strerror.restype = ctypes.c_char_p
     lib.omniattn_strerror.argtypes = [ctypes.c_int]
     lib.omniattn_last_hip_error.restype = ctypes.c_char_p
@@ -411,7 +428,9 @@ def _native():
         spec.loader.exec_module(module)
         module.setup(OmniAttnError, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
                      *(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.omniattn_table_extend, lib.omniattn_table_release,
-                                                                       lib.omniattn_gqa_append, lib.omniattn_gqa_decode)))
+                                                                       lib.omniattn_gqa_append, lib.omniattn_gqa_decode,
+                                                                       lib.omniattn_table_truncate, lib.omniattn_tree_masks, lib.omniattn_gqa_tree,
+                                                                       lib.omniattn_tree_verify, lib.omniattn_gqa_keep)))
         _marshal = module
     return _marshal
 
@@ -464,3 +483,63 @@ def gqa_decode(q, k_cache, v_cache, k_scales, v_scales, page_table, seq_lens, si
     omniattn_gqa_decode(q, k_cache, v_cache, k_scales, v_scales, page_table, seq_lens, q_start, out, lse, workspace, sink=sink, window=window,
                         softmax_scale=softmax_scale)
     return out, lse
+
+
+def omniattn_tree_masks(parents, seq_lens, q_start, masks, positions=None, stream=None):
+    """Of the nodes of every request's tree (all int32 CUDA tensors but masks): parents [nodes] holds each one's parent, as a number among the
+    request's nodes, lower than its own (other numbers: it follows the text).  seq_lens counts the nodes; q_start (int32 [batch + 1], None: one
+    each) says which of them are a request's.  masks (int64 [nodes]: the nodes that each follows and itself, as bits) and positions (int32
+    [nodes], in the text; or None) are written."""
+    _check((_marshal or _native()).tree_masks(parents, seq_lens, q_start, masks, positions, stream))
+
+
+def omniattn_gqa_tree(q, k_cache, v_cache, k_scales, v_scales, page_table, seq_lens, q_start, masks, out, lse, workspace, *, sink, window,
+                      softmax_scale, stream=None):
+    """omniattn_gqa_decode for the nodes of trees: a query sees the kept tokens of the text and the nodes of its mask (int64 [nodes], as
+    omniattn_tree_masks writes them).  The workspace is that of omniattn_gqa_workspace_bytes."""
+    _check((_marshal or _native()).tree(q, k_cache, v_cache, k_scales, v_scales, page_table, seq_lens, q_start, masks, out, lse, workspace, sink, window,
+                                        softmax_scale, stream))
+
+
+def gqa_tree(q, k_cache, v_cache, k_scales, v_scales, page_table, seq_lens, masks, sink, window, softmax_scale, q_start=None, out_dtype=None):
+    """Convenience wrapper of omniattn_gqa_tree: allocates results and workspace with torch.  Returns (out, lse)."""
+    import torch
+    if not q.is_cuda:
+        raise OmniAttnError(-4, "omniattn runs on the GPU only: tensors must be CUDA tensors")
+    out = torch.empty(q.shape, dtype=torch.bfloat16 if out_dtype is None else out_dtype, device=q.device)
+    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    size = omniattn_gqa_workspace_bytes(seq_lens.shape[0], q.shape[0], q.shape[1], k_cache.shape[1], q.shape[2])
+    workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+    omniattn_gqa_tree(q, k_cache, v_cache, k_scales, v_scales, page_table, seq_lens, q_start, masks, out, lse, workspace, sink=sink, window=window,
+                      softmax_scale=softmax_scale)
+    return out, lse
+
+
+def omniattn_tree_verify_workspace_bytes(num_tokens, vocab):
+    """Bytes of workspace that omniattn_tree_verify needs for so many nodes of all requests."""
+    rec = Verify(1, num_tokens, vocab, BF16)
+    n = int(load_library().omniattn_tree_verify_workspace_bytes(ctypes.byref(rec)))
+    _want(n > 0 or num_tokens == 0, "no valid problem")
+    return n
+
+
+def omniattn_tree_verify(logits, draft_probs, tokens, parents, q_start, temperature, uniforms, path, out_tokens, logprobs, dropped, workspace, stream=None):
+    """Which drafted tokens stay.  logits (bf16 or fp32 [nodes, vocabulary], any row stride) are the target's for the token behind each node,
+    draft_probs (fp32, alike; or None) the probabilities that the first child of each node was drawn from; tokens and parents (int32
+    [nodes]) the trees, temperature fp32 [batch] (0: the likeliest token), uniforms fp32 [nodes, 2] in [0, 1).  Written: path and out_tokens
+    (int32 [nodes]: of each request the nodes that stay and the token behind each of them, the last one new; then -1), logprobs
+    (fp32 [nodes] or None: of out_tokens) and dropped (int32 [batch]: nodes that do not stay)."""
+    _check((_marshal or _native()).verify(logits, draft_probs, tokens, parents, q_start, temperature, uniforms, path, out_tokens, logprobs, dropped,
+                                          workspace, stream))
+
+
+def omniattn_gqa_keep(path, seq_lens, q_start, page_table, k_cache, v_cache, k_scales, v_scales, stream=None):
+    """Rows of the nodes on each request's path move up behind its text.  The caches (changed in place) are one layer's, or several layers', with a
+    dimension more in front; seq_lens counts all nodes."""
+    _check((_marshal or _native()).keep(path, seq_lens, q_start, page_table, k_cache, v_cache, k_scales, v_scales, stream))
+
+
+def omniattn_table_truncate(seq_lens, dropped, page_table, free_pages, free_count, seq_lens_out, free_count_out, stream=None):
+    """Requests lose their last dropped[b] tokens, and pages that hold nothing else go back on the stack (free_pages changes in place;
+    seq_lens_out may be seq_lens, free_count_out may be free_count)."""
+    _check((_marshal or _native()).truncate(seq_lens, dropped, page_table, free_pages, free_count, seq_lens_out, free_count_out, stream))

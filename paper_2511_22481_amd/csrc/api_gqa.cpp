@@ -86,6 +86,67 @@ Workspace workspace_of(const omniattn_gqa_t* g, const GqaShape& shape) {
   return w;
 }
 
+// omniattn_gqa_decode, and omniattn_gqa_tree (tree).
+int attend(const omniattn_gqa_t* gqa, const void* q, int64_t q_stride, const void* k_cache, const void* v_cache, const float* k_scales, const float* v_scales,
+           const int32_t* page_table, const int32_t* seq_lens, const int32_t* q_start, bool tree, const uint64_t* masks, void* out, float* lse, void* workspace,
+           size_t workspace_bytes, void* hip_stream) {
+  int rc = check_gqa(gqa);
+  if (rc != OMNIATTN_OK) return rc;
+  if (gqa->page_table_stride < gqa->max_pages_per_seq) return OMNIATTN_EINVAL;
+  if (!std::isfinite(gqa->softmax_scale)) return OMNIATTN_EINVAL;
+  if (!q_start && gqa->num_queries != gqa->batch) return OMNIATTN_EINVAL;
+  if (gqa->num_queries == 0) return OMNIATTN_OK;
+  if (!q || !k_cache || !v_cache || !k_scales || !v_scales || !page_table || !seq_lens || !out || !lse) return OMNIATTN_EINVAL;
+  if (tree && (!masks || !aligned(masks, 8))) return OMNIATTN_EINVAL;
+  if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16)) return OMNIATTN_EINVAL;
+  if (q_stride % 8 != 0 || q_stride < (int64_t)gqa->num_q_heads * gqa->head_dim) return OMNIATTN_EINVAL;
+  int cus = 0;
+  rc = device_cus(&cus);
+  if (rc != OMNIATTN_OK) return rc;
+  GqaDecodeParams p;
+  p.group = gqa->num_q_heads / gqa->num_kv_heads;
+  const GqaShape shape = shape_of(gqa, cus);
+  const Workspace w = workspace_of(gqa, shape);
+  if (!workspace || workspace_bytes < w.bytes || !aligned(workspace, 256)) return OMNIATTN_EWORKSPACE;
+  p.q = (const uint16_t*)q;
+  p.q_stride = q_stride;
+  p.k_cache = (const uint8_t*)k_cache;
+  p.v_cache = (const uint8_t*)v_cache;
+  p.k_scales = k_scales;
+  p.v_scales = v_scales;
+  p.page_table = page_table;
+  p.table_stride = gqa->page_table_stride;
+  p.seq_lens = seq_lens;
+  p.q_start = q_start;
+  p.out = out;
+  p.lse = lse;
+  p.rows = (int2*)((char*)workspace + w.rows);
+  p.part_ml = (float4*)((char*)workspace + w.ml);
+  p.part_o = (float*)((char*)workspace + w.o);
+  p.batch = gqa->batch;
+  p.num_queries = gqa->num_queries;
+  p.q_heads = gqa->num_q_heads;
+  p.kv_heads = gqa->num_kv_heads;
+  p.head_dim = gqa->head_dim;
+  p.max_pages = gqa->max_pages_per_seq;
+  // (no request is longer than its table, 2^31 - 128 tokens at most: larger numbers mean the same, and W + 63 stays in 32 bits)
+  p.S = std::min(gqa->sink, gqa->max_pages_per_seq * kPage);
+  p.W = std::min(gqa->window, gqa->max_pages_per_seq * kPage);
+  p.scale_shift = gqa->scale_tokens == 32 ? 5 : gqa->scale_tokens == 64 ? 6 : 7;
+  p.out_fp32 = gqa->out_dtype == OMNIATTN_FP32;
+  p.uncut = shape.uncut;
+  p.scale_log2 = gqa->softmax_scale * 1.4426950408889634f;
+  p.masks = masks;
+  // Not more shares than there can be units of work (each block counts up to 2 beside its pages).
+  const int64_t blocks = ((int64_t)p.num_queries * p.group + shape.block_rows - 1) / shape.block_rows + p.batch;
+  const int64_t pages = std::min<int64_t>(p.max_pages, ((int64_t)p.S + kPage - 1) / kPage + ((int64_t)p.W + (tree ? p.num_queries + OMNIATTN_TREE_NODES : shape.block_rows) + kPage - 1) / kPage + 1);
+  const int64_t units = blocks * p.kv_heads * (shape.shares > 1 ? 4 * pages + 4 : pages + 2);
+  p.few_units = units <= INT32_MAX;
+  const int groups = (int)std::min<int64_t>(shape.groups, (units + shape.shares - 1) / shape.shares);
+  OA_HIP(launch_gqa_decode(p, shape, groups * shape.shares, (hipStream_t)hip_stream));
+  return OMNIATTN_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -132,6 +193,68 @@ int omniattn_table_release(const omniattn_table_t* table, const int32_t* done, i
   p.max_pages = table->max_pages_per_seq;
   p.num_pages = table->num_pages;
   OA_HIP(launch_table_release(p, (hipStream_t)hip_stream));
+  return OMNIATTN_OK;
+}
+
+int omniattn_table_truncate(const omniattn_table_t* table, const int32_t* seq_lens, const int32_t* dropped, const int32_t* page_table, int32_t* free_pages,
+                            const int32_t* free_count, int32_t* seq_lens_out, int32_t* free_count_out, void* hip_stream) {
+  const int rc = check_table(table);
+  if (rc != OMNIATTN_OK) return rc;
+  if (!seq_lens || !dropped || !page_table || !free_pages || !free_count || !seq_lens_out || !free_count_out) return OMNIATTN_EINVAL;
+  if (half_overlap(seq_lens, seq_lens_out, table->batch)) return OMNIATTN_EINVAL;
+  TruncateParams p;
+  p.seq_lens = seq_lens;
+  p.dropped = dropped;
+  p.page_table = page_table;
+  p.stride = table->page_table_stride;
+  p.free_pages = free_pages;
+  p.free_count = free_count;
+  p.seq_lens_out = seq_lens_out;
+  p.free_count_out = free_count_out;
+  p.batch = table->batch;
+  p.max_pages = table->max_pages_per_seq;
+  p.num_pages = table->num_pages;
+  OA_HIP(launch_table_truncate(p, (hipStream_t)hip_stream));
+  return OMNIATTN_OK;
+}
+
+int omniattn_tree_masks(int32_t batch, int32_t num_tokens, const int32_t* parents, const int32_t* seq_lens, const int32_t* q_start, uint64_t* masks,
+                        int32_t* positions, void* hip_stream) {
+  if (batch < 1 || num_tokens < 0 || (!q_start && num_tokens != batch)) return OMNIATTN_EINVAL;
+  if (num_tokens == 0) return OMNIATTN_OK;
+  if (!parents || !seq_lens || !masks || !aligned(masks, 8)) return OMNIATTN_EINVAL;
+  OA_HIP(launch_tree_masks(TreeMasksParams{parents, seq_lens, q_start, masks, positions, batch, num_tokens}, (hipStream_t)hip_stream));
+  return OMNIATTN_OK;
+}
+
+int omniattn_gqa_keep(const omniattn_gqa_t* gqa, int32_t num_layers, const int32_t* path, const int32_t* seq_lens, const int32_t* q_start,
+                      const int32_t* page_table, void* k_cache, void* v_cache, float* k_scales, float* v_scales, void* hip_stream) {
+  const int rc = check_gqa(gqa);
+  if (rc != OMNIATTN_OK) return rc;
+  if (num_layers < 0 || gqa->page_table_stride < gqa->max_pages_per_seq || (!q_start && gqa->num_queries != gqa->batch)) return OMNIATTN_EINVAL;
+  if (num_layers == 0 || gqa->num_queries == 0) return OMNIATTN_OK;
+  if (!path || !seq_lens || !page_table || !k_cache || !v_cache || !k_scales || !v_scales) return OMNIATTN_EINVAL;
+  if (!aligned(k_cache, 16) || !aligned(v_cache, 16)) return OMNIATTN_EINVAL;
+  if ((int64_t)num_layers * gqa->batch > INT32_MAX / 2 / gqa->num_kv_heads) return OMNIATTN_EUNSUPPORTED;
+  GqaKeepParams p;
+  p.path = path;
+  p.seq_lens = seq_lens;
+  p.q_start = q_start;
+  p.page_table = page_table;
+  p.table_stride = gqa->page_table_stride;
+  p.cache[0] = (uint8_t*)k_cache;
+  p.cache[1] = (uint8_t*)v_cache;
+  p.scales[0] = k_scales;
+  p.scales[1] = v_scales;
+  p.num_pages = gqa->num_pages;
+  p.batch = gqa->batch;
+  p.num_tokens = gqa->num_queries;
+  p.layers = num_layers;
+  p.kv_heads = gqa->num_kv_heads;
+  p.head_dim = gqa->head_dim;
+  p.scale_tokens = gqa->scale_tokens;
+  p.max_pages = gqa->max_pages_per_seq;
+  OA_HIP(launch_gqa_keep(p, (hipStream_t)hip_stream));
   return OMNIATTN_OK;
 }
 
@@ -188,59 +311,13 @@ size_t omniattn_gqa_workspace_bytes(const omniattn_gqa_t* gqa) {
 int omniattn_gqa_decode(const omniattn_gqa_t* gqa, const void* q, int64_t q_stride, const void* k_cache, const void* v_cache, const float* k_scales,
                         const float* v_scales, const int32_t* page_table, const int32_t* seq_lens, const int32_t* q_start, void* out, float* lse,
                         void* workspace, size_t workspace_bytes, void* hip_stream) {
-  int rc = check_gqa(gqa);
-  if (rc != OMNIATTN_OK) return rc;
-  if (gqa->page_table_stride < gqa->max_pages_per_seq) return OMNIATTN_EINVAL;
-  if (!std::isfinite(gqa->softmax_scale)) return OMNIATTN_EINVAL;
-  if (!q_start && gqa->num_queries != gqa->batch) return OMNIATTN_EINVAL;
-  if (gqa->num_queries == 0) return OMNIATTN_OK;
-  if (!q || !k_cache || !v_cache || !k_scales || !v_scales || !page_table || !seq_lens || !out || !lse) return OMNIATTN_EINVAL;
-  if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16)) return OMNIATTN_EINVAL;
-  if (q_stride % 8 != 0 || q_stride < (int64_t)gqa->num_q_heads * gqa->head_dim) return OMNIATTN_EINVAL;
-  int cus = 0;
-  rc = device_cus(&cus);
-  if (rc != OMNIATTN_OK) return rc;
-  GqaDecodeParams p;
-  p.group = gqa->num_q_heads / gqa->num_kv_heads;
-  const GqaShape shape = shape_of(gqa, cus);
-  const Workspace w = workspace_of(gqa, shape);
-  if (!workspace || workspace_bytes < w.bytes || !aligned(workspace, 256)) return OMNIATTN_EWORKSPACE;
-  p.q = (const uint16_t*)q;
-  p.q_stride = q_stride;
-  p.k_cache = (const uint8_t*)k_cache;
-  p.v_cache = (const uint8_t*)v_cache;
-  p.k_scales = k_scales;
-  p.v_scales = v_scales;
-  p.page_table = page_table;
-  p.table_stride = gqa->page_table_stride;
-  p.seq_lens = seq_lens;
-  p.q_start = q_start;
-  p.out = out;
-  p.lse = lse;
-  p.rows = (int2*)((char*)workspace + w.rows);
-  p.part_ml = (float4*)((char*)workspace + w.ml);
-  p.part_o = (float*)((char*)workspace + w.o);
-  p.batch = gqa->batch;
-  p.num_queries = gqa->num_queries;
-  p.q_heads = gqa->num_q_heads;
-  p.kv_heads = gqa->num_kv_heads;
-  p.head_dim = gqa->head_dim;
-  p.max_pages = gqa->max_pages_per_seq;
-  // (no request is longer than its table, 2^31 - 128 tokens at most: larger numbers mean the same, and W + 63 stays in 32 bits)
-  p.S = std::min(gqa->sink, gqa->max_pages_per_seq * kPage);
-  p.W = std::min(gqa->window, gqa->max_pages_per_seq * kPage);
-  p.scale_shift = gqa->scale_tokens == 32 ? 5 : gqa->scale_tokens == 64 ? 6 : 7;
-  p.out_fp32 = gqa->out_dtype == OMNIATTN_FP32;
-  p.uncut = shape.uncut;
-  p.scale_log2 = gqa->softmax_scale * 1.4426950408889634f;
-  // Not more shares than there can be units of work (each block counts up to 2 beside its pages).
-  const int64_t blocks = ((int64_t)p.num_queries * p.group + shape.block_rows - 1) / shape.block_rows + p.batch;
-  const int64_t pages = std::min<int64_t>(p.max_pages, ((int64_t)p.S + kPage - 1) / kPage + ((int64_t)p.W + shape.block_rows + kPage - 1) / kPage + 1);
-  const int64_t units = blocks * p.kv_heads * (shape.shares > 1 ? 4 * pages + 4 : pages + 2);
-  p.few_units = units <= INT32_MAX;
-  const int groups = (int)std::min<int64_t>(shape.groups, (units + shape.shares - 1) / shape.shares);
-  OA_HIP(launch_gqa_decode(p, shape, groups * shape.shares, (hipStream_t)hip_stream));
-  return OMNIATTN_OK;
+  return attend(gqa, q, q_stride, k_cache, v_cache, k_scales, v_scales, page_table, seq_lens, q_start, false, nullptr, out, lse, workspace, workspace_bytes, hip_stream);
+}
+
+int omniattn_gqa_tree(const omniattn_gqa_t* gqa, const void* q, int64_t q_stride, const void* k_cache, const void* v_cache, const float* k_scales,
+                      const float* v_scales, const int32_t* page_table, const int32_t* seq_lens, const int32_t* q_start, const uint64_t* masks, void* out,
+                      float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return attend(gqa, q, q_stride, k_cache, v_cache, k_scales, v_scales, page_table, seq_lens, q_start, true, masks, out, lse, workspace, workspace_bytes, hip_stream);
 }
 
 }  // extern "C"

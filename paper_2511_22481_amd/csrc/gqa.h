@@ -38,6 +38,43 @@ struct ReleaseParams {
 };
 hipError_t launch_table_release(const ReleaseParams& p, hipStream_t stream);
 
+struct TruncateParams {
+  const int32_t* seq_lens;
+  const int32_t* dropped;
+  const int32_t* page_table;
+  int64_t stride;
+  int32_t* free_pages;
+  const int32_t* free_count;
+  int32_t* seq_lens_out;
+  int32_t* free_count_out;
+  int batch, max_pages;
+  int64_t num_pages;  // entries of free_pages
+};
+hipError_t launch_table_truncate(const TruncateParams& p, hipStream_t stream);
+
+struct TreeMasksParams {
+  const int32_t* parents;
+  const int32_t* seq_lens;
+  const int32_t* q_start;  // [batch + 1], or null: node b belongs to request b
+  uint64_t* masks;
+  int32_t* positions;      // or null
+  int batch, num_tokens;
+};
+hipError_t launch_tree_masks(const TreeMasksParams& p, hipStream_t stream);
+
+struct GqaKeepParams {
+  const int32_t* path;
+  const int32_t* seq_lens;
+  const int32_t* q_start;   // [batch + 1], or null
+  const int32_t* page_table;
+  int64_t table_stride;
+  uint8_t* cache[2];        // e4m3 [layers, num_pages, kv_heads, 128, head_dim]
+  float* scales[2];         // [layers, num_pages, kv_heads, 128 / scale_tokens]
+  int64_t num_pages;
+  int batch, num_tokens, layers, kv_heads, head_dim, scale_tokens, max_pages;
+};
+hipError_t launch_gqa_keep(const GqaKeepParams& p, hipStream_t stream);
+
 struct GqaAppendParams {
   const uint16_t* rows[2];  // K and V, bf16 [tokens, kv_heads, head_dim]
   int64_t stride[2];        // elements from one token to the next
@@ -71,6 +108,7 @@ struct GqaDecodeParams {
   int few_units;            // a call's units of work (pages and blocks) are counted in 32 bits
   int uncut;                // blocks go whole to the share that has their first unit: no partial rows
   float scale_log2;         // softmax_scale * log2(e)
+  const uint64_t* masks;    // [num_queries]: the nodes that each query sees; null: the queries are a request's last tokens, each seeing those before it
 };
 // How a call is computed: by which kernel (gqa_decode_kernel.hip or gqa_wide_kernel.hip), tiles of 16 query rows per wave, rows of a
 // block, work groups at most, and shares of the work to each.

@@ -121,23 +121,66 @@ __device__ __forceinline__ int wave_sum_up_to(int x) {
   return x;
 }
 
+// Tokens that a query sees: those before `reach`; TREE: of the text, and the nodes of a set (without those that the rule does not keep).
+template <bool TREE>
+struct Sight {
+  int reach;
+};
+template <>
+struct Sight<true> {
+  int reach;
+  uint64_t nodes;
+};
+template <bool TREE>
+__device__ __forceinline__ Sight<TREE> sight_of(const GqaDecodeParams& p, const Piece& w, int t, bool valid) {
+  if constexpr (TREE) {
+    const int n = w.rq.n, text = w.rq.L - n;
+    uint64_t nodes = valid ? p.masks[w.rq.begin + t] : 0;
+    if (n < 64) nodes &= ((uint64_t)1 << n) - 1;
+    const int count = __popcll(nodes);
+    const int reach = count ? max(text + count, 0) : 0;
+    if (count > p.W) {  // nodes in front of the window, but for sinks
+      const int from = max(p.S - text, 0);
+      uint64_t rest = nodes;
+      for (int k = 0; k < count - p.W; ++k, rest &= rest - 1)
+        if (k >= from) nodes &= ~(rest & -rest);
+    }
+    return Sight<true>{reach, nodes};
+  } else {
+    return Sight<false>{valid ? w.reach(t) : 0};
+  }
+}
+// The 32 nodes whose slots begin `off` behind the first one's.
+__device__ __forceinline__ uint32_t nodes_at(uint64_t nodes, int off) {
+  if (off >= 0) return off < 64 ? (uint32_t)(nodes >> off) : 0;
+  return off > -32 ? (uint32_t)nodes << -off : 0;
+}
+template <bool TREE>
+__device__ __forceinline__ bool sees(const GqaDecodeParams& p, const Sight<TREE>& s, int text, int pos) {
+  if constexpr (TREE) {
+    if (pos >= text) return nodes_at(s.nodes, pos - text) & 1;
+  }
+  return retained(pos, s.reach, p.S, p.W);
+}
+
 // What a loop over a block's pages needs of it.
 struct Span {
   TileLayout pages;
-  int lo, hi;            // tokens that the block's first and last query see
+  int lo, hi;            // tokens that the block's first and last query see (of a tree: a first and a last node's)
   int tile_hi;
   bool several;          // several queries
+  int text;              // tokens before the request's queries
   __device__ __forceinline__ explicit Span(const Piece& w)
       : pages{uniform(w.bk.pages.ns), uniform(w.bk.pages.w0), uniform(w.bk.pages.w1)}, lo(uniform(w.reach(w.bk.t0))), hi(uniform(w.reach(w.bk.t1))),
-        tile_hi(uniform(w.tile_hi)), several(uniform(w.bk.t1 - w.bk.t0) > 0) {}
+        tile_hi(uniform(w.tile_hi)), several(uniform(w.bk.t1 - w.bk.t0) > 0), text(uniform(w.rq.L - w.rq.n)) {}
 };
 
 // Finds shares and walks through their blocks (see Walk in gqa_deal.h).  SHARES: of a work group, 1 or one for each wave, which counts quarters of
 // pages.  All threads call begin.
-template <int R, int THREADS, int START, int SHARES = 1>
+template <int R, int THREADS, int START, int SHARES = 1, bool TREE = false>
 struct Dealer {
   static constexpr int kGrain = SHARES > 1 ? kWaveTokens : kPage;
-  using Walker = Walk<R, START, kGrain, GqaDecodeParams>;
+  using Walker = Walk<R, START, kGrain, GqaDecodeParams, TREE>;
 
   // What is needed only from block to block stays here: in scalar registers it would push the loop's own out.
   struct Lds {
@@ -284,13 +327,13 @@ struct Rows {
 };
 
 // Weights of a tile of 32 tokens from its S^T (lane (n16, g) has tokens 16 h + 4 g + i of row n16), in two f16 terms (`low`: what
-// rounding to `high` leaves), references, sums and, where a reference rises, the output.  reach: tokens that the row's query sees; full: every
+// rounding to `high` leaves), references, sums and, where a reference rises, the output.  sight: tokens that the row's query sees; full: every
 // row keeps all 32 tokens, which begin at pos0.  (One term is 2^-11 of a weight: 7 to 9 in a hundred bf16 results then were the neighbour
 // of the right one.  With two a bf16 result is the fp32 result rounded.  us with one / two: 1 request of 131072 56.8 / 56.9, 64 of 32768
 // 713 / 714, 256 short ones of width 64 30.4 / 30.9; 64 requests of 2000 to 16000, 4 KV heads, 64 rows: width 64 75 / 86, 128 132 / 151,
 // 256 238 / 270.)
-template <int D, int RT>
-__device__ __forceinline__ void weigh(const GqaDecodeParams& p, Rows<D, RT>& a, const f32x4 (&s)[RT][2], const int (&reach)[RT], bool full, int pos0,
+template <int D, int RT, bool TREE>
+__device__ __forceinline__ void weigh(const GqaDecodeParams& p, Rows<D, RT>& a, const f32x4 (&s)[RT][2], const Sight<TREE> (&sight)[RT], int text, bool full, int pos0,
                                       int g, float k_factor, float v_scale, f16x8 (&high)[RT], f16x8 (&low)[RT]) {
   // (at least 2^-100: ratio stays finite)
   const float v_log = fmaxf(__log2f(v_scale), -100.f);
@@ -300,10 +343,14 @@ __device__ __forceinline__ void weigh(const GqaDecodeParams& p, Rows<D, RT>& a, 
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = s[rt][i / 4][i % 4] * k_factor;
     if (!full) {
+      uint32_t nodes = 0;
+      if constexpr (TREE) nodes = nodes_at(sight[rt].nodes, pos0 - text) >> (4 * g);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int pos = pos0 + 16 * (i / 4) + 4 * g + i % 4;
-        x[i] = retained(pos, reach[rt], p.S, p.W) ? x[i] : -INFINITY;
+        bool keep = retained(pos, sight[rt].reach, p.S, p.W);
+        if constexpr (TREE) keep = pos < text ? keep : nodes >> (16 * (i / 4) + i % 4) & 1;
+        x[i] = keep ? x[i] : -INFINITY;
       }
     }
     float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
@@ -328,6 +375,8 @@ __device__ __forceinline__ void weigh(const GqaDecodeParams& p, Rows<D, RT>& a, 
     for (int i = 0; i < 8; ++i) {
       w[i] = exp2_fast(x[i] - ref);
       float y = w[i] * value;
+      // (a tile that no row keeps anything of can be among a tree's, and its scale be anything)
+      if constexpr (TREE) y = x[i] == -INFINITY ? 0.f : y;
       // (fixed here: the compiler may fuse the product with one of its two uses and round the other in two steps, which
       // near a tie of f16 leaves the second term for another first term)
       asm("" : "+v"(y));
@@ -341,7 +390,7 @@ __device__ __forceinline__ void weigh(const GqaDecodeParams& p, Rows<D, RT>& a, 
 // A partial tile's value codes: tokens that no row of the block keeps may hold anything and become 0.  NaN in a kept one is for the rows
 // that keep the token, and only for those, but a weight of 0 would not stop it in the product: it goes on as 0 too, and the block's end
 // sees to it.  Lane (n16, g) has tokens 4 g + j % 4 (+ 16 from j = 4 on).
-template <int D, int RT>
+template <int D, int RT, bool TREE>
 __device__ __forceinline__ void sanitize(const GqaDecodeParams& p, Rows<D, RT>& a, typename VWord<D / 64>::type (&v)[8], const Span& now, int pos0, int g) {
   constexpr int kWords = D / 64;
   const int lo = now.lo, hi = now.hi;
@@ -349,12 +398,12 @@ __device__ __forceinline__ void sanitize(const GqaDecodeParams& p, Rows<D, RT>& 
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const int pos = pos0 + (j < 4 ? 0 : 16) + 4 * g + j % 4;
-    const bool keep = pos < hi && (pos < p.S || (p.W > 0 && pos >= lo - p.W));
+    const bool keep = pos < hi && (pos < p.S || (p.W > 0 && pos >= lo - p.W) || (TREE && pos >= now.text));
     if (!keep) v[j] = typename VWord<kWords>::type{};
 #pragma unroll
     for (int i = 0; i < kWords; ++i) any_nan |= nan_codes(word<kWords>(v[j], i));
   }
-  if (now.several && __ballot(any_nan != 0) != 0) {
+  if ((TREE || now.several) && __ballot(any_nan != 0) != 0) {
     a.saw_nan = 1.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = without_nan<kWords>(v[j]);
@@ -393,8 +442,12 @@ __device__ __forceinline__ bf16x8 k_operand(uint32_t lo, uint32_t hi) {
 struct Kept {
   bool some, full;
 };
+template <bool TREE>
 __device__ __forceinline__ Kept kept_of(const GqaDecodeParams& p, const Span& now, int pos0) {
   const int lo = now.lo, hi = now.hi;
+  if constexpr (TREE)
+    return Kept{pos0 < hi && (pos0 < p.S || (p.W > 0 && pos0 + kWaveTokens > lo - p.W) || pos0 + kWaveTokens > now.text),
+                pos0 + kWaveTokens <= now.text && (pos0 + kWaveTokens <= p.S || pos0 >= hi - p.W)};
   return Kept{pos0 < hi && (pos0 < p.S || (p.W > 0 && pos0 + kWaveTokens > lo - p.W)),
               pos0 + kWaveTokens <= lo && (pos0 + kWaveTokens <= p.S || pos0 >= hi - p.W)};
 }
@@ -402,8 +455,8 @@ __device__ __forceinline__ Kept kept_of(const GqaDecodeParams& p, const Span& no
 // End of a block: the shares of the TG waves that hold the same rows (tokens apart) meet in LDS, references and sums first (ml: [TG][R]),
 // then the outputs at the common reference, 1 / PARTS of every lane's columns at a time (o_lds: [TG][R][D / PARTS + 4]).  tg: which of the TG
 // the wave is; row0: its first row.  Blocks that other work groups share too leave partial rows in `slot`.
-template <int D, int RT, int R, int TG, int PARTS, int THREADS, bool OUT32, int START>
-__device__ __forceinline__ void finish(const Dealer<R, THREADS, START>& dealer, const Piece& now, Rows<D, RT>& a, float* o_lds, float4* ml,
+template <int D, int RT, int R, int TG, int PARTS, int THREADS, bool OUT32, int START, bool TREE>
+__device__ __forceinline__ void finish(const Dealer<R, THREADS, START, 1, TREE>& dealer, const Piece& now, Rows<D, RT>& a, float* o_lds, float4* ml,
                                        int tg, int row0, int slot) {
   constexpr int kCols = D / 16, kOStride = D / PARTS + 4;
   const int tid = threadIdx.x, lane = tid & 63, n16 = lane & 15, g = lane >> 4;
@@ -463,14 +516,14 @@ __device__ __forceinline__ void finish(const Dealer<R, THREADS, START>& dealer, 
       const uint32_t qt = (uint32_t)(now.rb * R + row) / (uint32_t)end.group, gi = (uint32_t)(now.rb * R + row) - qt * end.group;
       if (__builtin_expect(nans != 0.f, 0)) {
         // NaN that the loop has taken for 0: the columns of the tokens that this row keeps are looked through again
-        const int sees = now.reach((int)qt);
+        const Sight<TREE> sight = sight_of<TREE>(end, now, (int)qt, true);
 #pragma unroll 1
         for (int tile = now.tile_lo; tile < now.tile_hi; ++tile) {
           const int lp = now.bk.pages.logical(tile);
           const size_t ph = (size_t)end.page_table[now.b * end.table_stride + lp] * end.kv_heads + now.h;
 #pragma unroll 1
           for (int j = 0; j < kPage; ++j) {
-            if (!retained(lp * kPage + j, sees, end.S, end.W)) continue;
+            if (!sees<TREE>(end, sight, now.rq.L - now.rq.n, lp * kPage + j)) continue;
             const u32x2 codes = *(const u32x2*)(end.v_cache + (ph * kPage + j) * D + col);
             const uint32_t nan_lo = nan_codes(codes[0]), nan_hi = nan_codes(codes[1]);
 #pragma unroll
@@ -516,8 +569,8 @@ __device__ __forceinline__ void finish(const Dealer<R, THREADS, START>& dealer, 
 }
 
 // End of a block that one wave computes by itself, one row tile: every lane has D / 4 adjacent columns of its row, and writes them.
-template <int D, int THREADS, bool OUT32, int START, int SHARES>
-__device__ __forceinline__ void finish_alone(const Dealer<16, THREADS, START, SHARES>& dealer, const Piece& now, Rows<D, 1>& a, int slot) {
+template <int D, int THREADS, bool OUT32, int START, int SHARES, bool TREE>
+__device__ __forceinline__ void finish_alone(const Dealer<16, THREADS, START, SHARES, TREE>& dealer, const Piece& now, Rows<D, 1>& a, int slot) {
   constexpr int kCols = D / 16, kQuarters = kPage / kWaveTokens;
   const int lane = threadIdx.x & 63, row = lane & 15, g = lane >> 4, col = 4 * g * kCols;
   const float sum = row_sum(a.l[0]);
@@ -525,7 +578,7 @@ __device__ __forceinline__ void finish_alone(const Dealer<16, THREADS, START, SH
   const GqaDecodeParams& end = *late_arguments();
   const uint32_t qt = (uint32_t)(now.rb * 16 + row) / (uint32_t)end.group, gi = (uint32_t)(now.rb * 16 + row) - qt * end.group;
   if (__builtin_expect(a.saw_nan != 0.f, 0)) {  // (as in finish)
-    const int sees = now.reach((int)qt);
+    const Sight<TREE> sight = sight_of<TREE>(end, now, (int)qt, true);
     uint32_t nans = 0;  // of the lane's columns
 #pragma unroll 1
     for (int tile = now.tile_lo; tile < now.tile_hi; ++tile) {
@@ -533,7 +586,7 @@ __device__ __forceinline__ void finish_alone(const Dealer<16, THREADS, START, SH
       const size_t ph = (size_t)end.page_table[now.b * end.table_stride + lp / kQuarters] * end.kv_heads + now.h;
 #pragma unroll 1
       for (int j = 0; j < kWaveTokens; ++j) {
-        if (!retained(lp * kWaveTokens + j, sees, end.S, end.W)) continue;
+        if (!sees<TREE>(end, sight, now.rq.L - now.rq.n, lp * kWaveTokens + j)) continue;
         const uint32_t* codes = (const uint32_t*)(end.v_cache + (ph * kPage + lp % kQuarters * kWaveTokens + j) * D + col);
 #pragma unroll 1
         for (int i = 0; i < kCols; ++i) {

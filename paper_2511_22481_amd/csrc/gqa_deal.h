@@ -28,9 +28,19 @@ struct Block {
   int t0, t1;  // its query tokens, both included
   TileLayout pages;
 };
-template <int ROWS, int GRAIN, typename P>
+// TREE: the queries are nodes of a tree, of which any may see any, and which stand up to n - 1 tokens behind their positions: every block has the
+// nodes' pages and all that a query at the first node's position keeps of the text.
+template <int ROWS, int GRAIN, bool TREE = false, typename P>
 OA_INLINE Block block_of(const P& p, const Request& r, int rb) {
   Block k;
+  if constexpr (TREE) {
+    k.t0 = 0;
+    k.t1 = r.n - 1;
+    const int text = r.L - r.n;
+    // (without a window: the nodes that are sink tokens)
+    k.pages = tile_layout(r.L, p.W == 0 && text < p.S ? p.S + OMNIATTN_TREE_NODES : p.S, p.W > 0 ? (int)lesser((int64_t)p.W + k.t1, (int64_t)larger(r.L, 1)) : 0, GRAIN);
+    return k;
+  }
   // (rows of a call are counted in 32 bits; most requests have one block, and divisions are what a share's finding consists of)
   k.t0 = rb ? (int)((uint32_t)(rb * ROWS) / (uint32_t)p.group) : 0;
   k.t1 = (rb + 1) * ROWS >= r.n * p.group ? r.n - 1 : (int)((uint32_t)((rb + 1) * ROWS - 1) / (uint32_t)p.group);
@@ -79,13 +89,13 @@ struct Piece {
 
 // Walks through the blocks of a share.  R: rows of a block.  START: what a block costs beside its pages (its query, the meeting of the waves,
 // its results), in pages or what GRAIN makes of them.
-template <int R, int START, int GRAIN, typename P>
+template <int R, int START, int GRAIN, typename P, bool TREE = false>
 struct Walk {
   const P& p;
   OA_INLINE explicit Walk(const P& params) : p(params) {}
 
   OA_INLINE static int units(const Block& k) { return START + k.pages.count(); }
-  OA_INLINE Block block(const Request& r, int rb) const { return block_of<R, GRAIN>(p, r, rb); }
+  OA_INLINE Block block(const Request& r, int rb) const { return block_of<R, GRAIN, TREE>(p, r, rb); }
   // Units of one KV head of a request
   OA_INLINE int64_t cost_of(const Request& r) const {
     const int blocks = blocks_of<R>(p, r);

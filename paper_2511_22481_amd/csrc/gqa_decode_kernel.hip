@@ -90,10 +90,10 @@ struct Narrow {
   static constexpr size_t kLds = (size_t)4 * kRows * kOStride * 4 + 2 * 4 * kRows * 16 + 2 * kQBytes;
 };
 
-template <int D, int RT, bool OUT32, bool ALONE>
+template <int D, int RT, bool OUT32, bool ALONE, bool TREE>
 __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_kernel(GqaDecodeParams p) {
   using C = Narrow<D, RT>;
-  using Deal = Dealer<C::kRows, kThreads, ALONE ? 4 : 2, ALONE ? 4 : 1>;
+  using Deal = Dealer<C::kRows, kThreads, ALONE ? 4 : 2, ALONE ? 4 : 1, TREE>;
   constexpr int kGrain = Deal::kGrain;
   static_assert(!ALONE || (D == 64 && RT == 1));
   constexpr int R = C::kRows, kCols = D / 16, kWords = D / 64;
@@ -118,18 +118,21 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
     return last >= 0 ? p.page_table[b * p.table_stride + pages.logical(min(from + lane, last)) / (kPage / kGrain)] : 0;
   };
   // Query rows of a block: lane n16 of every group of 16 holds one row of each row tile, the columns that its K loads bring.  Rows past
-  // the last hold zeros.  reach: tokens that the row's query sees.
+  // the last hold zeros.  sight: tokens that the row's query sees.
   constexpr int kQs = C::kQLds ? kWords / 2 : 2 * kWords;  // operands of a row tile that the wave reads: its share, or all
   bf16x8 q[RT][kQs];
-  int reach[RT];
+  Sight<TREE> sight[RT];
+  bool blind = false;  // (of a tree) a row keeps nothing, not even of tiles that all others keep
   auto load_q = [&](const Piece& w) {
     const int rows = dealer.rows_of(w);
+    blind = false;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       const int row = rt * 16 + n16;
       const uint32_t t = (uint32_t)(w.rb * R + row) / (uint32_t)p.group, gi = (uint32_t)(w.rb * R + row) - t * p.group;
       const bool valid = row < rows;
-      reach[rt] = valid ? w.reach((int)t) : 0;
+      sight[rt] = sight_of<TREE>(p, w, (int)t, valid);
+      if constexpr (TREE) blind = blind || __any(valid && sight[rt].reach == 0);
       const uint16_t* src = p.q + (int64_t)(w.rq.begin + (int)t) * p.q_stride + (size_t)(w.h * p.group + (int)gi) * D + g * 16;
       // (operand 2 c + u holds columns 64 c + 16 g + 8 u on; in LDS, the wave brings those with the remainder `wave` by 4)
 #pragma unroll
@@ -198,7 +201,7 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
       ahead_b = b + 1;
       if (ahead_b < p.batch) {
         const Request r = dealer.request(ahead_b);
-        if (r.n > 0) ahead_ids = entries(ahead_b, block_of<R, kGrain>(p, r, 0).pages, 0);
+        if (r.n > 0) ahead_ids = entries(ahead_b, block_of<R, kGrain, TREE>(p, r, 0).pages, 0);
       }
     }
     // What the next block is (asked late, so that its description need not be kept through the loop), its query, and where its first page
@@ -226,7 +229,8 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
     // of a block is a copy of its own: what it has to find out would otherwise be carried through every pass.)
     auto step = [&](auto last) {
       const int pos0 = first_of(span.pages, tile);
-      const Kept kept = kept_of(p, span, pos0);
+      Kept kept = kept_of<TREE>(p, span, pos0);
+      if constexpr (TREE) kept.full = kept.full && !blind;
       f32x4 s[RT][2];
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) s[rt][0] = s[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -244,9 +248,9 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
       }
       // (the scale of a block without kept tokens may be anything)
       const float k_factor = p.scale_log2 * ks, v_scale = kept.some ? vs : 0.f;
-      int seen[RT];
+      Sight<TREE> seen[RT];
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) seen[rt] = reach[rt];
+      for (int rt = 0; rt < RT; ++rt) seen[rt] = sight[rt];
       Codes c;
       if constexpr (decltype(last)::value) {
         c = turn_to_next();
@@ -261,8 +265,8 @@ __global__ __launch_bounds__(kThreads, groups_per_cu(D, RT)) void gqa_decode_ker
       load_k<D>(t, c.k, k_at);
 
       f16x8 high[RT], low[RT];
-      weigh<D, RT>(p, a, s, seen, kept.full, pos0, g, k_factor, v_scale, high, low);
-      if (!kept.full) sanitize<D, RT>(p, a, t.v, span, pos0, g);
+      weigh<D, RT, TREE>(p, a, s, seen, span.text, kept.full, pos0, g, k_factor, v_scale, high, low);
+      if (!kept.full) sanitize<D, RT, TREE>(p, a, t.v, span, pos0, g);
       add_values<D, RT>(a, t.v, high, low);
       load_v<D>(t, c.v, v_at);
     };
@@ -414,7 +418,9 @@ hipError_t join(const GqaDecodeParams& p, int block_rows, int shares, hipStream_
 template <int D, int RT, bool OUT32, bool ALONE = false>
 hipError_t narrow(const GqaDecodeParams& p, int shares, hipStream_t stream) {
   constexpr size_t lds = ALONE ? 0 : Narrow<D, RT>::kLds;
-  hipLaunchKernelGGL((gqa_decode_kernel<D, RT, OUT32, ALONE>), dim3(ALONE ? shares / 4 : shares), dim3(kThreads), lds, stream, p);
+  const dim3 grid(ALONE ? shares / 4 : shares);
+  if (p.masks) hipLaunchKernelGGL((gqa_decode_kernel<D, RT, OUT32, ALONE, true>), grid, dim3(kThreads), lds, stream, p);
+  else hipLaunchKernelGGL((gqa_decode_kernel<D, RT, OUT32, ALONE, false>), grid, dim3(kThreads), lds, stream, p);
   return hipGetLastError();
 }
 
@@ -436,8 +442,10 @@ hipError_t start(const GqaDecodeParams& p, const GqaShape& shape, int shares, hi
 template <int D, int RT>
 hipError_t allow_lds() {
   constexpr int lds = (int)Narrow<D, RT>::kLds;
-  hipError_t e = hipFuncSetAttribute((const void*)gqa_decode_kernel<D, RT, false, false>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  if (e == hipSuccess) e = hipFuncSetAttribute((const void*)gqa_decode_kernel<D, RT, true, false>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  hipError_t e = hipSuccess;
+  for (const void* kernel : {(const void*)gqa_decode_kernel<D, RT, false, false, false>, (const void*)gqa_decode_kernel<D, RT, true, false, false>,
+                             (const void*)gqa_decode_kernel<D, RT, false, false, true>, (const void*)gqa_decode_kernel<D, RT, true, false, true>})
+    if (e == hipSuccess) e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   return e;
 }
 

@@ -89,7 +89,7 @@ __device__ __forceinline__ void wait_tile(bool one_behind) {
   else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
 }
 
-template <int D, int RT, bool OUT32>
+template <int D, int RT, bool OUT32, bool TREE>
 __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p) {
   using C = Wide<D, RT>;
   constexpr int R = C::kRows, TG = C::kTokenGroups, kWords = D / 64, kCols = D / 16, kStages = C::kStages;
@@ -97,11 +97,12 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
   uint8_t* const scale_ring = ring + kStages * 2 * C::kHalf;
   float* const o_lds = (float*)(ring + C::kRing);
   float4* const ml_lds = (float4*)(ring + C::kRing + C::kOBytes);
-  __shared__ typename Dealer<R, kThreads, kStart>::Lds dealt;
+  using Deal = Dealer<R, kThreads, kStart, 1, TREE>;
+  __shared__ typename Deal::Lds dealt;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int n16 = lane & 15, g = lane >> 4;
   const int tg = wave % TG, row0 = wave / TG * 16 * RT;
-  Dealer<R, kThreads, kStart> dealer(p, dealt);
+  Deal dealer(p, dealt);
   Piece now;
   if (!dealer.begin(now)) return;
   const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)ring;
@@ -170,15 +171,18 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
   }
 
   bf16x8 q[RT][2 * kWords];
-  int reach[RT];
+  Sight<TREE> sight[RT];
+  bool blind = false;  // (of a tree) a row keeps nothing, not even of tiles that all others keep
   auto load_q = [&](const Piece& w) {
     const int rows = dealer.rows_of(w);
+    blind = false;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       const int row = row0 + rt * 16 + n16;
       const uint32_t t = (uint32_t)(w.rb * R + row) / (uint32_t)p.group, gi = (uint32_t)(w.rb * R + row) - t * p.group;
       const bool valid = row < rows;
-      reach[rt] = valid ? w.reach((int)t) : 0;
+      sight[rt] = sight_of<TREE>(p, w, (int)t, valid);
+      if constexpr (TREE) blind = blind || __any(valid && sight[rt].reach == 0);
       const uint16_t* src = p.q + (int64_t)(w.rq.begin + (int)t) * p.q_stride + (size_t)(w.h * p.group + (int)gi) * D + g * 16;
 #pragma unroll
       for (int i = 0; i < 2 * kWords; ++i) q[rt][i] = valid ? *(const bf16x8*)(src + i / 2 * 64 + i % 2 * 8) : bf16x8{};
@@ -222,7 +226,8 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
         const float2 scale = *(const float2*)(scale_ring + (stage * kWaves + wave) * C::kScaleBytes);
         if (++stage == kStages) stage = 0;
         const int pos0 = span.pages.logical(tile) * kPage + half * C::kTokens + tg * kWaveTokens;
-        const Kept kept = kept_of(p, span, pos0);
+        Kept kept = kept_of<TREE>(p, span, pos0);
+        if constexpr (TREE) kept.full = kept.full && !blind;
         f32x4 s[RT][2];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) s[rt][0] = s[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -246,11 +251,11 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
         if (wave >= 4) issue();
         if (work) {
           f16x8 high[RT], low[RT];
-          weigh<D, RT>(p, a, s, reach, kept.full, pos0, g, p.scale_log2 * scale.x, scale.y, high, low);
+          weigh<D, RT, TREE>(p, a, s, sight, span.text, kept.full, pos0, g, p.scale_log2 * scale.x, scale.y, high, low);
           typename VWord<kWords>::type v[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[j] = *(const typename VWord<kWords>::type*)(from_stage + v_at[j % 4] + j / 4 * 16 * D);
-          if (!kept.full) sanitize<D, RT>(p, a, v, span, pos0, g);
+          if (!kept.full) sanitize<D, RT, TREE>(p, a, v, span, pos0, g);
           add_values<D, RT>(a, v, high, low);
         }
       }
@@ -278,14 +283,17 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_wide_kernel(GqaDecodeParams p
 template <int D, int RT, bool OUT32>
 hipError_t start(const GqaDecodeParams& p, int shares, hipStream_t stream) {
   constexpr size_t lds = Wide<D, RT>::kLds;
-  hipLaunchKernelGGL((gqa_wide_kernel<D, RT, OUT32>), dim3(shares), dim3(kThreads), lds, stream, p);
+  if (p.masks) hipLaunchKernelGGL((gqa_wide_kernel<D, RT, OUT32, true>), dim3(shares), dim3(kThreads), lds, stream, p);
+  else hipLaunchKernelGGL((gqa_wide_kernel<D, RT, OUT32, false>), dim3(shares), dim3(kThreads), lds, stream, p);
   return hipGetLastError();
 }
 template <int D, int RT>
 hipError_t allow_lds() {
   constexpr int lds = (int)Wide<D, RT>::kLds;
-  hipError_t e = hipFuncSetAttribute((const void*)gqa_wide_kernel<D, RT, false>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  if (e == hipSuccess) e = hipFuncSetAttribute((const void*)gqa_wide_kernel<D, RT, true>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  hipError_t e = hipSuccess;
+  for (const void* kernel : {(const void*)gqa_wide_kernel<D, RT, false, false>, (const void*)gqa_wide_kernel<D, RT, true, false>,
+                             (const void*)gqa_wide_kernel<D, RT, false, true>, (const void*)gqa_wide_kernel<D, RT, true, true>})
+    if (e == hipSuccess) e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   return e;
 }
 

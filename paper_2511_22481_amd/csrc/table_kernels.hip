@@ -227,6 +227,36 @@ __global__ __launch_bounds__(kThreads) void release_kernel(ReleaseParams p) {
   if (tid == 0) *p.free_count = (int)min((int64_t)count + pages, p.num_pages);
 }
 
+// Requests lose their last tokens: L - dropped are left, and the pages above ceil(L / 128) of them go back on the stack, in the order of
+// the requests and their rows.  As a release, one running sum (of pages) and one work group.
+__global__ __launch_bounds__(kThreads) void truncate_kernel(TruncateParams p) {
+  __shared__ uint32_t tot[kThreads / 64];
+  __shared__ uint32_t page_end[kThreads];
+  __shared__ int left[kThreads];  // pages that a request keeps
+  const int tid = threadIdx.x, threads = blockDim.x;
+  const int count = max(*p.free_count, 0);
+  uint32_t pages = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += threads) {
+    const int b = b0 + tid;
+    const int L = b < p.batch ? p.seq_lens[b] : 0, drop = b < p.batch ? min(max(p.dropped[b], 0), max(L, 0)) : 0;
+    const int had = min(pages_of(max(L, 0)), p.max_pages), has = min(pages_of(max(L, 0) - drop), p.max_pages);
+    const uint32_t many = (uint32_t)(had - has), end = sat(sat(pages, sum_before(many, tot)), many);
+    page_end[tid] = end;
+    left[tid] = has;
+    if (b < p.batch) p.seq_lens_out[b] = L - drop;
+    __syncthreads();
+    const uint32_t stop = page_end[threads - 1];
+    for (uint32_t k = pages + tid; k < stop; k += threads) {
+      const int o = owner(page_end, threads, k);
+      // (a stack that is already full takes no more, as in a release)
+      if ((int64_t)count + k < p.num_pages) p.free_pages[count + k] = p.page_table[(b0 + o) * p.stride + left[o] + (int)(k - (o ? page_end[o - 1] : pages))];
+    }
+    pages = stop;
+    __syncthreads();
+  }
+  if (tid == 0) *p.free_count_out = (int)min((int64_t)count + pages, p.num_pages);
+}
+
 }  // namespace
 
 hipError_t launch_table_extend(const TableParams& p, hipStream_t stream) {
@@ -250,6 +280,12 @@ hipError_t launch_table_extend(const TableParams& p, hipStream_t stream) {
 
 hipError_t launch_table_release(const ReleaseParams& p, hipStream_t stream) {
   hipLaunchKernelGGL(release_kernel, dim3(1), dim3(kThreads), 0, stream, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_table_truncate(const TruncateParams& p, hipStream_t stream) {
+  const int threads = std::min(kThreads, (p.batch + 63) / 64 * 64);
+  hipLaunchKernelGGL(truncate_kernel, dim3(1), dim3(threads), 0, stream, p);
   return hipGetLastError();
 }
 
