@@ -23,7 +23,9 @@ constexpr int64_t kMaxPages = INT32_MAX / kPage;  // slots are int32
 std::mutex g_mutex;
 int g_cus[kMaxDevices] = {};  // compute units; 0: kernel attributes not set yet
 
-int device_cus(int* cus) {
+}  // namespace
+
+int omniattn::device_cus(int* cus) {
   int dev = 0;
   OA_HIP(hipGetDevice(&dev));
   if (dev < 0 || dev >= kMaxDevices) return OMNIATTN_EINVAL;
@@ -37,6 +39,8 @@ int device_cus(int* cus) {
   *cus = g_cus[dev];
   return OMNIATTN_OK;
 }
+
+namespace {
 
 bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 

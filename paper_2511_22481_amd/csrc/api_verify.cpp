@@ -14,15 +14,16 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 int parts_of(int32_t vocab) { return (int)(((int64_t)vocab + kVerifyColumns - 1) / kVerifyColumns); }
 
-// Byte offset of the second array, and the whole.
 struct Workspace {
-  size_t rest, bytes;
+  size_t rest, rows, choices, bytes;  // offsets, and the whole
 };
 Workspace workspace_of(int32_t num_tokens, int32_t vocab) {
   const size_t parts = (size_t)num_tokens * parts_of(vocab);
   Workspace w;
   w.rest = align256(parts * sizeof(VerifyPart));
-  w.bytes = w.rest + parts * sizeof(double);
+  w.rows = w.rest + align256(parts * sizeof(double));
+  w.choices = w.rows + align256((size_t)num_tokens * sizeof(VerifyRow));
+  w.bytes = w.choices + (size_t)num_tokens * sizeof(VerifyChoice);
   return w;
 }
 
@@ -55,6 +56,9 @@ int omniattn_tree_verify(const omniattn_verify_t* verify, const void* logits, in
   if (logits_stride < verify->vocab || (draft_probs && draft_stride < verify->vocab)) return OMNIATTN_EINVAL;
   const Workspace w = workspace_of(verify->num_tokens, verify->vocab);
   if (w.bytes > 0 && (!workspace || workspace_bytes < w.bytes || ((uintptr_t)workspace & 255))) return OMNIATTN_EWORKSPACE;
+  int cus = 0;
+  const int found = device_cus(&cus);
+  if (found != OMNIATTN_OK) return found;
   VerifyParams p;
   p.logits = logits;
   p.stride = logits_stride;
@@ -71,12 +75,14 @@ int omniattn_tree_verify(const omniattn_verify_t* verify, const void* logits, in
   p.dropped = dropped;
   p.parts = (VerifyPart*)workspace;
   p.rest = (double*)((char*)workspace + w.rest);
+  p.rows = (VerifyRow*)((char*)workspace + w.rows);
+  p.choices = (VerifyChoice*)((char*)workspace + w.choices);
   p.batch = verify->batch;
   p.num_tokens = verify->num_tokens;
   p.vocab = verify->vocab;
   p.num_parts = parts_of(verify->vocab);
   p.logits_fp32 = verify->logits_dtype == OMNIATTN_FP32;
-  const hipError_t e = launch_tree_verify(p, (hipStream_t)hip_stream);
+  const hipError_t e = launch_tree_verify(p, cus, (hipStream_t)hip_stream);
   return e == hipSuccess ? OMNIATTN_OK : hip_fail(e, "launch_tree_verify");
 }
 

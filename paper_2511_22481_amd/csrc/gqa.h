@@ -11,6 +11,9 @@ namespace omniattn {
 // Keeps the text of a HIP error for omniattn_last_hip_error and returns OMNIATTN_EHIP (api.cpp).
 int hip_fail(hipError_t e, const char* what);
 
+// Compute units of the current device; also sets its kernels' attributes, the first time (api_gqa.cpp).
+int device_cus(int* cus);
+
 struct TableParams {
   const int32_t* seq_lens;
   const int32_t* new_lens;

@@ -17,6 +17,20 @@ struct VerifyPart {
   int32_t best;
 };
 
+// Of a row: these over all columns, the node's first child (-1: none, or the request takes the likeliest token), whether it is taken, and its token's logit.
+struct VerifyRow {
+  double sum;
+  float top;
+  int32_t best, child, taken;
+  float logit;
+  int32_t unused;
+};
+// Of a node: its token, the child that the walk goes to (-1: none), and the logarithm of the token's probability.
+struct VerifyChoice {
+  int32_t token, next;
+  float logprob;
+};
+
 struct VerifyParams {
   const void* logits;
   int64_t stride;          // elements from one row to the next
@@ -33,9 +47,12 @@ struct VerifyParams {
   int32_t* dropped;
   VerifyPart* parts;       // [num_tokens, num_parts]
   double* rest;            // the same; sums of max(p - q, 0)
+  VerifyRow* rows;         // [num_tokens]
+  VerifyChoice* choices;   // [num_tokens]
   int batch, num_tokens, vocab, num_parts;
   int logits_fp32;
 };
-hipError_t launch_tree_verify(const VerifyParams& p, hipStream_t stream);
+// cus: the device's compute units.
+hipError_t launch_tree_verify(const VerifyParams& p, int cus, hipStream_t stream);
 
 }  // namespace omniattn
