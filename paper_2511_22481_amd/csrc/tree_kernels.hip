@@ -13,6 +13,7 @@
 #include <algorithm>
 
 #include "gqa.h"
+#include "wave.h"
 
 namespace omniattn {
 namespace {
@@ -71,26 +72,23 @@ __device__ __forceinline__ uint32_t recode(uint32_t codes, float ratio) {
 __device__ __forceinline__ u32x4 recode(const u32x4& x, float ratio) {
   return u32x4{recode(x[0], ratio), recode(x[1], ratio), recode(x[2], ratio), recode(x[3], ratio)};
 }
-__device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
-  return x;
-}
 __device__ __forceinline__ float scale_ratio(float old, float now) { return now > 0.f ? old / now : 1.f; }
+// The largest of a wave's scales, which are not negative.
+__device__ __forceinline__ float wave_max(float x) {
+  return __builtin_bit_cast(float, wave_join(__builtin_bit_cast(uint32_t, x), [](uint32_t a, uint32_t b) { return max(a, b); }));
+}
 
-// A wave to a (layer, request, KV head, K or V).  Rows go up in order, kRows at a time: a row's source lies at or behind its place, so what a pass
-// writes is no later pass's source, and within a pass all loads are done before the first store.
+// A wave to a (layer, request) and kUnits of its (KV head, K or V).  Rows go up in order, kRows at a time: a row's source lies at or behind its place, so
+// what a pass writes is no later pass's source, and within a pass all loads are done before the first store.
+constexpr int kUnits = 2;
 template <int D>
 __global__ __launch_bounds__(kThreads) void gqa_keep_kernel(GqaKeepParams p) {
   constexpr int kLanes = D / 16, kRows = 64 / kLanes;  // lanes of a row, 16 codes each; rows of a pass
-  const int lane = threadIdx.x & 63, each = p.scale_tokens, blocks = kPage / each;
-  int64_t id = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kv = id % 2;
-  id /= 2;
-  const int head = id % p.kv_heads;
-  id /= p.kv_heads;
-  const int b = id % p.batch, layer = (int)(id / p.batch);
-  if (layer >= p.layers) return;
+  const int lane = threadIdx.x & 63, each = p.scale_tokens, blocks = kPage / each, sharers = (2 * p.kv_heads + kUnits - 1) / kUnits;
+  const uint32_t id = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t group = id / (uint32_t)sharers, layer = group / (uint32_t)p.batch;
+  const int b = (int)(group - layer * p.batch), unit0 = (int)(id - group * sharers) * kUnits, units = min(kUnits, 2 * p.kv_heads - unit0);
+  if (layer >= (uint32_t)p.layers) return;
   const Nodes r = nodes_of(p.q_start, b, p.num_tokens);
   const int text = min(p.seq_lens[b], p.max_pages * kPage) - r.n;
   if (r.n > kNodes || text < 0) return;
@@ -105,47 +103,76 @@ __global__ __launch_bounds__(kThreads) void gqa_keep_kernel(GqaKeepParams p) {
   const bool mine = lane >= first && lane < kept;
   const int32_t* const table = p.page_table + b * p.table_stride;
   const int src = text + (mine ? from : first), dst = text + (mine ? lane : first);
-  const int64_t src_ph = ((int64_t)layer * p.num_pages + table[src / kPage]) * p.kv_heads + head;
-  const int64_t dst_ph = ((int64_t)layer * p.num_pages + table[dst / kPage]) * p.kv_heads + head;
-  float* const scales = p.scales[kv];
-  const float old = scales[src_ph * blocks + src % kPage / each];
+  const int64_t src_page = (layer * p.num_pages + table[src / kPage]) * p.kv_heads, dst_page = (layer * p.num_pages + table[dst / kPage]) * p.kv_heads;
   // up to three blocks (64 tokens, 32 to a block)
-  const int block0 = (text + first) / each, block = dst / each - block0;
+  const int block0 = (text + first) / each, block = dst / each - block0, last_block = (text + kept - 1) / each - block0;
   const int held = text - block0 * each;  // tokens of the text in the first of them, if any
-  const int64_t ph0 = __shfl(dst_ph, first);
-  const float own = held > 0 ? scales[ph0 * blocks + block0 * each % kPage / each] : 0.f;
-  float now = 0.f, now0 = 0.f;
+  const int64_t page0 = __shfl(dst_page, first);
+  const int64_t src_at = (src_page * kPage + src % kPage) * D, dst_at = (dst_page * kPage + dst % kPage) * D;
+  const int col = lane % kLanes * 16, in_pass = lane / kLanes;
+  auto cache = [&](int j) { return p.cache[(unit0 + j) & 1] + (size_t)((unit0 + j) >> 1) * kPage * D; };
+  auto scale_at = [&](int j, int64_t page, int at) { return p.scales[(unit0 + j) & 1] + (page + ((unit0 + j) >> 1)) * blocks + at % kPage / each; };
+  u32x4 x[kUnits];
+  auto load = [&](int row0) {
+    const int64_t s = __shfl(src_at, min(row0 + in_pass, 63));
+    if (row0 + in_pass < kept) {
 #pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    float top = wave_max(mine && block == k ? old : 0.f);
-    if (k == 0) now0 = top = fmaxf(top, own);
-    if (block == k) now = top;
+      for (int j = 0; j < kUnits; ++j)
+        if (j < units) x[j] = *(const u32x4*)(cache(j) + s + col);
+    }
+  };
+  load(first);
+  float old[kUnits], own[kUnits], ratio[kUnits], now[kUnits], now0[kUnits];
+#pragma unroll
+  for (int j = 0; j < kUnits; ++j) {
+    old[j] = own[j] = 0.f;
+    if (j < units) {
+      old[j] = *scale_at(j, src_page, src);
+      if (held > 0) own[j] = *scale_at(j, page0, block0 * each);
+    }
   }
-  const float ratio = scale_ratio(old, now);
-  uint8_t* const cache = p.cache[kv];
-  const int64_t src_at = (src_ph * kPage + src % kPage) * D, dst_at = (dst_ph * kPage + dst % kPage) * D;
-  const int col = lane % kLanes * 16;
+#pragma unroll
+  for (int j = 0; j < kUnits; ++j) {
+    now[j] = 0.f;
+    for (int k = 0; k <= last_block; ++k) {
+      float top = wave_max(mine && block == k ? old[j] : 0.f);
+      if (k == 0) now0[j] = top = fmaxf(top, own[j]);
+      if (block == k) now[j] = top;
+    }
+    ratio[j] = scale_ratio(old[j], now[j]);
+  }
   for (int row0 = first; row0 < kept; row0 += kRows) {
-    const int row = row0 + lane / kLanes, at = min(row, 63);
-    const int64_t s = __shfl(src_at, at), d = __shfl(dst_at, at);
-    const float f = __shfl(ratio, at);
+    const int row = row0 + in_pass, at = min(row, 63);
+    const int64_t d = __shfl(dst_at, at);
+    u32x4 y[kUnits];
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) {
+      const float f = __shfl(ratio[j], at);
+      y[j] = x[j];
+      if (f != 1.f) y[j] = recode(y[j], f);
+    }
+    load(row0 + kRows);
     if (row < kept) {
-      u32x4 x = *(const u32x4*)(cache + s + col);
-      if (f != 1.f) x = recode(x, f);
-      *(u32x4*)(cache + d + col) = x;
+#pragma unroll
+      for (int j = 0; j < kUnits; ++j)
+        if (j < units) *(u32x4*)(cache(j) + d + col) = y[j];
     }
   }
-  // tokens of the text in the first block, if its scale has grown
-  if (held > 0 && now0 > own) {
-    const float f = scale_ratio(own, now0);
-    uint8_t* const rows = cache + (ph0 * kPage + block0 * each % kPage) * D;
-    for (int row = lane / kLanes; row < held; row += kRows) {
-      u32x4* const at = (u32x4*)(rows + row * D + col);
-      *at = recode(*at, f);
+#pragma unroll
+  for (int j = 0; j < kUnits; ++j) {
+    if (j >= units) break;
+    // tokens of the text in the first block, if its scale has grown
+    if (held > 0 && now0[j] > own[j]) {
+      const float f = scale_ratio(own[j], now0[j]);
+      uint8_t* const rows = cache(j) + (page0 * kPage + block0 * each % kPage) * D;
+      for (int row = in_pass; row < held; row += kRows) {
+        u32x4* const at = (u32x4*)(rows + row * D + col);
+        *at = recode(*at, f);
+      }
     }
+    // (the first row of each block writes its scale)
+    if (mine && (lane == first || dst % each == 0)) *scale_at(j, dst_page, dst) = now[j];
   }
-  // (the first row of each block writes its scale)
-  if (mine && (lane == first || dst % each == 0)) scales[dst_ph * blocks + dst % kPage / each] = now;
 }
 
 }  // namespace
@@ -156,7 +183,8 @@ hipError_t launch_tree_masks(const TreeMasksParams& p, hipStream_t stream) {
 }
 
 hipError_t launch_gqa_keep(const GqaKeepParams& p, hipStream_t stream) {
-  const dim3 grid((uint32_t)(((int64_t)p.layers * p.batch * p.kv_heads * 2 + kWaves - 1) / kWaves));
+  const int64_t waves = (int64_t)p.layers * p.batch * ((2 * p.kv_heads + kUnits - 1) / kUnits);
+  const dim3 grid((uint32_t)((waves + kWaves - 1) / kWaves));
   if (p.head_dim == 64) hipLaunchKernelGGL(gqa_keep_kernel<64>, grid, dim3(kThreads), 0, stream, p);
   else if (p.head_dim == 128) hipLaunchKernelGGL(gqa_keep_kernel<128>, grid, dim3(kThreads), 0, stream, p);
   else hipLaunchKernelGGL(gqa_keep_kernel<256>, grid, dim3(kThreads), 0, stream, p);

@@ -19,6 +19,7 @@
 #include <algorithm>
 
 #include "verify.h"
+#include "wave.h"
 
 namespace omniattn {
 namespace {
@@ -102,19 +103,6 @@ __device__ __forceinline__ double wave_sum_up_to(double x) {
   return x;
 }
 __device__ __forceinline__ double wave_sum(double x) { return readlane64(wave_sum_up_to(x), 63); }
-template <typename F>
-__device__ __forceinline__ uint32_t wave_join(uint32_t x, F f) {
-#define OMNIATTN_JOIN(ctrl) x = f(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, 0xf, 0xf, true))
-  OMNIATTN_JOIN(0xb1);   // the other of two
-  OMNIATTN_JOIN(0x4e);   // the other two of four
-  OMNIATTN_JOIN(0x141);  // eight, mirrored
-  OMNIATTN_JOIN(0x140);  // sixteen, mirrored
-#undef OMNIATTN_JOIN
-  const auto y = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-  x = f(y[0], y[1]);
-  const auto z = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-  return (uint32_t)uniform((int)f(z[0], z[1]));
-}
 __device__ __forceinline__ float wave_max(float x) {
   return __builtin_bit_cast(float, wave_join(__builtin_bit_cast(uint32_t, x), [](uint32_t a, uint32_t b) {
     return __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)));
