@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libomniattn.so")
 SOURCES = ["decode_kernels.hip", "decode_mid_kernel.hip", "decode_narrow_kernel.hip", "append_kernels.hip",
            "table_kernels.hip", "gqa_append_kernel.hip", "gqa_decode_kernel.hip",
-           "gqa_wide_kernel.hip", "tree_kernels.hip", "verify_kernels.hip", "api.cpp", "api_gqa.cpp", "api_verify.cpp", "plan.cpp"]
+           "gqa_wide_kernel.hip", "gqa_tree_kernel.hip", "tree_kernels.hip", "verify_kernels.hip", "api.cpp", "api_gqa.cpp", "api_verify.cpp", "plan.cpp"]
 HEADERS = ["kernels.h", "gqa.h", "verify.h", "wave.h", "gqa_common.h", "gqa_deal.h", "plan.h", "decode_common.h", os.path.join("..", "..", "include", "omniattn.h")]
 
 MARSHAL = os.path.join(HERE, "gqa_marshal.so")
@@ -123,7 +123,8 @@ def check_generated_code(verbose=False):
                                       ("decode_mid_kernel.hip", "decode_mid_kernel", True),
                                       ("decode_narrow_kernel.hip", "decode_narrow_kernel", False),
                                       ("gqa_decode_kernel.hip", "gqa_decode_kernel", True),
-                                      ("gqa_wide_kernel.hip", "gqa_wide_kernel", True)):
+                                      ("gqa_wide_kernel.hip", "gqa_wide_kernel", True),
+                                      ("gqa_tree_kernel.hip", "gqa_tree_kernel", True)):
             out = os.path.join(tmp, src + ".s")
             cmd = [hipcc(), "--offload-arch=gfx950", "-O3", "-std=c++20",
                    "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -71,9 +71,9 @@ int check_gqa(const omniattn_gqa_t* g) {
   return OMNIATTN_OK;
 }
 
-GqaShape shape_of(const omniattn_gqa_t* g, int cus) {
+GqaShape shape_of(const omniattn_gqa_t* g, int cus, bool tree) {
   const int64_t pages = std::min<int64_t>(g->max_pages_per_seq, ((int64_t)g->sink + kPage - 1) / kPage + ((int64_t)g->window + kPage - 1) / kPage + 1);
-  return gqa_shape(g->batch, g->num_queries, g->num_q_heads / g->num_kv_heads, g->num_kv_heads, g->head_dim, pages, cus);
+  return gqa_shape(g->batch, g->num_queries, g->num_q_heads / g->num_kv_heads, g->num_kv_heads, g->head_dim, pages, cus, tree);
 }
 
 struct Workspace {
@@ -109,7 +109,7 @@ int attend(const omniattn_gqa_t* gqa, const void* q, int64_t q_stride, const voi
   if (rc != OMNIATTN_OK) return rc;
   GqaDecodeParams p;
   p.group = gqa->num_q_heads / gqa->num_kv_heads;
-  const GqaShape shape = shape_of(gqa, cus);
+  const GqaShape shape = shape_of(gqa, cus, tree);
   const Workspace w = workspace_of(gqa, shape);
   if (!workspace || workspace_bytes < w.bytes || !aligned(workspace, 256)) return OMNIATTN_EWORKSPACE;
   p.q = (const uint16_t*)q;
@@ -144,7 +144,7 @@ int attend(const omniattn_gqa_t* gqa, const void* q, int64_t q_stride, const voi
   // Not more shares than there can be units of work (each block counts up to 2 beside its pages).
   const int64_t blocks = ((int64_t)p.num_queries * p.group + shape.block_rows - 1) / shape.block_rows + p.batch;
   const int64_t pages = std::min<int64_t>(p.max_pages, ((int64_t)p.S + kPage - 1) / kPage + ((int64_t)p.W + (tree ? p.num_queries + OMNIATTN_TREE_NODES : shape.block_rows) + kPage - 1) / kPage + 1);
-  const int64_t units = blocks * p.kv_heads * (shape.shares > 1 ? 4 * pages + 4 : pages + 2);
+  const int64_t units = blocks * p.kv_heads * (shape.shares > 1 || shape.kernel == kGqaTree ? 4 * pages + 4 : pages + 2);
   p.few_units = units <= INT32_MAX;
   const int groups = (int)std::min<int64_t>(shape.groups, (units + shape.shares - 1) / shape.shares);
   OA_HIP(launch_gqa_decode(p, shape, groups * shape.shares, (hipStream_t)hip_stream));
@@ -298,16 +298,17 @@ size_t omniattn_gqa_workspace_bytes(const omniattn_gqa_t* gqa) {
   int cus = 0;
   if (check_gqa(gqa) != OMNIATTN_OK || device_cus(&cus) != OMNIATTN_OK) return 0;
   // Enough for fewer queries too, and for any kept set and table width: the calls of a server share one.  (The number of queries decides
-  // by its rows to a request and KV head, up to 16, up to 32 or more; those that keep few pages have the most shares.)
+  // by its rows to a request and KV head, up to 16, up to 32 or more; those that keep few pages have the most shares, and trees over many the
+  // largest blocks.)
   size_t bytes = 0;
   omniattn_gqa_t g = *gqa;
   g.sink = g.window = 0;
   const int64_t group = gqa->num_q_heads / gqa->num_kv_heads;
   for (int rows : {16, 32, INT32_MAX}) {
     g.num_queries = (int32_t)std::min<int64_t>(gqa->num_queries, std::max<int64_t>(rows / group, 1) * gqa->batch);
-    GqaShape shape = shape_of(&g, cus);
+    const GqaShape shapes[2] = {shape_of(&g, cus, false), gqa_shape(g.batch, g.num_queries, (int)group, g.num_kv_heads, g.head_dim, kMaxPages, cus, true)};
     g.num_queries = gqa->num_queries;
-    bytes = std::max(bytes, workspace_of(&g, shape).bytes);
+    for (const GqaShape& shape : shapes) bytes = std::max(bytes, workspace_of(&g, shape).bytes);
   }
   return bytes;
 }

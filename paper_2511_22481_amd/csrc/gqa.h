@@ -102,7 +102,7 @@ struct GqaDecodeParams {
   const int32_t* q_start;   // [batch + 1], or null: query token b belongs to request b
   void* out;
   float* lse;
-  int2* rows;               // per output row: first partial slot; number of partials * 64 + row inside its block (0 partials: done)
+  int2* rows;               // per output row: first partial slot; number of partials * 64 (blocks of more rows: 128) + row inside its block (0 partials: done)
   float4* part_ml;          // [slots, block rows]: a partial row's reference (log2) and sum of weights, and its output's reference
   float* part_o;            // [slots, block rows, head_dim]: weighted sums, not yet divided
   int batch, num_queries, q_heads, kv_heads, group, head_dim;
@@ -113,19 +113,22 @@ struct GqaDecodeParams {
   float scale_log2;         // softmax_scale * log2(e)
   const uint64_t* masks;    // [num_queries]: the nodes that each query sees; null: the queries are a request's last tokens, each seeing those before it
 };
-// How a call is computed: by which kernel (gqa_decode_kernel.hip or gqa_wide_kernel.hip), tiles of 16 query rows per wave, rows of a
+// How a call is computed: by which kernel (gqa_decode_kernel.hip, gqa_wide_kernel.hip or gqa_tree_kernel.hip), tiles of 16 query rows per wave, rows of a
 // block, work groups at most, and shares of the work to each.
+enum GqaKernel { kGqaNarrow, kGqaWide, kGqaTree };
 struct GqaShape {
-  bool wide;
+  GqaKernel kernel;
   int row_tiles, block_rows, groups, shares;
   bool uncut;               // see GqaDecodeParams
 };
 // pages: those that a query's kept tokens can lie in.
-GqaShape gqa_shape(int batch, int num_queries, int group, int kv_heads, int head_dim, int64_t pages, int cus);
+GqaShape gqa_shape(int batch, int num_queries, int group, int kv_heads, int head_dim, int64_t pages, int cus, bool tree);
 hipError_t init_gqa_kernels();
 hipError_t init_gqa_wide_kernels();
+hipError_t init_gqa_tree_kernels();
 // The kernel of the shape, and the one that joins partial rows.
 hipError_t launch_gqa_decode(const GqaDecodeParams& p, const GqaShape& shape, int shares, hipStream_t stream);
 hipError_t launch_gqa_wide(const GqaDecodeParams& p, const GqaShape& shape, int shares, hipStream_t stream);
+hipError_t launch_gqa_tree(const GqaDecodeParams& p, int shares, hipStream_t stream);
 
 }  // namespace omniattn

@@ -335,8 +335,7 @@ struct Rows {
 template <int D, int RT, bool TREE>
 __device__ __forceinline__ void weigh(const GqaDecodeParams& p, Rows<D, RT>& a, const f32x4 (&s)[RT][2], const Sight<TREE> (&sight)[RT], int text, bool full, int pos0,
                                       int g, float k_factor, float v_scale, f16x8 (&high)[RT], f16x8 (&low)[RT]) {
-  // (at least 2^-100: ratio stays finite)
-  const float v_log = fmaxf(__log2f(v_scale), -100.f);
+  [[maybe_unused]] const float given_scale = v_scale;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     float x[8];
@@ -354,6 +353,9 @@ __device__ __forceinline__ void weigh(const GqaDecodeParams& p, Rows<D, RT>& a, 
       }
     }
     float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+    // (a tile that no row keeps anything of can be among a tree's, and its scale be anything)
+    if constexpr (TREE) v_scale = !full && !__any(top > -INFINITY) ? 0.f : given_scale;
+    const float v_log = fmaxf(__log2f(v_scale), -100.f);  // (at least 2^-100: ratio stays finite)
     if (__any(top > fminf(a.m[rt], a.n[rt] - v_log) + kSlack)) {
       top = row_max(top);
       const float next_m = top > a.m[rt] + kSlack ? top : a.m[rt];
@@ -375,8 +377,6 @@ __device__ __forceinline__ void weigh(const GqaDecodeParams& p, Rows<D, RT>& a, 
     for (int i = 0; i < 8; ++i) {
       w[i] = exp2_fast(x[i] - ref);
       float y = w[i] * value;
-      // (a tile that no row keeps anything of can be among a tree's, and its scale be anything)
-      if constexpr (TREE) y = x[i] == -INFINITY ? 0.f : y;
       // (fixed here: the compiler may fuse the product with one of its two uses and round the other in two steps, which
       // near a tie of f16 leaves the second term for another first term)
       asm("" : "+v"(y));

@@ -28,6 +28,14 @@ struct Block {
   int t0, t1;  // its query tokens, both included
   TileLayout pages;
 };
+// A block of up to 128 rows: how often a page is halved into units, so that a unit is the same work whatever the rows (32 rows: 128 tokens; 64: 64; more: 32).
+template <int ROWS, typename P>
+OA_INLINE int tree_split(const P& p, const Request& r, int rb) {
+  if (ROWS < 128) return 0;
+  const int rows = lesser(r.n * p.group - rb * ROWS, ROWS);
+  return rows <= 32 ? 0 : rows <= 64 ? 1 : 2;
+}
+
 // TREE: the queries are nodes of a tree, of which any may see any, and which stand up to n - 1 tokens behind their positions: every block has the
 // nodes' pages and all that a query at the first node's position keeps of the text.
 template <int ROWS, int GRAIN, bool TREE = false, typename P>
@@ -36,9 +44,9 @@ OA_INLINE Block block_of(const P& p, const Request& r, int rb) {
   if constexpr (TREE) {
     k.t0 = 0;
     k.t1 = r.n - 1;
-    const int text = r.L - r.n;
+    const int text = r.L - r.n, grain = GRAIN >> tree_split<ROWS>(p, r, rb);
     // (without a window: the nodes that are sink tokens)
-    k.pages = tile_layout(r.L, p.W == 0 && text < p.S ? p.S + OMNIATTN_TREE_NODES : p.S, p.W > 0 ? (int)lesser((int64_t)p.W + k.t1, (int64_t)larger(r.L, 1)) : 0, GRAIN);
+    k.pages = tile_layout(r.L, p.W == 0 && text < p.S ? p.S + OMNIATTN_TREE_NODES : p.S, p.W > 0 ? (int)lesser((int64_t)p.W + k.t1, (int64_t)larger(r.L, 1)) : 0, grain);
     return k;
   }
   // (rows of a call are counted in 32 bits; most requests have one block, and divisions are what a share's finding consists of)

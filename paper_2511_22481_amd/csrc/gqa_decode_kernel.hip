@@ -376,7 +376,7 @@ __device__ __forceinline__ void join_row(const GqaDecodeParams& p, int64_t row, 
 
 // ROWS: to a wave (with one wave to a row), of which it joins those that are in parts.
 template <int D, bool OUT32, int WAVES, int BATCH, int ROWS>
-__global__ __launch_bounds__(64 * (WAVES > 4 ? WAVES : 4)) void gqa_combine_kernel(GqaDecodeParams p, int block_rows, int shares) {
+__global__ __launch_bounds__(64 * (WAVES > 4 ? WAVES : 4)) void gqa_combine_kernel(GqaDecodeParams p, int block_rows, int shares, int shift) {
   static_assert(WAVES == 1 || ROWS == 1);
   __shared__ float sh_o[WAVES > 1 ? WAVES : 1][D];
   __shared__ float4 sh_ml[WAVES];
@@ -388,18 +388,18 @@ __global__ __launch_bounds__(64 * (WAVES > 4 ? WAVES : 4)) void gqa_combine_kern
       // (all three are asked for together)
       d = p.rows[row];
       const int token = (int)((uint32_t)row / (uint32_t)p.q_heads), first = p.q_start ? p.q_start[0] : 0, stop = p.q_start ? p.q_start[p.batch] : p.num_queries;
-      const int count = d.y / 64;
+      const int count = d.y >> shift;
       // (rows of no request: nothing was written for them)
       if (token < first || token >= stop || count <= 0 || d.x < 0 || d.x / 2 + count > shares) d.y = 0;
     }
   }
   if constexpr (ROWS == 1) {
     const int y = __builtin_amdgcn_readfirstlane(d.y);
-    if (y >= 64) join_row<D, OUT32, WAVES, BATCH>(p, row, d.x, y / 64, y % 64, block_rows, sh_o, sh_ml);
+    if (y >> shift) join_row<D, OUT32, WAVES, BATCH>(p, row, d.x, y >> shift, y & ((1 << shift) - 1), block_rows, sh_o, sh_ml);
   } else {
-    for (uint64_t rest = __ballot(d.y >= 64); rest; rest &= rest - 1) {
+    for (uint64_t rest = __ballot((d.y >> shift) > 0); rest; rest &= rest - 1) {
       const int k = __builtin_ctzll(rest), y = __builtin_amdgcn_readlane(d.y, k);
-      join_row<D, OUT32, 1, BATCH>(p, row0 + k, __builtin_amdgcn_readlane(d.x, k), y / 64, y % 64, block_rows, sh_o, sh_ml);
+      join_row<D, OUT32, 1, BATCH>(p, row0 + k, __builtin_amdgcn_readlane(d.x, k), y >> shift, y & ((1 << shift) - 1), block_rows, sh_o, sh_ml);
     }
   }
 }
@@ -407,11 +407,12 @@ __global__ __launch_bounds__(64 * (WAVES > 4 ? WAVES : 4)) void gqa_combine_kern
 template <int D, bool OUT32>
 hipError_t join(const GqaDecodeParams& p, int block_rows, int shares, hipStream_t stream) {
   const int64_t rows = (int64_t)p.num_queries * p.q_heads;
+  const int shift = block_rows > 64 ? 7 : 6;  // (see GqaDecodeParams::rows)
   // Few rows: eight waves to each.  Very many, of which few are in parts (prompts): a wave looks at 16 (524288 rows: 34 us less
   // than one to a wave).
-  if (rows <= 2048) hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 8, 4, 1>), dim3((uint32_t)rows), dim3(512), 0, stream, p, block_rows, shares);
-  else if (rows <= 65536) hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 1, 4, 1>), dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, stream, p, block_rows, shares);
-  else hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 1, 4, 16>), dim3((uint32_t)((rows + 63) / 64)), dim3(256), 0, stream, p, block_rows, shares);
+  if (rows <= 2048) hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 8, 4, 1>), dim3((uint32_t)rows), dim3(512), 0, stream, p, block_rows, shares, shift);
+  else if (rows <= 65536) hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 1, 4, 1>), dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, stream, p, block_rows, shares, shift);
+  else hipLaunchKernelGGL((gqa_combine_kernel<D, OUT32, 1, 4, 16>), dim3((uint32_t)((rows + 63) / 64)), dim3(256), 0, stream, p, block_rows, shares, shift);
   return hipGetLastError();
 }
 
@@ -427,7 +428,8 @@ hipError_t narrow(const GqaDecodeParams& p, int shares, hipStream_t stream) {
 template <int D, bool OUT32>
 hipError_t start(const GqaDecodeParams& p, const GqaShape& shape, int shares, hipStream_t stream) {
   hipError_t e = hipErrorInvalidValue;
-  if (shape.wide) e = launch_gqa_wide(p, shape, shares, stream);
+  if (shape.kernel == kGqaTree) e = launch_gqa_tree(p, shares, stream);
+  else if (shape.kernel == kGqaWide) e = launch_gqa_wide(p, shape, shares, stream);
   else if (shape.shares == 4) {
     if constexpr (D == 64) e = narrow<D, 1, OUT32, true>(p, shares, stream);
   }
@@ -475,17 +477,28 @@ hipError_t allow_lds() {
 //   width 256   1 x 2     9.8/8.3   11.3/9.6     11.3/10.9    11.3/12.1    11.3/14.6    11.4/17.1
 //   wide        1 x 2    14.9/13.4  16.0/17.3    16.1/21.1    16.0/24.7    16.0/32.2    16.3/39.6
 //              64 x 2    18.0/15.9  22.5/19.9    26.2/23.7    29.7/27.5    33.4/34.7    37.3/42.2
-GqaShape gqa_shape(int batch, int num_queries, int group, int kv_heads, int head_dim, int64_t pages, int cus) {
+// Trees with more than 32 rows of width 128: gqa_tree_kernel, where its work groups have 8 steps of 32 rows and a page each; with fewer, its blocks of up to 128 rows
+// leave too few of them something to do.  us a call (replayed), 8 KV heads, wide kernel / tree kernel:
+//   rows                     32           48           64           96           128          256
+//   1 x 4000 tokens        17 / 19      22 / 25      22 / 28      25 / 31      26 / 35      33 / 41
+//   1 x 60000              35 / 38      56 / 48      59 / 50      93 / 73      95 / 80     165 / 131
+//   16 x 300               19 / 21      22 / 24      23 / 25      24 / 38      25 / 40      45 / 44
+//   16 x 2000              28 / 31      42 / 37      44 / 39      61 / 55      62 / 60     119 / 93
+//   64 x 300               20 / 24      41 / 26      43 / 27      70 / 40      79 / 42     142 / 92
+//   64 x 6000             168 / 172    261 / 222    272 / 229    467 / 365    533 / 387   1040 / 742
+// (up to 32 rows: the narrow kernel.)
+GqaShape gqa_shape(int batch, int num_queries, int group, int kv_heads, int head_dim, int64_t pages, int cus, bool tree) {
   const int64_t rows = (int64_t)((num_queries + batch - 1) / batch) * group;
   if (rows <= 16) {
     const int groups = cus * groups_per_cu(head_dim, 1);
     const bool alone = head_dim == 64 && (int64_t)batch * kv_heads >= 2 * groups && pages <= 16;
-    return GqaShape{false, 1, 16, groups, alone ? 4 : 1, pages <= (alone || head_dim == 256 ? 3 : 4)};
+    return GqaShape{kGqaNarrow, 1, 16, groups, alone ? 4 : 1, pages <= (alone || head_dim == 256 ? 3 : 4)};
   }
-  if (head_dim == 256) return GqaShape{true, 1, 64, cus, 1, pages <= 2};
-  if (rows <= 32) return GqaShape{false, 2, 32, cus * groups_per_cu(head_dim, 2), 1, pages <= 4};
-  if (head_dim == 64) return GqaShape{false, 4, 64, cus * groups_per_cu(head_dim, 4), 1, pages <= 4};
-  return GqaShape{true, 2, 64, cus, 1, pages <= 2};
+  if (tree && head_dim == 128 && rows > 32 && batch * kv_heads * pages * ((rows + 31) / 32) >= 16 * cus) return GqaShape{kGqaTree, 0, 128, 2 * cus, 1, pages <= 3};
+  if (head_dim == 256) return GqaShape{kGqaWide, 1, 64, cus, 1, pages <= 2};
+  if (rows <= 32) return GqaShape{kGqaNarrow, 2, 32, cus * groups_per_cu(head_dim, 2), 1, pages <= 4};
+  if (head_dim == 64) return GqaShape{kGqaNarrow, 4, 64, cus * groups_per_cu(head_dim, 4), 1, pages <= 4};
+  return GqaShape{kGqaWide, 2, 64, cus, 1, pages <= 2};
 }
 
 hipError_t init_gqa_kernels() {
@@ -496,6 +509,7 @@ hipError_t init_gqa_kernels() {
   if (e == hipSuccess) e = allow_lds<128, 2>();
   if (e == hipSuccess) e = allow_lds<256, 1>();
   if (e == hipSuccess) e = init_gqa_wide_kernels();
+  if (e == hipSuccess) e = init_gqa_tree_kernels();
   return e;
 }
 

@@ -708,3 +708,102 @@ def test_workspaces_of_verification():
     assert sizes == sorted(sizes) and sizes[0] >= 3 * 24
     with pytest.raises(oa.OmniAttnError):
         oa.omniattn_tree_verify_workspace_bytes(5, 0)
+
+
+# ------------------------------------------------------------------------------------------------ the kernel for many rows of width 128
+
+MANY = 16 * 256   # steps of 32 rows and a page from which on it is taken, with 256 compute units
+
+
+def _width(batch, kv_heads, rows):
+    """Columns of a table that make a call large enough for it, whatever the lengths are."""
+    return -(-MANY // (batch * kv_heads * -(-rows // 32)))
+
+
+class Wide(Problem):
+    """A table with as many columns as the rule asks for."""
+
+    def run(self, *args, **kw):
+        batch, tokens, (q_heads, kv_heads) = len(self.lens), len(self.sets), (self.q.shape[1], self.codes.shape[2])
+        rows = -(-tokens // batch) * (q_heads // kv_heads)
+        assert rows > 32
+        short = self.table
+        self.table = [r + [0] * max(0, _width(batch, kv_heads, rows) - len(r)) for r in short]
+        try:
+            return super().run(*args, **kw)
+        finally:
+            self.table = short
+
+
+@gpu
+@pytest.mark.parametrize("out_dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("sink,window", [(0, 10 ** 6), (4, 60), (130, 0), (0, 1), (3, 200)])
+@pytest.mark.parametrize("group,kv_heads,news", [(1, 2, [64, 40, 33, 64]), (3, 1, [64, 1, 12, 0, 22]), (4, 2, [8, 9, 16, 17, 24, 25, 32, 33]), (16, 1, [3, 2, 64])])
+def test_many_rows(group, kv_heads, news, sink, window, out_dtype):
+    """Blocks of 32, 64, 96 and 128 rows, and several of them."""
+    rng = random.Random(group + sink)
+    lens = [n + rng.choice([0, 5, 100, 128 - n // 2, 300, 450]) for n in news]
+    for each, kind in ((32, "any"), (128, "chain")):
+        Wide(lens, sets_of(rng, news, kind), group * kv_heads, kv_heads, 128, each, sink, window, seed=group).check(out_dtype)
+
+
+@gpu
+@pytest.mark.parametrize("sink,window", [(0, 10 ** 6), (4, 40), (0, 3)])
+def test_many_rows_any_sets(sink, window):
+    rng = random.Random(window)
+    news = [40, 64, 90, 1, 2, 64]
+    lens = [n + t for n, t in zip(news, (300, 100, 30, 0, 128, -50))]
+    Wide(lens, sets_of(rng, news, "random"), 4, 2, 128, 64, sink, window, seed=3).check()
+    Wide(lens, sets_of(rng, news, "random"), 7, 1, 128, 32, sink, window, seed=4).check(torch.float32)
+
+
+@gpu
+@pytest.mark.parametrize("group,nodes", [(1, 40), (4, 12), (4, 40), (8, 64)])
+def test_many_rows_long_texts_are_split_and_joined(group, nodes):
+    rng = random.Random(nodes)
+    Wide([9000, 77 + nodes, 5003, 64], sets_of(rng, [nodes, 2, nodes, 64]), group, 1, 128, 64, 0, 10 ** 6, seed=5, poison=False).check(torch.float32)
+
+
+@gpu
+def test_many_rows_of_negative_and_zero_softmax_scale():
+    rng = random.Random(8)
+    news = [20, 12, 33]
+    p = Wide([n + 200 for n in news], sets_of(rng, news), 8, 2, 128, 64, 0, 150, seed=8)
+    for p.scale in (-0.1, 0.0, -1e-30, 3.0):
+        p.check(torch.float32)
+
+
+@gpu
+@pytest.mark.parametrize("group", [1, 8])
+def test_many_rows_nan_reaches_only_the_queries_that_see_it(group):
+    rng = random.Random(6)
+    n = 40 if group == 1 else 12
+    sets = ref.masks(tree_of(rng, n), 0)[0]
+    L, window = 200 + n, 150
+    for slot, in_k in ((200 + 5, False), (200 + 5, True), (200, False), (200 + 1 - 150, False), (200 + 2 - 150, True)):
+        p = Wide([L], [sets], 2 * group, 2, 128, 64, 0, window, seed=7, poison=False)
+        clean, clean_lse = p.run()
+        p.codes.view(torch.uint8)[0 if in_k else 1, p.table[0][slot // PAGE], 1, slot % PAGE, 3] = 0xff
+        out, lse = p.run()
+        for t, m in enumerate(sets):
+            hit = slot in ref.kept(m, L, n, 0, window)
+            mine, others = slice(group, 2 * group), slice(0, group)
+            assert torch.equal(out[t, others], clean[t, others])
+            assert torch.isnan(lse[t, mine]).all() == (hit and in_k) and (in_k or torch.equal(lse, clean_lse))
+            bad = torch.isnan(out[t, mine])
+            if not hit:
+                assert not bad.any() and torch.equal(out[t, mine], clean[t, mine])
+            else:
+                assert bad.all() if in_k else (bad[:, 3].all() and bad.sum() == group)
+
+
+@gpu
+def test_many_rows_bf16_results_are_the_fp32_results_rounded_and_the_same_every_time():
+    rng = random.Random(9)
+    news = [rng.randint(5, 40) for _ in range(60)]
+    p = Wide([n + rng.randint(0, 900) for n in news], sets_of(rng, news), 8, 2, 128, 32, 4, 300, seed=9)
+    out, lse = p.run(fill=0x7f)
+    wide, wide_lse = p.run(torch.float32, pad=2)
+    assert torch.equal(out, wide.bfloat16()) and torch.equal(lse, wide_lse)
+    again = p.run(fill=0)
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
