@@ -4,10 +4,12 @@ one by one; steps in which every request brings at most one token are captured o
 of the work are made on the device.
 
     python -m paper_2511_22481_amd.gqa_serve [--requests 64] [--prompt 1000] [--answer 100] [--layers 8] [--heads 32]
-                                             [--kv-heads 8] [--dim 128] [--sink 0] [--window 1000000]
+                                             [--kv-heads 8] [--dim 128] [--sink 0] [--window 1000000] [--drafts 0]
 
 Prints one line: requests, steps, tokens, the largest number of pages in use, and us per layer of a decode step.  (The model's other parts
-are left out: queries, keys and values are random rows.)
+are left out: queries, keys and values are random rows.)  With --drafts N a request's step brings a tree of its last token and N drafted ones,
+of which those stay that the target's logits agree with (here a rule that the drafts guess right two times in three), and the line says how
+many tokens a step gives.
 """
 import argparse
 import json
@@ -43,6 +45,22 @@ class Pool:
         omniattn_gqa_append(k, v, slots, *cache)
         omniattn_gqa_decode(q, *cache, self.table, self.lens, self.q_start, out, lse, workspace, sink=sink, window=window,
                             softmax_scale=out.shape[2] ** -0.5)
+
+    def attend_tree(self, layer, qkv, slots, masks, out, lse, workspace, sink, window):
+        """As attend, for the nodes of trees."""
+        from . import omniattn_gqa_append, omniattn_gqa_tree
+        heads, q_heads = self.k.shape[2], out.shape[1]
+        q, k, v = qkv[:, :q_heads], qkv[:, q_heads:q_heads + heads], qkv[:, q_heads + heads:]
+        cache = self.k[layer], self.v[layer], self.k_scales[layer], self.v_scales[layer]
+        omniattn_gqa_append(k, v, slots, *cache)
+        omniattn_gqa_tree(q, *cache, self.table, self.lens, self.q_start, masks, out, lse, workspace, sink=sink, window=window,
+                          softmax_scale=out.shape[2] ** -0.5)
+
+    def keep(self, path, dropped):
+        """Of the trees that the last extend counted, the nodes on `path` stay, dropped[b] others go."""
+        from . import omniattn_gqa_keep, omniattn_table_truncate
+        omniattn_gqa_keep(path, self.lens, self.q_start, self.table, self.k, self.v, self.k_scales, self.v_scales)
+        omniattn_table_truncate(self.lens, dropped, self.table, self.free, self.free_count, self.lens, self.free_count)
 
     def release(self, done):
         from . import omniattn_table_release
@@ -121,9 +139,101 @@ def serve(pool, prompts, answers, q_heads, sink, window, rows, chunk=512, graph=
             "decode_us_per_layer": sorted(decode_us)[len(decode_us) // 2] if decode_us else None}
 
 
+def speculate(pool, prompts, answers, q_heads, sink, window, rows, draft, logits, temperature=0.0, uniforms=None, chunk=512, out_dtype=None, observe=None):
+    """Requests with the prompts' tokens (lists) get answers[b] tokens each, by trees of drafted tokens.
+
+    rows(tokens, positions, buffer) fills the rows of all layers for tokens at positions of their texts, [layers, tokens, query heads + 2 KV heads,
+    head width]; logits(out) gives the target's logits [tokens, vocabulary] from what the layers give, [layers, tokens, query heads, head
+    width].  draft(texts) returns for every text (a list; None: nothing is wanted) the tree that follows it: tokens and parents, the first one the text's
+    last token, and the probabilities that the first children were drawn from (a tensor [nodes of all, vocabulary], or None).  uniforms(nodes)
+    returns the random numbers [nodes, 2] (needed with a temperature).  observe(step, texts) sees the texts as they grow.
+
+    A request whose tree finds no pages waits, as in serve.  Returns what happened, and the texts."""
+    import torch
+    from . import omniattn_gqa_workspace_bytes, omniattn_tree_masks, omniattn_tree_verify, omniattn_tree_verify_workspace_bytes
+    layers, pages, heads, _, dim = pool.k.shape
+    batch, device = len(prompts), pool.k.device
+    ints = dict(dtype=torch.int32, device=device)
+
+    def on_gpu(values, **kw):
+        return torch.tensor(values, **{**ints, **kw})
+    texts, goal = [list(p) for p in prompts], [len(p) + a for p, a in zip(prompts, answers)]
+    heat = torch.full((batch,), temperature, device=device)
+
+    def extend(news):
+        """True for the requests that the tokens fit."""
+        before = pool.lens.clone()
+        slots = torch.empty(sum(news), **ints)
+        pool.extend(on_gpu(news), slots)
+        return slots, pool.lens == before + on_gpu(news)
+
+    def call(tokens, positions, slots, masks):
+        n = slots.numel()
+        qkv = torch.empty((layers, n, q_heads + 2 * heads, dim), dtype=torch.bfloat16, device=device)
+        rows(tokens, positions, qkv)
+        out = torch.empty((layers, n, q_heads, dim), dtype=torch.bfloat16 if out_dtype is None else out_dtype, device=device)
+        lse = torch.empty((n, q_heads), device=device)
+        workspace = torch.empty(omniattn_gqa_workspace_bytes(batch, n, q_heads, heads, dim), dtype=torch.uint8, device=device)
+        for i in range(layers):
+            if masks is None:
+                pool.attend(i, qkv[i], slots, out[i], lse, workspace, sink, window)
+            else:
+                pool.attend_tree(i, qkv[i], slots, masks, out[i], lse, workspace, sink, window)
+        return out
+
+    # the prompts without their last tokens, which are the first trees' first nodes
+    at = [0] * batch
+    while any(a < len(p) - 1 for a, p in zip(at, prompts)):
+        news = [min(chunk, len(p) - 1 - a) if len(p) else 0 for a, p in zip(at, prompts)]
+        slots, fits = extend(news)
+        if not bool((fits & (on_gpu(news) > 0)).any()):
+            raise RuntimeError(f"{int(pool.free_count)} free pages of {pages} are too few for the prompts")
+        call(on_gpu([t for p, a, n in zip(prompts, at, news) for t in p[a:a + n]]), on_gpu([i for a, n in zip(at, news) for i in range(a, a + n)]), slots, None)
+        at = [a + n * f for a, n, f in zip(at, news, fits.tolist())]
+    steps = given = used = 0
+    while any(0 < len(t) < g for t, g in zip(texts, goal)):
+        tokens, parents, probs = draft([t if 0 < len(t) < g else None for t, g in zip(texts, goal)])
+        news = [len(t) for t in tokens]
+        slots, fits = extend(news)
+        if not bool((fits & (on_gpu(news) > 0)).any()):
+            raise RuntimeError(f"{int(pool.free_count)} free pages of {pages}, and no request's tree fits: lengths {pool.lens.tolist()}")
+        used = max(used, pages - int(pool.free_count))
+        total = sum(news)
+        node, parent = on_gpu([t for x in tokens for t in x]), on_gpu([p for x in parents for p in x])
+        masks, positions = torch.empty(total, dtype=torch.int64, device=device), torch.empty(total, **ints)
+        omniattn_tree_masks(parent, pool.lens, pool.q_start, masks, positions)
+        target = logits(call(node, positions, slots, masks))
+        path, following, dropped = torch.empty(total, **ints), torch.empty(total, **ints), torch.empty(batch, **ints)
+        workspace = torch.empty(omniattn_tree_verify_workspace_bytes(total, target.shape[1]), dtype=torch.uint8, device=device)
+        numbers = torch.zeros((total, 2), device=device) if uniforms is None else uniforms(total)
+        omniattn_tree_verify(target, probs, node, parent, pool.q_start, heat, numbers, path, following, None, dropped, workspace)
+        # (a request whose tree found no pages has no nodes in the cache: nothing of it moves or goes)
+        request = torch.repeat_interleave(torch.arange(batch, device=device), on_gpu(news), output_size=total)
+        path.masked_fill_(~fits[request], -1)
+        dropped.masked_fill_(~fits, 0)
+        pool.keep(path, dropped)
+        following, fit, start = following.tolist(), fits.tolist(), [0]
+        done = [0] * batch
+        for b, n in enumerate(news):
+            new = [t for t in following[start[-1]:start[-1] + n] if t >= 0] if fit[b] else []
+            start.append(start[-1] + n)
+            new = new[:goal[b] - len(texts[b])]
+            texts[b] += new
+            given += len(new)
+            done[b] = int(n > 0 and len(texts[b]) >= goal[b])
+        if observe:
+            observe(steps, texts)
+        steps += 1
+        if any(done):
+            pool.release(on_gpu(done))
+    return {"requests": batch, "steps": steps, "tokens": given, "pages": used, "free_at_the_end": int(pool.free_count),
+            "tokens_per_step": round(given / max(steps, 1), 2)}, texts
+
+
 def main():
     ap = argparse.ArgumentParser()
-    for name, default in (("requests", 64), ("prompt", 1000), ("answer", 100), ("layers", 8), ("heads", 32), ("kv-heads", 8), ("dim", 128), ("sink", 0), ("window", 10 ** 6)):
+    for name, default in (("requests", 64), ("prompt", 1000), ("answer", 100), ("layers", 8), ("heads", 32), ("kv-heads", 8), ("dim", 128), ("sink", 0), ("window", 10 ** 6),
+                          ("drafts", 0)):
         ap.add_argument("--" + name, type=int, default=default)
     args = ap.parse_args()
     import torch
@@ -131,9 +241,37 @@ def main():
         raise SystemExit("needs a GPU: the library has no CPU path")
     gen = torch.Generator().manual_seed(1)
     prompts, answers = (torch.randint(1, 2 * n + 1, (args.requests,), generator=gen).tolist() for n in (args.prompt, args.answer))
-    each = [-(-(p + a) // PAGE) for p, a in zip(prompts, answers)]
+    if not 0 <= args.drafts < 64:
+        ap.error("a tree has up to 64 nodes: at most 63 drafts")
+    each = [-(-(p + a + args.drafts) // PAGE) for p, a in zip(prompts, answers)]
     pool = Pool(args.requests, args.layers, sum(each), args.kv_heads, args.dim, max(each))
-    print(json.dumps(serve(pool, prompts, answers, args.heads, args.sink, args.window, lambda step, buffer: buffer.normal_())))
+    if args.drafts:
+        print(json.dumps(_guessed(pool, prompts, answers, args)))
+    else:
+        print(json.dumps(serve(pool, prompts, answers, args.heads, args.sink, args.window, lambda step, buffer: buffer.normal_())))
+
+
+def _guessed(pool, prompts, answers, args, vocab=1000):
+    """A rule in the target's place: behind token t follows 7 t + 1.  Every draft follows the node before it and is right two times in three."""
+    import random
+    import torch
+    rng = random.Random(1)
+    nodes = []
+
+    def draft(texts):
+        nodes.clear()
+        tokens = [[] if t is None else [t[-1]] for t in texts]
+        for tree in tokens:
+            for _ in range(args.drafts if tree else 0):
+                tree.append((7 * tree[-1] + (1 if rng.random() < 2 / 3 else 2)) % vocab)
+            nodes.extend(tree)
+        return tokens, [list(range(-1, len(t) - 1)) for t in tokens], None
+
+    def logits(out):
+        scores = torch.zeros((out.shape[1], vocab), dtype=torch.bfloat16, device=out.device)
+        return scores.scatter_(1, torch.tensor([[(7 * t + 1) % vocab] for t in nodes], device=out.device), 20.0)
+    texts = [[rng.randrange(vocab) for _ in range(p)] for p in prompts]
+    return speculate(pool, texts, answers, args.heads, args.sink, args.window, lambda tokens, positions, buffer: buffer.normal_(), draft, logits)[0]
 
 
 if __name__ == "__main__":
