@@ -226,6 +226,7 @@ int omniattn_tree_masks(int32_t batch, int32_t num_tokens, const int32_t* parent
                         int32_t* positions, void* hip_stream) {
   if (batch < 1 || num_tokens < 0 || (!q_start && num_tokens != batch)) return OMNIATTN_EINVAL;
   if (num_tokens == 0) return OMNIATTN_OK;
+  if (batch >= INT32_MAX >> 5) return OMNIATTN_EUNSUPPORTED;  // (a launch's threads are counted in 32 bits, as below)
   if (!parents || !seq_lens || !masks || !aligned(masks, 8)) return OMNIATTN_EINVAL;
   OA_HIP(launch_tree_masks(TreeMasksParams{parents, seq_lens, q_start, masks, positions, batch, num_tokens}, (hipStream_t)hip_stream));
   return OMNIATTN_OK;
@@ -239,7 +240,7 @@ int omniattn_gqa_keep(const omniattn_gqa_t* gqa, int32_t num_layers, const int32
   if (num_layers == 0 || gqa->num_queries == 0) return OMNIATTN_OK;
   if (!path || !seq_lens || !page_table || !k_cache || !v_cache || !k_scales || !v_scales) return OMNIATTN_EINVAL;
   if (!aligned(k_cache, 16) || !aligned(v_cache, 16)) return OMNIATTN_EINVAL;
-  if ((int64_t)num_layers * gqa->batch > INT32_MAX / 2 / gqa->num_kv_heads) return OMNIATTN_EUNSUPPORTED;
+  if ((int64_t)num_layers * gqa->batch >= (INT32_MAX >> 5) / gqa->num_kv_heads) return OMNIATTN_EUNSUPPORTED;
   GqaKeepParams p;
   p.path = path;
   p.seq_lens = seq_lens;

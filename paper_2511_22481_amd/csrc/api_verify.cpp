@@ -31,9 +31,9 @@ int check_verify(const omniattn_verify_t* v) {
   if (!v) return OMNIATTN_EINVAL;
   if (v->batch < 1 || v->num_tokens < 0 || v->vocab < 1) return OMNIATTN_EINVAL;
   if (v->logits_dtype != OMNIATTN_BF16 && v->logits_dtype != OMNIATTN_FP32) return OMNIATTN_EUNSUPPORTED;
-  // (columns are counted in 32 bits with a wave's columns on top, work groups in 31)
-  if (v->vocab > INT32_MAX - kVerifyColumns) return OMNIATTN_EUNSUPPORTED;
-  if ((int64_t)v->num_tokens * parts_of(v->vocab) > INT32_MAX) return OMNIATTN_EUNSUPPORTED;
+  // (columns are counted in 32 bits with a wave's columns on top, a launch's threads in 32: 64 of them to a part, 512 to a request)
+  if (v->vocab > INT32_MAX - kVerifyColumns || v->batch > INT32_MAX >> 8) return OMNIATTN_EUNSUPPORTED;
+  if ((int64_t)v->num_tokens * parts_of(v->vocab) >= INT32_MAX >> 5) return OMNIATTN_EUNSUPPORTED;
   return OMNIATTN_OK;
 }
 

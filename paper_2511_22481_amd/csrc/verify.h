@@ -25,7 +25,7 @@ struct VerifyRow {
   float logit;
   int32_t unused;
 };
-// Of a node: its token, the child that the walk goes to (-1: none), and the logarithm of the token's probability.
+// Of a node: its token, the child that the walk goes to (-1: none, -2: the node was not looked at), and the logarithm of the token's probability.
 struct VerifyChoice {
   int32_t token, next;
   float logprob;

@@ -357,8 +357,8 @@ __global__ __launch_bounds__(kThreads) void verify_rows_kernel(VerifyParams p) {
   }
   if (lane == 0) p.rows[row] = out;
 }
-// Nodes that the walk can come to as far as first children decide: such a node is passed to its first child if that is taken, and to others if not.
-// Lane a has node a.
+// Nodes that the walk is likely to come to: it goes to a first child that is taken, and to others if it is not.  (To a first child that is not taken
+// only if nothing is left of max(p - q, 0): the walk has such nodes looked at when it comes to them.)  Lane a has node a.
 __device__ __forceinline__ bool reached(int node, int parent, const VerifyRow& mine) {
   const int lane = threadIdx.x & 63, of = parent >= 0 && parent < lane ? parent : 0;
   const bool first = __shfl(mine.child, of) == lane, taken = __shfl(mine.taken, of) != 0;
@@ -386,7 +386,24 @@ __device__ __forceinline__ VerifyRow row_at(const VerifyRow& r, int lane) {
                    __builtin_amdgcn_readlane(r.taken, lane), readlane_f(r.logit, lane), 0};
 }
 
-// Sums of max(p - q, 0), of the rows whose first child is not taken and that the walk can come to (of a chain: one).  `slices` work groups to a request,
+// Of kVerifyColumns columns of a row.
+template <typename T>
+__device__ __forceinline__ void rest_of_part(const VerifyParams& p, const Row& r, double inverse, int row, int part, const Scale& c) {
+  const int lane = threadIdx.x & 63;
+  double sum = 0.0;
+#pragma unroll
+  for (int t = 0; t < Tile<T>::kMany; ++t) {
+    double w[Tile<T>::kEach];
+    float x[Tile<T>::kEach];
+    rest_of<T>(w, x, p, r, inverse, row, part * kVerifyColumns + t * Tile<T>::kColumns + lane * Tile<T>::kEach, c);
+#pragma unroll
+    for (int i = 0; i < Tile<T>::kEach; ++i) sum += w[i];
+  }
+  sum = wave_sum(sum);
+  if (lane == 0) p.rest[(size_t)row * p.num_parts + part] = sum;
+}
+
+// Sums of max(p - q, 0), of the rows whose first child is not taken and that the walk is likely to come to (of a chain: one).  `slices` work groups to a request,
 // a wave to every so many parts of kVerifyColumns columns.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void verify_rest_kernel(VerifyParams p, int slices) {
@@ -402,19 +419,7 @@ __global__ __launch_bounds__(kThreads) void verify_rest_kernel(VerifyParams p, i
     if (!reached(node, parent, mine)) continue;
     const Row all = row_of(row_at(mine, node));
     const double inverse = inverse_of(all);
-    for (int part = wave; part < p.num_parts; part += slices * kWaves) {
-      double sum = 0.0;
-#pragma unroll
-      for (int t = 0; t < Tile<T>::kMany; ++t) {
-        double w[Tile<T>::kEach];
-        float x[Tile<T>::kEach];
-        rest_of<T>(w, x, p, all, inverse, row, part * kVerifyColumns + t * Tile<T>::kColumns + lane * Tile<T>::kEach, c);
-#pragma unroll
-        for (int i = 0; i < Tile<T>::kEach; ++i) sum += w[i];
-      }
-      sum = wave_sum(sum);
-      if (lane == 0) p.rest[(size_t)row * p.num_parts + part] = sum;
-    }
+    for (int part = wave; part < p.num_parts; part += slices * kWaves) rest_of_part<T>(p, all, inverse, row, part, c);
   }
 }
 
@@ -494,21 +499,26 @@ __device__ __forceinline__ Found find(const VerifyParams& p, double border, F pa
   return last;
 }
 
-// The token of node `node` of a request, the child that the walk goes to (-1: none), and the logarithm of the token's probability.  A wave; lane a knows
-// parent and token of node a.
-template <typename T>
-__device__ __forceinline__ VerifyChoice choose(const VerifyParams& p, const Nodes& r, int node, float T0, int parent, int token) {
+// The token of node `node` of a request, the child that the walk goes to (-1: none; kUnseen: not looked at), and the logarithm of the token's
+// probability.  A wave; lane a knows parent and token of node a.  asked: the walk has come to it.
+constexpr int kUnseen = -2;
+template <typename T, bool DRAFTS>
+__device__ __forceinline__ VerifyChoice choose(const VerifyParams& p, const Nodes& r, int node, float T0, int parent, int token, bool asked) {
   const int lane = threadIdx.x & 63, row = r.begin + node;
   const Scale c = scale_of(T0);
   const uint64_t children = __ballot(lane > node && lane < r.n && parent == node);
   const Pair first = pair_of(p, row, 0);
   const float u = p.uniforms[2 * (int64_t)row + 1];
-  const bool drafted = p.draft_probs && T0 > 0.f && children;
+  const bool drafted = DRAFTS && T0 > 0.f && children;
   Row all;
   VerifyRow kept;
-  if (p.draft_probs) {
+  if constexpr (DRAFTS) {
     const VerifyRow mine = p.rows[r.begin + min(lane, r.n - 1)];
-    if (!reached(node, parent, mine)) return VerifyChoice{-1, -1, 0.f};
+    if (!reached(node, parent, mine)) {
+      if (!asked) return VerifyChoice{-1, kUnseen, 0.f};
+    } else {
+      asked = false;
+    }
     kept = row_at(mine, node);
     all = row_of(kept);
   } else {
@@ -523,6 +533,10 @@ __device__ __forceinline__ VerifyChoice choose(const VerifyParams& p, const Node
   } else if (T0 > 0.f) {
     bool found = false;
     if (drafted) {
+      if (asked) {
+        for (int part = 0; part < p.num_parts; ++part) rest_of_part<T>(p, all, inverse_of(all), row, part, c);
+        __threadfence();
+      }
       const double* const rest = p.rest + (size_t)row * p.num_parts;
       auto part_sums = [&](int k0) {
         const int k = k0 + 2 * lane;
@@ -564,14 +578,26 @@ __device__ __forceinline__ VerifyChoice choose(const VerifyParams& p, const Node
   return out;
 }
 
-// Down the tree, and the request's results.  A wave; lane a knows node a's choice.
-__device__ __forceinline__ void walk(const VerifyParams& p, int b, const Nodes& r, const VerifyChoice& mine) {
+// Down the tree.  A wave; lane a knows node a's choice.
+struct Way {
+  int kept, node;  // how many nodes, and lane i's: the i-th of them (-1: none)
+  int unseen;      // a node on it that was not looked at, or -1
+};
+__device__ __forceinline__ Way way_of(const Nodes& r, const VerifyChoice& mine) {
   const int lane = threadIdx.x & 63;
-  int kept = 0, node = -1;
-  for (int at = r.n > 0 ? 0 : -1; at >= 0; at = __builtin_amdgcn_readlane(mine.next, at)) {  // (a child's number is above its parent's)
-    if (lane == kept) node = at;
-    ++kept;
+  Way w = {0, -1, -1};
+  for (int at = r.n > 0 ? 0 : -1; at >= 0;) {  // (a child's number is above its parent's)
+    const int next = __builtin_amdgcn_readlane(mine.next, at);
+    if (lane == w.kept) w.node = at;
+    ++w.kept;
+    if (next == kUnseen) w.unseen = at;
+    at = next;
   }
+  return w;
+}
+// The request's results.
+__device__ __forceinline__ void write(const VerifyParams& p, int b, const Nodes& r, const Way& way, const VerifyChoice& mine) {
+  const int lane = threadIdx.x & 63, node = way.node;
   const int token = __shfl(mine.token, max(node, 0));
   const float logprob = __shfl(mine.logprob, max(node, 0));
   if (lane < r.n) {
@@ -579,7 +605,7 @@ __device__ __forceinline__ void walk(const VerifyParams& p, int b, const Nodes& 
     p.out_tokens[r.begin + lane] = node >= 0 ? token : -1;
     if (p.logprobs) p.logprobs[r.begin + lane] = node >= 0 ? logprob : 0.f;
   }
-  if (lane == 0) p.dropped[b] = r.n - kept;
+  if (lane == 0) p.dropped[b] = r.n - way.kept;
 }
 // A request with too many nodes keeps none.
 __device__ __forceinline__ void keep_none(const VerifyParams& p, int b, const Nodes& r) {
@@ -592,7 +618,7 @@ __device__ __forceinline__ void keep_none(const VerifyParams& p, int b, const No
 }
 
 // Trees of few nodes: a work group to a request, whose waves choose the nodes' tokens; then one walks down the tree.
-template <typename T>
+template <typename T, bool DRAFTS>
 __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(VerifyParams p) {
   __shared__ VerifyChoice choices[kNodes];
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), b = blockIdx.x;
@@ -600,15 +626,25 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(VerifyParams 
   if (r.n > kNodes) return keep_none(p, b, r);
   const float T0 = p.temperature[b];
   const int parent = lane < r.n ? p.parents[r.begin + lane] : -1, token = lane < r.n ? p.tokens[r.begin + lane] : -1;
-  for (int i = wave; i < r.n; i += kPickThreads / 64) {
-    const VerifyChoice choice = choose<T>(p, r, i, T0, parent, token);
-    if (lane == 0) choices[i] = choice;
+  for (int first = wave, end = r.n, asked = false;; asked = true) {
+    for (int i = first; i < end; i += kPickThreads / 64) {
+      const VerifyChoice choice = choose<T, DRAFTS>(p, r, i, T0, parent, token, asked);
+      if (lane == 0) choices[i] = choice;
+    }
+    __syncthreads();
+    const VerifyChoice mine = choices[min(lane, max(r.n - 1, 0))];
+    const Way way = way_of(r, mine);
+    if (!DRAFTS || way.unseen < 0) {
+      if (wave == 0) write(p, b, r, way, mine);
+      break;
+    }
+    first = way.unseen + wave;  // (by the first wave)
+    end = way.unseen + 1;
+    __syncthreads();
   }
-  __syncthreads();
-  if (wave == 0) walk(p, b, r, choices[min(lane, max(r.n - 1, 0))]);
 }
 // Trees of many: a wave to a node of the call; and then a wave to a request.
-template <typename T>
+template <typename T, bool DRAFTS>
 __global__ __launch_bounds__(kThreads) void verify_choose_kernel(VerifyParams p) {
   const int lane = threadIdx.x & 63, row = blockIdx.x * kWaves + uniform(threadIdx.x >> 6);
   if (row >= p.num_tokens) return;
@@ -617,42 +653,54 @@ __global__ __launch_bounds__(kThreads) void verify_choose_kernel(VerifyParams p)
   const Nodes r = nodes_of(p, owner.b);
   if (r.n > kNodes) return;
   const int parent = lane < r.n ? p.parents[r.begin + lane] : -1, token = lane < r.n ? p.tokens[r.begin + lane] : -1;
-  const VerifyChoice choice = choose<T>(p, r, row - r.begin, owner.T, parent, token);
+  const VerifyChoice choice = choose<T, DRAFTS>(p, r, row - r.begin, owner.T, parent, token, false);
   if (lane == 0) p.choices[row] = choice;
 }
+template <typename T, bool DRAFTS>
 __global__ __launch_bounds__(64) void verify_walk_kernel(VerifyParams p) {
   const int b = blockIdx.x, lane = threadIdx.x;
   const Nodes r = nodes_of(p, b);
   if (r.n > kNodes) return keep_none(p, b, r);
-  walk(p, b, r, lane < r.n ? p.choices[r.begin + lane] : VerifyChoice{-1, -1, 0.f});
+  VerifyChoice mine = lane < r.n ? p.choices[r.begin + lane] : VerifyChoice{-1, -1, 0.f};
+  Way way = way_of(r, mine);
+  if (DRAFTS && way.unseen >= 0) {
+    const int parent = lane < r.n ? p.parents[r.begin + lane] : -1, token = lane < r.n ? p.tokens[r.begin + lane] : -1;
+    do {
+      const VerifyChoice choice = choose<T, DRAFTS>(p, r, way.unseen, p.temperature[b], parent, token, true);
+      if (lane == way.unseen) mine = choice;
+      way = way_of(r, mine);
+    } while (way.unseen >= 0);
+  }
+  write(p, b, r, way, mine);
 }
 
-template <typename T>
+template <typename T, bool DRAFTS>
 hipError_t start(const VerifyParams& p, int cus, hipStream_t stream) {
   const dim3 by_row((p.num_tokens + kWaves - 1) / kWaves);
   if (p.num_tokens > 0) {
     const int64_t groups = ((int64_t)p.num_tokens * p.num_parts + kWaves - 1) / kWaves;
     hipLaunchKernelGGL(verify_sums_kernel<T>, dim3((uint32_t)groups), dim3(kThreads), 0, stream, p);
-    if (p.draft_probs) {
+    if constexpr (DRAFTS) {
       const int slices = std::max(1, std::min((p.num_parts + kWaves - 1) / kWaves, 8 * cus / p.batch));
       hipLaunchKernelGGL(verify_rows_kernel<T>, by_row, dim3(kThreads), 0, stream, p);
       hipLaunchKernelGGL(verify_rest_kernel<T>, dim3((uint32_t)p.batch * slices), dim3(kThreads), 0, stream, p, slices);
     }
     // (the host knows their mean)
     if (p.num_tokens > (int64_t)p.batch * (kPickThreads / 64)) {
-      hipLaunchKernelGGL(verify_choose_kernel<T>, by_row, dim3(kThreads), 0, stream, p);
-      hipLaunchKernelGGL(verify_walk_kernel, dim3(p.batch), dim3(64), 0, stream, p);
+      hipLaunchKernelGGL((verify_choose_kernel<T, DRAFTS>), by_row, dim3(kThreads), 0, stream, p);
+      hipLaunchKernelGGL((verify_walk_kernel<T, DRAFTS>), dim3(p.batch), dim3(64), 0, stream, p);
       return hipGetLastError();
     }
   }
-  hipLaunchKernelGGL(verify_pick_kernel<T>, dim3(p.batch), dim3(kPickThreads), 0, stream, p);
+  hipLaunchKernelGGL((verify_pick_kernel<T, DRAFTS>), dim3(p.batch), dim3(kPickThreads), 0, stream, p);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_tree_verify(const VerifyParams& p, int cus, hipStream_t stream) {
-  return p.logits_fp32 ? start<float>(p, cus, stream) : start<uint16_t>(p, cus, stream);
+  if (p.draft_probs) return p.logits_fp32 ? start<float, true>(p, cus, stream) : start<uint16_t, true>(p, cus, stream);
+  return p.logits_fp32 ? start<float, false>(p, cus, stream) : start<uint16_t, false>(p, cus, stream);
 }
 
 }  // namespace omniattn

@@ -402,6 +402,28 @@ def test_verify_drafts_that_equal_the_target_and_uniforms_at_the_ends():
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("batch,nodes,vocab", [(1, 6, 1000), (3, 20, 5000), (2, 64, 300000)])
+def test_verify_refused_first_children_that_are_sampled_after_all(batch, nodes, vocab, dtype):
+    """Drafts' probabilities above the target's everywhere: a first child is refused, nothing is left of max(p - q, 0), and p's sample is the same
+    token.  Node 9 has a q that leaves something of p."""
+    rng, gen = random.Random(vocab), torch.Generator().manual_seed(vocab)
+    logits, q, tokens, parents, start, u = _drafts(rng, gen, [nodes] * batch, vocab, dtype, True, [1.0] * batch, kind="chain")
+    for b in range(batch):
+        for t in range(nodes - 1):
+            row = start[b] + t
+            logits[row, tokens[row + 1]] = 30.0
+            if t % 4 != 3:
+                q[row] = 2.0
+                u[row, 0] = 0.75
+            if t == 9:   # (refused, and another token in its place)
+                q[row] = 0.0
+                q[row, tokens[row + 1]] = 2.0
+    path = _check_verify(logits.cuda(), q.cuda(), tokens, parents, start, [1.0] * batch, u.cuda())[0]
+    assert (path.view(batch, nodes)[:, :10].amax(1) == min(nodes - 1, 9)).all()
+
+
+@gpu
 def test_verify_nodes_that_the_walk_does_not_reach_and_too_many_of_them():
     rng, gen = random.Random(3), torch.Generator().manual_seed(3)
     vocab, news = 50, [65, 4, 64, 100, 6]
@@ -591,6 +613,7 @@ def test_tree_masks_refuses_bad_arguments():
     good = [2, 5, GOOD, GOOD, GOOD, GOOD, GOOD, None]
     for at, value in ((0, 0), (0, -1), (1, -1), (2, None), (3, None), (4, None), (5, None), (5, GOOD + 4)):
         assert lib.omniattn_tree_masks(*(good[:at] + [value] + good[at + 1:])) == -1, (at, value)
+    assert lib.omniattn_tree_masks(1 << 27, 5, *good[2:]) == -2
     assert lib.omniattn_tree_masks(2, 0, None, None, GOOD, None, None, None) == 0
 
 
@@ -613,7 +636,8 @@ def test_tree_attention_refuses_bad_problems(change, code):
 
 
 @pytest.mark.parametrize("change,code", [(dict(batch=0), -1), (dict(num_tokens=-1), -1), (dict(vocab=0), -1), (dict(vocab=-5), -1), (dict(logits_dtype=oa.FP8_E4M3), -2),
-                                         (dict(vocab=2 ** 31 - 1), -2), (dict(num_tokens=2 ** 31 - 1, vocab=2 ** 20), -2)])
+                                         (dict(vocab=2 ** 31 - 1), -2), (dict(num_tokens=2 ** 31 - 1, vocab=2 ** 20), -2),
+                                         (dict(num_tokens=2 ** 26), -2), (dict(num_tokens=2 ** 20, vocab=2 ** 17), -2), (dict(batch=2 ** 23), -2)])
 def test_verify_refuses_bad_problems(change, code):
     lib = oa.load_library()
     v = oa.Verify(**dict(dict(batch=2, num_tokens=5, vocab=100, logits_dtype=oa.BF16), **change))
@@ -637,7 +661,8 @@ def test_keep_refuses_bad_arguments():
     good = [ctypes.byref(g), 4, *[GOOD] * 8, None]
     for at, value in ((0, None), (1, -1), (2, None), (3, None), (4, None), (5, None), (6, None), (6, GOOD + 8), (7, None), (7, GOOD + 4), (8, None), (9, None)):
         assert lib.omniattn_gqa_keep(*(good[:at] + [value] + good[at + 1:])) == -1, (at, value)
-    for change, code in ((dict(batch=0), -1), (dict(head_dim=32), -2), (dict(scale_tokens=8), -2), (dict(page_table_stride=2), -1), (dict(num_pages=1 << 24), -2), (dict(batch=1 << 30), -2)):
+    for change, code in ((dict(batch=0), -1), (dict(head_dim=32), -2), (dict(scale_tokens=8), -2), (dict(page_table_stride=2), -1), (dict(num_pages=1 << 24), -2), (dict(batch=1 << 30), -2),
+                         (dict(batch=1 << 23), -2)):
         h = _gqa(**dict(dict(num_queries=3), **change))
         assert lib.omniattn_gqa_keep(ctypes.byref(h), 4, *[GOOD] * 8, None) == code, change
     assert lib.omniattn_gqa_keep(ctypes.byref(g), 0, *[GOOD] * 8, None) == 0
