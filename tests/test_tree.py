@@ -442,6 +442,18 @@ def test_verify_nodes_that_the_walk_does_not_reach_and_too_many_of_them():
 
 
 @gpu
+@pytest.mark.parametrize("with_q", [False, True])
+@pytest.mark.parametrize("batch,most,vocab", [(150, 3, 40), (150, 30, 2100), (2, 9, 270000), (3, 40, 300001)])
+def test_verify_many_requests_and_large_vocabularies(batch, most, vocab, with_q):
+    """More requests than a wave looks at at once, more parts of a row than it does; few nodes to a request and many."""
+    rng, gen = random.Random(batch + vocab), torch.Generator().manual_seed(vocab)
+    news = [rng.randint(0, most) for _ in range(batch)]
+    T = [rng.choice([0.0, 0.6, 1.0, 40.0]) for _ in news]      # (40: all of the parts have a share)
+    logits, q, tokens, parents, start, u = _drafts(rng, gen, news, vocab, torch.bfloat16, with_q, T)
+    _check_verify(logits.cuda(), None if q is None else q.cuda(), tokens, parents, start, T, u.cuda())
+
+
+@gpu
 def test_verify_of_nothing():
     got = _verify(torch.empty((0, 100), device="cuda"), None, [], [], [0, 0, 0], [1.0, 0.0], torch.empty((0, 2), device="cuda"))
     assert got[3].tolist() == [0, 0]
@@ -832,3 +844,55 @@ def test_many_rows_bf16_results_are_the_fp32_results_rounded_and_the_same_every_
     assert torch.equal(out, wide.bfloat16()) and torch.equal(lse, wide_lse)
     again = p.run(fill=0)
     assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
+# ------------------------------------------------------------------------------------------------ large caches, long texts
+
+@gpu
+@pytest.mark.parametrize("nodes", [2, 40])
+def test_a_cache_of_more_than_four_gigabytes(nodes):
+    """Pages at the end of a pool whose byte offsets pass 32 bits give what the same pages at its beginning give."""
+    heads, dim, each = 8, 128, 64
+    pages = 2 ** 32 // (heads * PAGE * dim) + 40
+    k, v = (torch.zeros((pages, heads, PAGE, dim), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn) for _ in range(2))
+    ks, vs = torch.zeros((2, pages, heads, PAGE // each), device="cuda")
+    p = (Wide if nodes > 32 else Problem)([300], sets_of(random.Random(1), [nodes]), 8, 8, dim, each, 0, 10 ** 6, seed=71, poison=False)
+    want, want_lse = p.check(torch.float32)
+    ws = torch.empty(oa.omniattn_gqa_workspace_bytes(1, nodes, 8, heads, dim), dtype=torch.uint8, device="cuda")
+    for own in ([3, 1, 2], [pages - 1, pages - 30, pages - 2]):
+        pick, was = torch.tensor(own, device="cuda"), torch.tensor(p.table[0], device="cuda")
+        for cache, codes in ((k, p.codes[0]), (v, p.codes[1])):
+            cache.view(torch.uint8)[pick] = codes.view(torch.uint8).cuda()[was]
+        ks[pick], vs[pick] = p.scales[0].cuda()[was], p.scales[1].cuda()[was]
+        out, lse = torch.empty_like(want), torch.empty_like(want_lse)
+        table = ints([own + [0] * (max(3, _width(1, heads, nodes)) - 3 if nodes > 32 else 0)])
+        oa.omniattn_gqa_tree(p.q.cuda(), k, v, ks, vs, table, ints([300]), None if nodes == 1 else ints([0, nodes]), longs(p.sets), out, lse, ws, sink=0, window=10 ** 6, softmax_scale=p.scale)
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+@gpu
+@pytest.mark.parametrize("sink,window", [(0, 2 ** 31 - 1), (2 ** 31 - 1, 0), (0, 2 ** 30 + 1000), (100, 2 ** 30 + 900), (0, 2 ** 30 - 100)])
+@pytest.mark.parametrize("dim,q_heads", [(64, 1), (128, 1), (128, 11), (256, 3), (128, 40)])
+def test_requests_of_more_than_2_30_tokens(dim, q_heads, sink, window):
+    """The first page holds nearly all of the weight, one page of zero keys and values stands for all the others, the nodes' among them.  Logits are 40 and 0,
+    so the 2^30 others are 2^30 exp(-40) / 128 = 4e-11 of the sum, and what the rounding of their own sum does is far below the tolerance: 128 weights
+    and their sum (2^-22, 2^-24 each), logits of 40 (2^-20 for the products, the factor and exp2)."""
+    length, nodes = 2 ** 30 + 1000, 3
+    table = torch.zeros((1, -(-length // PAGE)), dtype=torch.int32, device="cuda")
+    table[0, 0] = 1
+    k, v = torch.zeros((2, 2, 1, PAGE, dim), dtype=torch.float32)
+    k[1], v[1] = 1.0, (torch.arange(PAGE) % 5).float()[None, :, None]
+    k, v = (t.to(torch.float8_e4m3fn).cuda() for t in (k, v))
+    ones = torch.ones((2, 1, 2), device="cuda")
+    q = torch.ones((nodes, q_heads, dim), dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.empty((nodes, q_heads, dim), device="cuda"), torch.empty((nodes, q_heads), device="cuda")
+    ws = torch.empty(oa.omniattn_gqa_workspace_bytes(1, nodes, q_heads, 1, dim), dtype=torch.uint8, device="cuda")
+    oa.omniattn_gqa_tree(q, k, v, ones, ones, table, ints([length]), ints([0, nodes]), longs([1, 3, 5]), out, lse, ws, sink=sink, window=window, softmax_scale=40 / dim)
+    for t, position in enumerate((length - nodes, length - nodes + 1, length - nodes + 1)):
+        kept = [j for j in range(PAGE) if j < sink or j > position - window]
+        if kept:
+            want, want_lse = sum(j % 5 for j in kept) / len(kept), 40 + np.log(len(kept))
+        else:
+            want, want_lse = 0.0, np.log(window)
+        assert np.abs(gref.as_double(lse[t]) - want_lse).max() <= 40 * 2.0 ** -20 + 128 * 2.0 ** -23 + (0 if kept else 1e-3)
+        assert np.abs(gref.as_double(out[t]) - want).max() <= 4 * (40 * 2.0 ** -20 + 128 * 2.0 ** -22)
