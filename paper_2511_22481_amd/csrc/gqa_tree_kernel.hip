@@ -1,11 +1,18 @@
-// Attention of the nodes of drafted trees (see gqa_decode_kernel.hip for the formulas and how the work is dealt out) with more than 16 query
-// rows to a request and KV head, heads of 128 or 256.
+// Attention of the nodes of drafted trees (see gqa_decode_kernel.hip for the formulas and how the work is dealt out) with more than 32 query
+// rows to a request and KV head, heads of 128.
 //
 // A block has up to 128 rows.  A wave computes 32 of them, with the 32x32x16 matrix instructions: S^T = K Q^T leaves a lane 16 logits of one row, so that
 // a row's maximum, sum and references are one lane's.  A block of 32 rows gives each of the four waves 32 tokens of a page; one of 64 rows gives two
 // waves 64 tokens each for every half of its rows; of more, every wave all tokens of a page for its rows.  (So the codes come from memory once for all
 // rows of a block: waves with other rows ask for the same ones at about the same time.)  No LDS and no barrier in the loop but for the query's
 // operands, which come from LDS.
+//
+// What bounds it: from 96 rows on the vector and matrix instructions of the two waves of a SIMD, which take their times one after the other (of a step of 32
+// rows and tokens 24 products, 36 clocks each, and about 400 vector instructions, 4.6 each: codes to 16 bits, exponentials, two terms of each weight).
+// 64 requests of 6000 tokens, 8 KV heads: 128 rows 387 us, 520 TFLOP/s (780 with the second terms of the weights); 48 rows 222 us, 3.5 TB/s.  Without
+// the second terms it would be 13 in a hundred faster, and off by 2^-11 of a weight; without exponentials 5.  Heads of 256: sums of 32 rows take
+// half of a wave's registers and leave room for one tile under way; so a kernel of this kind took 222 us where the wide one takes 138 (64 requests of
+// 6000 tokens, 64 rows, 2 KV heads), as loads are waited for.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -21,7 +28,8 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 constexpr int kThreads = 256, kTreeStart = 2;
 constexpr int kTreeRowSlots = 128;  // (a partial row says how many there are in units of this)
 
-template <int D>
+constexpr int D = 128;
+
 struct TreeShape {
   static constexpr int kRowTiles = 4;                  // of 32 rows
   static constexpr int kRows = 32 * kRowTiles;
@@ -49,32 +57,25 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t codes_at(const uint8_t* base, 
 
 // Codes of a wave's tile.  Lane (m, h), m below 32: of K, token m's columns 32 c + 16 h + 0..15; of V, columns m D/32 + 0.. of the tokens
 // 8 i + 4 h + 0..3.
-template <int D>
 struct TreeTile {
   u32x4 k[D / 32];
-  typename VWord<D / 128>::type v[16];
+  uint32_t v[16];
   float ks, vs;  // scales
 };
-template <int D>
-__device__ __forceinline__ void load_k(TreeTile<D>& t, __amdgpu_buffer_rsrc_t rsrc, int at) {
+__device__ __forceinline__ void load_k(TreeTile& t, __amdgpu_buffer_rsrc_t rsrc, int at) {
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) t.k[c] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at + 32 * c, 0, 0));
 }
-template <int D>
-__device__ __forceinline__ void load_v(TreeTile<D>& t, __amdgpu_buffer_rsrc_t rsrc, int at) {
+__device__ __forceinline__ void load_v(TreeTile& t, __amdgpu_buffer_rsrc_t rsrc, int at) {
 #pragma unroll
-  for (int j = 0; j < 16; ++j) {
-    const int off = at + (8 * (j / 4) + j % 4) * D;
-    if constexpr (D == 128) t.v[j] = __builtin_amdgcn_raw_buffer_load_b32(rsrc, off, 0, 0);
-    else t.v[j] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rsrc, off, 0, 0));
-  }
+  for (int j = 0; j < 16; ++j)
+    t.v[j] = __builtin_amdgcn_raw_buffer_load_b32(rsrc, at + (8 * (j / 4) + j % 4) * D, 0, 0);
 }
 __device__ __forceinline__ void settle(int& x) { asm volatile("" : "+v"(x)); }
 
 // A wave's share of the output rows (as Rows in gqa_common.h): lane (m, h) has row m of the wave's 32, and of O columns (8 (i / 4) + 4 h + i % 4) D/32 + c.
-template <int D>
 struct TreeRows {
-  static constexpr int kCols = TreeShape<D>::kCols;
+  static constexpr int kCols = TreeShape::kCols;
   f32x16 o[kCols];
   float m, n, l, ratio, saw_nan;
   __device__ __forceinline__ void clear() {
@@ -101,8 +102,7 @@ typedef __attribute__((ext_vector_type(2))) float f32x2;
 // Weights of a tile's 32 tokens from S^T, as weigh in gqa_common.h: references, sums, and two f16 terms (the first one rounded to zero, so that
 // two conversions are an instruction; what it leaves is rounded to nearest: together 2^-22 of a weight).  Value i of a lane is token
 // 8 (i / 4) + 4 h + i % 4; the terms' operand u has values 8 u + 0..7.
-template <int D>
-__device__ __forceinline__ void weigh(const GqaDecodeParams& p, TreeRows<D>& a, f32x16& s, const Sight<true>& sight, int text, bool full, int pos0, int h,
+__device__ __forceinline__ void weigh(const GqaDecodeParams& p, TreeRows& a, f32x16& s, const Sight<true>& sight, int text, bool full, int pos0, int h,
                                       float k_factor, float v_scale, u32x4 (&high)[2], u32x4 (&low)[2]) {
   if (!full) {
     const uint32_t nodes = nodes_at(sight.nodes, pos0 - text) >> (4 * h);
@@ -154,9 +154,9 @@ __device__ __forceinline__ void weigh(const GqaDecodeParams& p, TreeRows<D>& a, 
 }
 
 // End of a block (as finish in gqa_common.h; o_lds: [4 waves][32 rows][kOStride], ml: [4 waves][32 rows]).
-template <int D, bool OUT32, typename DEALER>
-__device__ __forceinline__ void finish(const DEALER& dealer, const Piece& now, TreeRows<D>& a, float* o_lds, float4* ml, int wave, int slot) {
-  using C = TreeShape<D>;
+template <bool OUT32, typename DEALER>
+__device__ __forceinline__ void finish(const DEALER& dealer, const Piece& now, TreeRows& a, float* o_lds, float4* ml, int wave, int slot) {
+  using C = TreeShape;
   constexpr int R = C::kRows, kCols = C::kCols, kChunks = D / 8 / C::kParts;
   const int tid = threadIdx.x, lane = tid & 63, m32 = lane & 31, h = lane >> 5;
   const int rows = dealer.rows_of(now);
@@ -252,9 +252,9 @@ __device__ __forceinline__ void finish(const DEALER& dealer, const Piece& now, T
   }
 }
 
-template <int D, bool OUT32>
+template <bool OUT32>
 __global__ __launch_bounds__(kThreads, 2) void gqa_tree_kernel(GqaDecodeParams p) {
-  using C = TreeShape<D>;
+  using C = TreeShape;
   constexpr int R = C::kRows, kCols = C::kCols, kSteps = C::kSteps;
   using Deal = Dealer<R, kThreads, kTreeStart, 1, true>;
   extern __shared__ __align__(16) float lds[];
@@ -316,7 +316,7 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_tree_kernel(GqaDecodeParams p
   };
   const Codes none = {codes_at(p.k_cache, 0), codes_at(p.v_cache, 0)};
   auto first_of = [&](const TileLayout& pages, int tile) { return (pages.logical(tile) << (7 - split)) + mine; };
-  auto aim = [&](TreeTile<D>& t, const Span& span, int head, int tile, int ids, int held) {
+  auto aim = [&](TreeTile& t, const Span& span, int head, int tile, int ids, int held) {
     const int page = __builtin_amdgcn_readlane(ids, tile - held);
     const int pos = first_of(span.pages, tile), first = pos % kPage, live = max(min(span.hi - pos, kWaveTokens), 0);
     const size_t ph = (size_t)page * p.kv_heads + head, block = ph * blocks_per_page + (first >> p.scale_shift), code = (ph * kPage + first) * D;
@@ -326,7 +326,7 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_tree_kernel(GqaDecodeParams p
   };
 
   // Two tiles are under way: while one is computed, the loads of the one behind the other go out as soon as their registers are free.
-  TreeTile<D> even, odd;
+  TreeTile even, odd;
   int held = 0, ids = 0, tile = 0, b = 0, head = 0, row_tile = 0;
   bool idle = false;  // (a block of 65 to 96 rows: the last wave has none)
   Span span(now);
@@ -345,12 +345,12 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_tree_kernel(GqaDecodeParams p
     settle(ids);
     Codes c = none;
     if (tile < span.tile_hi) c = aim(even, span, head, tile, ids, held);
-    load_k<D>(even, c.k, k_at);
-    load_v<D>(even, c.v, v_at);
+    load_k(even, c.k, k_at);
+    load_v(even, c.v, v_at);
     c = none;
     if (tile + 1 < span.tile_hi) c = aim(odd, span, head, tile + 1, ids, held);
-    load_k<D>(odd, c.k, k_at);
-    load_v<D>(odd, c.v, v_at);
+    load_k(odd, c.k, k_at);
+    load_v(odd, c.v, v_at);
   };
   begin_block(now);
   dealer.keep(0, now);
@@ -358,9 +358,9 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_tree_kernel(GqaDecodeParams p
   lds_barrier();
 
   while (true) {
-    TreeRows<D> a;
+    TreeRows a;
     a.clear();
-    auto step = [&](TreeTile<D>& t) {
+    auto step = [&](TreeTile& t) {
       // (asked for together: one by one, each product would wait for its own)
       bf16x8 q[kSteps];
 #pragma unroll
@@ -386,9 +386,9 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_tree_kernel(GqaDecodeParams p
         }
         c = aim(t, span, head, tile + 2, ids, held);
       }
-      load_k<D>(t, c.k, k_at);
+      load_k(t, c.k, k_at);
       u32x4 high[2], low[2];
-      weigh<D>(p, a, s, sight, span.text, kept.full, pos0, h, k_factor, v_scale, high, low);
+      weigh(p, a, s, sight, span.text, kept.full, pos0, h, k_factor, v_scale, high, low);
       if (!kept.full) {
         // tokens that no row of the block keeps may hold anything; NaN in kept ones goes on as 0 (see sanitize in gqa_common.h)
         uint32_t any_nan = 0;
@@ -396,33 +396,30 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_tree_kernel(GqaDecodeParams p
         for (int j = 0; j < 16; ++j) {
           const int pos = pos0 + 8 * (j / 4) + 4 * h + j % 4;
           const bool keep = pos < span.hi && (pos < p.S || (p.W > 0 && pos >= span.lo - p.W) || pos >= span.text);
-          if (!keep) t.v[j] = typename VWord<D / 128>::type{};
-#pragma unroll
-          for (int i = 0; i < D / 128; ++i) any_nan |= nan_codes(word<D / 128>(t.v[j], i));
+          if (!keep) t.v[j] = 0;
+          any_nan |= nan_codes(t.v[j]);
         }
         if (__ballot(any_nan != 0) != 0) {
           a.saw_nan = 1.f;
 #pragma unroll
-          for (int j = 0; j < 16; ++j) t.v[j] = without_nan<D / 128>(t.v[j]);
+          for (int j = 0; j < 16; ++j) t.v[j] = without_nan<1>(t.v[j]);
         }
       }
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int wd = 0; wd < D / 128; ++wd)
+        for (int col = 0; col < 4; ++col) {
+          u32x4 f;
 #pragma unroll
-          for (int col = 0; col < 4; ++col) {
-            u32x4 f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) f[j] = f16_pair(token_pair(word<D / 128>(t.v[8 * u + 2 * j], wd), word<D / 128>(t.v[8 * u + 2 * j + 1], wd), col / 2), col % 2);
-            const f16x8 vt = __builtin_bit_cast(f16x8, f);
-            f32x16& acc = a.o[4 * wd + col];
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(vt, __builtin_bit_cast(f16x8, high[u]), acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(vt, __builtin_bit_cast(f16x8, low[u]), acc, 0, 0, 0);
-          }
+          for (int j = 0; j < 4; ++j) f[j] = f16_pair(token_pair(t.v[8 * u + 2 * j], t.v[8 * u + 2 * j + 1], col / 2), col % 2);
+          const f16x8 vt = __builtin_bit_cast(f16x8, f);
+          f32x16& acc = a.o[col];
+          acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(vt, __builtin_bit_cast(f16x8, high[u]), acc, 0, 0, 0);
+          acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(vt, __builtin_bit_cast(f16x8, low[u]), acc, 0, 0, 0);
+        }
       __builtin_amdgcn_s_setprio(0);
-      load_v<D>(t, c.v, v_at);
+      load_v(t, c.v, v_at);
       ++tile;
     };
     if (!idle) {
@@ -438,7 +435,7 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_tree_kernel(GqaDecodeParams p
       dealer.keep(1, next);
       begin_block(next);
     }
-    finish<D, OUT32>(dealer, dealer.kept(0), a, o_lds, ml_lds + parity * 4 * 32, wave, 2 * (int)blockIdx.x + first_partial);
+    finish<OUT32>(dealer, dealer.kept(0), a, o_lds, ml_lds + parity * 4 * 32, wave, 2 * (int)blockIdx.x + first_partial);
     parity ^= 1;
     first_partial = 1;
     if (!more_blocks) break;
@@ -449,28 +446,19 @@ __global__ __launch_bounds__(kThreads, 2) void gqa_tree_kernel(GqaDecodeParams p
   }
 }
 
-template <int D>
-hipError_t allow_lds() {
-  hipError_t e = hipSuccess;
-  for (const void* kernel : {(const void*)gqa_tree_kernel<D, false>, (const void*)gqa_tree_kernel<D, true>})
-    if (e == hipSuccess) e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)TreeShape<D>::kLds);
-  return e;
-}
-template <int D>
-hipError_t start(const GqaDecodeParams& p, int shares, hipStream_t stream) {
-  if (p.out_fp32) hipLaunchKernelGGL((gqa_tree_kernel<D, true>), dim3(shares), dim3(kThreads), TreeShape<D>::kLds, stream, p);
-  else hipLaunchKernelGGL((gqa_tree_kernel<D, false>), dim3(shares), dim3(kThreads), TreeShape<D>::kLds, stream, p);
-  return hipGetLastError();
-}
-
 }  // namespace
 
 hipError_t init_gqa_tree_kernels() {
-  return allow_lds<128>();
+  hipError_t e = hipSuccess;
+  for (const void* kernel : {(const void*)gqa_tree_kernel<false>, (const void*)gqa_tree_kernel<true>})
+    if (e == hipSuccess) e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)TreeShape::kLds);
+  return e;
 }
 
 hipError_t launch_gqa_tree(const GqaDecodeParams& p, int shares, hipStream_t stream) {
-  return start<128>(p, shares, stream);
+  if (p.out_fp32) hipLaunchKernelGGL(gqa_tree_kernel<true>, dim3(shares), dim3(kThreads), TreeShape::kLds, stream, p);
+  else hipLaunchKernelGGL(gqa_tree_kernel<false>, dim3(shares), dim3(kThreads), TreeShape::kLds, stream, p);
+  return hipGetLastError();
 }
 
 }  // namespace omniattn
