@@ -423,6 +423,9 @@ int omniattn_tree_masks(int32_t batch, int32_t num_tokens, const int32_t* parent
  * whose own positions L - n + (bits of the mask below a) pass the same test.  (Any set of nodes will do, a tree's or not.)  A query whose mask
  * has no bit of a node keeps nothing.
  *   masks       device, uint64 [N].  Bits of nodes that the request does not have do not count; nodes from number 64 on are seen by none.
+ *   page_table  entries are read of pages that hold nodes (with window 0: if the text is shorter than sink), or tokens that a query at the
+ *               first node's position keeps
+ *   workspace   omniattn_gqa_workspace_bytes, as for omniattn_gqa_decode: calls of either kind share one
  */
 int omniattn_gqa_tree(const omniattn_gqa_t* gqa, const void* q, int64_t q_stride, const void* k_cache, const void* v_cache, const float* k_scales,
                       const float* v_scales, const int32_t* page_table, const int32_t* seq_lens, const int32_t* q_start,

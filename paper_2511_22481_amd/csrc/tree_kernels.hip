@@ -36,7 +36,8 @@ __device__ __forceinline__ Nodes nodes_of(const int32_t* q_start, int b, int num
   return r;
 }
 
-// A wave to a request, a lane to a node.  Every pass doubles the way that a set reaches up.
+// A wave to a request, a lane to a node.  Every pass doubles the way that a set reaches up: six at the most, and no loop over a node's ancestors, of which a
+// chain has 63.  A launch, two loads one after the other, and the passes bound it: 1.6 us (1 request of 8 nodes), 3.7 us (1500 of up to 64).
 __global__ __launch_bounds__(kThreads) void tree_masks_kernel(TreeMasksParams p) {
   const int lane = threadIdx.x & 63, b = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (b >= p.batch) return;
@@ -80,6 +81,10 @@ __device__ __forceinline__ float wave_max(float x) {
 
 // A wave to a (layer, request) and kUnits of its (KV head, K or V).  Rows go up in order, kRows at a time: a row's source lies at or behind its place, so
 // what a pass writes is no later pass's source, and within a pass all loads are done before the first store.
+//
+// Chains of loads bound it (the request's nodes, its length and path, the pages, scales and rows, the store) and rows of 128 bytes here and there.  64
+// requests, 32 layers of 8 KV heads of 128: 14.0 us, 0.85 TB/s; 1 request, 4 layers: 5.2.  Of (KV head, K or V) to a wave, the same two in us: 1
+// 18.4 and 4.8, 2 14.0 and 5.2, 4 15.0 and 6.0, 8 13.3 and 8.7.  (The path is found again by every wave, which 2 halve; more work alone in small calls.)
 constexpr int kUnits = 2;
 template <int D>
 __global__ __launch_bounds__(kThreads) void gqa_keep_kernel(GqaKeepParams p) {

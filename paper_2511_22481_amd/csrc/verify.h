@@ -23,7 +23,6 @@ struct VerifyRow {
   float top;
   int32_t best, child, taken;
   float logit;
-  int32_t unused;
 };
 // Of a node: its token, the child that the walk goes to (-1: none, -2: the node was not looked at), and the logarithm of the token's probability.
 struct VerifyChoice {

@@ -12,7 +12,12 @@
 // thousand draws from a large vocabulary, and then the same inputs would give other tokens with another order of summation.
 //
 // Kernels: sums of 2048 columns each; with q, what becomes of first children, and the sums of max(p - q, 0) of rows that need them; the
-// nodes' tokens (a wave finds the part of 2048 columns whose running sum passes the border, and looks at these again); the walk.
+// nodes' tokens (a wave finds the part of 2048 columns whose running sum passes the border, and looks at these again); the walk.  Logits are read
+// once, but for the parts that tokens are found in and, with q, the rows whose first child is refused.
+//
+// What bounds them: the sums, in bf16, the exponentials (12 instructions of 64 bits and 4 others for a logit, about 5 clocks each; 64 requests of 6
+// nodes, 131072 columns: 38 us, 2.6 TB/s); in fp32 memory nearly (32 requests of 40 nodes, 100003 columns: 98 us, 5.2 TB/s; maxima
+// alone 89).  The kernels behind them take 5 to 14 us each, which are chains of loads; a node's part costs 2 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -383,7 +388,7 @@ __device__ __forceinline__ float readlane_f(float x, int lane) { return __builti
 // What lane `lane` holds.
 __device__ __forceinline__ VerifyRow row_at(const VerifyRow& r, int lane) {
   return VerifyRow{readlane64(r.sum, lane), readlane_f(r.top, lane), __builtin_amdgcn_readlane(r.best, lane), __builtin_amdgcn_readlane(r.child, lane),
-                   __builtin_amdgcn_readlane(r.taken, lane), readlane_f(r.logit, lane), 0};
+                   __builtin_amdgcn_readlane(r.taken, lane), readlane_f(r.logit, lane)};
 }
 
 // Of kVerifyColumns columns of a row.
@@ -617,7 +622,7 @@ __device__ __forceinline__ void keep_none(const VerifyParams& p, int b, const No
   if (threadIdx.x == 0) p.dropped[b] = r.n;
 }
 
-// Trees of few nodes: a work group to a request, whose waves choose the nodes' tokens; then one walks down the tree.
+// Trees of few nodes, or with drafts' probabilities: a work group to a request, whose waves choose the nodes' tokens; then one walks down the tree.
 template <typename T, bool DRAFTS>
 __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(VerifyParams p) {
   __shared__ VerifyChoice choices[kNodes];
@@ -644,7 +649,7 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(VerifyParams 
   }
 }
 // Trees of many: a wave to a node of the call; and then a wave to a request.
-template <typename T, bool DRAFTS>
+template <typename T>
 __global__ __launch_bounds__(kThreads) void verify_choose_kernel(VerifyParams p) {
   const int lane = threadIdx.x & 63, row = blockIdx.x * kWaves + uniform(threadIdx.x >> 6);
   if (row >= p.num_tokens) return;
@@ -653,31 +658,21 @@ __global__ __launch_bounds__(kThreads) void verify_choose_kernel(VerifyParams p)
   const Nodes r = nodes_of(p, owner.b);
   if (r.n > kNodes) return;
   const int parent = lane < r.n ? p.parents[r.begin + lane] : -1, token = lane < r.n ? p.tokens[r.begin + lane] : -1;
-  const VerifyChoice choice = choose<T, DRAFTS>(p, r, row - r.begin, owner.T, parent, token, false);
+  const VerifyChoice choice = choose<T, false>(p, r, row - r.begin, owner.T, parent, token, false);
   if (lane == 0) p.choices[row] = choice;
 }
-template <typename T, bool DRAFTS>
 __global__ __launch_bounds__(64) void verify_walk_kernel(VerifyParams p) {
   const int b = blockIdx.x, lane = threadIdx.x;
   const Nodes r = nodes_of(p, b);
   if (r.n > kNodes) return keep_none(p, b, r);
-  VerifyChoice mine = lane < r.n ? p.choices[r.begin + lane] : VerifyChoice{-1, -1, 0.f};
-  Way way = way_of(r, mine);
-  if (DRAFTS && way.unseen >= 0) {
-    const int parent = lane < r.n ? p.parents[r.begin + lane] : -1, token = lane < r.n ? p.tokens[r.begin + lane] : -1;
-    do {
-      const VerifyChoice choice = choose<T, DRAFTS>(p, r, way.unseen, p.temperature[b], parent, token, true);
-      if (lane == way.unseen) mine = choice;
-      way = way_of(r, mine);
-    } while (way.unseen >= 0);
-  }
-  write(p, b, r, way, mine);
+  const VerifyChoice mine = lane < r.n ? p.choices[r.begin + lane] : VerifyChoice{-1, -1, 0.f};
+  write(p, b, r, way_of(r, mine), mine);
 }
 
 template <typename T, bool DRAFTS>
 hipError_t start(const VerifyParams& p, int cus, hipStream_t stream) {
-  const dim3 by_row((p.num_tokens + kWaves - 1) / kWaves);
   if (p.num_tokens > 0) {
+    const dim3 by_row((p.num_tokens + kWaves - 1) / kWaves);
     const int64_t groups = ((int64_t)p.num_tokens * p.num_parts + kWaves - 1) / kWaves;
     hipLaunchKernelGGL(verify_sums_kernel<T>, dim3((uint32_t)groups), dim3(kThreads), 0, stream, p);
     if constexpr (DRAFTS) {
@@ -685,11 +680,22 @@ hipError_t start(const VerifyParams& p, int cus, hipStream_t stream) {
       hipLaunchKernelGGL(verify_rows_kernel<T>, by_row, dim3(kThreads), 0, stream, p);
       hipLaunchKernelGGL(verify_rest_kernel<T>, dim3((uint32_t)p.batch * slices), dim3(kThreads), 0, stream, p, slices);
     }
-    // (the host knows their mean)
-    if (p.num_tokens > (int64_t)p.batch * (kPickThreads / 64)) {
-      hipLaunchKernelGGL((verify_choose_kernel<T, DRAFTS>), by_row, dim3(kThreads), 0, stream, p);
-      hipLaunchKernelGGL((verify_walk_kernel<T, DRAFTS>), dim3(p.batch), dim3(64), 0, stream, p);
-      return hipGetLastError();
+    // More nodes to a request (their mean, which the host knows) than a work group has waves take turns there, which costs more than a second launch.
+    // With drafts' probabilities few of them are looked at, and a work group to a request is as fast for trees of any size.  us a call, bf16, work
+    // group to a request / wave to a node (vocabulary x requests; "q": drafts' probabilities given):
+    //   nodes             6             8             9            16            32            64
+    //    32000 x 1    12.4 / 13.6   12.9 / 13.8   16.3 / 13.9   19.7 / 13.8   32.6 / 14.1   57.5 / 14.3
+    //    32000 x 64   20.3 / 21.3   24.6 / 25.8   30.3 / 28.2   43.1 / 38.0   76.0 / 58.3    137 / 106
+    //   131072 x 64   44.1 / 45.9   52.4 / 53.9   61.0 / 58.1   94.1 / 90.6    193 / 185     371 / 355
+    //   q 32000 x 1   23.2 / 25.0   23.3 / 25.0   23.3 / 25.1   24.5 / 25.7   26.4 / 26.5   31.4 / 28.7
+    //   q 32000 x 64  34.7 / 37.8   38.6 / 41.9   40.9 / 44.2   51.7 / 53.4   72.2 / 73.2    113 / 117
+    //   q131072 x 64  63.4 / 66.9   73.0 / 75.5   76.4 / 79.5    114 / 117     199 / 199     369 / 370
+    if constexpr (!DRAFTS) {
+      if (p.num_tokens > (int64_t)p.batch * (kPickThreads / 64)) {
+        hipLaunchKernelGGL(verify_choose_kernel<T>, by_row, dim3(kThreads), 0, stream, p);
+        hipLaunchKernelGGL(verify_walk_kernel, dim3(p.batch), dim3(64), 0, stream, p);
+        return hipGetLastError();
+      }
     }
   }
   hipLaunchKernelGGL((verify_pick_kernel<T, DRAFTS>), dim3(p.batch), dim3(kPickThreads), 0, stream, p);
