@@ -494,7 +494,7 @@ GqaShape gqa_shape(int batch, int num_queries, int group, int kv_heads, int head
     const bool alone = head_dim == 64 && (int64_t)batch * kv_heads >= 2 * groups && pages <= 16;
     return GqaShape{kGqaNarrow, 1, 16, groups, alone ? 4 : 1, pages <= (alone || head_dim == 256 ? 3 : 4)};
   }
-  if (tree && head_dim == 128 && rows > 32 && batch * kv_heads * pages * ((rows + 31) / 32) >= 16 * cus) return GqaShape{kGqaTree, 0, 128, 2 * cus, 1, pages <= 3};
+  if (tree && head_dim == 128 && rows > 32 && (int64_t)batch * kv_heads * pages * ((rows + 31) / 32) >= 16 * cus) return GqaShape{kGqaTree, 0, 128, 2 * cus, 1, pages <= 3};
   if (head_dim == 256) return GqaShape{kGqaWide, 1, 64, cus, 1, pages <= 2};
   if (rows <= 32) return GqaShape{kGqaNarrow, 2, 32, cus * groups_per_cu(head_dim, 2), 1, pages <= 4};
   if (head_dim == 64) return GqaShape{kGqaNarrow, 4, 64, cus * groups_per_cu(head_dim, 4), 1, pages <= 4};

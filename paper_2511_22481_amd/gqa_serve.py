@@ -148,9 +148,12 @@ def speculate(pool, prompts, answers, q_heads, sink, window, rows, draft, logits
     last token, and the probabilities that the first children were drawn from (a tensor [nodes of all, vocabulary], or None).  uniforms(nodes)
     returns the random numbers [nodes, 2] (needed with a temperature).  observe(step, texts) sees the texts as they grow.
 
-    A request whose tree finds no pages waits, as in serve.  Returns what happened, and the texts."""
+    The prompts have to fit in the pool together; after that a request whose tree finds no pages waits, as in serve.  Returns what happened, and
+    the texts."""
     import torch
     from . import omniattn_gqa_workspace_bytes, omniattn_tree_masks, omniattn_tree_verify, omniattn_tree_verify_workspace_bytes
+    if temperature > 0 and uniforms is None:
+        raise ValueError("random numbers are needed with a temperature")
     layers, pages, heads, _, dim = pool.k.shape
     batch, device = len(prompts), pool.k.device
     ints = dict(dtype=torch.int32, device=device)

@@ -304,3 +304,40 @@ def test_the_command_serves_drafts():
     assert res.returncode == 0, res.stderr[-2000:]
     what = json.loads(res.stdout)
     assert what["tokens"] >= 6 and what["tokens_per_step"] > 2 and what["steps"] > 0
+
+
+def test_a_temperature_needs_random_numbers():
+    with pytest.raises(ValueError):
+        speculate(None, [[1]], [1], 1, 0, 1, None, None, None, temperature=0.5)
+
+
+@gpu
+def test_two_steps_at_once():
+    """Two pools' steps on two streams, call by call in turn, each with workspaces of its own."""
+    want, got = [], []
+    for k in range(2):
+        for states in (want, got):
+            s, _ = _state(2)
+            _inputs(s, torch.Generator(device="cuda").manual_seed(20 + k), k, "any")
+            states.append(s)
+    for s in want:
+        _step(s)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in got]
+
+    def in_turn(call):
+        for stream, s in zip(streams, got):
+            with torch.cuda.stream(stream):
+                call(s)
+    in_turn(lambda s: s["pool"].extend(s["news"], s["slots"]))
+    in_turn(lambda s: oa.omniattn_tree_masks(s["parents"], s["pool"].lens, s["pool"].q_start, s["masks"], s["positions"]))
+    for i in range(LAYERS):
+        in_turn(lambda s: s["pool"].attend_tree(i, s["qkv"][i], s["slots"], s["masks"], s["out"][i], s["lse"], s["ws"], 4, 100))
+    in_turn(lambda s: oa.omniattn_tree_verify(s["logits"], s["probs"], s["tokens"], s["parents"], s["pool"].q_start, s["heat"], s["uniforms"], s["path"], s["said"], s["chance"],
+                                              s["dropped"], s["vws"]))
+    in_turn(lambda s: s["pool"].keep(s["path"], s["dropped"]))
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        for name in NAMES:
+            assert torch.equal(a[name], b[name]), name
+        assert torch.equal(a["pool"].lens, b["pool"].lens) and torch.equal(a["pool"].k.view(torch.uint8), b["pool"].k.view(torch.uint8))
