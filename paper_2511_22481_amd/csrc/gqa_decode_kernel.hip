@@ -487,11 +487,28 @@ hipError_t allow_lds() {
 //   64 x 300               20 / 24      41 / 26      43 / 27      70 / 40      79 / 42     142 / 92
 //   64 x 6000             168 / 172    261 / 222    272 / 229    467 / 365    533 / 387   1040 / 742
 // (up to 32 rows: the narrow kernel.)
+// Small calls of trees: this kernel with one row tile whatever the rows are, as long as there are no more steps of 16 rows and a page than 16 to a
+// compute unit (8 at width 256).  Blocks that read the same pages run side by side then, and each ends sooner.  us a call (replayed), what the rule takes
+// otherwise / one row tile, with the steps of 16 rows to a compute unit; 8 KV heads (2 at width 256):
+//   rows                        32                 64                 128                256
+//   width 128   1 x 300     13.3 / 9.7  0      17.4 / 9.8   0      18.4 / 10.1  1     20.9 / 13.2  2
+//               1 x 4000    16.8 / 15.2 2      22.4 / 16.9  4      25.5 / 20.5  8     32.6 / 28.2 16
+//               4 x 4000    23.8 / 21.2 8      33.9 / 28.3 16      41.0 / 37.6 32     56.9 / 56.7 64
+//              16 x 1000    22.7 / 21.8 8      32.0 / 28.9 16      45.5 / 50.3 32     63.3 / 91.3 64
+//              16 x 4000    36.4 / 48.3 32     50.0 / 83.8 64      80.0 / 159 128      136 / 312 256
+//   width 64    1 x 300     11.2 / 8.8  0      16.5 / 8.9   0      16.6 / 9.2   1     16.7 / 10.0  2
+//              16 x 1000    18.4 / 18.6 8      27.8 / 23.7 16      40.0 / 32.6 32     45.8 / 54.2 64
+//              16 x 4000    27.9 / 30.9 32     43.4 / 48.4 64      65.0 / 88.6 128     101 / 167 256
+//   width 256   1 x 300     14.2 / 12.5 0      17.3 / 13.0  0      17.5 / 13.1  0     19.9 / 13.3  0
+//              16 x 1000    23.7 / 21.8 2      30.6 / 26.0  4      32.8 / 29.3  8     47.2 / 38.8 16
+//              16 x 4000    32.3 / 29.2 8      42.8 / 41.1 16      56.8 / 57.0 32     89.3 / 94.8 64
+// (48 rows of width 256, 12 steps to a compute unit: 16 x 4000 39.7 / 42.8, 4 x 16000 35.1 / 39.6.)
 GqaShape gqa_shape(int batch, int num_queries, int group, int kv_heads, int head_dim, int64_t pages, int cus, bool tree) {
   const int64_t rows = (int64_t)((num_queries + batch - 1) / batch) * group;
-  if (rows <= 16) {
+  const int64_t steps = (int64_t)batch * kv_heads * pages * ((rows + 15) / 16);
+  if (rows <= 16 || (tree && steps <= (head_dim == 256 ? 8 : 16) * cus)) {
     const int groups = cus * groups_per_cu(head_dim, 1);
-    const bool alone = head_dim == 64 && (int64_t)batch * kv_heads >= 2 * groups && pages <= 16;
+    const bool alone = rows <= 16 && head_dim == 64 && (int64_t)batch * kv_heads >= 2 * groups && pages <= 16;
     return GqaShape{kGqaNarrow, 1, 16, groups, alone ? 4 : 1, pages <= (alone || head_dim == 256 ? 3 : 4)};
   }
   if (tree && head_dim == 128 && rows > 32 && (int64_t)batch * kv_heads * pages * ((rows + 31) / 32) >= 16 * cus) return GqaShape{kGqaTree, 0, 128, 2 * cus, 1, pages <= 3};

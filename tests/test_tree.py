@@ -107,6 +107,12 @@ class Problem:
             bad = torch.tensor([float("nan"), float("inf")])[torch.randint(0, 2, self.scales.shape, generator=g)]
             self.scales = torch.where(empty[None, :, None, :], bad, self.scales)
 
+    def wide_table(self):
+        """The table with so many columns more that the call is none of the small ones, for which blocks of 16 rows are taken."""
+        batch, kv_heads, columns = len(self.lens), self.codes.shape[2], len(self.table[0])
+        tiles = -(-(-(-len(self.sets) // batch) * (self.q.shape[1] // kv_heads)) // 16)
+        return [r + [0] * max(0, 16 * 256 // (batch * kv_heads * tiles) + 1 - columns) for r in self.table]
+
     def run(self, out_dtype=torch.bfloat16, q_start=True, fill=0xff, pad=0):
         (k, v), (ks, vs), q = self.codes.cuda(), self.scales.cuda(), self.q.cuda()
         if pad:
@@ -123,6 +129,15 @@ class Problem:
         return out, lse
 
     def check(self, out_dtype=torch.bfloat16, **kw):
+        result, short = self._check(out_dtype, **kw), self.table
+        self.table = self.wide_table()
+        try:
+            self._check(out_dtype, **kw)
+        finally:
+            self.table = short
+        return result
+
+    def _check(self, out_dtype, **kw):
         out, lse = self.run(out_dtype, **kw)
         fn = ref.attend_fp32 if out_dtype == torch.float32 else ref.attend_bf16
         k, v = gref.as_double(self.codes)
