@@ -241,6 +241,9 @@ int omniattn_gqa_keep(const omniattn_gqa_t* gqa, int32_t num_layers, const int32
   if (!path || !seq_lens || !page_table || !k_cache || !v_cache || !k_scales || !v_scales) return OMNIATTN_EINVAL;
   if (!aligned(k_cache, 16) || !aligned(v_cache, 16)) return OMNIATTN_EINVAL;
   if ((int64_t)num_layers * gqa->batch >= (INT32_MAX >> 5) / gqa->num_kv_heads) return OMNIATTN_EUNSUPPORTED;
+  int cus = 0;
+  const int found = device_cus(&cus);
+  if (found != OMNIATTN_OK) return found;
   GqaKeepParams p;
   p.path = path;
   p.seq_lens = seq_lens;
@@ -259,7 +262,8 @@ int omniattn_gqa_keep(const omniattn_gqa_t* gqa, int32_t num_layers, const int32
   p.head_dim = gqa->head_dim;
   p.scale_tokens = gqa->scale_tokens;
   p.max_pages = gqa->max_pages_per_seq;
-  OA_HIP(launch_gqa_keep(p, (hipStream_t)hip_stream));
+  p.run = 1;
+  OA_HIP(launch_gqa_keep(p, cus, (hipStream_t)hip_stream));
   return OMNIATTN_OK;
 }
 

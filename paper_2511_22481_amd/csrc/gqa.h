@@ -75,8 +75,10 @@ struct GqaKeepParams {
   float* scales[2];         // [layers, num_pages, kv_heads, 128 / scale_tokens]
   int64_t num_pages;
   int batch, num_tokens, layers, kv_heads, head_dim, scale_tokens, max_pages;
+  int run;  // layers to a wave
 };
-hipError_t launch_gqa_keep(const GqaKeepParams& p, hipStream_t stream);
+// cus: the device's compute units.  (p.run is set.)
+hipError_t launch_gqa_keep(GqaKeepParams p, int cus, hipStream_t stream);
 
 struct GqaAppendParams {
   const uint16_t* rows[2];  // K and V, bf16 [tokens, kv_heads, head_dim]

@@ -79,21 +79,26 @@ __device__ __forceinline__ float wave_max(float x) {
   return __builtin_bit_cast(float, wave_join(__builtin_bit_cast(uint32_t, x), [](uint32_t a, uint32_t b) { return max(a, b); }));
 }
 
-// A wave to a (layer, request) and kUnits of its (KV head, K or V).  Rows go up in order, kRows at a time: a row's source lies at or behind its place, so
-// what a pass writes is no later pass's source, and within a pass all loads are done before the first store.
+// A wave to a request, kUnits of its (KV head, K or V), and up to kMostLayers layers, one after the other.  Rows go up in order, kRows at a time: a row's source
+// lies at or behind its place, so what a pass writes is no later pass's source, and within a pass all loads are done before the first store.
 //
-// Chains of loads bound it (the request's nodes, its length and path, the pages, scales and rows, the store) and rows of 128 bytes here and there.  64
-// requests, 32 layers of 8 KV heads of 128: 14.0 us, 0.85 TB/s; 1 request, 4 layers: 5.2.  Of (KV head, K or V) to a wave, the same two in us: 1
-// 18.4 and 4.8, 2 14.0 and 5.2, 4 15.0 and 6.0, 8 13.3 and 8.7.  (The path is found again by every wave, which 2 halve; more work alone in small calls.)
-constexpr int kUnits = 2;
+// Chains of loads bound it (the request's nodes, its length and path, the pages, scales and rows, the store) and rows of 128 bytes here and there.  So a
+// wave asks for the next layer's scales and first rows before it works on a layer's, and where there are more waves than the compute units hold (32 each),
+// they take more layers instead.  us a call (replayed), requests of up to 32 nodes, 8 KV heads of 128, layers to a wave up to 1 / 2 / 4 / 8:
+//   16 x 32 layers   6.5 / 6.6 / 6.5 / 6.5       64 x 64 layers   25.6 / 19.7 / 18.7 / 18.9
+//   64 x 32         15.2 / 12.6 / 12.6 / 12.6   256 x 32          37.1 / 27.2 / 24.0 / 28.5
+// (More layers from 16 waves on: 64 x 32 14.9.)  Of (KV head, K or V) to a wave, with a layer each, 64 x 32 and 1 x 4 layers: 1 18.4 and 4.8 us, 2
+// 14.0 and 5.2, 4 15.0 and 6.0, 8 13.3 and 8.7.
+constexpr int kUnits = 2, kMostLayers = 4;
 template <int D>
 __global__ __launch_bounds__(kThreads) void gqa_keep_kernel(GqaKeepParams p) {
   constexpr int kLanes = D / 16, kRows = 64 / kLanes;  // lanes of a row, 16 codes each; rows of a pass
   const int lane = threadIdx.x & 63, each = p.scale_tokens, blocks = kPage / each, sharers = (2 * p.kv_heads + kUnits - 1) / kUnits;
   const uint32_t id = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t group = id / (uint32_t)sharers, layer = group / (uint32_t)p.batch;
-  const int b = (int)(group - layer * p.batch), unit0 = (int)(id - group * sharers) * kUnits, units = min(kUnits, 2 * p.kv_heads - unit0);
-  if (layer >= (uint32_t)p.layers) return;
+  const uint32_t group = id / (uint32_t)sharers, run = group / (uint32_t)p.batch;
+  const int b = (int)(group - run * p.batch), unit0 = (int)(id - group * sharers) * kUnits, units = min(kUnits, 2 * p.kv_heads - unit0);
+  if (run * (uint32_t)p.run >= (uint32_t)p.layers) return;
+  const int layer0 = (int)run * p.run, layers = min(p.run, p.layers - layer0);
   const Nodes r = nodes_of(p.q_start, b, p.num_tokens);
   const int text = min(p.seq_lens[b], p.max_pages * kPage) - r.n;
   if (r.n > kNodes || text < 0) return;
@@ -108,75 +113,87 @@ __global__ __launch_bounds__(kThreads) void gqa_keep_kernel(GqaKeepParams p) {
   const bool mine = lane >= first && lane < kept;
   const int32_t* const table = p.page_table + b * p.table_stride;
   const int src = text + (mine ? from : first), dst = text + (mine ? lane : first);
-  const int64_t src_page = (layer * p.num_pages + table[src / kPage]) * p.kv_heads, dst_page = (layer * p.num_pages + table[dst / kPage]) * p.kv_heads;
+  const int64_t src_page = ((int64_t)layer0 * p.num_pages + table[src / kPage]) * p.kv_heads, dst_page = ((int64_t)layer0 * p.num_pages + table[dst / kPage]) * p.kv_heads;
+  const int64_t next_layer = p.num_pages * p.kv_heads;
   // up to three blocks (64 tokens, 32 to a block)
   const int block0 = (text + first) / each, block = dst / each - block0, last_block = (text + kept - 1) / each - block0;
   const int held = text - block0 * each;  // tokens of the text in the first of them, if any
   const int64_t page0 = __shfl(dst_page, first);
   const int64_t src_at = (src_page * kPage + src % kPage) * D, dst_at = (dst_page * kPage + dst % kPage) * D;
   const int col = lane % kLanes * 16, in_pass = lane / kLanes;
-  auto cache = [&](int j) { return p.cache[(unit0 + j) & 1] + (size_t)((unit0 + j) >> 1) * kPage * D; };
+  auto cache = [&](int j, int64_t pages) { return p.cache[(unit0 + j) & 1] + (size_t)(pages + ((unit0 + j) >> 1)) * kPage * D; };
   auto scale_at = [&](int j, int64_t page, int at) { return p.scales[(unit0 + j) & 1] + (page + ((unit0 + j) >> 1)) * blocks + at % kPage / each; };
   u32x4 x[kUnits];
-  auto load = [&](int row0) {
+  auto load = [&](int64_t pages, int row0) {
     const int64_t s = __shfl(src_at, min(row0 + in_pass, 63));
     if (row0 + in_pass < kept) {
 #pragma unroll
       for (int j = 0; j < kUnits; ++j)
-        if (j < units) x[j] = *(const u32x4*)(cache(j) + s + col);
+        if (j < units) x[j] = *(const u32x4*)(cache(j, pages) + s + col);
     }
   };
-  load(first);
-  float old[kUnits], own[kUnits], ratio[kUnits], now[kUnits], now0[kUnits];
-#pragma unroll
-  for (int j = 0; j < kUnits; ++j) {
-    old[j] = own[j] = 0.f;
-    if (j < units) {
-      old[j] = *scale_at(j, src_page, src);
-      if (held > 0) own[j] = *scale_at(j, page0, block0 * each);
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < kUnits; ++j) {
-    now[j] = 0.f;
-    for (int k = 0; k <= last_block; ++k) {
-      float top = wave_max(mine && block == k ? old[j] : 0.f);
-      if (k == 0) now0[j] = top = fmaxf(top, own[j]);
-      if (block == k) now[j] = top;
-    }
-    ratio[j] = scale_ratio(old[j], now[j]);
-  }
-  for (int row0 = first; row0 < kept; row0 += kRows) {
-    const int row = row0 + in_pass, at = min(row, 63);
-    const int64_t d = __shfl(dst_at, at);
-    u32x4 y[kUnits];
+  float old[kUnits], own[kUnits], next_old[kUnits], next_own[kUnits];
+  auto load_scales = [&](int64_t pages) {
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
-      const float f = __shfl(ratio[j], at);
-      y[j] = x[j];
-      if (f != 1.f) y[j] = recode(y[j], f);
-    }
-    load(row0 + kRows);
-    if (row < kept) {
-#pragma unroll
-      for (int j = 0; j < kUnits; ++j)
-        if (j < units) *(u32x4*)(cache(j) + d + col) = y[j];
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < kUnits; ++j) {
-    if (j >= units) break;
-    // tokens of the text in the first block, if its scale has grown
-    if (held > 0 && now0[j] > own[j]) {
-      const float f = scale_ratio(own[j], now0[j]);
-      uint8_t* const rows = cache(j) + (page0 * kPage + block0 * each % kPage) * D;
-      for (int row = in_pass; row < held; row += kRows) {
-        u32x4* const at = (u32x4*)(rows + row * D + col);
-        *at = recode(*at, f);
+      next_old[j] = next_own[j] = 0.f;
+      if (j < units) {
+        next_old[j] = *scale_at(j, pages + src_page, src);
+        if (held > 0) next_own[j] = *scale_at(j, pages + page0, block0 * each);
       }
     }
-    // (the first row of each block writes its scale)
-    if (mine && (lane == first || dst % each == 0)) *scale_at(j, dst_page, dst) = now[j];
+  };
+  load(0, first);
+  load_scales(0);
+  int64_t pages = 0;  // those of the layers before
+  for (int i = 0; i < layers; ++i, pages += next_layer) {
+    float ratio[kUnits], now[kUnits], now0[kUnits];
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) {
+      old[j] = next_old[j];
+      own[j] = next_own[j];
+      now[j] = now0[j] = 0.f;
+      for (int k = 0; k <= last_block; ++k) {
+        float top = wave_max(mine && block == k ? old[j] : 0.f);
+        if (k == 0) now0[j] = top = fmaxf(top, own[j]);
+        if (block == k) now[j] = top;
+      }
+      ratio[j] = scale_ratio(old[j], now[j]);
+    }
+    if (i + 1 < layers) load_scales(pages + next_layer);
+    for (int row0 = first; row0 < kept; row0 += kRows) {
+      const int row = row0 + in_pass, at = min(row, 63);
+      const int64_t d = __shfl(dst_at, at);
+      u32x4 y[kUnits];
+#pragma unroll
+      for (int j = 0; j < kUnits; ++j) {
+        const float f = __shfl(ratio[j], at);
+        y[j] = x[j];
+        if (f != 1.f) y[j] = recode(y[j], f);
+      }
+      if (row0 + kRows < kept) load(pages, row0 + kRows);
+      else if (i + 1 < layers) load(pages + next_layer, first);
+      if (row < kept) {
+#pragma unroll
+        for (int j = 0; j < kUnits; ++j)
+          if (j < units) *(u32x4*)(cache(j, pages) + d + col) = y[j];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) {
+      if (j >= units) break;
+      // tokens of the text in the first block, if its scale has grown
+      if (held > 0 && now0[j] > own[j]) {
+        const float f = scale_ratio(own[j], now0[j]);
+        uint8_t* const rows = cache(j, pages) + (page0 * kPage + block0 * each % kPage) * D;
+        for (int row = in_pass; row < held; row += kRows) {
+          u32x4* const at = (u32x4*)(rows + row * D + col);
+          *at = recode(*at, f);
+        }
+      }
+      // (the first row of each block writes its scale)
+      if (mine && (lane == first || dst % each == 0)) *scale_at(j, pages + dst_page, dst) = now[j];
+    }
   }
 }
 
@@ -187,8 +204,10 @@ hipError_t launch_tree_masks(const TreeMasksParams& p, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_gqa_keep(const GqaKeepParams& p, hipStream_t stream) {
-  const int64_t waves = (int64_t)p.layers * p.batch * ((2 * p.kv_heads + kUnits - 1) / kUnits);
+hipError_t launch_gqa_keep(GqaKeepParams p, int cus, hipStream_t stream) {
+  const int64_t of_layer = (int64_t)p.batch * ((2 * p.kv_heads + kUnits - 1) / kUnits);
+  p.run = (int)std::min<int64_t>(kMostLayers, std::max<int64_t>(1, of_layer * p.layers / (32 * cus)));
+  const int64_t waves = (p.layers + p.run - 1) / p.run * of_layer;
   const dim3 grid((uint32_t)((waves + kWaves - 1) / kWaves));
   if (p.head_dim == 64) hipLaunchKernelGGL(gqa_keep_kernel<64>, grid, dim3(kThreads), 0, stream, p);
   else if (p.head_dim == 128) hipLaunchKernelGGL(gqa_keep_kernel<128>, grid, dim3(kThreads), 0, stream, p);

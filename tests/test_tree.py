@@ -570,6 +570,28 @@ def test_keep_paths_that_end_early_and_requests_that_are_left_alone():
 
 
 @gpu
+@pytest.mark.parametrize("layers,heads,each", [(46, 2, 32), (31, 5, 64)])
+def test_keep_of_more_layers_than_waves_at_once_is_that_of_each_layer(layers, heads, each):
+    """A wave takes several layers then, the last one fewer."""
+    batch, dim = 300, 64
+    rng, g = random.Random(layers), torch.Generator(device="cuda").manual_seed(layers)
+    news = [rng.choice([0, 1, 5, 31, 64]) for _ in range(batch)]
+    lens = [n + rng.randint(0, 200) for n in news]
+    used = [-(-n // PAGE) for n in lens]
+    order = rng.sample(range(sum(used) + 2), sum(used))
+    table = ints([[order.pop() if c < u else 0 for c in range(max(used))] for u in used])
+    codes = torch.randint(0, 0x7f, (2, layers, sum(used) + 2, heads, PAGE, dim), generator=g, dtype=torch.uint8, device="cuda")
+    scales = 2.0 ** torch.randint(-4, 5, (2, layers, sum(used) + 2, heads, PAGE // each), generator=g, device="cuda").float()
+    path, args = ints(_paths(rng, news)), (ints(lens), ints(starts(news)), table)
+    want, want_scales = codes.clone(), scales.clone()
+    for i in range(layers):
+        oa.omniattn_gqa_keep(path, *args, *(t[i].view(torch.float8_e4m3fn) for t in want), want_scales[0][i], want_scales[1][i])
+    assert not torch.equal(want, codes)
+    oa.omniattn_gqa_keep(path, *args, *(t.view(torch.float8_e4m3fn) for t in codes), scales[0], scales[1])
+    assert torch.equal(codes, want) and torch.equal(scales, want_scales)
+
+
+@gpu
 def test_keep_of_many_layers_past_two_gigabytes():
     """Layers whose codes lie more than 2^32 bytes behind the first."""
     layers, pages, heads, dim = 70, 512, 8, 128
