@@ -250,6 +250,15 @@ def test_nan_reaches_only_the_queries_that_see_it(dim, group):
 
 
 @gpu
+@pytest.mark.parametrize("dim,q_heads", [(64, 40), (128, 24), (128, 70), (256, 33)])
+def test_groups_of_more_rows_than_a_block_of_16(dim, q_heads):
+    """A node's query heads over several blocks, in small calls and others."""
+    rng = random.Random(dim + q_heads)
+    news = [5, 1, 9]
+    Problem([n + rng.randint(0, 700) for n in news], sets_of(rng, news), q_heads, 1, dim, 64, 4, 300, seed=q_heads).check(torch.float32)
+
+
+@gpu
 def test_strides_one_node_each_and_what_the_workspace_holds():
     p = Problem([129, 1, 300], [[1], [1], [0]], 8, 2, 128, 64, 0, 10 ** 6)
     out, lse = p.check(pad=3)
@@ -836,6 +845,18 @@ def test_many_rows_any_sets(sink, window):
 def test_many_rows_long_texts_are_split_and_joined(group, nodes):
     rng = random.Random(nodes)
     Wide([9000, 77 + nodes, 5003, 64], sets_of(rng, [nodes, 2, nodes, 64]), group, 1, 128, 64, 0, 10 ** 6, seed=5, poison=False).check(torch.float32)
+
+
+@gpu
+@pytest.mark.parametrize("sink,window,group,each", [(0, 100, 8, 32), (4, 100, 8, 64), (0, 20, 13, 128), (7, 0, 8, 64)])
+def test_many_rows_of_many_short_requests(sink, window, group, each):
+    """Blocks of few pages, which are not cut."""
+    rng = random.Random(window)
+    news = [rng.choice([0, 1, 12, 25, 33, 40, 64, 70]) for _ in range(200)]
+    lens = [n + rng.randint(0, 260) for n in news]
+    pages = min(max(-(-n // PAGE) for n in lens), -(-sink // PAGE) + -(-window // PAGE) + 1)
+    assert pages <= 3 and 200 * 2 * pages * -(-(-(-sum(news) // 200) * group) // 32) >= MANY
+    Problem(lens, sets_of(rng, news), 2 * group, 2, 128, each, sink, window, seed=window)._check(torch.float32)
 
 
 @gpu
