@@ -563,7 +563,8 @@ __device__ __forceinline__ VerifyChoice choose(const VerifyParams& p, const Node
       y = find<T>(p, (double)u * all.sum,
                [&](int k0) {
                  const Pair at = k0 ? pair_of(p, row, k0) : first;
-                 return double2{at.e[0].sum * weight(at.e[0].top, all.top, c), at.e[1].sum * weight(at.e[1].top, all.top, c)};
+                 // (nothing where the part's largest logit has no weight: find is to come to parts with a column that has one)
+                 return double2{at.e[0].sum * weight_or_0(at.e[0].top, all.top, c), at.e[1].sum * weight_or_0(at.e[1].top, all.top, c)};
                },
                [&](auto& w, auto& x, int col) {
                  load<T>(x, logits_of<T>(p, row), col, p.vocab);

@@ -427,6 +427,44 @@ def test_verify_drafts_that_equal_the_target_and_uniforms_at_the_ends():
 
 @gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("drafts", ["none", "near", "above"])
+@pytest.mark.parametrize("vocab,front,back", [(6000, 2048, 1500), (6001, 3000, 0), (4097, 0, 2048), (270000, 130 * 2048, 100)])
+def test_verify_uniforms_at_the_ends_over_many_parts(vocab, front, back, dtype, drafts):
+    """The first and the last token that has a probability, where whole parts of a row have none: behind masks of large negative numbers, or because a
+    small temperature leaves nothing of them.  Few nodes to a request, and more than a work group has waves.  (Distances from a row's top are whole numbers where the
+    temperature is small: over it none lies between 707, from where on the kernel takes a weight for 0, and 746, from where on exp in 64 bits is 0.)"""
+    rng, gen = random.Random(vocab + front), torch.Generator().manual_seed(vocab + front)
+    ends = (0.0, 1 - 2.0 ** -24)
+    for nodes, kinds in ((3, [(T, mask, u1) for T in (1.0, 0.02, 0.005) for mask in (-1e9, -3e38, -float("inf")) for u1 in ends]),
+                         (20, [(1.0, -1e9, 0.0), (0.02, -1e9, 0.0), (0.005, -40.0, 0.0), (0.005, -40.0, ends[1])])):
+        if vocab > 10 ** 5:
+            nodes, kinds = 9 if nodes == 20 else 2, rng.sample(kinds, 3)
+        total = nodes * len(kinds)
+        logits, parents, start = torch.empty((total, vocab)), [t - 1 for t in range(nodes)] * len(kinds), starts([nodes] * len(kinds))
+        q = {"none": None, "near": torch.empty((total, vocab)), "above": torch.full((total, vocab), 2.0)}[drafts]
+        u, tokens = torch.empty((total, 2)), [0] * total
+        for b, (T, mask, u1) in enumerate(kinds):
+            rows = slice(start[b], start[b + 1])
+            logits[rows] = torch.randn((nodes, vocab), generator=gen) * 3 if T == 1.0 else -torch.randint(0, 40, (nodes, vocab), generator=gen).float()
+            logits[rows, :front] = mask
+            logits[rows, vocab - back:] = mask
+            logits[rows, vocab - back - 1] = 0.0      # (a token next to the masked ones that has a probability at any temperature)
+            u[rows, 0], u[rows, 1] = 0.9, u1
+            exact = logits[rows].to(dtype).double()
+            for i, row in enumerate(exact):
+                t = float(np.float32(T))
+                if drafts == "near":
+                    q[start[b] + i] = torch.softmax((row + torch.randn(vocab, generator=gen).double()) / t, -1).float()
+                if i + 1 < nodes:    # (the token that follows without drafts' probabilities: the walk goes on)
+                    tokens[start[b] + i + 1] = ref.verify(gref.as_double(row[None]), None, [0], [-1], t, np.array([[0.9, u1]]))[1][0]
+        path, out = _check_verify(logits.to(dtype).cuda(), None if q is None else q.cuda(), tokens, parents, start, [T for T, _, _ in kinds], u.cuda())[:2]
+        assert (out.cpu()[torch.tensor(start[:-1])] >= 0).all()
+        if drafts != "near":
+            assert path.tolist() == list(range(nodes)) * len(kinds)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("batch,nodes,vocab", [(1, 6, 1000), (3, 20, 5000), (2, 64, 300000)])
 def test_verify_refused_first_children_that_are_sampled_after_all(batch, nodes, vocab, dtype):
     """Drafts' probabilities above the target's everywhere: a first child is refused, nothing is left of max(p - q, 0), and p's sample is the same
