@@ -148,8 +148,8 @@ def speculate(pool, prompts, answers, q_heads, sink, window, rows, draft, logits
     last token, and the probabilities that the first children were drawn from (a tensor [nodes of all, vocabulary], or None).  uniforms(nodes)
     returns the random numbers [nodes, 2] (needed with a temperature).  observe(step, texts) sees the texts as they grow.
 
-    The prompts have to fit in the pool together; after that a request whose tree finds no pages waits, as in serve.  Returns what happened, and
-    the texts."""
+    The prompts have to fit in the pool together; after that a request whose tree finds no pages waits, as in serve.  A request ends early where the
+    target has no token (logits of -inf or NaN only); "cut_short" says how many have.  Returns what happened, and the texts."""
     import torch
     from . import omniattn_gqa_workspace_bytes, omniattn_tree_masks, omniattn_tree_verify, omniattn_tree_verify_workspace_bytes
     if temperature > 0 and uniforms is None:
@@ -193,7 +193,7 @@ def speculate(pool, prompts, answers, q_heads, sink, window, rows, draft, logits
             raise RuntimeError(f"{int(pool.free_count)} free pages of {pages} are too few for the prompts")
         call(on_gpu([t for p, a, n in zip(prompts, at, news) for t in p[a:a + n]]), on_gpu([i for a, n in zip(at, news) for i in range(a, a + n)]), slots, None)
         at = [a + n * f for a, n, f in zip(at, news, fits.tolist())]
-    steps = given = used = 0
+    steps = given = used = short = 0
     while any(0 < len(t) < g for t, g in zip(texts, goal)):
         tokens, parents, probs = draft([t if 0 < len(t) < g else None for t, g in zip(texts, goal)])
         news = [len(t) for t in tokens]
@@ -215,14 +215,19 @@ def speculate(pool, prompts, answers, q_heads, sink, window, rows, draft, logits
         path.masked_fill_(~fits[request], -1)
         dropped.masked_fill_(~fits, 0)
         pool.keep(path, dropped)
-        following, fit, start = following.tolist(), fits.tolist(), [0]
+        following, gone, fit, start = following.tolist(), dropped.tolist(), fits.tolist(), [0]
         done = [0] * batch
         for b, n in enumerate(news):
             new = [t for t in following[start[-1]:start[-1] + n] if t >= 0] if fit[b] else []
             start.append(start[-1] + n)
+            # (the path's last node has no token behind it: the cache holds what the text ends with already, and the next tree could not begin with it)
+            ended = fit[b] and len(new) < n - gone[b]
             new = new[:goal[b] - len(texts[b])]
             texts[b] += new
             given += len(new)
+            if ended and len(texts[b]) < goal[b]:
+                goal[b] = len(texts[b])
+                short += 1
             done[b] = int(n > 0 and len(texts[b]) >= goal[b])
         if observe:
             observe(steps, texts)
@@ -230,7 +235,7 @@ def speculate(pool, prompts, answers, q_heads, sink, window, rows, draft, logits
         if any(done):
             pool.release(on_gpu(done))
     return {"requests": batch, "steps": steps, "tokens": given, "pages": used, "free_at_the_end": int(pool.free_count),
-            "tokens_per_step": round(given / max(steps, 1), 2)}, texts
+            "tokens_per_step": round(given / max(steps, 1), 2), "cut_short": short}, texts
 
 
 def main():

@@ -341,3 +341,60 @@ def test_two_steps_at_once():
         for name in NAMES:
             assert torch.equal(a[name], b[name]), name
         assert torch.equal(a["pool"].lens, b["pool"].lens) and torch.equal(a["pool"].k.view(torch.uint8), b["pool"].k.view(torch.uint8))
+
+
+class Rule:
+    """Behind token t follows 21 t + 7 (which comes by all tokens), with a logit that no other token comes near; behind the tokens of `dead` the target has nothing to say (`nothing` for
+    every logit).  Drafts guess right two times in three."""
+
+    def __init__(self, seed, dead=(), nothing=float("-inf")):
+        self.rng, self.dead, self.nothing, self.nodes = random.Random(seed), set(dead), nothing, []
+
+    def after(self, token):
+        return (21 * token + 7) % VOCAB
+
+    def text(self, prompt, answer):
+        """What a prompt becomes."""
+        out = list(prompt)
+        while answer and out[-1] not in self.dead:
+            out.append(self.after(out[-1]))
+            answer -= 1
+        return out
+
+    def draft(self, texts):
+        self.nodes.clear()
+        trees = [[] if t is None else [t[-1]] for t in texts]
+        for tree in trees:
+            for _ in range(self.rng.randint(0, 9) if tree else 0):
+                tree.append(self.after(tree[-1]) if self.rng.random() < 2 / 3 else self.rng.randrange(VOCAB))
+            self.nodes.extend(tree)
+        return trees, [list(range(-1, len(t) - 1)) for t in trees], None
+
+    def logits(self, out):
+        scores = torch.zeros((out.shape[1], VOCAB), device="cuda").scatter_(1, torch.tensor([[self.after(t)] for t in self.nodes], device="cuda"), 200.0)
+        return torch.where(torch.tensor([t in self.dead for t in self.nodes], device="cuda")[:, None], self.nothing, scores)
+
+
+def _rows(tokens, positions, buffer):
+    buffer.normal_()
+
+
+@gpu
+@pytest.mark.parametrize("temperature,nothing", [(0.0, float("-inf")), (0.9, float("-inf")), (0.9, float("nan"))])
+def test_a_request_ends_where_the_target_has_no_token(temperature, nothing):
+    """Behind a prompt, or on the way.  The others go on, with as many tokens in the cache as their texts say, and all pages come back."""
+    rule = Rule(3, dead=(11,), nothing=nothing)
+    prompts = [[5, 3], [2, 11], [9, 17], [30], [1] * 130, [4]]
+    answers = [20, 20, 25, 10, 9, 1]
+    want = [rule.text(p, a) for p, a in zip(prompts, answers)]
+    short = [len(w) < len(p) + a for w, p, a in zip(want, prompts, answers)]
+    assert any(short) and not all(short) and any(s and len(w) > len(p) + 1 for s, w, p in zip(short, want, prompts))
+    pool = Pool(len(prompts), LAYERS, 20, HEADS, 64, 3, scale_tokens=32)
+
+    def observe(step, texts):
+        for n, text, full in zip(pool.lens.tolist(), texts, want):
+            assert text == full[:len(text)] and (n in (0, len(text) - 1) or text == full)
+    what, texts = speculate(pool, prompts, answers, Q_HEADS, 0, 10 ** 6, _rows, rule.draft, rule.logits, temperature=temperature,
+                            uniforms=lambda n: torch.rand((n, 2), device="cuda"), observe=observe)
+    assert texts == want
+    assert what["free_at_the_end"] == 20 and what["cut_short"] == sum(short) and what["tokens"] == sum(len(w) - len(p) for w, p in zip(want, prompts))
