@@ -15,6 +15,7 @@ import argparse
 import json
 
 PAGE = 128
+NODES = 64  # of a tree, at most
 
 
 class Pool:
@@ -144,9 +145,10 @@ def speculate(pool, prompts, answers, q_heads, sink, window, rows, draft, logits
 
     rows(tokens, positions, buffer) fills the rows of all layers for tokens at positions of their texts, [layers, tokens, query heads + 2 KV heads,
     head width]; logits(out) gives the target's logits [tokens, vocabulary] from what the layers give, [layers, tokens, query heads, head
-    width].  draft(texts) returns for every text (a list; None: nothing is wanted) the tree that follows it: tokens and parents, the first one the text's
-    last token, and the probabilities that the first children were drawn from (a tensor [nodes of all, vocabulary], or None).  uniforms(nodes)
-    returns the random numbers [nodes, 2] (needed with a temperature).  observe(step, texts) sees the texts as they grow.
+    width].  draft(texts) returns for every text (a list; None: nothing is wanted, no nodes) the tree that follows it: tokens and parents of 1 to 64 nodes
+    (ValueError otherwise), the first one the text's last token, and the probabilities that the first children were drawn from (a tensor [nodes of all,
+    vocabulary], or None).  uniforms(nodes) returns the random numbers [nodes, 2] (needed with a temperature).  observe(step, texts) sees the texts as they
+    grow.
 
     The prompts have to fit in the pool together; after that a request whose tree finds no pages waits, as in serve.  A request ends early where the
     target has no token (logits of -inf or NaN only); "cut_short" says how many have.  Returns what happened, and the texts."""
@@ -195,7 +197,14 @@ def speculate(pool, prompts, answers, q_heads, sink, window, rows, draft, logits
         at = [a + n * f for a, n, f in zip(at, news, fits.tolist())]
     steps = given = used = short = 0
     while any(0 < len(t) < g for t, g in zip(texts, goal)):
-        tokens, parents, probs = draft([t if 0 < len(t) < g else None for t, g in zip(texts, goal)])
+        wanted = [t if 0 < len(t) < g else None for t, g in zip(texts, goal)]
+        tokens, parents, probs = draft(wanted)
+        if len(tokens) != batch or len(parents) != batch:
+            raise ValueError(f"{len(tokens)} and {len(parents)} trees' tokens and parents for {batch} texts")
+        for b, (text, tree, up) in enumerate(zip(wanted, tokens, parents)):
+            # (of a larger tree verification keeps nothing, again and again)
+            if len(tree) > NODES or len(up) != len(tree) or (text is not None and not len(tree)):
+                raise ValueError(f"text {b}: a tree of {len(tree)} tokens and {len(up)} parents; as many of either wanted, 1 to {NODES}")
         news = [len(t) for t in tokens]
         slots, fits = extend(news)
         if not bool((fits & (on_gpu(news) > 0)).any()):
@@ -249,8 +258,8 @@ def main():
         raise SystemExit("needs a GPU: the library has no CPU path")
     gen = torch.Generator().manual_seed(1)
     prompts, answers = (torch.randint(1, 2 * n + 1, (args.requests,), generator=gen).tolist() for n in (args.prompt, args.answer))
-    if not 0 <= args.drafts < 64:
-        ap.error("a tree has up to 64 nodes: at most 63 drafts")
+    if not 0 <= args.drafts < NODES:
+        ap.error(f"a tree has up to {NODES} nodes: at most {NODES - 1} drafts")
     each = [-(-(p + a + args.drafts) // PAGE) for p, a in zip(prompts, answers)]
     pool = Pool(args.requests, args.layers, sum(each), args.kv_heads, args.dim, max(each))
     if args.drafts:

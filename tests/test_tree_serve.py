@@ -398,3 +398,11 @@ def test_a_request_ends_where_the_target_has_no_token(temperature, nothing):
                             uniforms=lambda n: torch.rand((n, 2), device="cuda"), observe=observe)
     assert texts == want
     assert what["free_at_the_end"] == 20 and what["cut_short"] == sum(short) and what["tokens"] == sum(len(w) - len(p) for w, p in zip(want, prompts))
+
+
+@pytest.mark.parametrize("tokens,parents", [([[1] * 65, [2]], [[-1] + [0] * 64, [-1]]), ([[1], []], [[-1], []]), ([[1, 3], [2]], [[-1], [-1]]), ([[1]], [[-1]])])
+def test_trees_that_speculate_refuses(tokens, parents):
+    """More nodes than a tree may have, none for a text that is to grow, tokens and parents of other numbers, a tree too few."""
+    pool = Pool(2, LAYERS, 4, HEADS, 64, 2, device="cpu")
+    with pytest.raises(ValueError):
+        speculate(pool, [[1], [2]], [5, 5], Q_HEADS, 0, 10, _rows, lambda texts: (tokens, parents, None), None)
