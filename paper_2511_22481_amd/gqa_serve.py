@@ -150,7 +150,7 @@ def speculate(pool, prompts, answers, q_heads, sink, window, rows, draft, logits
     vocabulary], or None).  uniforms(nodes) returns the random numbers [nodes, 2] (needed with a temperature).  observe(step, texts) sees the texts as they
     grow.
 
-    The prompts have to fit in the pool together; after that a request whose tree finds no pages waits, as in serve.  A request ends early where the
+    The prompts (of requests with an answer) have to fit in the pool together; after that a request whose tree finds no pages waits, as in serve.  A request ends early where the
     target has no token (logits of -inf or NaN only); "cut_short" says how many have.  Returns what happened, and the texts."""
     import torch
     from . import omniattn_gqa_workspace_bytes, omniattn_tree_masks, omniattn_tree_verify, omniattn_tree_verify_workspace_bytes
@@ -186,10 +186,10 @@ def speculate(pool, prompts, answers, q_heads, sink, window, rows, draft, logits
                 pool.attend_tree(i, qkv[i], slots, masks, out[i], lse, workspace, sink, window)
         return out
 
-    # the prompts without their last tokens, which are the first trees' first nodes
-    at = [0] * batch
-    while any(a < len(p) - 1 for a, p in zip(at, prompts)):
-        news = [min(chunk, len(p) - 1 - a) if len(p) else 0 for a, p in zip(at, prompts)]
+    # the prompts without their last tokens, which are the first trees' first nodes (of a request that wants no answer nothing is looked at: it has no pages)
+    at, last = [0] * batch, [max(len(p) - 1, 0) if a > 0 else 0 for p, a in zip(prompts, answers)]
+    while any(a < n for a, n in zip(at, last)):
+        news = [min(chunk, n - a) for a, n in zip(at, last)]
         slots, fits = extend(news)
         if not bool((fits & (on_gpu(news) > 0)).any()):
             raise RuntimeError(f"{int(pool.free_count)} free pages of {pages} are too few for the prompts")

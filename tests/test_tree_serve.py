@@ -400,6 +400,20 @@ def test_a_request_ends_where_the_target_has_no_token(temperature, nothing):
     assert what["free_at_the_end"] == 20 and what["cut_short"] == sum(short) and what["tokens"] == sum(len(w) - len(p) for w, p in zip(want, prompts))
 
 
+@gpu
+def test_requests_without_an_answer_hold_no_pages():
+    """Among others that would find too few pages if they did, and alone."""
+    rule = Rule(4)
+    prompts, answers = [[1] * 300, [2] * 100, [3] * 260, [], [4]], [0, 50, 0, 5, 0]
+    pool = Pool(5, LAYERS, 2, HEADS, 64, 3, scale_tokens=32)
+    what, texts = speculate(pool, prompts, answers, Q_HEADS, 0, 10 ** 6, _rows, rule.draft, rule.logits)
+    assert texts == [rule.text(p, a) if p else [] for p, a in zip(prompts, answers)]
+    assert what["free_at_the_end"] == 2 and pool.lens.tolist() == [0] * 5 and what["tokens"] == 50 and what["cut_short"] == 0
+    pool = Pool(2, LAYERS, 4, HEADS, 64, 3, scale_tokens=32)
+    what, texts = speculate(pool, [[1] * 140, [2] * 5], [0, 0], Q_HEADS, 0, 10 ** 6, _rows, rule.draft, rule.logits)
+    assert texts == [[1] * 140, [2] * 5] and what["free_at_the_end"] == 4 and what["steps"] == 0
+
+
 @pytest.mark.parametrize("tokens,parents", [([[1] * 65, [2]], [[-1] + [0] * 64, [-1]]), ([[1], []], [[-1], []]), ([[1, 3], [2]], [[-1], [-1]]), ([[1]], [[-1]])])
 def test_trees_that_speculate_refuses(tokens, parents):
     """More nodes than a tree may have, none for a text that is to grow, tokens and parents of other numbers, a tree too few."""
