@@ -380,9 +380,11 @@ int omniattn_gqa_append(const omniattn_gqa_t* gqa, int32_t num_tokens, const voi
  * 2^-14 of the row's largest such product, and 2^-36 of that below).  A bf16 result is the fp32 result rounded.
  *
  * omniattn_gqa_workspace_bytes depends on the current device and on batch, num_queries, the head counts and head_dim;
- * 0 for an invalid problem.
+ * 0 for an invalid problem.  It is enough for omniattn_gqa_tree too, whose blocks are larger; omniattn_gqa_decode_workspace_bytes, which is that or less,
+ * for omniattn_gqa_decode alone (head_dim 128, more than 32 query rows to a request and KV head, 256 compute units: 17 MB instead of 69).
  */
 size_t omniattn_gqa_workspace_bytes(const omniattn_gqa_t* gqa);
+size_t omniattn_gqa_decode_workspace_bytes(const omniattn_gqa_t* gqa);
 int omniattn_gqa_decode(const omniattn_gqa_t* gqa, const void* q, int64_t q_stride, const void* k_cache, const void* v_cache,
                         const float* k_scales, const float* v_scales, const int32_t* page_table, const int32_t* seq_lens,
                         const int32_t* q_start, void* out, float* lse, void* workspace, size_t workspace_bytes,

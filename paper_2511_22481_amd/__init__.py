@@ -23,6 +23,7 @@ from .binding import (  # noqa: F401
     omniattn_table_release,
     omniattn_gqa_append,
     omniattn_gqa_workspace_bytes,
+    omniattn_gqa_decode_workspace_bytes,
     omniattn_gqa_decode,
     gqa_decode,
     omniattn_tree_masks,

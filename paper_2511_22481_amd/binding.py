@@ -118,8 +118,9 @@ def load_library():
     lib.omniattn_table_release.argtypes = [ctypes.POINTER(Table)] + [P] * 6
     lib.omniattn_gqa_append.restype = ctypes.c_int
     lib.omniattn_gqa_append.argtypes = [ctypes.POINTER(Gqa), ctypes.c_int32, P, ctypes.c_int64, P, ctypes.c_int64] + [P] * 6
-    lib.omniattn_gqa_workspace_bytes.restype = ctypes.c_size_t
-    lib.omniattn_gqa_workspace_bytes.argtypes = [ctypes.POINTER(Gqa)]
+    for size in (lib.omniattn_gqa_workspace_bytes, lib.omniattn_gqa_decode_workspace_bytes):
+        size.restype = ctypes.c_size_t
+        size.argtypes = [ctypes.POINTER(Gqa)]
     lib.omniattn_gqa_decode.restype = ctypes.c_int
     lib.omniattn_gqa_decode.argtypes = [ctypes.POINTER(Gqa), P, ctypes.c_int64] + [P] * 10 + [ctypes.c_size_t, P]
     lib.omniattn_tree_masks.restype = ctypes.c_int
@@ -455,9 +456,17 @@ def omniattn_gqa_append(k_new, v_new, slot_map, k_cache, v_cache, k_scales, v_sc
 
 
 def omniattn_gqa_workspace_bytes(batch, num_queries, num_q_heads, num_kv_heads, head_dim):
-    """Bytes of workspace that omniattn_gqa_decode needs for such a call on the current device."""
-    rec = _gqa_record(batch, num_queries, num_q_heads, num_kv_heads, head_dim, 128, 128, 1, 1, 1, 0, 0, 1.0, BF16)
-    n = int(load_library().omniattn_gqa_workspace_bytes(rec))
+    """Bytes of workspace that omniattn_gqa_decode or omniattn_gqa_tree needs for such a call on the current device."""
+    return _gqa_bytes(load_library().omniattn_gqa_workspace_bytes, batch, num_queries, num_q_heads, num_kv_heads, head_dim)
+
+
+def omniattn_gqa_decode_workspace_bytes(batch, num_queries, num_q_heads, num_kv_heads, head_dim):
+    """The same for omniattn_gqa_decode alone, which can do with less."""
+    return _gqa_bytes(load_library().omniattn_gqa_decode_workspace_bytes, batch, num_queries, num_q_heads, num_kv_heads, head_dim)
+
+
+def _gqa_bytes(size, batch, num_queries, num_q_heads, num_kv_heads, head_dim):
+    n = int(size(_gqa_record(batch, num_queries, num_q_heads, num_kv_heads, head_dim, 128, 128, 1, 1, 1, 0, 0, 1.0, BF16)))
     _want(n > 0, "no valid problem, or no GPU")
     return n
 
@@ -478,7 +487,7 @@ def gqa_decode(q, k_cache, v_cache, k_scales, v_scales, page_table, seq_lens, si
         raise OmniAttnError(-4, "omniattn runs on the GPU only: tensors must be CUDA tensors")
     out = torch.empty(q.shape, dtype=torch.bfloat16 if out_dtype is None else out_dtype, device=q.device)
     lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-    size = omniattn_gqa_workspace_bytes(seq_lens.shape[0], q.shape[0], q.shape[1], k_cache.shape[1], q.shape[2])
+    size = omniattn_gqa_decode_workspace_bytes(seq_lens.shape[0], q.shape[0], q.shape[1], k_cache.shape[1], q.shape[2])
     workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
     omniattn_gqa_decode(q, k_cache, v_cache, k_scales, v_scales, page_table, seq_lens, q_start, out, lse, workspace, sink=sink, window=window,
                         softmax_scale=softmax_scale)

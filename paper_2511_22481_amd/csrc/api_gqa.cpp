@@ -90,6 +90,24 @@ Workspace workspace_of(const omniattn_gqa_t* g, const GqaShape& shape) {
   return w;
 }
 
+// Enough for fewer queries too, and for any kept set and table width: the calls of a server share one.  (The number of queries decides
+// by its rows to a request and KV head, up to 16, up to 32 or more; those that keep few pages have the most shares, and trees over many the
+// largest blocks.)
+size_t most_workspace(const omniattn_gqa_t* gqa, bool trees) {
+  int cus = 0;
+  if (check_gqa(gqa) != OMNIATTN_OK || device_cus(&cus) != OMNIATTN_OK) return 0;
+  size_t bytes = 0;
+  omniattn_gqa_t g = *gqa;
+  g.sink = g.window = 0;
+  const int64_t group = gqa->num_q_heads / gqa->num_kv_heads;
+  for (int rows : {16, 32, INT32_MAX}) {
+    g.num_queries = (int32_t)std::min<int64_t>(gqa->num_queries, std::max<int64_t>(rows / group, 1) * gqa->batch);
+    bytes = std::max(bytes, workspace_of(gqa, shape_of(&g, cus, false)).bytes);
+    if (trees) bytes = std::max(bytes, workspace_of(gqa, gqa_shape(g.batch, g.num_queries, (int)group, g.num_kv_heads, g.head_dim, kMaxPages, cus, true)).bytes);
+  }
+  return bytes;
+}
+
 // omniattn_gqa_decode, and omniattn_gqa_tree (tree).
 int attend(const omniattn_gqa_t* gqa, const void* q, int64_t q_stride, const void* k_cache, const void* v_cache, const float* k_scales, const float* v_scales,
            const int32_t* page_table, const int32_t* seq_lens, const int32_t* q_start, bool tree, const uint64_t* masks, void* out, float* lse, void* workspace,
@@ -299,24 +317,9 @@ int omniattn_gqa_append(const omniattn_gqa_t* gqa, int32_t num_tokens, const voi
   return OMNIATTN_OK;
 }
 
-size_t omniattn_gqa_workspace_bytes(const omniattn_gqa_t* gqa) {
-  int cus = 0;
-  if (check_gqa(gqa) != OMNIATTN_OK || device_cus(&cus) != OMNIATTN_OK) return 0;
-  // Enough for fewer queries too, and for any kept set and table width: the calls of a server share one.  (The number of queries decides
-  // by its rows to a request and KV head, up to 16, up to 32 or more; those that keep few pages have the most shares, and trees over many the
-  // largest blocks.)
-  size_t bytes = 0;
-  omniattn_gqa_t g = *gqa;
-  g.sink = g.window = 0;
-  const int64_t group = gqa->num_q_heads / gqa->num_kv_heads;
-  for (int rows : {16, 32, INT32_MAX}) {
-    g.num_queries = (int32_t)std::min<int64_t>(gqa->num_queries, std::max<int64_t>(rows / group, 1) * gqa->batch);
-    const GqaShape shapes[2] = {shape_of(&g, cus, false), gqa_shape(g.batch, g.num_queries, (int)group, g.num_kv_heads, g.head_dim, kMaxPages, cus, true)};
-    g.num_queries = gqa->num_queries;
-    for (const GqaShape& shape : shapes) bytes = std::max(bytes, workspace_of(&g, shape).bytes);
-  }
-  return bytes;
-}
+size_t omniattn_gqa_workspace_bytes(const omniattn_gqa_t* gqa) { return most_workspace(gqa, true); }
+
+size_t omniattn_gqa_decode_workspace_bytes(const omniattn_gqa_t* gqa) { return most_workspace(gqa, false); }
 
 int omniattn_gqa_decode(const omniattn_gqa_t* gqa, const void* q, int64_t q_stride, const void* k_cache, const void* v_cache, const float* k_scales,
                         const float* v_scales, const int32_t* page_table, const int32_t* seq_lens, const int32_t* q_start, void* out, float* lse,

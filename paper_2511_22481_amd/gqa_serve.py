@@ -74,7 +74,7 @@ def serve(pool, prompts, answers, q_heads, sink, window, rows, chunk=512, graph=
     layers give.  A request for whose new tokens there are no pages keeps its length (pool.lens; its rows of out and lse mean nothing) and brings
     them again in the next step, when others may have given pages back.  RuntimeError if a step has pages for none.  Returns what happened."""
     import torch
-    from . import omniattn_gqa_workspace_bytes
+    from . import omniattn_gqa_decode_workspace_bytes
     layers, pages, heads, _, dim = pool.k.shape
     batch, device = len(prompts), pool.k.device
     # (a request without a prompt begins with its answer, a token a step)
@@ -84,7 +84,7 @@ def serve(pool, prompts, answers, q_heads, sink, window, rows, chunk=512, graph=
     lse = torch.empty((layers, most, q_heads), device=device)
     slots = torch.empty(most, dtype=torch.int32, device=device)
     new_lens, done = (torch.zeros(batch, dtype=torch.int32, device=device) for _ in range(2))
-    workspace = torch.empty(omniattn_gqa_workspace_bytes(batch, most, q_heads, heads, dim), dtype=torch.uint8, device=device)
+    workspace = torch.empty(omniattn_gqa_decode_workspace_bytes(batch, most, q_heads, heads, dim), dtype=torch.uint8, device=device)
 
     def step(n):
         """A step of up to n new tokens."""

@@ -268,6 +268,47 @@ def test_strides_one_node_each_and_what_the_workspace_holds():
 
 
 @gpu
+@pytest.mark.parametrize("dim,nodes,group", [(64, 1, 1), (64, 40, 4), (128, 3, 4), (128, 7, 4), (128, 20, 4), (128, 2, 40), (256, 30, 2)])
+def test_calls_without_trees_ask_for_no_more_than_they_need(dim, nodes, group):
+    """Rows of a block, their outputs and statistics in 32 bits, two blocks to a work group, and a word of 64 bits to a row of the call; blocks of a decode have 64
+    rows at most (two work groups to a compute unit, or one where they have 64 rows of a width above 64; four of 16 rows, with four shares each, at width 64)."""
+    batch, heads = 9, 2
+    sizes = [f(batch, batch * nodes, heads * group, heads, dim) for f in (oa.omniattn_gqa_decode_workspace_bytes, oa.omniattn_gqa_workspace_bytes)]
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    slots = 2 * cus * (64 if dim > 64 else 256)
+    assert sizes[0] <= sizes[1] and sizes[0] <= slots * (16 + 4 * dim) + 8 * batch * nodes * heads * group + 512
+    p = Problem([n + 300 for n in [nodes] * batch], sets_of(random.Random(dim), [nodes] * batch, "chain"), heads * group, heads, dim, 64, 0, 10 ** 6, poison=False)
+    (k, v), (ks, vs), q = p.codes.cuda(), p.scales.cuda(), p.q.cuda()
+    args = q, k, v, ks, vs, ints(p.table), ints(p.lens)
+    start = ints(p.q_start)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    held = torch.cuda.memory_allocated()
+    torch.cuda.reset_peak_memory_stats()
+    want, want_lse = oa.gqa_decode(*args, 0, 10 ** 6, p.scale, q_start=start)
+    # (torch rounds tensors to 512 bytes, and those above 10 MB to 2 MB: 17848832 bytes of workspace become 18874368)
+    assert torch.cuda.max_memory_allocated() - held <= sizes[0] + 2 * q.numel() + 4 * want_lse.numel() + 2 * 512 + 2 ** 21
+    out, lse = torch.empty_like(want), torch.empty_like(want_lse)
+    ws = torch.full((sizes[0],), 0xff, dtype=torch.uint8, device="cuda")
+    for n in (batch * nodes, batch):   # (fewer queries, too)
+        oa.omniattn_gqa_decode(q[:n], k, v, ks, vs, ints(p.table), ints(p.lens), start if n == batch * nodes else None, out[:n], lse[:n], ws, sink=0, window=10 ** 6, softmax_scale=p.scale)
+        if n == batch * nodes:
+            assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    torch.cuda.synchronize()
+
+
+@gpu
+def test_a_workspace_without_trees_is_refused_where_a_tree_needs_more():
+    p = Problem([20000] * 8, sets_of(random.Random(1), [16] * 8), 32, 8, 128, 64, 0, 10 ** 6, poison=False)
+    (k, v), (ks, vs), q = p.codes.cuda(), p.scales.cuda(), p.q.cuda()
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    ws = torch.empty(oa.omniattn_gqa_decode_workspace_bytes(8, 128, 32, 8, 128), dtype=torch.uint8, device="cuda")
+    with pytest.raises(oa.OmniAttnError) as e:
+        oa.omniattn_gqa_tree(q, k, v, ks, vs, ints(p.table), ints(p.lens), ints(p.q_start), longs(p.sets), out, lse, ws, sink=0, window=10 ** 6, softmax_scale=p.scale)
+    assert e.value.code == -3
+
+
+@gpu
 def test_a_chain_is_what_decode_computes():
     p = Problem([150, 260, 700], sets_of(random.Random(1), [20, 3, 64], "chain"), 8, 2, 128, 64, 4, 100, poison=False)
     out, lse = p.check()
