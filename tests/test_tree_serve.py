@@ -420,3 +420,54 @@ def test_trees_that_speculate_refuses(tokens, parents):
     pool = Pool(2, LAYERS, 4, HEADS, 64, 2, device="cpu")
     with pytest.raises(ValueError):
         speculate(pool, [[1], [2]], [5, 5], Q_HEADS, 0, 10, _rows, lambda texts: (tokens, parents, None), None)
+
+
+@gpu
+def test_the_cache_where_scales_change():
+    """Rows whose largest numbers lie up to 2^6 apart, drafted and kept or dropped: what a text's slots hold is its rows, as far as a block's scale allows, which
+    may be one that a dropped node has left (append raises a block's scale, and nothing lowers it again as long as tokens of the text lie in the block).
+    A row is rounded when it is appended, to 2^-4 of a number or to half a subnormal step, 2^-10 of the scale; after that scales only grow, at least twofold,
+    and codes times a power of two are rounded again only where they become subnormal: together 2^-10 of the last scale times 1 + 1/2 + .. < 2."""
+    dim, rng = 64, random.Random(8)
+    model, rule = Model(dim, 8), Rule(8)
+    g = torch.Generator().manual_seed(8)
+    factor = 2.0 ** torch.randint(-3, 4, (LAYERS, TABLE, 2 * HEADS, 1), generator=g).float()
+    model.rows_of[:, :, Q_HEADS:] *= factor.cuda().bfloat16()
+    prompts = [[rng.randrange(VOCAB) for _ in range(n)] for n in (3, 120, 64, 250)]
+    pool = Pool(len(prompts), LAYERS, 30, HEADS, dim, 6, scale_tokens=32)
+    seen = {"blocks": 0, "raised": 0, "steps": 0}
+
+    def least(rows):
+        """The smallest power of two by which the largest magnitude is at most 448."""
+        part, exponent = torch.frexp(rows.abs().amax((-1, -2)).double() / 448)
+        return torch.ldexp(torch.ones_like(part), exponent - (part == 0.5).int())
+
+    def observe(step, texts):
+        lens, table = pool.lens.tolist(), pool.table.tolist()
+        for b, text in enumerate(texts):
+            n = lens[b]
+            if n != len(text) - 1:
+                continue      # (it has its answer)
+            at = torch.arange(n, device="cuda")
+            slot = torch.tensor(table[b], device="cuda")[at // PAGE]
+            want = model.rows_of[:, model.index(torch.tensor(text[:n], device="cuda"), at), Q_HEADS:].double()
+            for cache, scales, rows in ((pool.k, pool.k_scales, want[:, :, :HEADS]), (pool.v, pool.v_scales, want[:, :, HEADS:])):
+                codes = cache.view(torch.uint8)[:, slot, :, at % PAGE].view(torch.float8_e4m3fn).double()      # [tokens, layers, heads, dim]
+                scale = scales[:, slot, :, at % PAGE // 32].double()                                           # [tokens, layers, heads]
+                rows = rows.transpose(0, 1)
+                assert ((codes * scale[..., None] - rows).abs() <= 2.0 ** -4 * rows.abs() + 2.0 ** -9 * scale[..., None]).all()
+                for first in range(0, n, 32):
+                    here, need = scale[first], least(rows[first:first + 32].permute(1, 2, 0, 3))
+                    assert (scale[first:first + 32] == here).all() and (here >= need).all() and (here <= 2.0 ** -8 * 2.0 ** 3).all()
+                    seen["blocks"] += here.numel()
+                    seen["raised"] += int((here > need).sum())
+        seen["steps"] += 1
+    trees = _trees(rng, 20, lambda text: rule.after(text[-1]))
+
+    def draft(texts):
+        tokens, parents, probs = trees(texts)
+        rule.nodes[:] = [t for tree in tokens for t in tree]
+        return tokens, parents, probs
+    what, texts = speculate(pool, prompts, [60] * 4, Q_HEADS, 0, 10 ** 6, model.rows, draft, rule.logits, observe=observe)
+    assert texts == [rule.text(p, 60) for p in prompts] and what["steps"] < 40
+    assert 0 < seen["raised"] < seen["blocks"], seen
