@@ -466,8 +466,8 @@ typedef struct {
  *   dropped      device, int32 [B]: nodes that do not stay
  *   workspace    device, omniattn_tree_verify_workspace_bytes(verify) bytes, 256-byte aligned (enough for fewer nodes, too); calls in
  *                flight at once need one each
- * A request with too many nodes keeps none.  Numbers are held in 64 bits; an exponential is good to 5.6e-11 of itself, a probability to 2.8e-10 (its own and
- * four in the sum).  A token whose weight beside its row's likeliest is not above 2^-1020 has none, with u1 = 0 too.  Same inputs give the same results.
+ * A request with too many nodes keeps none.  Numbers are held in 64 bits; an exponential is good to 4.7e-11 of itself, a probability to 1.9e-10 (its own and
+ * three in the sum); exp(0) is 1.  A token whose weight beside its row's likeliest is not above 2^-1020 has none, with u1 = 0 too.  Same inputs give the same results.
  */
 size_t omniattn_tree_verify_workspace_bytes(const omniattn_verify_t* verify);
 int omniattn_tree_verify(const omniattn_verify_t* verify, const void* logits, int64_t logits_stride, const float* draft_probs, int64_t draft_stride,

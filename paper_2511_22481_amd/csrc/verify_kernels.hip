@@ -15,7 +15,7 @@
 // nodes' tokens (a wave finds the part of 2048 columns whose running sum passes the border, and looks at these again); the walk.  Logits are read
 // once, but for the parts that tokens are found in and, with q, the rows whose first child is refused.
 //
-// What bounds them: the sums, in bf16, the exponentials (12 instructions of 64 bits and 4 others for a logit, about 5 clocks each; 64 requests of 6
+// What bounds them: the sums, in bf16, the exponentials (13 instructions of 64 bits for a logit, about 5 clocks each; 64 requests of 6
 // nodes, 131072 columns: 38 us, 2.6 TB/s); in fp32 memory nearly (32 requests of 40 nodes, 100003 columns: 98 us, 5.2 TB/s; maxima
 // alone 89).  The kernels behind them take 5 to 14 us each, which are chains of loads; a node's part costs 2 us.
 #include <hip/hip_runtime.h>
@@ -51,22 +51,24 @@ struct Scale {
 };
 // (A request without a temperature takes the likeliest token; its probabilities are those at 1.  An infinite one: c is not 0, or -inf would get a weight.)
 __device__ __forceinline__ Scale scale_of(float T) {
-  const double c = T > 0.f ? fmax(kLog2e / (double)T, 0x1p-1000) : kLog2e;
-  return Scale{c, kLeast / c};
+  const double c = T > 0.f ? fmax(kLog2e / (double)T, 0x1p-1000) : kLog2e, inverse = T > 0.f ? fmin(kLn2 * (double)T, 0x1p+1000) : kLn2;
+  return Scale{c, kLeast * inverse};
 }
 // 2^(c d) for d <= 0 (NaN: as for `least`), by rounding c d to an integer: by adding and taking away 1.5 * 2^52, in whose low word the integer then stands.
 // (The instructions for that, for the conversion and for the scaling take longer than an addition, which takes twice as long as in 32 bits.)
 constexpr double kMagic = 6755399441055744.0;
-// 2^f 2^n for f in [-1/2, 1/2] and n in the low word of t.  The polynomial of degree 7 that equals 2^f at the Chebyshev nodes, off by at most 5.6e-11.
+// 2^f 2^n for f in [-1/2, 1/2] and n in the low word of t.  Of the polynomials of degree 7 that are 1 at 0 the one that is off by the least part of 2^f: by
+// 4.7e-11.  (1 at 0, so that the largest logits' weights are 1: sums of tokens that are equally likely are exact then, and a u1 on the border between
+// two of them gives the one behind it.)
 __device__ __forceinline__ double power_of(double f, double t) {
-  double y = 1.5303700711425663e-05;
-  y = fma(y, f, 1.5469729214122798e-04);
-  y = fma(y, f, 1.3333478473685175e-03);
-  y = fma(y, f, 9.6180256133180180e-03);
-  y = fma(y, f, 5.5504109063258665e-02);
-  y = fma(y, f, 2.4022651213498092e-01);
-  y = fma(y, f, 6.9314718055683240e-01);
-  y = fma(y, f, 0.9999999999595618);
+  double y = 1.519615685518997e-05;
+  y = fma(y, f, 1.5466756311730684e-04);
+  y = fma(y, f, 1.333393505442565e-03);
+  y = fma(y, f, 9.6180381320883e-03);
+  y = fma(y, f, 5.550410365992507e-02);
+  y = fma(y, f, 2.402265106656079e-01);
+  y = fma(y, f, 6.931471807045319e-01);
+  y = fma(y, f, 1.0);
   // (asked for by name: the compiler makes a sum of 64 bits of it, in five instructions)
   u32x2 bits = __builtin_bit_cast(u32x2, y);
   asm("v_lshl_add_u32 %0, %1, 20, %0" : "+v"(bits[1]) : "v"(__builtin_bit_cast(u32x2, t)[0]));
@@ -233,18 +235,15 @@ __global__ __launch_bounds__(kThreads, 8) void verify_sums_kernel(VerifyParams p
   top = wave_max(top);
   double m = top, sum = 0.0;
   if (fabs(m * c.c) < 0x1p+30 && c.c > 1e-30) {
-    // 2^(c l - high): without a subtraction for each logit, and with `least` in 32 bits (off by 2^-24 of a product below 2^31: by 128 at most)
-    const double high = ceil(m * c.c), magic = kMagic - high;
-    const float least = (float)((high + (kLeast + 160.0)) / c.c);
+    // (with `least` in 32 bits: off by 2^-24 of a product below 2^31, by 128 at most)
+    const float least = (float)fma(c.least, (kLeast + 160.0) / kLeast, m);
 #pragma unroll
     for (int t = 0; t < Of::kMany; ++t)
 #pragma unroll
       for (int i = 0; i < Of::kEach; ++i) {
-        const double l = max2(x.at(t, i), least), n = fma(l, c.c, magic);
-        sum += power_of(fma(l, c.c, magic - n), n);
+        const double d = (double)max2(x.at(t, i), least) - m, n = fma(d, c.c, kMagic);
+        sum += power_of(fma(d, c.c, kMagic - n), n);
       }
-    const double y = fma(m, -c.c, high), n = y + kMagic;  // (to sums of 2^(c (l - top)))
-    sum *= power_of(y - (n - kMagic), n);
     asm volatile("" : "+v"(sum));  // (added up here: behind a condition the compiler keeps all the weights until there, in the room of half of the waves)
     sum = wave_sum(sum);
   } else {

@@ -506,6 +506,43 @@ def test_verify_uniforms_at_the_ends_over_many_parts(vocab, front, back, dtype, 
 
 @gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("drafts", ["none", "above", "half"])
+@pytest.mark.parametrize("nodes,vocab", [(3, 8), (12, 64), (3, 5000), (20, 5001), (2, 300000)])
+def test_verify_borders_between_tokens_of_the_same_logit(nodes, vocab, dtype, drafts):
+    """2^a likeliest tokens, all others far away: weights of 1 and 0, so that sums, probabilities and borders at u1 = j / 2^a are exact in 64 bits, and the token is
+    the one behind the border.  half: the drafts' probabilities are 2 / 2^a for half of these tokens, and u0 lies on the border to the first child's or a step of 32
+    bits below it."""
+    rng, gen = random.Random(vocab + nodes), torch.Generator().manual_seed(vocab + nodes)
+    batch = 12 if vocab < 10 ** 5 else 3
+    total = batch * nodes
+    # (one temperature so small that nothing else is left, and logits near 0)
+    T = [rng.choice([1.0, 0.7, 1.9, 0.001]) for _ in range(batch)]
+    logits, u, tokens = torch.empty((total, vocab)), torch.empty((total, 2)), [0] * total
+    q = {"none": None, "above": torch.full((total, vocab), 2.0), "half": torch.zeros((total, vocab))}[drafts]
+    for i in range(total):
+        many = 2 ** rng.randint(1, min(12, vocab.bit_length() - 1))
+        top = rng.choice([0.0, 7.3, -11.6, 30.1])
+        far = rng.choice([-float("inf"), -1e9]) if T[i // nodes] > 0.01 else top - 2.0 - 10 * torch.rand(vocab, generator=gen)
+        logits[i] = far
+        at = torch.randperm(vocab, generator=gen)[:many].sort().values
+        logits[i, at] = top
+        u[i] = torch.tensor([0.9, rng.randrange(many) / many])
+        if drafts == "half":
+            some = at[torch.randperm(many, generator=gen)[:many // 2]]
+            q[i, some] = 2 / many
+            u[i] = torch.tensor([rng.choice([0.5, 0.5 - 2.0 ** -24]), rng.randrange(many) / many])
+            if (i + 1) % nodes:
+                tokens[i + 1] = some[rng.randrange(len(some))].item()
+        elif (i + 1) % nodes:    # (the walk goes on)
+            tokens[i + 1] = at[int(u[i, 1] * many)].item()
+    parents, start = [t - 1 for t in range(nodes)] * batch, starts([nodes] * batch)
+    path = _check_verify(logits.to(dtype).cuda(), None if q is None else q.cuda(), tokens, parents, start, T, u.cuda())[0]
+    if drafts != "half":
+        assert path.tolist() == list(range(nodes)) * batch
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("batch,nodes,vocab", [(1, 6, 1000), (3, 20, 5000), (2, 64, 300000)])
 def test_verify_refused_first_children_that_are_sampled_after_all(batch, nodes, vocab, dtype):
     """Drafts' probabilities above the target's everywhere: a first child is refused, nothing is left of max(p - q, 0), and p's sample is the same
