@@ -250,6 +250,34 @@ def test_nan_reaches_only_the_queries_that_see_it(dim, group):
 
 
 @gpu
+@pytest.mark.parametrize("dim,group,nodes", [(64, 6, 12), (64, 2, 12), (128, 2, 12), (128, 4, 12), (128, 5, 12), (128, 8, 12), (128, 8, 40), (256, 2, 12), (256, 6, 12)])
+def test_nan_in_calls_that_are_not_small(dim, group, nodes):
+    """As above, by the kernels of large calls, texts cut into shares, and a token that every node keeps among them."""
+    rng = random.Random(7)
+    sets = [ref.masks(tree_of(rng, nodes), 0)[0] for _ in range(2)]
+    text, window = 1500, 900
+    p = Problem([text + nodes, 300 + nodes], sets, 2 * group, 2, dim, 64, 4, window, seed=7, poison=False)
+    p.table = p.wide_table()
+    clean, clean_lse = p.run()
+    k = p.codes.clone()
+    for slot, in_k in ((text + 5, False), (text + 5, True), (text, False), (text + 2 - window, True), (text + 3 - window, False), (1100, False), (1100, True), (2, False), (50, False)):
+        p.codes = k.clone()
+        p.codes.view(torch.uint8)[0 if in_k else 1, p.table[0][slot // PAGE], 1, slot % PAGE, 3] = 0xff
+        out, lse = p.run()
+        assert torch.equal(out[nodes:], clean[nodes:]) and torch.equal(lse[nodes:], clean_lse[nodes:])
+        for t, m in enumerate(sets[0]):
+            hit = slot in ref.kept(m, text + nodes, nodes, 4, window)
+            mine, others = slice(group, 2 * group), slice(0, group)
+            assert torch.equal(out[t, others], clean[t, others]) and torch.equal(lse[t, others], clean_lse[t, others])
+            assert torch.isnan(lse[t, mine]).all() == (hit and in_k) and (in_k or torch.equal(lse, clean_lse))
+            bad = torch.isnan(out[t, mine])
+            if not hit:
+                assert not bad.any() and torch.equal(out[t, mine], clean[t, mine])
+            else:
+                assert bad.all() if in_k else (bad[:, 3].all() and bad.sum() == group)
+
+
+@gpu
 @pytest.mark.parametrize("dim,q_heads", [(64, 40), (128, 24), (128, 70), (256, 33)])
 def test_groups_of_more_rows_than_a_block_of_16(dim, q_heads):
     """A node's query heads over several blocks, in small calls and others."""
