@@ -326,6 +326,10 @@ struct Rows {
   }
 };
 
+// What a weight is multiplied by.  It stays finite where a row has kept values with a scale of 0 or next to it so far, and others' is very large: the row's weights
+// there are 0 or as good as that, but 0 times infinity is NaN.
+__device__ __forceinline__ float value_factor(float ratio, float v_scale) { return fminf(ratio * v_scale, 0x1.fffffep+127f); }
+
 // Weights of a tile of 32 tokens from its S^T (lane (n16, g) has tokens 16 h + 4 g + i of row n16), in two f16 terms (`low`: what
 // rounding to `high` leaves), references, sums and, where a reference rises, the output.  sight: tokens that the row's query sees; full: every
 // row keeps all 32 tokens, which begin at pos0.  (One term is 2^-11 of a weight: 7 to 9 in a hundred bf16 results then were the neighbour
@@ -371,7 +375,7 @@ __device__ __forceinline__ void weigh(const GqaDecodeParams& p, Rows<D, RT>& a, 
         for (int i = 0; i < 4; ++i) a.o[rt][c][i] *= shrink;
     }
     // (a row that has kept nothing so far has reference -inf, and only masked logits)
-    const float ref = a.m[rt] == -INFINITY ? 0.f : a.m[rt] - kLift, value = a.ratio[rt] * v_scale;
+    const float ref = a.m[rt] == -INFINITY ? 0.f : a.m[rt] - kLift, value = value_factor(a.ratio[rt], v_scale);
     float w[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {

@@ -135,7 +135,7 @@ __device__ __forceinline__ void weigh(const GqaDecodeParams& p, TreeRows& a, f32
 #pragma unroll
       for (int i = 0; i < 16; ++i) a.o[c][i] *= shrink;
   }
-  const float ref = a.m == -INFINITY ? 0.f : a.m - kLift, value = a.ratio * v_scale;
+  const float ref = a.m == -INFINITY ? 0.f : a.m - kLift, value = value_factor(a.ratio, v_scale);
   float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; i += 2) {

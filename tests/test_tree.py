@@ -278,6 +278,24 @@ def test_nan_in_calls_that_are_not_small(dim, group, nodes):
 
 
 @gpu
+@pytest.mark.parametrize("kind", ["any", "chain"])
+@pytest.mark.parametrize("dim,group", [(64, 1), (64, 4), (128, 1), (128, 4), (256, 1)])
+def test_a_block_of_zeros_before_one_of_very_large_values(dim, group, kind):
+    """The text's values are 0 with scales of 0, those of the nodes in the second page have a scale of 2^60: the queries that see none of these give 0 or what
+    the nodes of the first page hold."""
+    text = 103
+    p = Problem([text + 64], sets_of(random.Random(dim), [64], kind), 2 * group, 2, dim, 32, 0, 10 ** 6, seed=dim, poison=False)
+    p.scales[1, p.table[0][0], :, :3], p.scales[1, p.table[0][1], :, 0] = 0.0, 2.0 ** 60
+    out, lse = p.check(torch.float32)
+    first = [t for t, m in enumerate(p.sets) if m >> 128 - text == 0]
+    assert len(first) >= 25 and (out[first].abs() < 10).all()
+    if kind == "chain":
+        (k, v), (ks, vs) = p.codes.cuda(), p.scales.cuda()
+        got = oa.gqa_decode(p.q.cuda(), k, v, ks, vs, ints(p.table), ints(p.lens), 0, 10 ** 6, p.scale, q_start=ints(p.q_start), out_dtype=torch.float32)[0]
+        assert (got[first].abs() < 10).all() and torch.isfinite(got).all()
+
+
+@gpu
 @pytest.mark.parametrize("dim,q_heads", [(64, 40), (128, 24), (128, 70), (256, 33)])
 def test_groups_of_more_rows_than_a_block_of_16(dim, q_heads):
     """A node's query heads over several blocks, in small calls and others."""
