@@ -405,6 +405,9 @@ int omniattn_gqa_decode(const omniattn_gqa_t* gqa, const void* q, int64_t q_stri
  * A request has n = q_start[b + 1] - q_start[b] <= OMNIATTN_TREE_NODES nodes, as omniattn_table_extend numbers them (q_start NULL: one
  * each).  Like the calls above these are asynchronous, allocate nothing and read no length on the host; arrays of nodes lie behind one another
  * as the requests do; rows of no request are left as they are.
+ *
+ * A node's row can raise the scale of a block that holds text (see omniattn_gqa_append), whose codes are rounded again then.  That stays when
+ * the node goes: the scale of such a block never falls, and numbers of the text that have become subnormal under it keep what bits they have left.
  */
 #define OMNIATTN_TREE_NODES 64
 

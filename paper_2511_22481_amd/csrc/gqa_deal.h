@@ -28,7 +28,8 @@ struct Block {
   int t0, t1;  // its query tokens, both included
   TileLayout pages;
 };
-// A block of up to 128 rows: how often a page is halved into units, so that a unit is the same work whatever the rows (32 rows: 128 tokens; 64: 64; more: 32).
+// A block of up to 128 rows: how often a page is halved into units, so that a unit is the same steps of 32 rows and tokens whatever the rows (32 rows: 128
+// tokens; 64: 64; more: 32).  (Not the same bytes: one of 32 rows has the codes of four of 128.)
 template <int ROWS, typename P>
 OA_INLINE int tree_split(const P& p, const Request& r, int rb) {
   if (ROWS < 128) return 0;
