@@ -280,7 +280,6 @@ int omniattn_gqa_keep(const omniattn_gqa_t* gqa, int32_t num_layers, const int32
   p.head_dim = gqa->head_dim;
   p.scale_tokens = gqa->scale_tokens;
   p.max_pages = gqa->max_pages_per_seq;
-  p.run = 1;
   OA_HIP(launch_gqa_keep(p, cus, (hipStream_t)hip_stream));
   return OMNIATTN_OK;
 }

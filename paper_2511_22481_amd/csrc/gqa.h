@@ -75,9 +75,9 @@ struct GqaKeepParams {
   float* scales[2];         // [layers, num_pages, kv_heads, 128 / scale_tokens]
   int64_t num_pages;
   int batch, num_tokens, layers, kv_heads, head_dim, scale_tokens, max_pages;
-  int run;  // layers to a wave
+  int run;  // layers to a wave (the launch sets it)
 };
-// cus: the device's compute units.  (p.run is set.)
+// cus: the device's compute units.
 hipError_t launch_gqa_keep(GqaKeepParams p, int cus, hipStream_t stream);
 
 struct GqaAppendParams {

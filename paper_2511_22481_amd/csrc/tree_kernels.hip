@@ -90,13 +90,14 @@ __device__ __forceinline__ float wave_max(float x) {
 // (More layers from 16 waves on: 64 x 32 14.9.)  Of (KV head, K or V) to a wave, with a layer each, 64 x 32 and 1 x 4 layers: 1 18.4 and 4.8 us, 2
 // 14.0 and 5.2, 4 15.0 and 6.0, 8 13.3 and 8.7.
 constexpr int kUnits = 2, kMostLayers = 4;
+static_assert(2 % kUnits == 0);  // (a wave's units are all there, however many KV heads)
 template <int D>
 __global__ __launch_bounds__(kThreads) void gqa_keep_kernel(GqaKeepParams p) {
   constexpr int kLanes = D / 16, kRows = 64 / kLanes;  // lanes of a row, 16 codes each; rows of a pass
-  const int lane = threadIdx.x & 63, each = p.scale_tokens, blocks = kPage / each, sharers = (2 * p.kv_heads + kUnits - 1) / kUnits;
+  const int lane = threadIdx.x & 63, each = p.scale_tokens, blocks = kPage / each, sharers = 2 * p.kv_heads / kUnits;
   const uint32_t id = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t group = id / (uint32_t)sharers, run = group / (uint32_t)p.batch;
-  const int b = (int)(group - run * p.batch), unit0 = (int)(id - group * sharers) * kUnits, units = min(kUnits, 2 * p.kv_heads - unit0);
+  const int b = (int)(group - run * p.batch), unit0 = (int)(id - group * sharers) * kUnits;
   if (run * (uint32_t)p.run >= (uint32_t)p.layers) return;
   const int layer0 = (int)run * p.run, layers = min(p.run, p.layers - layer0);
   const Nodes r = nodes_of(p.q_start, b, p.num_tokens);
@@ -128,19 +129,15 @@ __global__ __launch_bounds__(kThreads) void gqa_keep_kernel(GqaKeepParams p) {
     const int64_t s = __shfl(src_at, min(row0 + in_pass, 63));
     if (row0 + in_pass < kept) {
 #pragma unroll
-      for (int j = 0; j < kUnits; ++j)
-        if (j < units) x[j] = *(const u32x4*)(cache(j, pages) + s + col);
+      for (int j = 0; j < kUnits; ++j) x[j] = *(const u32x4*)(cache(j, pages) + s + col);
     }
   };
   float old[kUnits], own[kUnits], next_old[kUnits], next_own[kUnits];
   auto load_scales = [&](int64_t pages) {
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
-      next_old[j] = next_own[j] = 0.f;
-      if (j < units) {
-        next_old[j] = *scale_at(j, pages + src_page, src);
-        if (held > 0) next_own[j] = *scale_at(j, pages + page0, block0 * each);
-      }
+      next_old[j] = *scale_at(j, pages + src_page, src);
+      next_own[j] = held > 0 ? *scale_at(j, pages + page0, block0 * each) : 0.f;
     }
   };
   load(0, first);
@@ -175,13 +172,11 @@ __global__ __launch_bounds__(kThreads) void gqa_keep_kernel(GqaKeepParams p) {
       else if (i + 1 < layers) load(pages + next_layer, first);
       if (row < kept) {
 #pragma unroll
-        for (int j = 0; j < kUnits; ++j)
-          if (j < units) *(u32x4*)(cache(j, pages) + d + col) = y[j];
+        for (int j = 0; j < kUnits; ++j) *(u32x4*)(cache(j, pages) + d + col) = y[j];
       }
     }
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
-      if (j >= units) break;
       // tokens of the text in the first block, if its scale has grown
       if (held > 0 && now0[j] > own[j]) {
         const float f = scale_ratio(own[j], now0[j]);
@@ -205,7 +200,7 @@ hipError_t launch_tree_masks(const TreeMasksParams& p, hipStream_t stream) {
 }
 
 hipError_t launch_gqa_keep(GqaKeepParams p, int cus, hipStream_t stream) {
-  const int64_t of_layer = (int64_t)p.batch * ((2 * p.kv_heads + kUnits - 1) / kUnits);
+  const int64_t of_layer = (int64_t)p.batch * (2 * p.kv_heads / kUnits);
   p.run = (int)std::min<int64_t>(kMostLayers, std::max<int64_t>(1, of_layer * p.layers / (32 * cus)));
   const int64_t waves = (p.layers + p.run - 1) / p.run * of_layer;
   const dim3 grid((uint32_t)((waves + kWaves - 1) / kWaves));
