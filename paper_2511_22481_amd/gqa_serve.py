@@ -214,13 +214,15 @@ def speculate(pool, prompts, answers, q_heads, sink, window, rows, draft, logits
         node, parent = on_gpu([t for x in tokens for t in x]), on_gpu([p for x in parents for p in x])
         masks, positions = torch.empty(total, dtype=torch.int64, device=device), torch.empty(total, **ints)
         omniattn_tree_masks(parent, pool.lens, pool.q_start, masks, positions)
+        # (lengths of requests that wait do not count their nodes: these would stand that much too far in front)
+        request = torch.repeat_interleave(torch.arange(batch, device=device), on_gpu(news), output_size=total)
+        positions += (on_gpu(news) * ~fits)[request]
         target = logits(call(node, positions, slots, masks))
         path, following, dropped = torch.empty(total, **ints), torch.empty(total, **ints), torch.empty(batch, **ints)
         workspace = torch.empty(omniattn_tree_verify_workspace_bytes(total, target.shape[1]), dtype=torch.uint8, device=device)
         numbers = torch.zeros((total, 2), device=device) if uniforms is None else uniforms(total)
         omniattn_tree_verify(target, probs, node, parent, pool.q_start, heat, numbers, path, following, None, dropped, workspace)
         # (a request whose tree found no pages has no nodes in the cache: nothing of it moves or goes)
-        request = torch.repeat_interleave(torch.arange(batch, device=device), on_gpu(news), output_size=total)
         path.masked_fill_(~fits[request], -1)
         dropped.masked_fill_(~fits, 0)
         pool.keep(path, dropped)

@@ -471,3 +471,24 @@ def test_the_cache_where_scales_change():
     what, texts = speculate(pool, prompts, [60] * 4, Q_HEADS, 0, 10 ** 6, model.rows, draft, rule.logits, observe=observe)
     assert texts == [rule.text(p, 60) for p in prompts] and what["steps"] < 40
     assert 0 < seen["raised"] < seen["blocks"], seen
+
+
+@gpu
+def test_nodes_of_requests_that_wait_have_their_positions():
+    """rows is asked for their rows too: at the positions that they will have, not in front of the text."""
+    rule, expected, waited = Rule(9), [], []
+    prompts, answers = [[3] * 100, [7], [9], [11] * 2], [20, 12, 15, 9]
+    pool = Pool(4, LAYERS, 2, HEADS, 64, 2, scale_tokens=32)
+
+    def draft(texts):
+        trees = rule.draft(texts)
+        expected[:] = [len(text) - 1 + depth for text, tree in zip(texts, trees[0]) for depth in range(len(tree))]
+        waited.append(sum(t is not None for t in texts))
+        return trees
+
+    def rows(tokens, positions, buffer):
+        if waited:    # (after the prompts)
+            assert positions.tolist() == expected and tokens.tolist() == rule.nodes
+        buffer.normal_()
+    what, texts = speculate(pool, prompts, answers, Q_HEADS, 0, 10 ** 6, rows, draft, rule.logits)
+    assert texts == [rule.text(p, a) for p, a in zip(prompts, answers)] and what["pages"] == 2 and what["free_at_the_end"] == 2 and waited[0] == 4
