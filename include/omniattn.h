@@ -457,7 +457,8 @@ typedef struct {
  * u1).  u0, u1 = uniforms[i], in [0, 1).
  *
  *   logits       device, logits_dtype [N, V]; logits_stride elements from one row to the next.  NaN counts as -inf.  A row with +inf gives
- *                the first such token, one of -inf only gives -1, which ends the path.
+ *                the first such token, one of -inf only gives -1, which ends the path.  (Its node stays on it, so that no token is new: the text
+ *                ends with one whose row is in the cache, and no tree can follow.)
  *   draft_probs  device, fp32 [N, V], draft_stride elements from one row to the next; or NULL
  *   tokens       device, int32 [N]: the nodes' tokens (those outside [0, V) are never taken)
  *   parents      as for omniattn_tree_masks; nodes that do not descend from node 0 are not reached
